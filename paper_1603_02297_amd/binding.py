@@ -85,6 +85,7 @@ class TtcError(RuntimeError):
 
 
 _lib = None
+_on_load = []                               # functions that declare more entry points of the library, called once with it
 
 
 def lib() -> ctypes.CDLL:
@@ -132,6 +133,8 @@ def lib() -> ctypes.CDLL:
         L.ttc_plan_cache_lookup.argtypes = [vp, ctypes.c_char_p]
         L.ttc_debug_emulate_map.restype = i
         L.ttc_debug_emulate_map.argtypes = [vp, i64p]
+        for declare in _on_load:
+            declare(L)
         _lib = L
         if _call is not None:
             _call.bind(ctypes.cast(L.ttc_execute, vp).value)

@@ -1,0 +1,97 @@
+// Internal declarations of the moves whose index map is data (include/ttc_moves.h), shared by the host part
+// (ttc_moves.cpp) and the kernels (ttc_route.hip, ttc_pages.hip).
+#pragma once
+
+#include <cstdint>
+
+#include "ttc_internal.h"
+#include "ttc_moves.h"
+
+struct ttc_route_s {
+    int      dtype;
+    int64_t  width;
+    int      topk, experts;
+    int64_t  first;
+    int      align, id_bytes;
+    float    alpha, beta;
+};
+
+struct ttc_pages_s {
+    int      dtype, cache_dtype;
+    int64_t  heads, dim, page, pages;
+    int64_t  stride_head, stride_slot, stride_page;    // elements
+    int64_t  span;                                     // elements from the first to the last of the cache, inclusive
+    ttc::FastDiv page_div;
+};
+
+namespace ttc {
+
+constexpr int kMoveThreads = 256;          // workgroup of the row moves
+constexpr int kSortThreads = 1024;         // largest workgroup of the sort
+constexpr int kSortBlocks = 8;             // ids a lane of the sort holds at most
+constexpr int kSortOne = 8192;             // assignments up to which one workgroup sorts alone
+constexpr int kSortSums = 128;             // chunks up to which every workgroup adds up the counts of the others by itself
+
+inline int elem_bytes(int dtype) { return dtype == TTC_F32 ? 4 : dtype == TTC_F8 ? 1 : 2; }
+
+// How a sort of n assignments is cut: `blocks` ids per lane, `chunk` assignments per workgroup.
+struct SortShape {
+    int      threads, blocks;
+    int64_t  chunk, chunks;
+};
+SortShape sort_shape(int64_t n, int experts);
+
+// Kernel launchers; the callers have checked every argument.  They return TTC_OK or TTC_ERR_HIP.
+struct SortArgs {
+    const void* ids;
+    int64_t     ld_ids;
+    int64_t     first;
+    int32_t    *offsets, *counts, *position, *source;
+    int32_t*    hist;                      // [chunks][experts], then [experts] totals (three-kernel form only)
+    uint32_t    n, rows;                   // assignments, rows of a sorted tensor
+    int32_t     topk, experts, align, id_bytes;
+    FastDiv     topk_div;
+};
+int launch_sort(const SortArgs& a, const SortShape& s, void* stream);
+
+struct RowArgs {
+    const void    *x;                      // tokens' side, read (gather: x, grad: dy)
+    const void    *rows;                   // sorted side, read (combine, grad)
+    void          *y;                      // written (gather: rows, combine: y, grad: drows)
+    const float   *weights;
+    const int32_t *position, *offsets, *counts;
+    float         *dweights;
+    int64_t        ld_x, ld_rows, ld_y;
+    float          alpha, beta;
+    uint32_t       tokens, width, row_count;
+    int32_t        topk, experts, align, dtype;
+};
+int launch_gather(const RowArgs& a, void* stream);
+int launch_combine(const RowArgs& a, void* stream);
+int launch_combine_grad(const RowArgs& a, void* stream);
+
+struct MapArgs {
+    const int32_t *first, *cached, *fresh, *free_list;
+    int32_t       *table, *starts, *page_starts, *slots, *positions, *owner;
+    int64_t        ld_table;
+    int32_t        requests, free_count, tokens;
+    uint32_t       pages;
+    FastDiv        page;
+};
+int launch_map(const MapArgs& a, void* stream);
+
+struct SlotArgs {
+    const int32_t *slots;
+    const void    *k, *v;                  // write: packed; read: cache
+    void          *k_out, *v_out;          // write: cache; read: packed
+    const float   *k_scale, *v_scale;
+    int64_t        ld_k, ld_v;
+    int64_t        stride_head, stride_slot, stride_page;
+    uint32_t       tokens, slot_count, heads, dim;
+    FastDiv        page;
+    int32_t        dtype, cache_dtype;
+};
+int launch_write(const SlotArgs& a, void* stream);
+int launch_read(const SlotArgs& a, void* stream);
+
+}  // namespace ttc

@@ -1,0 +1,294 @@
+// Pages of a cache (include/ttc_moves.h, ttc_pages_*), for gfx950 (MI355X): block tables and slots from request
+// lengths, and the moves of keys and values by those slots.
+#include "ttc_moves_device.h"
+
+namespace ttc {
+
+// ---------------------------------------------------------------------------------
+// The map.  Two prefix sums over the requests (listed positions, pages taken), then every listed position by itself: its
+// request by bisection, its page from the table where the request held it already, from the free list where not.
+// Nothing that one lane writes is read by another, so that one launch does it: every workgroup makes the prefix sums for
+// itself as long as they fit its LDS (they are a few KB out of L2).
+// ---------------------------------------------------------------------------------
+namespace {
+
+constexpr int kMapThreads = 256;
+constexpr int kMapEach = 4;                // listed positions per lane
+constexpr int kMapRequests = 4096;         // requests whose sums every workgroup makes for itself
+
+// sums stop at 2^31-1; adding up this way is associative, too
+__device__ __forceinline__ uint32_t capped(uint32_t a, uint32_t b) { return a + b < 0x7fffffffu ? a + b : 0x7fffffffu; }
+
+struct Request {
+    uint32_t first, have, listed, taken;   // first listed position, pages held, positions listed, pages to take
+};
+
+__device__ __forceinline__ uint32_t blocks_of(uint32_t length, const FastDiv& page) { return length ? fdiv(length - 1, page) + 1 : 0; }
+
+__device__ __forceinline__ Request request(const MapArgs& p, int r)
+{
+    const int32_t c = p.cached[r], f = p.fresh[r];
+    const uint32_t cached = c < 0 ? 0 : (uint32_t)c, end = capped(cached, f < 0 ? 0 : (uint32_t)f);
+    Request q;
+    q.first = cached;
+    if (p.first) {
+        const int32_t b = p.first[r];
+        q.first = b < 0 ? 0 : (uint32_t)b < cached ? (uint32_t)b : cached;
+    }
+    q.have = blocks_of(cached, p.page);
+    q.listed = end - q.first;
+    q.taken = blocks_of(end, p.page) - q.have;
+    return q;
+}
+
+struct Two { uint32_t a, b; };
+
+// Sums over the threads before this one, and over all; `part` holds two words per wavefront.
+__device__ __forceinline__ Two sums_before(Two v, uint32_t (*part)[2], Two* all)
+{
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
+    Two s = v;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+        const uint32_t a = __shfl_up(s.a, d), b = __shfl_up(s.b, d);
+        if (lane >= d) { s.a = capped(s.a, a); s.b = capped(s.b, b); }
+    }
+    if (lane == kWave - 1) { part[wave][0] = s.a; part[wave][1] = s.b; }
+    __syncthreads();
+    Two before = {0, 0}, total = {0, 0};
+    for (int w = 0; w < waves; ++w) {
+        if (w == wave) before = total;
+        total.a = capped(total.a, part[w][0]);
+        total.b = capped(total.b, part[w][1]);
+    }
+    __syncthreads();
+    *all = total;
+    // the lanes before in this wavefront
+    const uint32_t a = __shfl_up(s.a, 1), b = __shfl_up(s.b, 1);
+    if (lane > 0) { before.a = capped(before.a, a); before.b = capped(before.b, b); }
+    return before;
+}
+
+// Both prefix sums of all requests into `starts` and `page_starts` (LDS or global), each thread over neighbouring ones.
+template <typename Put> __device__ __forceinline__ void sum_requests(const MapArgs& p, uint32_t (*part)[2], Put put)
+{
+    const int each = (p.requests + (int)blockDim.x - 1) / (int)blockDim.x;
+    const int64_t from = (int64_t)threadIdx.x * each;
+    const int lo = (int)(from < p.requests ? from : p.requests), hi = lo + each < p.requests ? lo + each : p.requests;
+    Two mine = {0, 0};
+    for (int r = lo; r < hi; ++r) {
+        const Request q = request(p, r);
+        mine.a = capped(mine.a, q.listed);
+        mine.b = capped(mine.b, q.taken);
+    }
+    Two all, at = sums_before(mine, part, &all);
+    for (int r = lo; r < hi; ++r) {
+        const Request q = request(p, r);
+        put(r, at);
+        at.a = capped(at.a, q.listed);
+        at.b = capped(at.b, q.taken);
+    }
+    if (threadIdx.x == 0) put(p.requests, all);
+}
+
+__global__ __launch_bounds__(1024) void starts_kernel(MapArgs p)
+{
+    __shared__ uint32_t part[1024 / kWave][2];
+    sum_requests(p, part, [&](int r, Two s) { p.starts[r] = (int32_t)s.a; p.page_starts[r] = (int32_t)s.b; });
+}
+
+// FUSED: makes the sums itself; otherwise starts_kernel has left them where they belong.
+template <bool FUSED>
+__global__ __launch_bounds__(kMapThreads) void map_kernel(MapArgs p)
+{
+    extern __shared__ uint32_t sums[];      // FUSED: starts, then page_starts
+    __shared__ uint32_t part[kMapThreads / kWave][2];
+    const uint32_t* starts = FUSED ? sums : reinterpret_cast<const uint32_t*>(p.starts);
+    const uint32_t* page_starts = FUSED ? sums + p.requests + 1 : reinterpret_cast<const uint32_t*>(p.page_starts);
+    const uint32_t block = block_id();
+    if (FUSED) {
+        sum_requests(p, part, [&](int r, Two s) {
+            sums[r] = s.a;
+            sums[p.requests + 1 + r] = s.b;
+            if (block == 0) { p.starts[r] = (int32_t)s.a; p.page_starts[r] = (int32_t)s.b; }
+        });
+        __syncthreads();
+    }
+    const uint64_t i0 = ((uint64_t)block * kMapThreads + threadIdx.x) * kMapEach;
+    if (i0 >= (uint64_t)p.tokens) return;
+    // the last request that starts at or before i0: requests that list nothing share a start with the next
+    int lo = 0, hi = p.requests;            // starts[lo] <= i0 < starts[hi], or past the end
+    if (i0 >= starts[p.requests]) lo = p.requests;
+    while (hi - lo > 1) {
+        const int mid = lo + (hi - lo) / 2;
+        if (starts[mid] <= i0) lo = mid; else hi = mid;
+    }
+    int r = lo;
+    Request q = {};
+    if (r < p.requests) q = request(p, r);
+    const int count = (uint64_t)p.tokens - i0 < kMapEach ? (int)((uint64_t)p.tokens - i0) : kMapEach;
+    for (int j = 0; j < count; ++j) {
+        const uint32_t i = (uint32_t)i0 + j;
+        if (r < p.requests && i >= starts[r + 1]) {
+            do ++r; while (r < p.requests && i >= starts[r + 1]);
+            if (r < p.requests) q = request(p, r);
+        }
+        int32_t slot = -1, at = -1, who = -1;
+        if (r < p.requests) {
+            const uint32_t pos = q.first + (i - starts[r]), block_no = fdiv(pos, p.page), inside = pos - block_no * p.page.div;
+            int32_t* entry = p.table + (int64_t)r * p.ld_table + block_no;
+            const bool fits = (int64_t)block_no < p.ld_table;
+            int32_t page = -1;
+            if (block_no < q.have) {
+                if (fits) page = *entry;
+            } else {
+                const uint64_t pick = (uint64_t)page_starts[r] + (block_no - q.have);
+                if (pick < (uint64_t)p.free_count) page = p.free_list[pick];
+            }
+            if ((uint32_t)page >= p.pages) page = -1;
+            if (block_no >= q.have && inside == 0 && fits) *entry = page;          // the first token of a page enters it
+            if (fits && page >= 0) slot = (int32_t)((uint32_t)page * p.page.div + inside);
+            at = (int32_t)pos;
+            who = r;
+        }
+        p.slots[i] = slot;
+        if (p.positions) p.positions[i] = at;
+        if (p.owner) p.owner[i] = who;
+    }
+}
+
+}  // namespace
+
+int launch_map(const MapArgs& a, void* stream)
+{
+    MapArgs p = a;
+    const bool fused = p.requests <= kMapRequests;
+    const uint64_t per_block = (uint64_t)kMapThreads * kMapEach;
+    uint64_t blocks = ((uint64_t)p.tokens + per_block - 1) / per_block;
+    if (fused) {
+        const size_t lds = 2 * sizeof(uint32_t) * (size_t)(p.requests + 1);
+        return launch_blocks(reinterpret_cast<const void*>(&map_kernel<true>), blocks ? blocks : 1, kMapThreads, lds, &p, stream);
+    }
+    const int st = launch_blocks(reinterpret_cast<const void*>(&starts_kernel), 1, 1024, 0, &p, stream);
+    return st != TTC_OK ? st : launch_blocks(reinterpret_cast<const void*>(&map_kernel<false>), blocks, kMapThreads, 0, &p, stream);
+}
+
+// ---------------------------------------------------------------------------------
+// Keys and values into and out of the cache.  A lane moves one vector of a token's keys and the same one of its values; the
+// vectors of a token are numbered through its heads, tokens follow each other, so that no lane is idle whatever the
+// number of heads and their size.
+// ---------------------------------------------------------------------------------
+namespace {
+
+struct PlaceArgs {
+    SlotArgs s;
+    uint32_t units;                        // tokens * heads * vecs
+    uint32_t vecs;                         // vectors of a head
+    FastDiv  token_div, head_div;          // by heads * vecs, by vecs
+};
+
+// Eight elements a lane: 16 bytes of a 16-bit type, two accesses of 32 bits, 8 bytes of an 8-bit cache.  (f32 alone: four.)
+template <typename T, typename C> struct SlotVec { static constexpr int value = sizeof(T) == 4 && sizeof(C) == 4 ? 4 : 8; };
+
+template <typename T, typename C, bool WRITE> struct SlotTypes { typedef T from; typedef C to; };
+template <typename T, typename C> struct SlotTypes<T, C, false> { typedef C from; typedef T to; };
+
+// from -> to, through float with the head's scale where the cache is narrower
+template <typename T, typename C, bool WRITE, int V>
+__device__ __forceinline__ void convert(const Vec<typename SlotTypes<T, C, WRITE>::from, V>& x, float scale, Vec<typename SlotTypes<T, C, WRITE>::to, V>& r)
+{
+    float f[V];
+    widen(x, f);
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = WRITE ? f[i] / scale : f[i] * scale;
+    narrow(f, r);
+}
+
+template <typename T, typename C, bool WRITE>
+__global__ __launch_bounds__(kMoveThreads) void slots_kernel(PlaceArgs p)
+{
+    constexpr int V = SlotVec<T, C>::value;
+    constexpr bool same = sizeof(T) == sizeof(C);
+    typedef typename SlotTypes<T, C, WRITE>::from From;
+    typedef typename SlotTypes<T, C, WRITE>::to To;
+    const uint32_t unit = block_id() * kMoveThreads + threadIdx.x;
+    if (unit >= p.units) return;
+    const uint32_t token = fdiv(unit, p.token_div), in_token = unit - token * p.token_div.div;
+    const uint32_t head = fdiv(in_token, p.head_div), c = (in_token - head * p.vecs) * V;
+    const int n = (int)(p.s.dim - c);
+    const uint32_t slot = (uint32_t)p.s.slots[token];
+    const bool here = slot < p.s.slot_count;
+    if (WRITE && !here) return;
+    const uint32_t page = here ? fdiv(slot, p.s.page) : 0, inside = here ? slot - page * p.s.page.div : 0;
+    const int64_t in_cache = (int64_t)page * p.s.stride_page + (int64_t)inside * p.s.stride_slot + (int64_t)head * p.s.stride_head + c;
+    const int64_t packed = (int64_t)head * p.s.dim + c;
+    const int64_t at_k = (int64_t)token * p.s.ld_k + packed, at_v = (int64_t)token * p.s.ld_v + packed;
+    const bool both = p.s.v_out != nullptr;
+    Vec<From, V> k = {}, v = {};
+    if (here) {
+        k = load_row<From, V>(static_cast<const From*>(p.s.k) + (WRITE ? at_k : in_cache), n);
+        if (both) v = load_row<From, V>(static_cast<const From*>(p.s.v) + (WRITE ? at_v : in_cache), n);
+    }
+    To* to_k = static_cast<To*>(p.s.k_out) + (WRITE ? in_cache : at_k);
+    To* to_v = static_cast<To*>(p.s.v_out) + (WRITE ? in_cache : at_v);
+    if constexpr (same) {
+        store_row<To, V>(to_k, k, n);
+        if (both) store_row<To, V>(to_v, v, n);
+    } else {
+        const float scale_k = p.s.k_scale ? p.s.k_scale[head] : 1.f, scale_v = p.s.v_scale ? p.s.v_scale[head] : 1.f;
+        Vec<To, V> r = {};
+        if (here) convert<T, C, WRITE, V>(k, scale_k, r);       // nowhere: zero, whatever the scale
+        store_row<To, V>(to_k, r, n);
+        if (both) {
+            if (here) convert<T, C, WRITE, V>(v, scale_v, r);
+            store_row<To, V>(to_v, r, n);
+        }
+    }
+}
+
+template <typename T, typename C, bool WRITE> int launch_slots_types(const SlotArgs& a, void* stream)
+{
+    constexpr int V = SlotVec<T, C>::value;
+    PlaceArgs p = {};
+    p.s = a;
+    p.vecs = (a.dim + V - 1) / V;
+    const uint32_t per_token = a.heads * p.vecs;        // heads * dim < 2^30
+    p.token_div = make_fastdiv(per_token);
+    p.head_div = make_fastdiv(p.vecs);
+    // lane numbers stay below 2^31: very long lists go in several launches
+    const uint32_t most = (uint32_t)INT32_MAX / per_token;
+    for (uint64_t done = 0; done < a.tokens; done += most) {
+        const uint32_t tokens = a.tokens - done < most ? (uint32_t)(a.tokens - done) : most;
+        p.s.slots = a.slots + done;
+        const int64_t skip_k = (int64_t)done * a.ld_k * (int64_t)sizeof(T), skip_v = (int64_t)done * a.ld_v * (int64_t)sizeof(T);
+        if (WRITE) {
+            p.s.k = static_cast<const char*>(a.k) + skip_k;
+            if (a.v) p.s.v = static_cast<const char*>(a.v) + skip_v;
+        } else {
+            p.s.k_out = static_cast<char*>(a.k_out) + skip_k;
+            if (a.v_out) p.s.v_out = static_cast<char*>(a.v_out) + skip_v;
+        }
+        p.units = tokens * per_token;
+        const int st = launch_blocks(reinterpret_cast<const void*>(&slots_kernel<T, C, WRITE>), ((uint64_t)p.units + kMoveThreads - 1) / kMoveThreads, kMoveThreads, 0, &p, stream);
+        if (st != TTC_OK) return st;
+    }
+    return TTC_OK;
+}
+
+template <bool WRITE> int launch_slots(const SlotArgs& a, void* stream)
+{
+    const bool narrow = a.cache_dtype == TTC_F8;
+    switch (a.dtype) {
+    case TTC_F32:  return narrow ? launch_slots_types<float, f8, WRITE>(a, stream) : launch_slots_types<float, float, WRITE>(a, stream);
+    case TTC_BF16: return narrow ? launch_slots_types<__bf16, f8, WRITE>(a, stream) : launch_slots_types<__bf16, __bf16, WRITE>(a, stream);
+    case TTC_F16:  return narrow ? launch_slots_types<_Float16, f8, WRITE>(a, stream) : launch_slots_types<_Float16, _Float16, WRITE>(a, stream);
+    default:       return TTC_ERR_UNSUPPORTED_DTYPE;
+    }
+}
+
+}  // namespace
+
+int launch_write(const SlotArgs& a, void* stream) { return launch_slots<true>(a, stream); }
+int launch_read(const SlotArgs& a, void* stream) { return launch_slots<false>(a, stream); }
+
+}  // namespace ttc

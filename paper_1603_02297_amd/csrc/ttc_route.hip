@@ -1,0 +1,547 @@
+// Rows sorted by expert, and back (include/ttc_moves.h, ttc_route_*), for gfx950 (MI355X).
+//
+// The sort is a stable counting sort of the assignments by expert.  A wavefront ranks 64 assignments at a time: one
+// ballot per bit of the expert's number leaves every lane with the lanes that chose the same expert, the lanes before
+// it among those are its rank, and a counter per wavefront and expert in LDS carries on to the next 64.  No atomics on
+// what is returned: the order is the assignments' own, on every run.
+//
+// The moves walk over tokens, not over sorted rows: a token's row is read once and written topk times (gather), topk
+// rows are read and one is written (combine), and the gradient does both in one pass, dy's vector being in registers
+// when the dot product with the expert's row wants it.  All are bound by memory.
+#include "ttc_moves_device.h"
+
+namespace ttc {
+
+// ---------------------------------------------------------------------------------
+// The sort
+// ---------------------------------------------------------------------------------
+namespace {
+
+// expert of assignment a, or `experts` for nowhere
+__device__ __forceinline__ uint32_t expert_of(const SortArgs& p, uint32_t a)
+{
+    const uint32_t t = fdiv(a, p.topk_div), k = a - t * (uint32_t)p.topk;
+    const int64_t at = (int64_t)t * p.ld_ids + k;
+    const int64_t id = p.id_bytes == 8 ? static_cast<const int64_t*>(p.ids)[at] : (int64_t)static_cast<const int32_t*>(p.ids)[at];
+    const uint64_t e = (uint64_t)id - (uint64_t)p.first;
+    return e < (uint64_t)p.experts ? (uint32_t)e : (uint32_t)p.experts;
+}
+
+// Sum of v over the threads before this one; *all is the sum over all.  `part` holds a value per wavefront.
+__device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t* part, uint32_t* all)
+{
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
+    uint32_t s = v;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+        const uint32_t o = __shfl_up(s, d);
+        if (lane >= d) s += o;
+    }
+    if (lane == kWave - 1) part[wave] = s;
+    __syncthreads();
+    uint32_t before = 0, total = 0;
+    for (int w = 0; w < waves; ++w) {
+        const uint32_t x = part[w];
+        before += w < wave ? x : 0;
+        total += x;
+    }
+    __syncthreads();
+    *all = total;
+    return before + s - v;
+}
+
+__device__ __forceinline__ uint32_t padded(uint32_t count, uint32_t align) { return (count + align - 1) / align * align; }
+
+// A workgroup's chunk: every assignment's rank among those of its expert in the chunk, and the experts' counts.
+// ALONE: the chunk is all there is, and the result is finished here.  Otherwise ranks are left in `position` and counts
+// in `hist` for place_kernel.
+// LDS: counters [waves][experts] (16 bits: a wavefront holds at most 64 * kSortBlocks ids, a chunk kSortOne), then
+// the experts' first rows, then one word per wavefront.
+template <int B, bool ALONE>
+__global__ __launch_bounds__(kSortThreads) void sort_kernel(SortArgs p)
+{
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int waves = blockDim.x / kWave, wave = threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
+    const int experts = p.experts;
+    uint32_t* part = reinterpret_cast<uint32_t*>(lds);
+    uint32_t* row = part + kSortThreads / kWave;
+    volatile uint16_t* counter = reinterpret_cast<volatile uint16_t*>(row + experts);
+    const uint32_t chunk = blockIdx.x;
+    for (int i = threadIdx.x; i < waves * experts; i += blockDim.x) counter[i] = 0;
+    if (p.source)                           // -1 everywhere; the rows that hold an assignment are written after it
+        for (uint64_t i = (uint64_t)chunk * blockDim.x + threadIdx.x; i < p.rows; i += (uint64_t)gridDim.x * blockDim.x) p.source[i] = -1;
+    uint32_t e[B], rank[B];
+    const uint64_t start = ((uint64_t)chunk * waves + wave) * (B * kWave) + lane;
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+        const uint64_t a = start + b * kWave;
+        e[b] = a < p.n ? expert_of(p, (uint32_t)a) : (uint32_t)experts;
+    }
+    __syncthreads();
+    volatile uint16_t* mine = counter + wave * experts;
+    const int bits = 32 - __clz(experts);   // experts itself (nowhere) has to be told apart, too
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+        uint64_t same = ~uint64_t(0);
+        for (int i = 0; i < bits; ++i) {
+            const bool set = (e[b] >> i) & 1;
+            const uint64_t with = __ballot(set);
+            same &= set ? with : ~with;
+        }
+        const uint32_t before = (uint32_t)__popcll(same & ((uint64_t(1) << lane) - 1));
+        rank[b] = 0;
+        if (e[b] < (uint32_t)experts) {
+            const uint32_t base = mine[e[b]];
+            rank[b] = base + before;
+            __builtin_amdgcn_wave_barrier();
+            if (before == 0) mine[e[b]] = (uint16_t)(base + (uint32_t)__popcll(same));
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    __syncthreads();
+    // one thread per expert: its counters become sums over the wavefronts before
+    uint32_t total = 0;
+    if ((int)threadIdx.x < experts)
+        for (int w = 0; w < waves; ++w) {
+            const uint32_t c = counter[w * experts + threadIdx.x];
+            counter[w * experts + threadIdx.x] = (uint16_t)total;
+            total += c;
+        }
+    if (ALONE) {
+        uint32_t all;
+        const uint32_t first = sum_before(padded(total, (uint32_t)p.align), part, &all);
+        if ((int)threadIdx.x < experts) {
+            row[threadIdx.x] = first;
+            p.offsets[threadIdx.x] = (int32_t)first;
+            p.counts[threadIdx.x] = (int32_t)total;
+        }
+        if (threadIdx.x == 0) p.offsets[experts] = (int32_t)all;
+    } else if ((int)threadIdx.x < experts) {
+        p.hist[(int64_t)chunk * experts + threadIdx.x] = (int32_t)total;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+        const uint64_t a = start + b * kWave;
+        if (a >= p.n) continue;
+        const bool here = e[b] < (uint32_t)experts;
+        uint32_t at = 0;
+        if (here) at = rank[b] + mine[e[b]] + (ALONE ? row[e[b]] : 0u);
+        p.position[a] = here ? (int32_t)at : -1;
+        if (ALONE && here && p.source) p.source[at] = (int32_t)a;
+    }
+}
+
+// Counts of the chunks before, per expert, in place; totals behind the last chunk.  Only for more than kSortSums chunks:
+// 64 experts a workgroup, the chunks in as many ranges as it has wavefronts.
+__global__ __launch_bounds__(kSortThreads) void sum_kernel(int32_t* hist, int64_t chunks, int experts)
+{
+    __shared__ int32_t range_sum[kSortThreads / kWave][kWave];
+    const int e = blockIdx.x * kWave + (threadIdx.x & (kWave - 1)), range = threadIdx.x / kWave, ranges = kSortThreads / kWave;
+    const int64_t each = (chunks + ranges - 1) / ranges, lo = range * each, hi = lo + each < chunks ? lo + each : chunks;
+    int32_t s = 0;
+    if (e < experts)
+        for (int64_t g = lo; g < hi; ++g) s += hist[g * experts + e];
+    range_sum[range][threadIdx.x & (kWave - 1)] = s;
+    __syncthreads();
+    if (e >= experts) return;
+    int32_t before = 0;
+    for (int r = 0; r < range; ++r) before += range_sum[r][threadIdx.x & (kWave - 1)];
+    for (int64_t g = lo; g < hi; ++g) {
+        const int32_t c = hist[g * experts + e];
+        hist[g * experts + e] = before;
+        before += c;
+    }
+    if (range == ranges - 1) hist[chunks * experts + e] = before;
+}
+
+// Ranks within a chunk become rows.  SUMMED: sum_kernel has been over the counts; otherwise every workgroup adds up
+// those of the other chunks by itself (a few 64 KB out of L2), which saves a launch.
+template <bool SUMMED>
+__global__ __launch_bounds__(kSortThreads) void place_kernel(SortArgs p, int64_t chunk_len, int32_t chunks)
+{
+    extern __shared__ __align__(16) unsigned char lds[];
+    uint32_t* part = reinterpret_cast<uint32_t*>(lds);
+    uint32_t* row = part + kSortThreads / kWave;
+    uint32_t* sums = row + p.experts;       // totals; only where not SUMMED
+    const int experts = p.experts, chunk = blockIdx.x;
+    uint32_t total = 0, before = 0;
+    if (SUMMED) {
+        if ((int)threadIdx.x < experts) {
+            total = (uint32_t)p.hist[(int64_t)chunks * experts + threadIdx.x];
+            before = (uint32_t)p.hist[(int64_t)chunk * experts + threadIdx.x];
+        }
+    } else {
+        for (int i = threadIdx.x; i < experts; i += kSortThreads) row[i] = sums[i] = 0;
+        __syncthreads();
+        int log = 0;
+        while ((1 << log) < experts) ++log;
+        const int e = threadIdx.x & ((1 << log) - 1), lanes = kSortThreads >> log;
+        if (e < experts) {
+            uint32_t t = 0, b = 0;
+#pragma unroll 8
+            for (int g = threadIdx.x >> log; g < chunks; g += lanes) {
+                const uint32_t c = (uint32_t)p.hist[(int64_t)g * experts + e];
+                t += c;
+                b += g < chunk ? c : 0;
+            }
+            atomicAdd(&sums[e], t);          // whole numbers: the order does not matter
+            atomicAdd(&row[e], b);
+        }
+        __syncthreads();
+        if ((int)threadIdx.x < experts) {
+            total = sums[threadIdx.x];
+            before = row[threadIdx.x];
+        }
+    }
+    uint32_t all;
+    const uint32_t first = sum_before(padded(total, (uint32_t)p.align), part, &all);
+    if ((int)threadIdx.x < experts) {
+        row[threadIdx.x] = first + before;
+        if (chunk == 0) {
+            p.offsets[threadIdx.x] = (int32_t)first;
+            p.counts[threadIdx.x] = (int32_t)total;
+        }
+    }
+    if (chunk == 0 && threadIdx.x == 0) p.offsets[experts] = (int32_t)all;
+    __syncthreads();
+    const uint64_t lo = (uint64_t)chunk * (uint64_t)chunk_len, end = lo + (uint64_t)chunk_len, hi = end < p.n ? end : p.n;
+    for (uint64_t a = lo + threadIdx.x; a < hi; a += kSortThreads) {
+        const uint32_t e = expert_of(p, (uint32_t)a);
+        if (e >= (uint32_t)experts) continue;                       // its position is -1 already
+        const uint32_t at = (uint32_t)p.position[a] + row[e];
+        p.position[a] = (int32_t)at;
+        if (p.source) p.source[at] = (int32_t)a;
+    }
+}
+
+template <int B> int launch_sort_blocks(const SortArgs& p, const SortShape& s, void* stream)
+{
+    const size_t head = sizeof(uint32_t) * (size_t)(kSortThreads / kWave + p.experts);
+    const size_t lds = head + sizeof(uint16_t) * (size_t)(s.threads / kWave) * (size_t)p.experts;
+    if (s.chunks == 1) return launch_blocks(reinterpret_cast<const void*>(&sort_kernel<B, true>), 1, s.threads, lds, const_cast<SortArgs*>(&p), stream);
+    hipStream_t st = (hipStream_t)stream;
+    SortArgs a = p;
+    int64_t len = s.chunk, chunks64 = s.chunks;
+    int32_t chunks = (int32_t)s.chunks;
+    int experts = p.experts;
+    void* sort_args[] = {&a};
+    void* sum_args[] = {&a.hist, &chunks64, &experts};
+    void* place_args[] = {&a, &len, &chunks};
+    const bool summed = s.chunks > kSortSums;
+    if (hipLaunchKernel(reinterpret_cast<const void*>(&sort_kernel<B, false>), dim3((uint32_t)chunks), dim3(s.threads), sort_args, lds, st) != hipSuccess) return TTC_ERR_HIP;
+    if (summed && hipLaunchKernel(reinterpret_cast<const void*>(&sum_kernel), dim3((uint32_t)((experts + kWave - 1) / kWave)), dim3(kSortThreads), sum_args, 0, st) != hipSuccess)
+        return TTC_ERR_HIP;
+    const void* place = summed ? reinterpret_cast<const void*>(&place_kernel<true>) : reinterpret_cast<const void*>(&place_kernel<false>);
+    const size_t place_lds = head + (summed ? 0 : sizeof(uint32_t) * (size_t)experts);
+    return hipLaunchKernel(place, dim3((uint32_t)chunks), dim3(kSortThreads), place_args, place_lds, st) == hipSuccess ? TTC_OK : TTC_ERR_HIP;
+}
+
+}  // namespace
+
+int launch_sort(const SortArgs& a, const SortShape& s, void* stream)
+{
+    switch (s.blocks) {
+    case 1: return launch_sort_blocks<1>(a, s, stream);
+    case 2: return launch_sort_blocks<2>(a, s, stream);
+    case 4: return launch_sort_blocks<4>(a, s, stream);
+    default: return launch_sort_blocks<8>(a, s, stream);
+    }
+}
+
+// ---------------------------------------------------------------------------------
+// The moves.  A row is `vecs` vectors of 16 bytes, the last of which may be cut.  2^lanes_log lanes (at most a
+// wavefront, fewer where the row is shorter) take one vector each, `parts` such groups make a row.
+// ---------------------------------------------------------------------------------
+namespace {
+
+template <typename T> struct RowVec { static constexpr int value = 16 / (int)sizeof(T); };
+
+struct MoveArgs {
+    RowArgs  r;
+    uint32_t lanes_log, parts, vecs;
+    FastDiv  parts_div;
+    uint32_t units;                        // tokens * parts
+    uint32_t blocks, total;                // workgroups over the units, and with those after them that clear padding
+    uint32_t pad_parts;                    // workgroups per expert for its padding
+};
+
+// Padding rows of expert `e`: those of its segment that hold no token, cleared by `pad_parts` workgroups.
+template <typename T> __device__ __forceinline__ void clear_padding(const MoveArgs& p, uint32_t block)
+{
+    constexpr int V = RowVec<T>::value;
+    if (block >= p.total) return;
+    const uint32_t index = block - p.blocks;
+    const uint32_t e = index / p.pad_parts, part = index - e * p.pad_parts;
+    const int64_t end = p.r.offsets[e + 1], first = (int64_t)p.r.offsets[e] + p.r.counts[e];
+    const int64_t lo = first < 0 ? 0 : first, hi = end < (int64_t)p.r.row_count ? end : (int64_t)p.r.row_count;
+    if (lo >= hi) return;
+    const uint64_t vectors = (uint64_t)(hi - lo) * p.vecs;
+    const Vec<T, V> zero = {};
+    for (uint64_t i = (uint64_t)part * blockDim.x + threadIdx.x; i < vectors; i += (uint64_t)p.pad_parts * blockDim.x) {
+        const uint64_t row = i / p.vecs;
+        const uint32_t c = (uint32_t)(i - row * p.vecs) * V;
+        store_row<T, V>(static_cast<T*>(p.r.y) + (lo + (int64_t)row) * p.r.ld_y + c, zero, (int)(p.r.width - c));
+    }
+}
+
+// This lane's token and vector; false if it has none.  WHOLE: a wavefront has one token, which the compiler is told.
+template <bool WHOLE> __device__ __forceinline__ bool lane_place(const MoveArgs& p, uint32_t block, uint32_t* token, uint32_t* vec)
+{
+    const uint32_t unit = block * (kMoveThreads >> p.lanes_log) + (threadIdx.x >> p.lanes_log);
+    if (unit >= p.units) return false;
+    uint32_t t = fdiv(unit, p.parts_div);
+    const uint32_t part = unit - t * p.parts;
+    if (WHOLE) t = __builtin_amdgcn_readfirstlane(t);
+    *token = t;
+    *vec = (part << p.lanes_log) + (threadIdx.x & ((1u << p.lanes_log) - 1));
+    return *vec < p.vecs;
+}
+
+constexpr int kTogether = 8;               // choices whose rows are in flight at a time
+
+template <typename T, bool WHOLE>
+__global__ __launch_bounds__(kMoveThreads) void gather_kernel(MoveArgs p)
+{
+    constexpr int V = RowVec<T>::value;
+    const uint32_t b = block_id();
+    if (b >= p.blocks) { clear_padding<T>(p, b); return; }
+    uint32_t t, vec;
+    if (!lane_place<WHOLE>(p, b, &t, &vec)) return;
+    const uint32_t c = vec * V;
+    const int n = (int)(p.r.width - c);
+    const Vec<T, V> x = load_row<T, V>(static_cast<const T*>(p.r.x) + (int64_t)t * p.r.ld_x + c, n);
+    const uint64_t a = (uint64_t)t * (uint32_t)p.r.topk;
+    for (int k0 = 0; k0 < p.r.topk; k0 += kTogether) {
+        uint32_t at[kTogether];             // read before anything is stored: scalar loads where the token is the wavefront's
+        float w[kTogether];
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) {
+            at[k] = k0 + k < p.r.topk ? (uint32_t)p.r.position[a + k0 + k] : ~0u;
+            w[k] = p.r.weights && k0 + k < p.r.topk ? p.r.weights[a + k0 + k] : 1.f;
+        }
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) {
+            if (at[k] >= p.r.row_count) continue;
+            T* to = static_cast<T*>(p.r.y) + (int64_t)at[k] * p.r.ld_y + c;
+            if (p.r.weights) {
+                float f[V];
+                widen(x, f);
+#pragma unroll
+                for (int i = 0; i < V; ++i) f[i] *= w[k];
+                Vec<T, V> r;
+                narrow(f, r);
+                store_row<T, V>(to, r, n);
+            } else {
+                store_row<T, V>(to, x, n);
+            }
+        }
+    }
+}
+
+template <typename T, bool WHOLE>
+__global__ __launch_bounds__(kMoveThreads) void combine_kernel(MoveArgs p)
+{
+    constexpr int V = RowVec<T>::value;
+    uint32_t t, vec;
+    if (!lane_place<WHOLE>(p, block_id(), &t, &vec)) return;
+    const uint32_t c = vec * V;
+    const int n = (int)(p.r.width - c);
+    const T* rows = static_cast<const T*>(p.r.rows) + c;
+    const uint64_t a = (uint64_t)t * (uint32_t)p.r.topk;
+    float sum[V] = {};
+    for (int k0 = 0; k0 < p.r.topk; k0 += kTogether) {
+        Vec<T, V> x[kTogether];
+        float w[kTogether];
+        bool here[kTogether];
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) {
+            x[k] = {};
+            w[k] = 1.f;
+            here[k] = false;
+            if (k0 + k < p.r.topk) {
+                const uint32_t at = (uint32_t)p.r.position[a + k0 + k];
+                here[k] = at < p.r.row_count;
+                if (here[k]) {
+                    x[k] = load_row<T, V>(rows + (int64_t)at * p.r.ld_rows, n);
+                    if (p.r.weights) w[k] = p.r.weights[a + k0 + k];
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) {
+            if (!here[k]) continue;
+            float f[V];
+            widen(x[k], f);
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum[i] = __builtin_fmaf(w[k], f[i], sum[i]);
+        }
+    }
+    T* to = static_cast<T*>(p.r.y) + (int64_t)t * p.r.ld_y + c;
+#pragma unroll
+    for (int i = 0; i < V; ++i) sum[i] *= p.r.alpha;
+    if (p.r.beta != 0.f) {
+        float f[V];
+        widen(load_row<T, V>(to, n), f);
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum[i] = __builtin_fmaf(p.r.beta, f[i], sum[i]);
+    }
+    Vec<T, V> r;
+    narrow(sum, r);
+    store_row<T, V>(to, r, n);
+}
+
+// The gradient: 2^lanes_log lanes walk over a whole row, because the dot products need all of it.  Their partial sums
+// meet by shuffles inside a wavefront and through LDS between wavefronts, always in the same order.
+template <typename T, bool WHOLE>
+__global__ __launch_bounds__(kSortThreads) void combine_grad_kernel(MoveArgs p)
+{
+    constexpr int V = RowVec<T>::value;
+    __shared__ float dots[kSortThreads / kWave][kTogether];
+    const uint32_t b = block_id();
+    if (b >= p.blocks) { clear_padding<T>(p, b); return; }
+    const uint32_t lanes = 1u << p.lanes_log, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> p.lanes_log;
+    uint32_t token = b * (blockDim.x >> p.lanes_log) + group;
+    if (WHOLE) token = __builtin_amdgcn_readfirstlane(token);
+    const bool some = token < p.r.tokens;
+    const uint32_t t = some ? token : 0;
+    const uint64_t a = (uint64_t)t * (uint32_t)p.r.topk;
+    const T* dy = static_cast<const T*>(p.r.x) + (int64_t)t * p.r.ld_x;
+    for (int k0 = 0; k0 < p.r.topk; k0 += kTogether) {
+        uint32_t at[kTogether];
+        float w[kTogether], dot[kTogether];
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) {
+            at[k] = ~0u;
+            w[k] = p.r.alpha;
+            dot[k] = 0.f;
+            if (some && k0 + k < p.r.topk) {
+                at[k] = (uint32_t)p.r.position[a + k0 + k];
+                if (p.r.weights) w[k] *= p.r.weights[a + k0 + k];
+            }
+        }
+        if (some)
+            for (uint32_t vec = lane; vec < p.vecs; vec += lanes) {
+                const uint32_t c = vec * V;
+                const int n = (int)(p.r.width - c);
+                float g[V];
+                widen(load_row<T, V>(dy + c, n), g);
+                Vec<T, V> x[kTogether];
+                if (p.r.dweights) {
+#pragma unroll
+                    for (int k = 0; k < kTogether; ++k) {
+                        x[k] = {};
+                        if (at[k] < p.r.row_count) x[k] = load_row<T, V>(static_cast<const T*>(p.r.rows) + (int64_t)at[k] * p.r.ld_rows + c, n);
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < kTogether; ++k) {
+                    if (at[k] >= p.r.row_count) continue;
+                    if (p.r.y) {
+                        float f[V];
+#pragma unroll
+                        for (int i = 0; i < V; ++i) f[i] = w[k] * g[i];
+                        Vec<T, V> r;
+                        narrow(f, r);
+                        store_row<T, V>(static_cast<T*>(p.r.y) + (int64_t)at[k] * p.r.ld_y + c, r, n);
+                    }
+                    if (p.r.dweights) {
+                        float f[V];
+                        widen(x[k], f);
+#pragma unroll
+                        for (int i = 0; i < V; ++i) dot[k] = __builtin_fmaf(g[i], f[i], dot[k]);
+                    }
+                }
+            }
+        if (!p.r.dweights) continue;
+        const uint32_t inside = lanes < kWave ? lanes : kWave;
+        for (uint32_t d = inside / 2; d > 0; d /= 2)
+#pragma unroll
+            for (int k = 0; k < kTogether; ++k) dot[k] += __shfl_xor(dot[k], (int)d);
+        if (lanes > kWave) {
+            __syncthreads();                // the last eight choices' sums have been read
+            if ((threadIdx.x & (kWave - 1)) == 0)
+#pragma unroll
+                for (int k = 0; k < kTogether; ++k) dots[threadIdx.x / kWave][k] = dot[k];
+            __syncthreads();
+            if (lane < kTogether && some && k0 + (int)lane < p.r.topk) {
+                const uint32_t waves = lanes / kWave;
+                float s = 0.f;
+                for (uint32_t w0 = 0; w0 < waves; ++w0) s += dots[group * waves + w0][lane];
+                p.r.dweights[a + k0 + lane] = p.r.alpha * s;
+            }
+        } else if (some && lane == 0) {
+#pragma unroll
+            for (int k = 0; k < kTogether; ++k)
+                if (k0 + k < p.r.topk) p.r.dweights[a + k0 + k] = p.r.alpha * dot[k];
+        }
+    }
+}
+
+template <typename T> MoveArgs move_args(const RowArgs& r)
+{
+    constexpr int V = RowVec<T>::value;
+    MoveArgs p = {};
+    p.r = r;
+    p.vecs = (r.width + V - 1) / V;
+    p.lanes_log = (uint32_t)log2_ceil(p.vecs < (uint32_t)kWave ? p.vecs : (uint32_t)kWave);
+    p.parts = (p.vecs + (1u << p.lanes_log) - 1) >> p.lanes_log;
+    p.parts_div = make_fastdiv(p.parts);
+    p.pad_parts = 1;
+    return p;
+}
+
+// Workgroups over the units, and behind them those that clear padding: one per expert and 32 KB that it may have to clear.
+template <typename T> int launch_units(const void* fn, MoveArgs& p, int threads, uint64_t units, uint64_t per_block, bool padding, void* stream)
+{
+    uint64_t blocks = (units + per_block - 1) / per_block, pads = 0;
+    if (units > INT32_MAX) return TTC_ERR_OVERFLOW;
+    p.units = (uint32_t)units;
+    p.blocks = (uint32_t)blocks;
+    if (padding && p.r.align > 1) {
+        const uint64_t bytes = (uint64_t)(p.r.align - 1) * p.r.width * sizeof(T), parts = (bytes + 32767) / 32768;
+        p.pad_parts = (uint32_t)(parts < 64 ? parts : 64);
+        pads = (uint64_t)p.r.experts * p.pad_parts;
+    }
+    p.total = (uint32_t)(blocks + pads);
+    return launch_blocks(fn, blocks + pads, threads, 0, &p, stream);
+}
+
+template <typename T> int launch_gather_type(const RowArgs& r, void* stream)
+{
+    MoveArgs p = move_args<T>(r);
+    const void* fn = p.lanes_log == 6 ? reinterpret_cast<const void*>(&gather_kernel<T, true>) : reinterpret_cast<const void*>(&gather_kernel<T, false>);
+    return launch_units<T>(fn, p, kMoveThreads, (uint64_t)r.tokens * p.parts, kMoveThreads >> p.lanes_log, true, stream);
+}
+
+template <typename T> int launch_combine_type(const RowArgs& r, void* stream)
+{
+    MoveArgs p = move_args<T>(r);
+    const void* fn = p.lanes_log == 6 ? reinterpret_cast<const void*>(&combine_kernel<T, true>) : reinterpret_cast<const void*>(&combine_kernel<T, false>);
+    return launch_units<T>(fn, p, kMoveThreads, (uint64_t)r.tokens * p.parts, kMoveThreads >> p.lanes_log, false, stream);
+}
+
+template <typename T> int launch_grad_type(const RowArgs& r, void* stream)
+{
+    MoveArgs p = move_args<T>(r);
+    p.lanes_log = (uint32_t)log2_ceil(p.vecs < (uint32_t)kSortThreads ? p.vecs : (uint32_t)kSortThreads);
+    const int threads = p.lanes_log > 8 ? 1 << p.lanes_log : kMoveThreads;
+    const void* fn = p.lanes_log >= 6 ? reinterpret_cast<const void*>(&combine_grad_kernel<T, true>) : reinterpret_cast<const void*>(&combine_grad_kernel<T, false>);
+    return launch_units<T>(fn, p, threads, r.tokens, (uint64_t)threads >> p.lanes_log, r.y != nullptr, stream);
+}
+
+}  // namespace
+
+#define TTC_BY_ROW_TYPE(launch, a, stream)                  \
+    switch ((a).dtype) {                                    \
+    case TTC_F32:  return launch<float>(a, stream);         \
+    case TTC_BF16: return launch<__bf16>(a, stream);        \
+    case TTC_F16:  return launch<_Float16>(a, stream);      \
+    default:       return TTC_ERR_UNSUPPORTED_DTYPE;        \
+    }
+
+int launch_gather(const RowArgs& a, void* stream) { TTC_BY_ROW_TYPE(launch_gather_type, a, stream) }
+int launch_combine(const RowArgs& a, void* stream) { TTC_BY_ROW_TYPE(launch_combine_type, a, stream) }
+int launch_combine_grad(const RowArgs& a, void* stream) { TTC_BY_ROW_TYPE(launch_grad_type, a, stream) }
+
+}  // namespace ttc
