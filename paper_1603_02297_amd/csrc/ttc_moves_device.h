@@ -29,20 +29,22 @@ template <> struct Chunk<2> { static constexpr int value = 2; };
 template <> struct Chunk<4> { static constexpr int value = 4; };
 template <> struct Chunk<8> { static constexpr int value = 4; };
 
-template <typename T, int V> __device__ __forceinline__ Vec<T, V> load_vec(const T* p)
+// NT: with the non-temporal hint.
+template <typename T, int V, bool NT> __device__ __forceinline__ Vec<T, V> load_vec(const T* p)
 {
     constexpr int C = Chunk<Vec<T, V>::kWords>::value;
     typedef typename Bits<C * 4>::type W;
     Vec<T, V> r;
 #pragma unroll
     for (int i = 0; i < Vec<T, V>::kWords / C; ++i) {
-        const W x = reinterpret_cast<const W*>(p)[i];
+        const W* from = reinterpret_cast<const W*>(p) + i;
+        const W x = NT ? __builtin_nontemporal_load(from) : *from;
         __builtin_memcpy(r.w + i * C, &x, sizeof(x));
     }
     return r;
 }
 
-template <typename T, int V> __device__ __forceinline__ void store_vec(T* p, const Vec<T, V>& r)
+template <typename T, int V, bool NT> __device__ __forceinline__ void store_vec(T* p, const Vec<T, V>& r)
 {
     constexpr int C = Chunk<Vec<T, V>::kWords>::value;
     typedef typename Bits<C * 4>::type W;
@@ -50,7 +52,8 @@ template <typename T, int V> __device__ __forceinline__ void store_vec(T* p, con
     for (int i = 0; i < Vec<T, V>::kWords / C; ++i) {
         W x;
         __builtin_memcpy(&x, r.w + i * C, sizeof(x));
-        reinterpret_cast<W*>(p)[i] = x;
+        W* to = reinterpret_cast<W*>(p) + i;
+        if (NT) __builtin_nontemporal_store(x, to); else *to = x;
     }
 }
 
@@ -74,13 +77,13 @@ template <typename T, int V> __device__ __forceinline__ void store_some(T* p, co
         if (i < n) p[i] = e[i];
 }
 
-template <typename T, int V> __device__ __forceinline__ Vec<T, V> load_row(const T* p, int n)
+template <typename T, int V, bool NT> __device__ __forceinline__ Vec<T, V> load_row(const T* p, int n)
 {
-    return n >= V ? load_vec<T, V>(p) : load_some<T, V>(p, n);
+    return n >= V ? load_vec<T, V, NT>(p) : load_some<T, V>(p, n);
 }
-template <typename T, int V> __device__ __forceinline__ void store_row(T* p, const Vec<T, V>& r, int n)
+template <typename T, int V, bool NT> __device__ __forceinline__ void store_row(T* p, const Vec<T, V>& r, int n)
 {
-    if (n >= V) store_vec<T, V>(p, r); else store_some<T, V>(p, r, n);
+    if (n >= V) store_vec<T, V, NT>(p, r); else store_some<T, V>(p, r, n);
 }
 
 // Widening is exact.

@@ -14,7 +14,7 @@ namespace {
 
 constexpr int kMapThreads = 256;
 constexpr int kMapEach = 4;                // listed positions per lane
-constexpr int kMapRequests = 4096;         // requests whose sums every workgroup makes for itself
+constexpr int kMapRequests = 2048;         // requests whose sums every workgroup makes for itself (16 bytes of LDS each)
 
 // sums stop at 2^31-1; adding up this way is associative, too
 __device__ __forceinline__ uint32_t capped(uint32_t a, uint32_t b) { return a + b < 0x7fffffffu ? a + b : 0x7fffffffu; }
@@ -69,47 +69,53 @@ __device__ __forceinline__ Two sums_before(Two v, uint32_t (*part)[2], Two* all)
     return before;
 }
 
-// Both prefix sums of all requests into `starts` and `page_starts` (LDS or global), each thread over neighbouring ones.
+// Both prefix sums of all requests, each thread over neighbouring ones: put(r, sums before r, request r), and at last
+// put(requests, sums of all, nothing).
 template <typename Put> __device__ __forceinline__ void sum_requests(const MapArgs& p, uint32_t (*part)[2], Put put)
 {
     const int each = (p.requests + (int)blockDim.x - 1) / (int)blockDim.x;
     const int64_t from = (int64_t)threadIdx.x * each;
     const int lo = (int)(from < p.requests ? from : p.requests), hi = lo + each < p.requests ? lo + each : p.requests;
+    Request q = {};
     Two mine = {0, 0};
-    for (int r = lo; r < hi; ++r) {
-        const Request q = request(p, r);
+    for (int r = hi - 1; r >= lo; --r) {    // backwards: the one left in q is the first that is put
+        q = request(p, r);
         mine.a = capped(mine.a, q.listed);
         mine.b = capped(mine.b, q.taken);
     }
     Two all, at = sums_before(mine, part, &all);
     for (int r = lo; r < hi; ++r) {
-        const Request q = request(p, r);
-        put(r, at);
+        if (r > lo) q = request(p, r);
+        put(r, at, q);
         at.a = capped(at.a, q.listed);
         at.b = capped(at.b, q.taken);
     }
-    if (threadIdx.x == 0) put(p.requests, all);
+    if (threadIdx.x == 0) put(p.requests, all, Request{});
 }
 
 __global__ __launch_bounds__(1024) void starts_kernel(MapArgs p)
 {
     __shared__ uint32_t part[1024 / kWave][2];
-    sum_requests(p, part, [&](int r, Two s) { p.starts[r] = (int32_t)s.a; p.page_starts[r] = (int32_t)s.b; });
+    sum_requests(p, part, [&](int r, Two s, const Request&) { p.starts[r] = (int32_t)s.a; p.page_starts[r] = (int32_t)s.b; });
 }
 
-// FUSED: makes the sums itself; otherwise starts_kernel has left them where they belong.
+// FUSED: makes the sums itself, and keeps what else it needs of the requests beside them; otherwise starts_kernel has left
+// the sums where they belong.
 template <bool FUSED>
 __global__ __launch_bounds__(kMapThreads) void map_kernel(MapArgs p)
 {
-    extern __shared__ uint32_t sums[];      // FUSED: starts, then page_starts
+    extern __shared__ uint32_t sums[];      // FUSED: starts, page_starts, first listed positions, pages held
     __shared__ uint32_t part[kMapThreads / kWave][2];
+    const int n = p.requests + 1;
     const uint32_t* starts = FUSED ? sums : reinterpret_cast<const uint32_t*>(p.starts);
-    const uint32_t* page_starts = FUSED ? sums + p.requests + 1 : reinterpret_cast<const uint32_t*>(p.page_starts);
+    const uint32_t* page_starts = FUSED ? sums + n : reinterpret_cast<const uint32_t*>(p.page_starts);
     const uint32_t block = block_id();
     if (FUSED) {
-        sum_requests(p, part, [&](int r, Two s) {
+        sum_requests(p, part, [&](int r, Two s, const Request& q) {
             sums[r] = s.a;
-            sums[p.requests + 1 + r] = s.b;
+            sums[n + r] = s.b;
+            sums[2 * n + r] = q.first;
+            sums[3 * n + r] = q.have;
             if (block == 0) { p.starts[r] = (int32_t)s.a; p.page_starts[r] = (int32_t)s.b; }
         });
         __syncthreads();
@@ -124,36 +130,62 @@ __global__ __launch_bounds__(kMapThreads) void map_kernel(MapArgs p)
         if (starts[mid] <= i0) lo = mid; else hi = mid;
     }
     int r = lo;
-    Request q = {};
-    if (r < p.requests) q = request(p, r);
+    uint32_t first = 0, have = 0;
+    auto take = [&] {
+        if (r >= p.requests) return;
+        if (FUSED) {
+            first = sums[2 * n + r];
+            have = sums[3 * n + r];
+        } else {
+            const Request q = request(p, r);
+            first = q.first;
+            have = q.have;
+        }
+    };
+    take();
     const int count = (uint64_t)p.tokens - i0 < kMapEach ? (int)((uint64_t)p.tokens - i0) : kMapEach;
-    for (int j = 0; j < count; ++j) {
+    // where every position's page is found, then the pages themselves: their loads are in flight together
+    const int32_t* from[kMapEach];
+    int32_t* entry[kMapEach];
+    int32_t inside[kMapEach], at[kMapEach], who[kMapEach];
+#pragma unroll
+    for (int j = 0; j < kMapEach; ++j) {
+        from[j] = nullptr;
+        entry[j] = nullptr;
+        inside[j] = 0;
+        at[j] = who[j] = -1;
         const uint32_t i = (uint32_t)i0 + j;
+        if (j >= count) continue;
         if (r < p.requests && i >= starts[r + 1]) {
             do ++r; while (r < p.requests && i >= starts[r + 1]);
-            if (r < p.requests) q = request(p, r);
+            take();
         }
-        int32_t slot = -1, at = -1, who = -1;
-        if (r < p.requests) {
-            const uint32_t pos = q.first + (i - starts[r]), block_no = fdiv(pos, p.page), inside = pos - block_no * p.page.div;
-            int32_t* entry = p.table + (int64_t)r * p.ld_table + block_no;
-            const bool fits = (int64_t)block_no < p.ld_table;
-            int32_t page = -1;
-            if (block_no < q.have) {
-                if (fits) page = *entry;
-            } else {
-                const uint64_t pick = (uint64_t)page_starts[r] + (block_no - q.have);
-                if (pick < (uint64_t)p.free_count) page = p.free_list[pick];
-            }
-            if ((uint32_t)page >= p.pages) page = -1;
-            if (block_no >= q.have && inside == 0 && fits) *entry = page;          // the first token of a page enters it
-            if (fits && page >= 0) slot = (int32_t)((uint32_t)page * p.page.div + inside);
-            at = (int32_t)pos;
-            who = r;
+        if (r >= p.requests) continue;
+        const uint32_t pos = first + (i - starts[r]), block_no = fdiv(pos, p.page);
+        inside[j] = (int32_t)(pos - block_no * p.page.div);
+        at[j] = (int32_t)pos;
+        who[j] = r;
+        if ((int64_t)block_no >= p.ld_table) continue;
+        int32_t* e = p.table + (int64_t)r * p.ld_table + block_no;
+        if (block_no < have) {
+            from[j] = e;
+        } else {
+            const uint64_t pick = (uint64_t)page_starts[r] + (block_no - have);
+            if (pick < (uint64_t)p.free_count) from[j] = p.free_list + pick;
+            if (inside[j] == 0) entry[j] = e;           // the first token of a page enters it
         }
-        p.slots[i] = slot;
-        if (p.positions) p.positions[i] = at;
-        if (p.owner) p.owner[i] = who;
+    }
+    int32_t page[kMapEach];
+#pragma unroll
+    for (int j = 0; j < kMapEach; ++j) page[j] = from[j] ? *from[j] : -1;
+#pragma unroll
+    for (int j = 0; j < kMapEach; ++j) {
+        if (j >= count) continue;
+        if ((uint32_t)page[j] >= p.pages) page[j] = -1;
+        if (entry[j]) *entry[j] = page[j];
+        p.slots[i0 + j] = page[j] >= 0 ? (int32_t)((uint32_t)page[j] * p.page.div + (uint32_t)inside[j]) : -1;
+        if (p.positions) p.positions[i0 + j] = at[j];
+        if (p.owner) p.owner[i0 + j] = who[j];
     }
 }
 
@@ -166,7 +198,7 @@ int launch_map(const MapArgs& a, void* stream)
     const uint64_t per_block = (uint64_t)kMapThreads * kMapEach;
     uint64_t blocks = ((uint64_t)p.tokens + per_block - 1) / per_block;
     if (fused) {
-        const size_t lds = 2 * sizeof(uint32_t) * (size_t)(p.requests + 1);
+        const size_t lds = 4 * sizeof(uint32_t) * (size_t)(p.requests + 1);
         return launch_blocks(reinterpret_cast<const void*>(&map_kernel<true>), blocks ? blocks : 1, kMapThreads, lds, &p, stream);
     }
     const int st = launch_blocks(reinterpret_cast<const void*>(&starts_kernel), 1, 1024, 0, &p, stream);
@@ -193,18 +225,43 @@ template <typename T, typename C> struct SlotVec { static constexpr int value = 
 template <typename T, typename C, bool WRITE> struct SlotTypes { typedef T from; typedef C to; };
 template <typename T, typename C> struct SlotTypes<T, C, false> { typedef C from; typedef T to; };
 
-// from -> to, through float with the head's scale where the cache is narrower
-template <typename T, typename C, bool WRITE, int V>
-__device__ __forceinline__ void convert(const Vec<typename SlotTypes<T, C, WRITE>::from, V>& x, float scale, Vec<typename SlotTypes<T, C, WRITE>::to, V>& r)
+// Into the narrower cache: x / scale.  Divisions cost a dozen instructions each, enough to bound the kernel by arithmetic (524 MB
+// in 97 us with them, 89 without; 33 MB 5.9 and 5.2).  With r = 1 / scale rounded once, q = x * r is off by two units at most, and q + (x - q * scale) * r rounds the quotient
+// itself: ties of the 8-bit format, which are quotients that 32 bits hold, stay ties.  q is held to +-512 before that, so that an infinite
+// one does not become a NaN; beyond 448 the cut follows anyhow.  Scales outside 2^-60 .. 2^60, where r or the remainder could leave the
+// normal range, take the division.
+template <typename From, typename To, int V>
+__device__ __forceinline__ void convert_in(const Vec<From, V>& x, float scale, Vec<To, V>& r)
+{
+    float f[V];
+    widen(x, f);
+    const float size = __builtin_fabsf(scale);
+    if (size >= 0x1p-60f && size <= 0x1p60f) {
+        const float inverse = 1.f / scale;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const float q = __builtin_fminf(__builtin_fmaxf(f[i] * inverse, -512.f), 512.f);
+            f[i] = __builtin_fmaf(__builtin_fmaf(-q, scale, f[i]), inverse, q);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[i] = f[i] / scale;
+    }
+    narrow(f, r);
+}
+
+// And out of it.
+template <typename From, typename To, int V>
+__device__ __forceinline__ void convert_out(const Vec<From, V>& x, float scale, Vec<To, V>& r)
 {
     float f[V];
     widen(x, f);
 #pragma unroll
-    for (int i = 0; i < V; ++i) f[i] = WRITE ? f[i] / scale : f[i] * scale;
+    for (int i = 0; i < V; ++i) f[i] *= scale;
     narrow(f, r);
 }
 
-template <typename T, typename C, bool WRITE>
+template <typename T, typename C, bool WRITE, bool NTL, bool NTS>
 __global__ __launch_bounds__(kMoveThreads) void slots_kernel(PlaceArgs p)
 {
     constexpr int V = SlotVec<T, C>::value;
@@ -226,25 +283,33 @@ __global__ __launch_bounds__(kMoveThreads) void slots_kernel(PlaceArgs p)
     const bool both = p.s.v_out != nullptr;
     Vec<From, V> k = {}, v = {};
     if (here) {
-        k = load_row<From, V>(static_cast<const From*>(p.s.k) + (WRITE ? at_k : in_cache), n);
-        if (both) v = load_row<From, V>(static_cast<const From*>(p.s.v) + (WRITE ? at_v : in_cache), n);
+        k = load_row<From, V, NTL>(static_cast<const From*>(p.s.k) + (WRITE ? at_k : in_cache), n);
+        if (both) v = load_row<From, V, NTL>(static_cast<const From*>(p.s.v) + (WRITE ? at_v : in_cache), n);
     }
     To* to_k = static_cast<To*>(p.s.k_out) + (WRITE ? in_cache : at_k);
     To* to_v = static_cast<To*>(p.s.v_out) + (WRITE ? in_cache : at_v);
     if constexpr (same) {
-        store_row<To, V>(to_k, k, n);
-        if (both) store_row<To, V>(to_v, v, n);
+        store_row<To, V, NTS>(to_k, k, n);
+        if (both) store_row<To, V, NTS>(to_v, v, n);
     } else {
         const float scale_k = p.s.k_scale ? p.s.k_scale[head] : 1.f, scale_v = p.s.v_scale ? p.s.v_scale[head] : 1.f;
         Vec<To, V> r = {};
-        if (here) convert<T, C, WRITE, V>(k, scale_k, r);       // nowhere: zero, whatever the scale
-        store_row<To, V>(to_k, r, n);
+        auto convert = [](const Vec<From, V>& x, float scale, Vec<To, V>& y) {
+            if constexpr (WRITE) convert_in(x, scale, y); else convert_out(x, scale, y);
+        };
+        if (here) convert(k, scale_k, r);       // nowhere: zero, whatever the scale
+        store_row<To, V, NTS>(to_k, r, n);
         if (both) {
-            if (here) convert<T, C, WRITE, V>(v, scale_v, r);
-            store_row<To, V>(to_v, r, n);
+            if (here) convert(v, scale_v, r);
+            store_row<To, V, NTS>(to_v, r, n);
         }
     }
 }
+
+// Non-temporal hints by the bytes moved, stores from 16 MB, loads from 256 MB on.  Measured with 8 heads of 128 bf16 into (out of) pages of
+// bf16, without hints, stores only, both: 44 MB 8.1, 8.1, 10.0 us (8.4, 8.0, 9.8); 175 MB 35.4, 29.4, 31.9 (36.3, 28.6, 30.9); 700 MB
+// 130, 123, 122 (132, 123, 117); with an 8-bit cache 33 MB 9.1, 8.1, 8.5 (7.1, 6.5, 8.6); 524 MB 101, 98, 97 (96, 89, 88).
+constexpr uint64_t kStreamStores = uint64_t(16) << 20, kStreamLoads = uint64_t(256) << 20;
 
 template <typename T, typename C, bool WRITE> int launch_slots_types(const SlotArgs& a, void* stream)
 {
@@ -269,7 +334,11 @@ template <typename T, typename C, bool WRITE> int launch_slots_types(const SlotA
             if (a.v_out) p.s.v_out = static_cast<char*>(a.v_out) + skip_v;
         }
         p.units = tokens * per_token;
-        const int st = launch_blocks(reinterpret_cast<const void*>(&slots_kernel<T, C, WRITE>), ((uint64_t)p.units + kMoveThreads - 1) / kMoveThreads, kMoveThreads, 0, &p, stream);
+        const uint64_t bytes = (uint64_t)tokens * a.heads * a.dim * (sizeof(T) + sizeof(C)) * (a.v_out ? 2 : 1);
+        const void* fn = bytes < kStreamStores ? reinterpret_cast<const void*>(&slots_kernel<T, C, WRITE, false, false>)
+                       : bytes < kStreamLoads ? reinterpret_cast<const void*>(&slots_kernel<T, C, WRITE, false, true>)
+                                              : reinterpret_cast<const void*>(&slots_kernel<T, C, WRITE, true, true>);
+        const int st = launch_blocks(fn, ((uint64_t)p.units + kMoveThreads - 1) / kMoveThreads, kMoveThreads, 0, &p, stream);
         if (st != TTC_OK) return st;
     }
     return TTC_OK;

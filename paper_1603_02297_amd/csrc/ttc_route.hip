@@ -39,15 +39,15 @@ __device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t* part, uint3
     }
     if (lane == kWave - 1) part[wave] = s;
     __syncthreads();
-    uint32_t before = 0, total = 0;
-    for (int w = 0; w < waves; ++w) {
-        const uint32_t x = part[w];
-        before += w < wave ? x : 0;
-        total += x;
+    uint32_t w = lane < waves ? part[lane] : 0;          // the wavefronts' sums, summed by every wavefront for itself
+#pragma unroll
+    for (int d = 1; d < kSortThreads / kWave; d *= 2) {
+        const uint32_t o = __shfl_up(w, d);
+        if (lane >= d) w += o;
     }
-    __syncthreads();
-    *all = total;
-    return before + s - v;
+    *all = __shfl(w, waves - 1);
+    const uint32_t before = __shfl(w, wave > 0 ? wave - 1 : 0);
+    return (wave > 0 ? before : 0) + s - v;
 }
 
 __device__ __forceinline__ uint32_t padded(uint32_t count, uint32_t align) { return (count + align - 1) / align * align; }
@@ -67,9 +67,6 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(SortArgs p)
     uint32_t* row = part + kSortThreads / kWave;
     volatile uint16_t* counter = reinterpret_cast<volatile uint16_t*>(row + experts);
     const uint32_t chunk = blockIdx.x;
-    for (int i = threadIdx.x; i < waves * experts; i += blockDim.x) counter[i] = 0;
-    if (p.source)                           // -1 everywhere; the rows that hold an assignment are written after it
-        for (uint64_t i = (uint64_t)chunk * blockDim.x + threadIdx.x; i < p.rows; i += (uint64_t)gridDim.x * blockDim.x) p.source[i] = -1;
     uint32_t e[B], rank[B];
     const uint64_t start = ((uint64_t)chunk * waves + wave) * (B * kWave) + lane;
 #pragma unroll
@@ -77,6 +74,9 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(SortArgs p)
         const uint64_t a = start + b * kWave;
         e[b] = a < p.n ? expert_of(p, (uint32_t)a) : (uint32_t)experts;
     }
+    for (int i = threadIdx.x; i < waves * experts; i += blockDim.x) counter[i] = 0;
+    if (p.source)                           // -1 everywhere; the rows that hold an assignment are written after it
+        for (uint64_t i = (uint64_t)chunk * blockDim.x + threadIdx.x; i < p.rows; i += (uint64_t)gridDim.x * blockDim.x) p.source[i] = -1;
     __syncthreads();
     volatile uint16_t* mine = counter + wave * experts;
     const int bits = 32 - __clz(experts);   // experts itself (nowhere) has to be told apart, too
@@ -101,12 +101,17 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(SortArgs p)
     __syncthreads();
     // one thread per expert: its counters become sums over the wavefronts before
     uint32_t total = 0;
-    if ((int)threadIdx.x < experts)
-        for (int w = 0; w < waves; ++w) {
-            const uint32_t c = counter[w * experts + threadIdx.x];
-            counter[w * experts + threadIdx.x] = (uint16_t)total;
-            total += c;
+    if ((int)threadIdx.x < experts) {
+        uint16_t* column = const_cast<uint16_t*>(counter) + threadIdx.x;
+        uint32_t held[kSortThreads / kWave];
+#pragma unroll
+        for (int w = 0; w < kSortThreads / kWave; ++w) held[w] = w < waves ? column[w * experts] : 0;
+#pragma unroll
+        for (int w = 0; w < kSortThreads / kWave; ++w) {
+            if (w < waves) column[w * experts] = (uint16_t)total;
+            total += held[w];
         }
+    }
     if (ALONE) {
         uint32_t all;
         const uint32_t first = sum_before(padded(total, (uint32_t)p.align), part, &all);
@@ -157,14 +162,23 @@ __global__ __launch_bounds__(kSortThreads) void sum_kernel(int32_t* hist, int64_
 
 // Ranks within a chunk become rows.  SUMMED: sum_kernel has been over the counts; otherwise every workgroup adds up
 // those of the other chunks by itself (a few 64 KB out of L2), which saves a launch.
-template <bool SUMMED>
-__global__ __launch_bounds__(kSortThreads) void place_kernel(SortArgs p, int64_t chunk_len, int32_t chunks)
+template <int B, bool SUMMED>
+__global__ __launch_bounds__(kSortThreads) void place_kernel(SortArgs p, int32_t chunks)
 {
     extern __shared__ __align__(16) unsigned char lds[];
     uint32_t* part = reinterpret_cast<uint32_t*>(lds);
     uint32_t* row = part + kSortThreads / kWave;
     uint32_t* sums = row + p.experts;       // totals; only where not SUMMED
     const int experts = p.experts, chunk = blockIdx.x;
+    // what the last step needs, on its way while the counts are added up
+    uint32_t expert[B], rank[B];
+    const uint64_t start = (uint64_t)chunk * (B * kSortThreads) + threadIdx.x;
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+        const uint64_t a = start + b * kSortThreads;
+        expert[b] = a < p.n ? expert_of(p, (uint32_t)a) : (uint32_t)experts;
+        rank[b] = a < p.n ? (uint32_t)p.position[a] : 0;
+    }
     uint32_t total = 0, before = 0;
     if (SUMMED) {
         if ((int)threadIdx.x < experts) {
@@ -205,11 +219,11 @@ __global__ __launch_bounds__(kSortThreads) void place_kernel(SortArgs p, int64_t
     }
     if (chunk == 0 && threadIdx.x == 0) p.offsets[experts] = (int32_t)all;
     __syncthreads();
-    const uint64_t lo = (uint64_t)chunk * (uint64_t)chunk_len, end = lo + (uint64_t)chunk_len, hi = end < p.n ? end : p.n;
-    for (uint64_t a = lo + threadIdx.x; a < hi; a += kSortThreads) {
-        const uint32_t e = expert_of(p, (uint32_t)a);
-        if (e >= (uint32_t)experts) continue;                       // its position is -1 already
-        const uint32_t at = (uint32_t)p.position[a] + row[e];
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+        if (expert[b] >= (uint32_t)experts) continue;               // its position is -1 already
+        const uint64_t a = start + b * kSortThreads;
+        const uint32_t at = rank[b] + row[expert[b]];
         p.position[a] = (int32_t)at;
         if (p.source) p.source[at] = (int32_t)a;
     }
@@ -222,17 +236,17 @@ template <int B> int launch_sort_blocks(const SortArgs& p, const SortShape& s, v
     if (s.chunks == 1) return launch_blocks(reinterpret_cast<const void*>(&sort_kernel<B, true>), 1, s.threads, lds, const_cast<SortArgs*>(&p), stream);
     hipStream_t st = (hipStream_t)stream;
     SortArgs a = p;
-    int64_t len = s.chunk, chunks64 = s.chunks;
+    int64_t chunks64 = s.chunks;
     int32_t chunks = (int32_t)s.chunks;
     int experts = p.experts;
     void* sort_args[] = {&a};
     void* sum_args[] = {&a.hist, &chunks64, &experts};
-    void* place_args[] = {&a, &len, &chunks};
+    void* place_args[] = {&a, &chunks};
     const bool summed = s.chunks > kSortSums;
     if (hipLaunchKernel(reinterpret_cast<const void*>(&sort_kernel<B, false>), dim3((uint32_t)chunks), dim3(s.threads), sort_args, lds, st) != hipSuccess) return TTC_ERR_HIP;
     if (summed && hipLaunchKernel(reinterpret_cast<const void*>(&sum_kernel), dim3((uint32_t)((experts + kWave - 1) / kWave)), dim3(kSortThreads), sum_args, 0, st) != hipSuccess)
         return TTC_ERR_HIP;
-    const void* place = summed ? reinterpret_cast<const void*>(&place_kernel<true>) : reinterpret_cast<const void*>(&place_kernel<false>);
+    const void* place = summed ? reinterpret_cast<const void*>(&place_kernel<B, true>) : reinterpret_cast<const void*>(&place_kernel<B, false>);
     const size_t place_lds = head + (summed ? 0 : sizeof(uint32_t) * (size_t)experts);
     return hipLaunchKernel(place, dim3((uint32_t)chunks), dim3(kSortThreads), place_args, place_lds, st) == hipSuccess ? TTC_OK : TTC_ERR_HIP;
 }
@@ -267,7 +281,7 @@ struct MoveArgs {
 };
 
 // Padding rows of expert `e`: those of its segment that hold no token, cleared by `pad_parts` workgroups.
-template <typename T> __device__ __forceinline__ void clear_padding(const MoveArgs& p, uint32_t block)
+template <typename T, bool NT> __device__ __forceinline__ void clear_padding(const MoveArgs& p, uint32_t block)
 {
     constexpr int V = RowVec<T>::value;
     if (block >= p.total) return;
@@ -281,7 +295,7 @@ template <typename T> __device__ __forceinline__ void clear_padding(const MoveAr
     for (uint64_t i = (uint64_t)part * blockDim.x + threadIdx.x; i < vectors; i += (uint64_t)p.pad_parts * blockDim.x) {
         const uint64_t row = i / p.vecs;
         const uint32_t c = (uint32_t)(i - row * p.vecs) * V;
-        store_row<T, V>(static_cast<T*>(p.r.y) + (lo + (int64_t)row) * p.r.ld_y + c, zero, (int)(p.r.width - c));
+        store_row<T, V, NT>(static_cast<T*>(p.r.y) + (lo + (int64_t)row) * p.r.ld_y + c, zero, (int)(p.r.width - c));
     }
 }
 
@@ -300,17 +314,17 @@ template <bool WHOLE> __device__ __forceinline__ bool lane_place(const MoveArgs&
 
 constexpr int kTogether = 8;               // choices whose rows are in flight at a time
 
-template <typename T, bool WHOLE>
+template <typename T, bool WHOLE, bool NT>
 __global__ __launch_bounds__(kMoveThreads) void gather_kernel(MoveArgs p)
 {
     constexpr int V = RowVec<T>::value;
     const uint32_t b = block_id();
-    if (b >= p.blocks) { clear_padding<T>(p, b); return; }
+    if (b >= p.blocks) { clear_padding<T, NT>(p, b); return; }
     uint32_t t, vec;
     if (!lane_place<WHOLE>(p, b, &t, &vec)) return;
     const uint32_t c = vec * V;
     const int n = (int)(p.r.width - c);
-    const Vec<T, V> x = load_row<T, V>(static_cast<const T*>(p.r.x) + (int64_t)t * p.r.ld_x + c, n);
+    const Vec<T, V> x = load_row<T, V, false>(static_cast<const T*>(p.r.x) + (int64_t)t * p.r.ld_x + c, n);
     const uint64_t a = (uint64_t)t * (uint32_t)p.r.topk;
     for (int k0 = 0; k0 < p.r.topk; k0 += kTogether) {
         uint32_t at[kTogether];             // read before anything is stored: scalar loads where the token is the wavefront's
@@ -331,15 +345,15 @@ __global__ __launch_bounds__(kMoveThreads) void gather_kernel(MoveArgs p)
                 for (int i = 0; i < V; ++i) f[i] *= w[k];
                 Vec<T, V> r;
                 narrow(f, r);
-                store_row<T, V>(to, r, n);
+                store_row<T, V, NT>(to, r, n);
             } else {
-                store_row<T, V>(to, x, n);
+                store_row<T, V, NT>(to, x, n);
             }
         }
     }
 }
 
-template <typename T, bool WHOLE>
+template <typename T, bool WHOLE, bool NT>
 __global__ __launch_bounds__(kMoveThreads) void combine_kernel(MoveArgs p)
 {
     constexpr int V = RowVec<T>::value;
@@ -363,7 +377,7 @@ __global__ __launch_bounds__(kMoveThreads) void combine_kernel(MoveArgs p)
                 const uint32_t at = (uint32_t)p.r.position[a + k0 + k];
                 here[k] = at < p.r.row_count;
                 if (here[k]) {
-                    x[k] = load_row<T, V>(rows + (int64_t)at * p.r.ld_rows, n);
+                    x[k] = load_row<T, V, NT>(rows + (int64_t)at * p.r.ld_rows, n);
                     if (p.r.weights) w[k] = p.r.weights[a + k0 + k];
                 }
             }
@@ -382,24 +396,24 @@ __global__ __launch_bounds__(kMoveThreads) void combine_kernel(MoveArgs p)
     for (int i = 0; i < V; ++i) sum[i] *= p.r.alpha;
     if (p.r.beta != 0.f) {
         float f[V];
-        widen(load_row<T, V>(to, n), f);
+        widen(load_row<T, V, NT>(to, n), f);
 #pragma unroll
         for (int i = 0; i < V; ++i) sum[i] = __builtin_fmaf(p.r.beta, f[i], sum[i]);
     }
     Vec<T, V> r;
     narrow(sum, r);
-    store_row<T, V>(to, r, n);
+    store_row<T, V, NT>(to, r, n);
 }
 
 // The gradient: 2^lanes_log lanes walk over a whole row, because the dot products need all of it.  Their partial sums
 // meet by shuffles inside a wavefront and through LDS between wavefronts, always in the same order.
-template <typename T, bool WHOLE>
+template <typename T, bool WHOLE, bool NT>
 __global__ __launch_bounds__(kSortThreads) void combine_grad_kernel(MoveArgs p)
 {
     constexpr int V = RowVec<T>::value;
     __shared__ float dots[kSortThreads / kWave][kTogether];
     const uint32_t b = block_id();
-    if (b >= p.blocks) { clear_padding<T>(p, b); return; }
+    if (b >= p.blocks) { clear_padding<T, NT>(p, b); return; }
     const uint32_t lanes = 1u << p.lanes_log, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> p.lanes_log;
     uint32_t token = b * (blockDim.x >> p.lanes_log) + group;
     if (WHOLE) token = __builtin_amdgcn_readfirstlane(token);
@@ -425,13 +439,13 @@ __global__ __launch_bounds__(kSortThreads) void combine_grad_kernel(MoveArgs p)
                 const uint32_t c = vec * V;
                 const int n = (int)(p.r.width - c);
                 float g[V];
-                widen(load_row<T, V>(dy + c, n), g);
+                widen(load_row<T, V, false>(dy + c, n), g);
                 Vec<T, V> x[kTogether];
                 if (p.r.dweights) {
 #pragma unroll
                     for (int k = 0; k < kTogether; ++k) {
                         x[k] = {};
-                        if (at[k] < p.r.row_count) x[k] = load_row<T, V>(static_cast<const T*>(p.r.rows) + (int64_t)at[k] * p.r.ld_rows + c, n);
+                        if (at[k] < p.r.row_count) x[k] = load_row<T, V, NT>(static_cast<const T*>(p.r.rows) + (int64_t)at[k] * p.r.ld_rows + c, n);
                     }
                 }
 #pragma unroll
@@ -443,7 +457,7 @@ __global__ __launch_bounds__(kSortThreads) void combine_grad_kernel(MoveArgs p)
                         for (int i = 0; i < V; ++i) f[i] = w[k] * g[i];
                         Vec<T, V> r;
                         narrow(f, r);
-                        store_row<T, V>(static_cast<T*>(p.r.y) + (int64_t)at[k] * p.r.ld_y + c, r, n);
+                        store_row<T, V, NT>(static_cast<T*>(p.r.y) + (int64_t)at[k] * p.r.ld_y + c, r, n);
                     }
                     if (p.r.dweights) {
                         float f[V];
@@ -491,6 +505,19 @@ template <typename T> MoveArgs move_args(const RowArgs& r)
     return p;
 }
 
+// Non-temporal accesses to the sorted rows, by their size: what will not stay in the last-level cache anyhow does better
+// without pushing the rest out.  Measured at 4096 bf16, 256 to 8192 tokens, three sets of tensors in turn:
+//   gather (stores of rows; x stays plain): 8 choices, 512 tokens 15.9 us with the hint, 17.2 without; 2048: 35.0, 39.8; 8192: 109, 119
+//   combine (rows and y): 8 choices, 1024 tokens 13.5, 12.5; 2048: 26.2, 30.8; 8192: 104, 117
+//   gradient (rows and drows; dy stays plain): 4 choices, 512 tokens 15.5, 15.5; 1024: 26.9, 31.6; 8192: 173, 193
+constexpr uint64_t kStreamGather = uint64_t(32) << 20, kStreamCombine = uint64_t(96) << 20, kStreamGrad = uint64_t(24) << 20;
+template <typename T> bool streams(const RowArgs& r, uint64_t from) { return (uint64_t)r.tokens * r.topk * r.width * sizeof(T) >= from; }
+
+inline const void* pick(bool whole, bool nt, void (*wn)(MoveArgs), void (*w)(MoveArgs), void (*n)(MoveArgs), void (*plain)(MoveArgs))
+{
+    return reinterpret_cast<const void*>(whole ? (nt ? wn : w) : (nt ? n : plain));
+}
+
 // Workgroups over the units, and behind them those that clear padding: one per expert and 32 KB that it may have to clear.
 template <typename T> int launch_units(const void* fn, MoveArgs& p, int threads, uint64_t units, uint64_t per_block, bool padding, void* stream)
 {
@@ -510,14 +537,14 @@ template <typename T> int launch_units(const void* fn, MoveArgs& p, int threads,
 template <typename T> int launch_gather_type(const RowArgs& r, void* stream)
 {
     MoveArgs p = move_args<T>(r);
-    const void* fn = p.lanes_log == 6 ? reinterpret_cast<const void*>(&gather_kernel<T, true>) : reinterpret_cast<const void*>(&gather_kernel<T, false>);
+    const void* fn = pick(p.lanes_log == 6, streams<T>(r, kStreamGather), &gather_kernel<T, true, true>, &gather_kernel<T, true, false>, &gather_kernel<T, false, true>, &gather_kernel<T, false, false>);
     return launch_units<T>(fn, p, kMoveThreads, (uint64_t)r.tokens * p.parts, kMoveThreads >> p.lanes_log, true, stream);
 }
 
 template <typename T> int launch_combine_type(const RowArgs& r, void* stream)
 {
     MoveArgs p = move_args<T>(r);
-    const void* fn = p.lanes_log == 6 ? reinterpret_cast<const void*>(&combine_kernel<T, true>) : reinterpret_cast<const void*>(&combine_kernel<T, false>);
+    const void* fn = pick(p.lanes_log == 6, streams<T>(r, kStreamCombine), &combine_kernel<T, true, true>, &combine_kernel<T, true, false>, &combine_kernel<T, false, true>, &combine_kernel<T, false, false>);
     return launch_units<T>(fn, p, kMoveThreads, (uint64_t)r.tokens * p.parts, kMoveThreads >> p.lanes_log, false, stream);
 }
 
@@ -526,7 +553,7 @@ template <typename T> int launch_grad_type(const RowArgs& r, void* stream)
     MoveArgs p = move_args<T>(r);
     p.lanes_log = (uint32_t)log2_ceil(p.vecs < (uint32_t)kSortThreads ? p.vecs : (uint32_t)kSortThreads);
     const int threads = p.lanes_log > 8 ? 1 << p.lanes_log : kMoveThreads;
-    const void* fn = p.lanes_log >= 6 ? reinterpret_cast<const void*>(&combine_grad_kernel<T, true>) : reinterpret_cast<const void*>(&combine_grad_kernel<T, false>);
+    const void* fn = pick(p.lanes_log >= 6, streams<T>(r, kStreamGrad), &combine_grad_kernel<T, true, true>, &combine_grad_kernel<T, true, false>, &combine_grad_kernel<T, false, true>, &combine_grad_kernel<T, false, false>);
     return launch_units<T>(fn, p, threads, r.tokens, (uint64_t)threads >> p.lanes_log, r.y != nullptr, stream);
 }
 
