@@ -16,9 +16,10 @@ SortShape sort_shape(int64_t n, int experts)
     if (n <= kSortThreads) {                // as few wavefronts as hold the ids; a thread for every expert
         const int64_t need = std::max<int64_t>(std::max<int64_t>(n, experts), 1);
         s.threads = (int)((need + kWave - 1) / kWave * kWave);
-    } else {
-        const int64_t most = n <= kSortOne ? 1 : kSortSums;
-        while (s.blocks < kSortBlocks && (n + s.blocks * kSortThreads - 1) / (s.blocks * kSortThreads) > most) s.blocks *= 2;
+    } else if (n <= kSortOne) {
+        s.blocks = kSortOneBlocks;
+    } else {                                // as many workgroups as may add up each other's counts, and beyond that as few as can be
+        while (s.blocks < kSortBlocks && (n + s.blocks * s.threads - 1) / (s.blocks * s.threads) > kSortSums) s.blocks *= 2;
     }
     s.chunk = (int64_t)s.threads * s.blocks;
     s.chunks = std::max<int64_t>(1, (n + s.chunk - 1) / s.chunk);

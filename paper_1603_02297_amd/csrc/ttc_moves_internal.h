@@ -29,7 +29,9 @@ namespace ttc {
 constexpr int kMoveThreads = 256;          // workgroup of the row moves
 constexpr int kSortThreads = 1024;         // largest workgroup of the sort
 constexpr int kSortBlocks = 8;             // ids a lane of the sort holds at most
-constexpr int kSortOne = 8192;             // assignments up to which one workgroup sorts alone
+constexpr int kSortOneBlocks = 2;          // and where one workgroup sorts alone: 2048 ids in 4.7 us, two kernels of two workgroups 3.4 + 3.2 and the
+                                           // way from one to the other; 4000 ids the other way round (7.5 us alone)
+constexpr int kSortOne = kSortOneBlocks * kSortThreads;
 constexpr int kSortSums = 128;             // chunks up to which every workgroup adds up the counts of the others by itself
 
 inline int elem_bytes(int dtype) { return dtype == TTC_F32 ? 4 : dtype == TTC_F8 ? 1 : 2; }

@@ -12,12 +12,13 @@ namespace ttc {
 // ---------------------------------------------------------------------------------
 namespace {
 
-constexpr int kMapThreads = 256;
-constexpr int kMapEach = 4;                // listed positions per lane
-constexpr int kMapRequests = 2048;         // requests whose sums every workgroup makes for itself (16 bytes of LDS each)
+constexpr int kMapThreads = 1024;          // largest workgroup
+constexpr int kMapRequests = 4000;         // requests whose sums every workgroup makes for itself (16 bytes of LDS each)
 
 // sums stop at 2^31-1; adding up this way is associative, too
 __device__ __forceinline__ uint32_t capped(uint32_t a, uint32_t b) { return a + b < 0x7fffffffu ? a + b : 0x7fffffffu; }
+
+constexpr int kMapFew = 1 << 18;           // 200,000 positions of 2000 requests 6.2 us with one per lane, 9.4 with four; 1,000,000 14.4 and 11.0
 
 struct Request {
     uint32_t first, have, listed, taken;   // first listed position, pages held, positions listed, pages to take
@@ -47,50 +48,51 @@ struct Two { uint32_t a, b; };
 __device__ __forceinline__ Two sums_before(Two v, uint32_t (*part)[2], Two* all)
 {
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
-    Two s = v;
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-        const uint32_t a = __shfl_up(s.a, d), b = __shfl_up(s.b, d);
-        if (lane >= d) { s.a = capped(s.a, a); s.b = capped(s.b, b); }
-    }
+    const Two s = {over_lanes(v.a, capped), over_lanes(v.b, capped)};
     if (lane == kWave - 1) { part[wave][0] = s.a; part[wave][1] = s.b; }
     __syncthreads();
-    Two before = {0, 0}, total = {0, 0};
-    for (int w = 0; w < waves; ++w) {
-        if (w == wave) before = total;
-        total.a = capped(total.a, part[w][0]);
-        total.b = capped(total.b, part[w][1]);
-    }
-    __syncthreads();
-    *all = total;
-    // the lanes before in this wavefront
-    const uint32_t a = __shfl_up(s.a, 1), b = __shfl_up(s.b, 1);
-    if (lane > 0) { before.a = capped(before.a, a); before.b = capped(before.b, b); }
-    return before;
+    // the wavefronts' sums, summed by every wavefront for itself
+    const Two w = {over_lanes(lane < waves ? part[lane][0] : 0, capped), over_lanes(lane < waves ? part[lane][1] : 0, capped)};
+    all->a = __shfl(w.a, waves - 1);
+    all->b = __shfl(w.b, waves - 1);
+    const uint32_t a = __shfl_up(s.a, 1), b = __shfl_up(s.b, 1);               // the lanes before in this wavefront
+    const uint32_t wa = __shfl(w.a, wave > 0 ? wave - 1 : 0), wb = __shfl(w.b, wave > 0 ? wave - 1 : 0);
+    return {capped(wave > 0 ? wa : 0, lane > 0 ? a : 0), capped(wave > 0 ? wb : 0, lane > 0 ? b : 0)};
 }
 
-// Both prefix sums of all requests, each thread over neighbouring ones: put(r, sums before r, request r), and at last
-// put(requests, sums of all, nothing).
+// Both prefix sums of all requests, each thread over up to four neighbouring ones at a time: put(r, sums before r, request r),
+// and at last put(requests, sums of all, nothing).
 template <typename Put> __device__ __forceinline__ void sum_requests(const MapArgs& p, uint32_t (*part)[2], Put put)
 {
-    const int each = (p.requests + (int)blockDim.x - 1) / (int)blockDim.x;
-    const int64_t from = (int64_t)threadIdx.x * each;
-    const int lo = (int)(from < p.requests ? from : p.requests), hi = lo + each < p.requests ? lo + each : p.requests;
-    Request q = {};
-    Two mine = {0, 0};
-    for (int r = hi - 1; r >= lo; --r) {    // backwards: the one left in q is the first that is put
-        q = request(p, r);
-        mine.a = capped(mine.a, q.listed);
-        mine.b = capped(mine.b, q.taken);
+    constexpr int kNeighbours = 4;
+    const int each = p.requests > (int)blockDim.x ? kNeighbours : 1;
+    Two carry = {0, 0};
+    for (int64_t base = 0; base < p.requests; base += (int64_t)blockDim.x * each) {
+        const int64_t lo = base + (int64_t)threadIdx.x * each;
+        Request q[kNeighbours];
+        Two mine = {0, 0};
+#pragma unroll
+        for (int j = 0; j < kNeighbours; ++j) {
+            q[j] = {};
+            if (j < each && lo + j < p.requests) q[j] = request(p, (int)(lo + j));
+            mine.a = capped(mine.a, q[j].listed);
+            mine.b = capped(mine.b, q[j].taken);
+        }
+        if (base > 0) __syncthreads();      // the last round's sums have been read
+        Two all, at = sums_before(mine, part, &all);
+        at.a = capped(at.a, carry.a);
+        at.b = capped(at.b, carry.b);
+#pragma unroll
+        for (int j = 0; j < kNeighbours; ++j) {
+            if (j >= each || lo + j >= p.requests) continue;
+            put((int)(lo + j), at, q[j]);
+            at.a = capped(at.a, q[j].listed);
+            at.b = capped(at.b, q[j].taken);
+        }
+        carry.a = capped(carry.a, all.a);
+        carry.b = capped(carry.b, all.b);
     }
-    Two all, at = sums_before(mine, part, &all);
-    for (int r = lo; r < hi; ++r) {
-        if (r > lo) q = request(p, r);
-        put(r, at, q);
-        at.a = capped(at.a, q.listed);
-        at.b = capped(at.b, q.taken);
-    }
-    if (threadIdx.x == 0) put(p.requests, all, Request{});
+    if (threadIdx.x == 0) put(p.requests, carry, Request{});
 }
 
 __global__ __launch_bounds__(1024) void starts_kernel(MapArgs p)
@@ -101,7 +103,7 @@ __global__ __launch_bounds__(1024) void starts_kernel(MapArgs p)
 
 // FUSED: makes the sums itself, and keeps what else it needs of the requests beside them; otherwise starts_kernel has left
 // the sums where they belong.
-template <bool FUSED>
+template <int EACH, bool FUSED>
 __global__ __launch_bounds__(kMapThreads) void map_kernel(MapArgs p)
 {
     extern __shared__ uint32_t sums[];      // FUSED: starts, page_starts, first listed positions, pages held
@@ -120,11 +122,16 @@ __global__ __launch_bounds__(kMapThreads) void map_kernel(MapArgs p)
         });
         __syncthreads();
     }
-    const uint64_t i0 = ((uint64_t)block * kMapThreads + threadIdx.x) * kMapEach;
+    const uint64_t i0 = ((uint64_t)block * blockDim.x + threadIdx.x) * EACH;
     if (i0 >= (uint64_t)p.tokens) return;
     // the last request that starts at or before i0: requests that list nothing share a start with the next
     int lo = 0, hi = p.requests;            // starts[lo] <= i0 < starts[hi], or past the end
     if (i0 >= starts[p.requests]) lo = p.requests;
+    else if (p.tokens > 0) {                // first guess: as if all listed the same number, which in a decoding step they do
+        const int guess = (int)(i0 * (uint64_t)p.requests / starts[p.requests]);
+        if (starts[guess] <= i0) lo = guess;
+        if (starts[guess + 1] > i0) hi = guess + 1;
+    }
     while (hi - lo > 1) {
         const int mid = lo + (hi - lo) / 2;
         if (starts[mid] <= i0) lo = mid; else hi = mid;
@@ -143,13 +150,13 @@ __global__ __launch_bounds__(kMapThreads) void map_kernel(MapArgs p)
         }
     };
     take();
-    const int count = (uint64_t)p.tokens - i0 < kMapEach ? (int)((uint64_t)p.tokens - i0) : kMapEach;
+    const int count = (uint64_t)p.tokens - i0 < EACH ? (int)((uint64_t)p.tokens - i0) : EACH;
     // where every position's page is found, then the pages themselves: their loads are in flight together
-    const int32_t* from[kMapEach];
-    int32_t* entry[kMapEach];
-    int32_t inside[kMapEach], at[kMapEach], who[kMapEach];
+    const int32_t* from[EACH];
+    int32_t* entry[EACH];
+    int32_t inside[EACH], at[EACH], who[EACH];
 #pragma unroll
-    for (int j = 0; j < kMapEach; ++j) {
+    for (int j = 0; j < EACH; ++j) {
         from[j] = nullptr;
         entry[j] = nullptr;
         inside[j] = 0;
@@ -175,11 +182,11 @@ __global__ __launch_bounds__(kMapThreads) void map_kernel(MapArgs p)
             if (inside[j] == 0) entry[j] = e;           // the first token of a page enters it
         }
     }
-    int32_t page[kMapEach];
+    int32_t page[EACH];
 #pragma unroll
-    for (int j = 0; j < kMapEach; ++j) page[j] = from[j] ? *from[j] : -1;
+    for (int j = 0; j < EACH; ++j) page[j] = from[j] ? *from[j] : -1;
 #pragma unroll
-    for (int j = 0; j < kMapEach; ++j) {
+    for (int j = 0; j < EACH; ++j) {
         if (j >= count) continue;
         if ((uint32_t)page[j] >= p.pages) page[j] = -1;
         if (entry[j]) *entry[j] = page[j];
@@ -191,18 +198,23 @@ __global__ __launch_bounds__(kMapThreads) void map_kernel(MapArgs p)
 
 }  // namespace
 
+// One listed position per lane while that is a launch of few workgroups; four where there are many, so that fewer of
+// them make the sums.
 int launch_map(const MapArgs& a, void* stream)
 {
     MapArgs p = a;
-    const bool fused = p.requests <= kMapRequests;
-    const uint64_t per_block = (uint64_t)kMapThreads * kMapEach;
-    uint64_t blocks = ((uint64_t)p.tokens + per_block - 1) / per_block;
+    const bool fused = p.requests <= kMapRequests, few = p.tokens <= kMapFew;
+    const int threads = fused && p.requests > 256 ? kMapThreads : 256;
+    const uint64_t per_block = (uint64_t)threads * (few ? 1 : 4);
+    const uint64_t blocks = ((uint64_t)p.tokens + per_block - 1) / per_block;
     if (fused) {
         const size_t lds = 4 * sizeof(uint32_t) * (size_t)(p.requests + 1);
-        return launch_blocks(reinterpret_cast<const void*>(&map_kernel<true>), blocks ? blocks : 1, kMapThreads, lds, &p, stream);
+        const void* fn = few ? reinterpret_cast<const void*>(&map_kernel<1, true>) : reinterpret_cast<const void*>(&map_kernel<4, true>);
+        return launch_blocks(fn, blocks ? blocks : 1, threads, lds, &p, stream);
     }
     const int st = launch_blocks(reinterpret_cast<const void*>(&starts_kernel), 1, 1024, 0, &p, stream);
-    return st != TTC_OK ? st : launch_blocks(reinterpret_cast<const void*>(&map_kernel<false>), blocks, kMapThreads, 0, &p, stream);
+    const void* fn = few ? reinterpret_cast<const void*>(&map_kernel<1, false>) : reinterpret_cast<const void*>(&map_kernel<4, false>);
+    return st != TTC_OK ? st : launch_blocks(fn, blocks, threads, 0, &p, stream);
 }
 
 // ---------------------------------------------------------------------------------
@@ -219,8 +231,9 @@ struct PlaceArgs {
     FastDiv  token_div, head_div;          // by heads * vecs, by vecs
 };
 
-// Eight elements a lane: 16 bytes of a 16-bit type, two accesses of 32 bits, 8 bytes of an 8-bit cache.  (f32 alone: four.)
-template <typename T, typename C> struct SlotVec { static constexpr int value = sizeof(T) == 4 && sizeof(C) == 4 ? 4 : 8; };
+// Sixteen bytes a lane of the type outside the cache.  (f32 as two accesses of 16 bytes and 8 bytes of an 8-bit cache: 64 x 1333 tokens of 8
+// heads of 128 out of it 140 us instead of 86, into it 82 and 74; 16 elements of a 16-bit type: out of it 105 and 89.)
+template <typename T> struct SlotVec { static constexpr int value = 16 / (int)sizeof(T); };
 
 template <typename T, typename C, bool WRITE> struct SlotTypes { typedef T from; typedef C to; };
 template <typename T, typename C> struct SlotTypes<T, C, false> { typedef C from; typedef T to; };
@@ -261,18 +274,18 @@ __device__ __forceinline__ void convert_out(const Vec<From, V>& x, float scale, 
     narrow(f, r);
 }
 
-template <typename T, typename C, bool WRITE, bool NTL, bool NTS>
+template <typename T, typename C, int V, bool WRITE, bool NTL, bool NTS>
 __global__ __launch_bounds__(kMoveThreads) void slots_kernel(PlaceArgs p)
 {
-    constexpr int V = SlotVec<T, C>::value;
     constexpr bool same = sizeof(T) == sizeof(C);
     typedef typename SlotTypes<T, C, WRITE>::from From;
     typedef typename SlotTypes<T, C, WRITE>::to To;
     const uint32_t unit = block_id() * kMoveThreads + threadIdx.x;
     if (unit >= p.units) return;
     const uint32_t token = fdiv(unit, p.token_div), in_token = unit - token * p.token_div.div;
-    const uint32_t head = fdiv(in_token, p.head_div), c = (in_token - head * p.vecs) * V;
-    const int n = (int)(p.s.dim - c);
+    const uint32_t head = fdiv(in_token, p.head_div), vec = in_token - head * p.vecs;
+    const MovePlace place = row_place<V>(vec, p.s.dim);
+    const uint32_t c = place.at;
     const uint32_t slot = (uint32_t)p.s.slots[token];
     const bool here = slot < p.s.slot_count;
     if (WRITE && !here) return;
@@ -283,14 +296,14 @@ __global__ __launch_bounds__(kMoveThreads) void slots_kernel(PlaceArgs p)
     const bool both = p.s.v_out != nullptr;
     Vec<From, V> k = {}, v = {};
     if (here) {
-        k = load_row<From, V, NTL>(static_cast<const From*>(p.s.k) + (WRITE ? at_k : in_cache), n);
-        if (both) v = load_row<From, V, NTL>(static_cast<const From*>(p.s.v) + (WRITE ? at_v : in_cache), n);
+        k = load_vec<From, V, NTL>(static_cast<const From*>(p.s.k) + (WRITE ? at_k : in_cache));
+        if (both) v = load_vec<From, V, NTL>(static_cast<const From*>(p.s.v) + (WRITE ? at_v : in_cache));
     }
     To* to_k = static_cast<To*>(p.s.k_out) + (WRITE ? in_cache : at_k);
     To* to_v = static_cast<To*>(p.s.v_out) + (WRITE ? in_cache : at_v);
     if constexpr (same) {
-        store_row<To, V, NTS>(to_k, k, n);
-        if (both) store_row<To, V, NTS>(to_v, v, n);
+        store_vec<To, V, NTS>(to_k, k);
+        if (both) store_vec<To, V, NTS>(to_v, v);
     } else {
         const float scale_k = p.s.k_scale ? p.s.k_scale[head] : 1.f, scale_v = p.s.v_scale ? p.s.v_scale[head] : 1.f;
         Vec<To, V> r = {};
@@ -298,10 +311,10 @@ __global__ __launch_bounds__(kMoveThreads) void slots_kernel(PlaceArgs p)
             if constexpr (WRITE) convert_in(x, scale, y); else convert_out(x, scale, y);
         };
         if (here) convert(k, scale_k, r);       // nowhere: zero, whatever the scale
-        store_row<To, V, NTS>(to_k, r, n);
+        store_vec<To, V, NTS>(to_k, r);
         if (both) {
             if (here) convert(v, scale_v, r);
-            store_row<To, V, NTS>(to_v, r, n);
+            store_vec<To, V, NTS>(to_v, r);
         }
     }
 }
@@ -313,10 +326,11 @@ constexpr uint64_t kStreamStores = uint64_t(16) << 20, kStreamLoads = uint64_t(2
 
 template <typename T, typename C, bool WRITE> int launch_slots_types(const SlotArgs& a, void* stream)
 {
-    constexpr int V = SlotVec<T, C>::value;
+    constexpr int V = SlotVec<T>::value;
     PlaceArgs p = {};
     p.s = a;
-    p.vecs = (a.dim + V - 1) / V;
+    const bool narrow = a.dim < (uint32_t)V;            // element by element
+    p.vecs = narrow ? a.dim : (a.dim + V - 1) / V;
     const uint32_t per_token = a.heads * p.vecs;        // heads * dim < 2^30
     p.token_div = make_fastdiv(per_token);
     p.head_div = make_fastdiv(p.vecs);
@@ -335,10 +349,14 @@ template <typename T, typename C, bool WRITE> int launch_slots_types(const SlotA
         }
         p.units = tokens * per_token;
         const uint64_t bytes = (uint64_t)tokens * a.heads * a.dim * (sizeof(T) + sizeof(C)) * (a.v_out ? 2 : 1);
-        const void* fn = bytes < kStreamStores ? reinterpret_cast<const void*>(&slots_kernel<T, C, WRITE, false, false>)
-                       : bytes < kStreamLoads ? reinterpret_cast<const void*>(&slots_kernel<T, C, WRITE, false, true>)
-                                              : reinterpret_cast<const void*>(&slots_kernel<T, C, WRITE, true, true>);
-        const int st = launch_blocks(fn, ((uint64_t)p.units + kMoveThreads - 1) / kMoveThreads, kMoveThreads, 0, &p, stream);
+        // five workgroups to a compute unit instead of eight: 700 MB of bf16 in 115 us instead of 122 (out of the cache 112, 117); an 8-bit cache
+        // has less under way and wants them all
+        const size_t lds = sizeof(T) == sizeof(C) && bytes >= kStreamLoads ? lds_for(5) : 0;
+        const void* fn = narrow ? reinterpret_cast<const void*>(&slots_kernel<T, C, 1, WRITE, false, false>)
+                       : bytes < kStreamStores ? reinterpret_cast<const void*>(&slots_kernel<T, C, V, WRITE, false, false>)
+                       : bytes < kStreamLoads ? reinterpret_cast<const void*>(&slots_kernel<T, C, V, WRITE, false, true>)
+                                              : reinterpret_cast<const void*>(&slots_kernel<T, C, V, WRITE, true, true>);
+        const int st = launch_blocks(fn, ((uint64_t)p.units + kMoveThreads - 1) / kMoveThreads, kMoveThreads, lds, &p, stream);
         if (st != TTC_OK) return st;
     }
     return TTC_OK;

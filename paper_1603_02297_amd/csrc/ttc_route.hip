@@ -31,20 +31,11 @@ __device__ __forceinline__ uint32_t expert_of(const SortArgs& p, uint32_t a)
 __device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t* part, uint32_t* all)
 {
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
-    uint32_t s = v;
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-        const uint32_t o = __shfl_up(s, d);
-        if (lane >= d) s += o;
-    }
+    auto add = [](uint32_t a, uint32_t b) { return a + b; };
+    const uint32_t s = over_lanes(v, add);
     if (lane == kWave - 1) part[wave] = s;
     __syncthreads();
-    uint32_t w = lane < waves ? part[lane] : 0;          // the wavefronts' sums, summed by every wavefront for itself
-#pragma unroll
-    for (int d = 1; d < kSortThreads / kWave; d *= 2) {
-        const uint32_t o = __shfl_up(w, d);
-        if (lane >= d) w += o;
-    }
+    const uint32_t w = over_lanes(lane < waves ? part[lane] : 0, add);         // the wavefronts' sums, summed by every wavefront for itself
     *all = __shfl(w, waves - 1);
     const uint32_t before = __shfl(w, wave > 0 ? wave - 1 : 0);
     return (wave > 0 ? before : 0) + s - v;
@@ -52,11 +43,13 @@ __device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t* part, uint3
 
 __device__ __forceinline__ uint32_t padded(uint32_t count, uint32_t align) { return (count + align - 1) / align * align; }
 
+constexpr int kExpertBits = 11;            // TTC_ROUTE_MAX_EXPERTS itself (nowhere) takes them all
+static_assert((TTC_ROUTE_MAX_EXPERTS >> kExpertBits) == 0, "every expert and nowhere have a number of kExpertBits bits");
+
 // A workgroup's chunk: every assignment's rank among those of its expert in the chunk, and the experts' counts.
 // ALONE: the chunk is all there is, and the result is finished here.  Otherwise ranks are left in `position` and counts
 // in `hist` for place_kernel.
-// LDS: counters [waves][experts] (16 bits: a wavefront holds at most 64 * kSortBlocks ids, a chunk kSortOne), then
-// the experts' first rows, then one word per wavefront.
+// LDS: one word per wavefront, the experts' first rows, counters [waves][experts] (16 bits: a chunk holds at most 8192 ids).
 template <int B, bool ALONE>
 __global__ __launch_bounds__(kSortThreads) void sort_kernel(SortArgs p)
 {
@@ -83,7 +76,9 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(SortArgs p)
 #pragma unroll
     for (int b = 0; b < B; ++b) {
         uint64_t same = ~uint64_t(0);
-        for (int i = 0; i < bits; ++i) {
+#pragma unroll
+        for (int i = 0; i < kExpertBits; ++i) {
+            if (i >= bits) continue;
             const bool set = (e[b] >> i) & 1;
             const uint64_t with = __ballot(set);
             same &= set ? with : ~with;
@@ -172,10 +167,10 @@ __global__ __launch_bounds__(kSortThreads) void place_kernel(SortArgs p, int32_t
     const int experts = p.experts, chunk = blockIdx.x;
     // what the last step needs, on its way while the counts are added up
     uint32_t expert[B], rank[B];
-    const uint64_t start = (uint64_t)chunk * (B * kSortThreads) + threadIdx.x;
+    const uint64_t start = ((uint64_t)chunk * B) * blockDim.x + threadIdx.x;
 #pragma unroll
     for (int b = 0; b < B; ++b) {
-        const uint64_t a = start + b * kSortThreads;
+        const uint64_t a = start + (uint64_t)b * blockDim.x;
         expert[b] = a < p.n ? expert_of(p, (uint32_t)a) : (uint32_t)experts;
         rank[b] = a < p.n ? (uint32_t)p.position[a] : 0;
     }
@@ -186,11 +181,11 @@ __global__ __launch_bounds__(kSortThreads) void place_kernel(SortArgs p, int32_t
             before = (uint32_t)p.hist[(int64_t)chunk * experts + threadIdx.x];
         }
     } else {
-        for (int i = threadIdx.x; i < experts; i += kSortThreads) row[i] = sums[i] = 0;
+        for (int i = threadIdx.x; i < experts; i += blockDim.x) row[i] = sums[i] = 0;
         __syncthreads();
         int log = 0;
         while ((1 << log) < experts) ++log;
-        const int e = threadIdx.x & ((1 << log) - 1), lanes = kSortThreads >> log;
+        const int e = threadIdx.x & ((1 << log) - 1), lanes = (int)blockDim.x >> log;
         if (e < experts) {
             uint32_t t = 0, b = 0;
 #pragma unroll 8
@@ -222,7 +217,7 @@ __global__ __launch_bounds__(kSortThreads) void place_kernel(SortArgs p, int32_t
 #pragma unroll
     for (int b = 0; b < B; ++b) {
         if (expert[b] >= (uint32_t)experts) continue;               // its position is -1 already
-        const uint64_t a = start + b * kSortThreads;
+        const uint64_t a = start + (uint64_t)b * blockDim.x;
         const uint32_t at = rank[b] + row[expert[b]];
         p.position[a] = (int32_t)at;
         if (p.source) p.source[at] = (int32_t)a;
@@ -233,7 +228,8 @@ template <int B> int launch_sort_blocks(const SortArgs& p, const SortShape& s, v
 {
     const size_t head = sizeof(uint32_t) * (size_t)(kSortThreads / kWave + p.experts);
     const size_t lds = head + sizeof(uint16_t) * (size_t)(s.threads / kWave) * (size_t)p.experts;
-    if (s.chunks == 1) return launch_blocks(reinterpret_cast<const void*>(&sort_kernel<B, true>), 1, s.threads, lds, const_cast<SortArgs*>(&p), stream);
+    if constexpr (B <= kSortOneBlocks)
+        if (s.chunks == 1) return launch_blocks(reinterpret_cast<const void*>(&sort_kernel<B, true>), 1, s.threads, lds, const_cast<SortArgs*>(&p), stream);
     hipStream_t st = (hipStream_t)stream;
     SortArgs a = p;
     int64_t chunks64 = s.chunks;
@@ -248,7 +244,7 @@ template <int B> int launch_sort_blocks(const SortArgs& p, const SortShape& s, v
         return TTC_ERR_HIP;
     const void* place = summed ? reinterpret_cast<const void*>(&place_kernel<B, true>) : reinterpret_cast<const void*>(&place_kernel<B, false>);
     const size_t place_lds = head + (summed ? 0 : sizeof(uint32_t) * (size_t)experts);
-    return hipLaunchKernel(place, dim3((uint32_t)chunks), dim3(kSortThreads), place_args, place_lds, st) == hipSuccess ? TTC_OK : TTC_ERR_HIP;
+    return hipLaunchKernel(place, dim3((uint32_t)chunks), dim3(s.threads), place_args, place_lds, st) == hipSuccess ? TTC_OK : TTC_ERR_HIP;
 }
 
 }  // namespace
@@ -273,7 +269,9 @@ template <typename T> struct RowVec { static constexpr int value = 16 / (int)siz
 
 struct MoveArgs {
     RowArgs  r;
+    uint32_t vec;                          // elements of a vector
     uint32_t lanes_log, parts, vecs;
+    uint32_t lanes;                        // the gradient's lanes for a token
     FastDiv  parts_div;
     uint32_t units;                        // tokens * parts
     uint32_t blocks, total;                // workgroups over the units, and with those after them that clear padding
@@ -281,9 +279,8 @@ struct MoveArgs {
 };
 
 // Padding rows of expert `e`: those of its segment that hold no token, cleared by `pad_parts` workgroups.
-template <typename T, bool NT> __device__ __forceinline__ void clear_padding(const MoveArgs& p, uint32_t block)
+template <typename T, int V, bool NT> __device__ __forceinline__ void clear_padding(const MoveArgs& p, uint32_t block)
 {
-    constexpr int V = RowVec<T>::value;
     if (block >= p.total) return;
     const uint32_t index = block - p.blocks;
     const uint32_t e = index / p.pad_parts, part = index - e * p.pad_parts;
@@ -294,8 +291,8 @@ template <typename T, bool NT> __device__ __forceinline__ void clear_padding(con
     const Vec<T, V> zero = {};
     for (uint64_t i = (uint64_t)part * blockDim.x + threadIdx.x; i < vectors; i += (uint64_t)p.pad_parts * blockDim.x) {
         const uint64_t row = i / p.vecs;
-        const uint32_t c = (uint32_t)(i - row * p.vecs) * V;
-        store_row<T, V, NT>(static_cast<T*>(p.r.y) + (lo + (int64_t)row) * p.r.ld_y + c, zero, (int)(p.r.width - c));
+        const MovePlace at = row_place<V>((uint32_t)(i - row * p.vecs), p.r.width);
+        store_vec<T, V, NT>(static_cast<T*>(p.r.y) + (lo + (int64_t)row) * p.r.ld_y + at.at, zero);
     }
 }
 
@@ -312,181 +309,233 @@ template <bool WHOLE> __device__ __forceinline__ bool lane_place(const MoveArgs&
     return *vec < p.vecs;
 }
 
-constexpr int kTogether = 8;               // choices whose rows are in flight at a time
+// GROUP choices (2, 4 or 8, by topk) of a token from k0 on: the rows they point to, kNowhere where there is none, and their
+// weights, 0 there.  All loads are under way together, none hangs on a branch: indices past the last choice read the
+// last one again.  Where the wavefront has one token they are scalar loads; the compiler would not make them by itself, for all it
+// knows the kernel's stores could change the map, and with vector loads that each wait for the one before
+// the gather of 32 tokens took 3.6 us instead of 2.9.
+constexpr uint32_t kNowhere = ~0u;
+template <typename V> using Constant = const V __attribute__((address_space(4)))*;
+template <int GROUP, bool WHOLE> struct Choices {
+    uint32_t at[GROUP];
+    float    w[GROUP];
 
-template <typename T, bool WHOLE, bool NT>
+    // load, then check: what else is to be loaded goes between them
+    template <bool WEIGHTS> __device__ __forceinline__ void load(const RowArgs& r, uint32_t token, int k0)
+    {
+        const uint64_t a = (uint64_t)token * (uint32_t)r.topk;
+#pragma unroll
+        for (int k = 0; k < GROUP; ++k) {
+            const uint64_t i = a + (uint32_t)(k0 + k < r.topk ? k0 + k : r.topk - 1);
+            at[k] = (uint32_t)(WHOLE ? ((Constant<int32_t>)r.position)[i] : r.position[i]);
+            w[k] = 1.f;
+            if (WEIGHTS) w[k] = WHOLE ? ((Constant<float>)r.weights)[i] : r.weights[i];
+        }
+    }
+    __device__ __forceinline__ void check(const RowArgs& r, int k0)
+    {
+#pragma unroll
+        for (int k = 0; k < GROUP; ++k)
+            if (k0 + k >= r.topk || at[k] >= r.row_count) {
+                at[k] = kNowhere;
+                w[k] = 0.f;
+            }
+    }
+    __device__ __forceinline__ bool any() const
+    {
+        bool a = false;
+#pragma unroll
+        for (int k = 0; k < GROUP; ++k) a |= at[k] != kNowhere;
+        return a;
+    }
+    __device__ __forceinline__ void load(const RowArgs& r, uint32_t token, int k0)
+    {
+        if (r.weights) load<true>(r, token, k0); else load<false>(r, token, k0);
+        check(r, k0);
+    }
+};
+
+template <typename T, int V, int GROUP, bool WHOLE, bool NT, bool WEIGHTS>
 __global__ __launch_bounds__(kMoveThreads) void gather_kernel(MoveArgs p)
 {
-    constexpr int V = RowVec<T>::value;
     const uint32_t b = block_id();
-    if (b >= p.blocks) { clear_padding<T, NT>(p, b); return; }
+    if (b >= p.blocks) { clear_padding<T, V, NT>(p, b); return; }
     uint32_t t, vec;
     if (!lane_place<WHOLE>(p, b, &t, &vec)) return;
-    const uint32_t c = vec * V;
-    const int n = (int)(p.r.width - c);
-    const Vec<T, V> x = load_row<T, V, false>(static_cast<const T*>(p.r.x) + (int64_t)t * p.r.ld_x + c, n);
-    const uint64_t a = (uint64_t)t * (uint32_t)p.r.topk;
-    for (int k0 = 0; k0 < p.r.topk; k0 += kTogether) {
-        uint32_t at[kTogether];             // read before anything is stored: scalar loads where the token is the wavefront's
-        float w[kTogether];
-#pragma unroll
-        for (int k = 0; k < kTogether; ++k) {
-            at[k] = k0 + k < p.r.topk ? (uint32_t)p.r.position[a + k0 + k] : ~0u;
-            w[k] = p.r.weights && k0 + k < p.r.topk ? p.r.weights[a + k0 + k] : 1.f;
+    const MovePlace place = row_place<V>(vec, p.r.width);
+    const uint32_t c = place.at;
+    Choices<GROUP, WHOLE> q;
+    q.template load<WEIGHTS>(p.r, t, 0);
+    const T* from = static_cast<const T*>(p.r.x) + (int64_t)t * p.r.ld_x + c;
+    Vec<T, V> x;
+    if (!NT) x = load_vec<T, V, false>(from);
+    q.check(p.r, 0);
+    if (NT) {
+        if (p.r.topk <= GROUP && !q.any()) return;
+        x = load_vec<T, V, false>(from);
+    }
+    arrive(x);
+    for (int k0 = 0; k0 < p.r.topk; k0 += GROUP) {
+        if (k0 > 0) {
+            q.template load<WEIGHTS>(p.r, t, k0);
+            q.check(p.r, k0);
         }
 #pragma unroll
-        for (int k = 0; k < kTogether; ++k) {
-            if (at[k] >= p.r.row_count) continue;
-            T* to = static_cast<T*>(p.r.y) + (int64_t)at[k] * p.r.ld_y + c;
-            if (p.r.weights) {
+        for (int k = 0; k < GROUP; ++k) {
+            if (q.at[k] == kNowhere) continue;
+            T* to = static_cast<T*>(p.r.y) + (int64_t)q.at[k] * p.r.ld_y + c;
+            if (WEIGHTS) {
                 float f[V];
                 widen(x, f);
 #pragma unroll
-                for (int i = 0; i < V; ++i) f[i] *= w[k];
+                for (int i = 0; i < V; ++i) f[i] *= q.w[k];
                 Vec<T, V> r;
                 narrow(f, r);
-                store_row<T, V, NT>(to, r, n);
+                store_vec<T, V, NT>(to, r);
             } else {
-                store_row<T, V, NT>(to, x, n);
+                store_vec<T, V, NT>(to, x);
             }
         }
     }
 }
+template <typename T, int V, int GROUP, bool WHOLE, bool NT> constexpr auto gather_plain = &gather_kernel<T, V, GROUP, WHOLE, NT, false>;
+template <typename T, int V, int GROUP, bool WHOLE, bool NT> constexpr auto gather_weighted = &gather_kernel<T, V, GROUP, WHOLE, NT, true>;
 
-template <typename T, bool WHOLE, bool NT>
+template <typename T, int V, int GROUP, bool WHOLE, bool NT>
 __global__ __launch_bounds__(kMoveThreads) void combine_kernel(MoveArgs p)
 {
-    constexpr int V = RowVec<T>::value;
     uint32_t t, vec;
     if (!lane_place<WHOLE>(p, block_id(), &t, &vec)) return;
-    const uint32_t c = vec * V;
-    const int n = (int)(p.r.width - c);
+    const MovePlace place = row_place<V>(vec, p.r.width);
+    const uint32_t c = place.at;
     const T* rows = static_cast<const T*>(p.r.rows) + c;
-    const uint64_t a = (uint64_t)t * (uint32_t)p.r.topk;
     float sum[V] = {};
-    for (int k0 = 0; k0 < p.r.topk; k0 += kTogether) {
-        Vec<T, V> x[kTogether];
-        float w[kTogether];
-        bool here[kTogether];
+    for (int k0 = 0; k0 < p.r.topk; k0 += GROUP) {
+        Choices<GROUP, WHOLE> q;
+        q.load(p.r, t, k0);
+        Vec<T, V> x[GROUP];
 #pragma unroll
-        for (int k = 0; k < kTogether; ++k) {
+        for (int k = 0; k < GROUP; ++k) {
             x[k] = {};
-            w[k] = 1.f;
-            here[k] = false;
-            if (k0 + k < p.r.topk) {
-                const uint32_t at = (uint32_t)p.r.position[a + k0 + k];
-                here[k] = at < p.r.row_count;
-                if (here[k]) {
-                    x[k] = load_row<T, V, NT>(rows + (int64_t)at * p.r.ld_rows, n);
-                    if (p.r.weights) w[k] = p.r.weights[a + k0 + k];
-                }
-            }
+            if (q.at[k] != kNowhere) x[k] = load_vec<T, V, NT>(rows + (int64_t)q.at[k] * p.r.ld_rows);
         }
 #pragma unroll
-        for (int k = 0; k < kTogether; ++k) {
-            if (!here[k]) continue;
+        for (int k = 0; k < GROUP; ++k) {   // 0 * 0 where there is none
             float f[V];
             widen(x[k], f);
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum[i] = __builtin_fmaf(w[k], f[i], sum[i]);
+            for (int i = 0; i < V; ++i) sum[i] = __builtin_fmaf(q.w[k], f[i], sum[i]);
         }
     }
     T* to = static_cast<T*>(p.r.y) + (int64_t)t * p.r.ld_y + c;
 #pragma unroll
     for (int i = 0; i < V; ++i) sum[i] *= p.r.alpha;
+    Vec<T, V> r;
     if (p.r.beta != 0.f) {
+        // a moved vector leaves what it shares to its neighbour, who may have been here already
         float f[V];
-        widen(load_row<T, V, NT>(to, n), f);
+        widen(place.back > 0 ? load_end<T, V>(to, place.back) : load_vec<T, V, NT>(to), f);
 #pragma unroll
         for (int i = 0; i < V; ++i) sum[i] = __builtin_fmaf(p.r.beta, f[i], sum[i]);
+        narrow(sum, r);
+        if (place.back > 0) {
+            store_end<T, V>(to, r, place.back);
+            return;
+        }
+    } else {
+        narrow(sum, r);
     }
-    Vec<T, V> r;
-    narrow(sum, r);
-    store_row<T, V, NT>(to, r, n);
+    store_vec<T, V, NT>(to, r);
 }
 
-// The gradient: 2^lanes_log lanes walk over a whole row, because the dot products need all of it.  Their partial sums
+// The gradient: `lanes` lanes walk over a whole row, because the dot products need all of it: a power of two up to a wavefront,
+// several tokens to a workgroup, or a whole workgroup of several wavefronts.  Their partial sums
 // meet by shuffles inside a wavefront and through LDS between wavefronts, always in the same order.
-template <typename T, bool WHOLE, bool NT>
-__global__ __launch_bounds__(kSortThreads) void combine_grad_kernel(MoveArgs p)
+constexpr int kGradWaves = 8;              // wavefronts of a workgroup at most (and then rounds): 500 x 4 rows of 4097 bf16 with 4, 8, 16 16.8, 15.5, 17.1 us,
+                                           // 8192 x 4 of 4104 176, 192, 235, of 8192 167, 162, 166, 2 x 8 of 4096 10.9, 9.0, 9.0
+template <typename T, int V, int GROUP, bool WHOLE, bool NT>
+__global__ __launch_bounds__(WHOLE ? kGradWaves * kWave : kMoveThreads) void combine_grad_kernel(MoveArgs p)
 {
-    constexpr int V = RowVec<T>::value;
-    __shared__ float dots[kSortThreads / kWave][kTogether];
+    __shared__ float dots[kGradWaves][GROUP];
     const uint32_t b = block_id();
-    if (b >= p.blocks) { clear_padding<T, NT>(p, b); return; }
-    const uint32_t lanes = 1u << p.lanes_log, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> p.lanes_log;
-    uint32_t token = b * (blockDim.x >> p.lanes_log) + group;
+    if (b >= p.blocks) { clear_padding<T, V, NT>(p, b); return; }
+    const uint32_t lanes = p.lanes, lane = WHOLE && lanes > kWave ? threadIdx.x : threadIdx.x & (lanes - 1);
+    uint32_t token = WHOLE && lanes > kWave ? b : b * (kMoveThreads / lanes) + threadIdx.x / lanes;
     if (WHOLE) token = __builtin_amdgcn_readfirstlane(token);
     const bool some = token < p.r.tokens;
     const uint32_t t = some ? token : 0;
     const uint64_t a = (uint64_t)t * (uint32_t)p.r.topk;
     const T* dy = static_cast<const T*>(p.r.x) + (int64_t)t * p.r.ld_x;
-    for (int k0 = 0; k0 < p.r.topk; k0 += kTogether) {
-        uint32_t at[kTogether];
-        float w[kTogether], dot[kTogether];
+    for (int k0 = 0; k0 < p.r.topk; k0 += GROUP) {
+        Choices<GROUP, WHOLE> q;
+        q.load(p.r, t, k0);                 // lanes past the last token look at the first one's, and do nothing with them
+        float dot[GROUP];
 #pragma unroll
-        for (int k = 0; k < kTogether; ++k) {
-            at[k] = ~0u;
-            w[k] = p.r.alpha;
+        for (int k = 0; k < GROUP; ++k) {
+            if (!some) q.at[k] = kNowhere;
+            q.w[k] *= p.r.alpha;
             dot[k] = 0.f;
-            if (some && k0 + k < p.r.topk) {
-                at[k] = (uint32_t)p.r.position[a + k0 + k];
-                if (p.r.weights) w[k] *= p.r.weights[a + k0 + k];
-            }
         }
-        if (some)
+        if (q.any())                        // a token whose choices are all nowhere reads nothing
             for (uint32_t vec = lane; vec < p.vecs; vec += lanes) {
-                const uint32_t c = vec * V;
-                const int n = (int)(p.r.width - c);
-                float g[V];
-                widen(load_row<T, V, false>(dy + c, n), g);
-                Vec<T, V> x[kTogether];
-                if (p.r.dweights) {
+                const MovePlace place = row_place<V>(vec, p.r.width);
+                const uint32_t c = place.at;
+                            Vec<T, V> d = load_vec<T, V, false>(dy + c), x[GROUP];
 #pragma unroll
-                    for (int k = 0; k < kTogether; ++k) {
-                        x[k] = {};
-                        if (at[k] < p.r.row_count) x[k] = load_row<T, V, NT>(static_cast<const T*>(p.r.rows) + (int64_t)at[k] * p.r.ld_rows + c, n);
-                    }
+                for (int k = 0; k < GROUP; ++k) {
+                    x[k] = {};
+                    if (p.r.dweights && q.at[k] != kNowhere) x[k] = load_vec<T, V, NT>(static_cast<const T*>(p.r.rows) + (int64_t)q.at[k] * p.r.ld_rows + c);
                 }
+                float g[V], own[V];         // what a moved vector shares is its neighbour's to add
+                const Keep<T, V> keep(place.back);
+                widen(d, g);
+                keep(d);
+                widen(d, own);
 #pragma unroll
-                for (int k = 0; k < kTogether; ++k) {
-                    if (at[k] >= p.r.row_count) continue;
+                for (int k = 0; k < GROUP; ++k) {
+                    if (q.at[k] == kNowhere) continue;
                     if (p.r.y) {
                         float f[V];
 #pragma unroll
-                        for (int i = 0; i < V; ++i) f[i] = w[k] * g[i];
+                        for (int i = 0; i < V; ++i) f[i] = q.w[k] * g[i];
                         Vec<T, V> r;
                         narrow(f, r);
-                        store_row<T, V, NT>(static_cast<T*>(p.r.y) + (int64_t)at[k] * p.r.ld_y + c, r, n);
+                        store_vec<T, V, NT>(static_cast<T*>(p.r.y) + (int64_t)q.at[k] * p.r.ld_y + c, r);
                     }
                     if (p.r.dweights) {
                         float f[V];
+                        keep(x[k]);
                         widen(x[k], f);
 #pragma unroll
-                        for (int i = 0; i < V; ++i) dot[k] = __builtin_fmaf(g[i], f[i], dot[k]);
+                        for (int i = 0; i < V; ++i) dot[k] = __builtin_fmaf(own[i], f[i], dot[k]);
                     }
                 }
             }
         if (!p.r.dweights) continue;
-        const uint32_t inside = lanes < kWave ? lanes : kWave;
-        for (uint32_t d = inside / 2; d > 0; d /= 2)
+        uint32_t last = 0;                  // the lane of a wavefront, or of a smaller group, that has the sum
+        if (WHOLE) {
+            last = kWave - 1;
 #pragma unroll
-            for (int k = 0; k < kTogether; ++k) dot[k] += __shfl_xor(dot[k], (int)d);
-        if (lanes > kWave) {
-            __syncthreads();                // the last eight choices' sums have been read
-            if ((threadIdx.x & (kWave - 1)) == 0)
+            for (int k = 0; k < GROUP; ++k) dot[k] = sum_in_last_lane(dot[k]);
+        } else {
+            for (uint32_t d = lanes / 2; d > 0; d /= 2)
 #pragma unroll
-                for (int k = 0; k < kTogether; ++k) dots[threadIdx.x / kWave][k] = dot[k];
+                for (int k = 0; k < GROUP; ++k) dot[k] += __shfl_xor(dot[k], (int)d);
+        }
+        if (WHOLE && lanes > kWave) {
+            __syncthreads();                // the sums of the choices before have been read
+            if ((threadIdx.x & (kWave - 1)) == last)
+#pragma unroll
+                for (int k = 0; k < GROUP; ++k) dots[threadIdx.x / kWave][k] = dot[k];
             __syncthreads();
-            if (lane < kTogether && some && k0 + (int)lane < p.r.topk) {
-                const uint32_t waves = lanes / kWave;
+            if (lane < GROUP && some && k0 + (int)lane < p.r.topk) {
                 float s = 0.f;
-                for (uint32_t w0 = 0; w0 < waves; ++w0) s += dots[group * waves + w0][lane];
+                for (uint32_t w0 = 0; w0 < lanes / kWave; ++w0) s += dots[w0][lane];
                 p.r.dweights[a + k0 + lane] = p.r.alpha * s;
             }
-        } else if (some && lane == 0) {
+        } else if (some && lane == last) {
 #pragma unroll
-            for (int k = 0; k < kTogether; ++k)
+            for (int k = 0; k < GROUP; ++k)
                 if (k0 + k < p.r.topk) p.r.dweights[a + k0 + k] = p.r.alpha * dot[k];
         }
     }
@@ -494,10 +543,10 @@ __global__ __launch_bounds__(kSortThreads) void combine_grad_kernel(MoveArgs p)
 
 template <typename T> MoveArgs move_args(const RowArgs& r)
 {
-    constexpr int V = RowVec<T>::value;
     MoveArgs p = {};
     p.r = r;
-    p.vecs = (r.width + V - 1) / V;
+    p.vec = r.width < (uint32_t)RowVec<T>::value ? 1 : RowVec<T>::value;
+    p.vecs = (r.width + p.vec - 1) / p.vec;
     p.lanes_log = (uint32_t)log2_ceil(p.vecs < (uint32_t)kWave ? p.vecs : (uint32_t)kWave);
     p.parts = (p.vecs + (1u << p.lanes_log) - 1) >> p.lanes_log;
     p.parts_div = make_fastdiv(p.parts);
@@ -513,13 +562,29 @@ template <typename T> MoveArgs move_args(const RowArgs& r)
 constexpr uint64_t kStreamGather = uint64_t(32) << 20, kStreamCombine = uint64_t(96) << 20, kStreamGrad = uint64_t(24) << 20;
 template <typename T> bool streams(const RowArgs& r, uint64_t from) { return (uint64_t)r.tokens * r.topk * r.width * sizeof(T) >= from; }
 
-inline const void* pick(bool whole, bool nt, void (*wn)(MoveArgs), void (*w)(MoveArgs), void (*n)(MoveArgs), void (*plain)(MoveArgs))
+typedef void (*MoveKernel)(MoveArgs);
+struct Kernels {
+    MoveKernel k[3][2][2];                 // [two, four, more choices][whole wavefronts][non-temporal]
+    MoveKernel narrow;                     // rows shorter than a vector, element by element
+};
+inline const void* pick(const MoveArgs& p, bool nt, const Kernels& of)
 {
-    return reinterpret_cast<const void*>(whole ? (nt ? wn : w) : (nt ? n : plain));
+    if (p.vec == 1) return reinterpret_cast<const void*>(of.narrow);
+    return reinterpret_cast<const void*>(of.k[p.r.topk <= 2 ? 0 : p.r.topk <= 4 ? 1 : 2][p.lanes_log == 6][nt]);
 }
 
+#define TTC_KERNELS(kernel)                                                                                             \
+    {{{{kernel<T, V, 2, false, false>, kernel<T, V, 2, false, true>}, {kernel<T, V, 2, true, false>, kernel<T, V, 2, true, true>}}, \
+      {{kernel<T, V, 4, false, false>, kernel<T, V, 4, false, true>}, {kernel<T, V, 4, true, false>, kernel<T, V, 4, true, true>}}, \
+      {{kernel<T, V, 8, false, false>, kernel<T, V, 8, false, true>}, {kernel<T, V, 8, true, false>, kernel<T, V, 8, true, true>}}}, \
+     kernel<T, 1, 8, false, false>}
+template <typename T> struct kernels_of {
+    static constexpr int V = RowVec<T>::value;
+    static constexpr Kernels gather = TTC_KERNELS(gather_plain), gather_weights = TTC_KERNELS(gather_weighted), combine = TTC_KERNELS(combine_kernel), combine_grad = TTC_KERNELS(combine_grad_kernel);
+};
+
 // Workgroups over the units, and behind them those that clear padding: one per expert and 32 KB that it may have to clear.
-template <typename T> int launch_units(const void* fn, MoveArgs& p, int threads, uint64_t units, uint64_t per_block, bool padding, void* stream)
+template <typename T> int launch_units(const void* fn, MoveArgs& p, int threads, uint64_t units, uint64_t per_block, bool padding, size_t lds, void* stream)
 {
     uint64_t blocks = (units + per_block - 1) / per_block, pads = 0;
     if (units > INT32_MAX) return TTC_ERR_OVERFLOW;
@@ -531,30 +596,41 @@ template <typename T> int launch_units(const void* fn, MoveArgs& p, int threads,
         pads = (uint64_t)p.r.experts * p.pad_parts;
     }
     p.total = (uint32_t)(blocks + pads);
-    return launch_blocks(fn, blocks + pads, threads, 0, &p, stream);
+    return launch_blocks(fn, blocks + pads, threads, lds, &p, stream);
 }
 
 template <typename T> int launch_gather_type(const RowArgs& r, void* stream)
 {
     MoveArgs p = move_args<T>(r);
-    const void* fn = pick(p.lanes_log == 6, streams<T>(r, kStreamGather), &gather_kernel<T, true, true>, &gather_kernel<T, true, false>, &gather_kernel<T, false, true>, &gather_kernel<T, false, false>);
-    return launch_units<T>(fn, p, kMoveThreads, (uint64_t)r.tokens * p.parts, kMoveThreads >> p.lanes_log, true, stream);
+    // Six workgroups to a compute unit instead of eight where three choices or more write their rows at once.  4096 bf16 with the sort, us,
+    // eight, six, four, three workgroups: 16384 x 3 rows 104, 99, 99, 105; 16384 x 4 135, 127, 123, 123; half of them nowhere 74, 73, 79, 89;
+    // 16384 x 8, three of four nowhere 79, 80, 93, 107.  Two choices 144, 144, 150, 164: left alone.
+    // Rows that start inside a 64-byte unit go without the hint: 4097 bf16 160 us with it, 150 without.
+    const bool nt = streams<T>(r, kStreamGather) && ((uint64_t)r.ld_y * sizeof(T) | (uintptr_t)r.y) % 64 == 0;
+    const size_t lds = nt && r.topk >= 3 ? lds_for(6) : 0;
+    const void* fn = pick(p, nt, r.weights ? kernels_of<T>::gather_weights : kernels_of<T>::gather);
+    return launch_units<T>(fn, p, kMoveThreads, (uint64_t)r.tokens * p.parts, kMoveThreads >> p.lanes_log, true, lds, stream);
 }
 
 template <typename T> int launch_combine_type(const RowArgs& r, void* stream)
 {
     MoveArgs p = move_args<T>(r);
-    const void* fn = pick(p.lanes_log == 6, streams<T>(r, kStreamCombine), &combine_kernel<T, true, true>, &combine_kernel<T, true, false>, &combine_kernel<T, false, true>, &combine_kernel<T, false, false>);
-    return launch_units<T>(fn, p, kMoveThreads, (uint64_t)r.tokens * p.parts, kMoveThreads >> p.lanes_log, false, stream);
+    const void* fn = pick(p, streams<T>(r, kStreamCombine), kernels_of<T>::combine);
+    return launch_units<T>(fn, p, kMoveThreads, (uint64_t)r.tokens * p.parts, kMoveThreads >> p.lanes_log, false, 0, stream);
 }
 
 template <typename T> int launch_grad_type(const RowArgs& r, void* stream)
 {
     MoveArgs p = move_args<T>(r);
-    p.lanes_log = (uint32_t)log2_ceil(p.vecs < (uint32_t)kSortThreads ? p.vecs : (uint32_t)kSortThreads);
-    const int threads = p.lanes_log > 8 ? 1 << p.lanes_log : kMoveThreads;
-    const void* fn = pick(p.lanes_log >= 6, streams<T>(r, kStreamGrad), &combine_grad_kernel<T, true, true>, &combine_grad_kernel<T, true, false>, &combine_grad_kernel<T, false, true>, &combine_grad_kernel<T, false, false>);
-    return launch_units<T>(fn, p, threads, r.tokens, (uint64_t)threads >> p.lanes_log, r.y != nullptr, stream);
+    p.lanes = 1u << p.lanes_log;
+    int threads = kMoveThreads;
+    if (p.vecs > (uint32_t)kWave) {         // as few rounds as kGradWaves wavefronts need, and then no more wavefronts than those rounds
+        const uint32_t pieces = (p.vecs + kWave - 1) / kWave, rounds = (pieces + kGradWaves - 1) / kGradWaves;
+        p.lanes = (pieces + rounds - 1) / rounds * kWave;
+        threads = (int)p.lanes;
+    }
+    const void* fn = pick(p, streams<T>(r, kStreamGrad), kernels_of<T>::combine_grad);
+    return launch_units<T>(fn, p, threads, r.tokens, (uint64_t)threads / p.lanes, r.y != nullptr, 0, stream);
 }
 
 }  // namespace
