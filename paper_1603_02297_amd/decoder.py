@@ -1,0 +1,211 @@
+"""A decoder layer with routed experts over a paged cache: the moves by data (include/ttc_moves.h) as they are used together.
+
+    python -m paper_1603_02297_amd.decoder [--steps N]
+
+serves prompts and then single tokens of several requests, and trains the experts on a batch.  A step of serving:
+
+    request lengths --ttc_pages_map--> block tables, packed offsets, slots --ttc_pages_write--> keys and values in their pages
+    --ttc_pages_map (all positions), ttc_pages_read--> every request's context, packed --> attention
+    --> router --ttc_route_sort--> rows by expert --ttc_route_gather--> the experts' products --ttc_route_combine--> residual
+
+Everything else (projections, attention, the experts) is plain torch: this is the path that the moves serve, not a model.
+"""
+from __future__ import annotations
+
+import argparse
+import weakref
+
+import torch
+
+import paper_1603_02297_amd as ttc
+
+CODES = {torch.float32: ttc.TTC_F32, torch.bfloat16: ttc.TTC_BF16, torch.float16: ttc.TTC_F16, torch.float8_e4m3fn: ttc.TTC_F8}
+
+
+def _stream() -> int:
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _ptr(x) -> int:
+    return 0 if x is None else x.data_ptr()
+
+
+def _rows_apart(x: torch.Tensor) -> int:
+    """The leading dimension of a row-major matrix, which may be part of a wider one."""
+    if x.stride(-1) != 1:
+        raise ValueError("the elements of a row are neighbours")
+    return max(x.stride(0), x.shape[-1])
+
+
+class Routing:
+    """The rows of one batch sorted by expert: what ttc_route_sort found, and the moves along it."""
+
+    def __init__(self, ids: torch.Tensor, experts: int, width: int, dtype: torch.dtype, first: int = 0, align: int = 1):
+        self.tokens, self.topk = ids.shape
+        self.width, self.dtype, self.experts, self.device = width, dtype, experts, ids.device
+        self.handle = ttc.ttc_route_create(CODES[dtype], width, self.topk, experts, first, align, ids.element_size())
+        weakref.finalize(self, ttc.ttc_route_destroy, self.handle)
+        self.row_count = ttc.ttc_route_rows(self.handle, self.tokens)
+        i32 = lambda *shape: torch.empty(shape, dtype=torch.int32, device=self.device)  # noqa: E731
+        self.offsets, self.counts, self.position = i32(experts + 1), i32(experts), i32(self.tokens, self.topk)
+        work = torch.empty(ttc.ttc_route_workspace(self.handle, self.tokens), dtype=torch.uint8, device=self.device)
+        ttc.ttc_route_sort(self.handle, self.tokens, _ptr(ids), _rows_apart(ids), _ptr(self.offsets), _ptr(self.counts), _ptr(self.position), 0, _ptr(work), _stream())
+
+    def gather(self, x: torch.Tensor) -> torch.Tensor:
+        """Tokens to their rows; rows past the last segment are 0."""
+        rows = torch.zeros(self.row_count, self.width, dtype=self.dtype, device=self.device)
+        ttc.ttc_route_gather(self.handle, self.tokens, _ptr(x), _rows_apart(x), 0, _ptr(self.position), _ptr(self.offsets), _ptr(self.counts), _ptr(rows), self.width, _stream())
+        return rows
+
+    def combine(self, rows: torch.Tensor, weights) -> torch.Tensor:
+        y = torch.empty(self.tokens, self.width, dtype=self.dtype, device=self.device)
+        ttc.ttc_route_combine(self.handle, self.tokens, _ptr(rows), _rows_apart(rows), _ptr(weights), _ptr(self.position), _ptr(y), self.width, _stream())
+        return y
+
+    def combine_grad(self, dy: torch.Tensor, rows: torch.Tensor, weights: torch.Tensor):
+        drows, dweights = torch.zeros_like(rows), torch.empty_like(weights)
+        ttc.ttc_route_combine_grad(self.handle, self.tokens, _ptr(dy), _rows_apart(dy), _ptr(rows), _rows_apart(rows), _ptr(weights), _ptr(self.position),
+                                   _ptr(self.offsets), _ptr(self.counts), _ptr(drows), self.width, _ptr(dweights), _stream())
+        return drows, dweights
+
+
+class Gather(torch.autograd.Function):
+    """Tokens to their rows; the gradient adds the rows up again."""
+
+    @staticmethod
+    def forward(ctx, x, routing):
+        ctx.routing = routing
+        return routing.gather(x)
+
+    @staticmethod
+    def backward(ctx, drows):
+        return ctx.routing.combine(drows.contiguous(), None), None
+
+
+class Combine(torch.autograd.Function):
+    """Rows back to their tokens, weighted; the gradients of rows and weights in one pass."""
+
+    @staticmethod
+    def forward(ctx, rows, weights, routing):
+        ctx.routing = routing
+        ctx.save_for_backward(rows, weights)
+        return routing.combine(rows, weights)
+
+    @staticmethod
+    def backward(ctx, dy):
+        drows, dweights = ctx.routing.combine_grad(dy.contiguous(), *ctx.saved_tensors)
+        return drows, dweights, None
+
+
+def experts_forward(x: torch.Tensor, router: torch.Tensor, up: torch.Tensor, down: torch.Tensor, topk: int, align: int = 16) -> torch.Tensor:
+    """x [tokens, width] through the experts that the router chooses: up [experts, width, hidden], down [experts, hidden, width]."""
+    logits = x.float() @ router.float()
+    best, ids = logits.topk(topk, dim=1)
+    routing = Routing(ids.contiguous(), up.shape[0], x.shape[1], x.dtype, align=align)
+    rows = Gather.apply(x, routing)
+    ends = routing.offsets.tolist()                               # the segments' sizes shape the products
+    out = [torch.nn.functional.silu(rows[a:b] @ up[e]) @ down[e] for e, (a, b) in enumerate(zip(ends, ends[1:]))]
+    out.append(rows[ends[-1]:])                                   # rows that nothing points to
+    return Combine.apply(torch.cat(out), best.softmax(1).contiguous(), routing)
+
+
+class PagedCache:
+    """Keys and values of several requests in pages; the requests' lengths say where everything goes."""
+
+    def __init__(self, requests: int, heads: int, dim: int, page: int, pages: int, longest: int, dtype: torch.dtype, cache_dtype: torch.dtype, device="cuda"):
+        self.heads, self.dim, self.page, self.requests, self.device = heads, dim, page, requests, device
+        self.dtype = dtype
+        self.handle = ttc.ttc_pages_create(CODES[dtype], CODES[cache_dtype], heads, dim, page, pages)
+        weakref.finalize(self, ttc.ttc_pages_destroy, self.handle)
+        self.k, self.v = (torch.zeros(pages, page, heads, dim, dtype=torch.uint8, device=device).to(cache_dtype) for _ in range(2))
+        self.scale = torch.full((heads,), 0.0625, device=device) if cache_dtype == torch.float8_e4m3fn else None
+        self.table = torch.full((requests, -(-longest // page)), -1, dtype=torch.int32, device=device)
+        self.free = torch.randperm(pages, device=device).to(torch.int32)
+        self.cached = torch.zeros(requests, dtype=torch.int32, device=device)
+
+    def _map(self, first, fresh, tokens):
+        i32 = lambda n: torch.empty(n, dtype=torch.int32, device=self.device)  # noqa: E731
+        starts, page_starts, slots = i32(self.requests + 1), i32(self.requests + 1), i32(tokens)
+        ttc.ttc_pages_map(self.handle, self.requests, _ptr(first), _ptr(self.cached), _ptr(fresh), _ptr(self.table), self.table.shape[1], _ptr(self.free),
+                          self.free.numel(), tokens, _ptr(starts), _ptr(page_starts), _ptr(slots), 0, 0, _stream())
+        return starts, page_starts, slots
+
+    def append(self, fresh: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> torch.Tensor:
+        """fresh [requests]: how many of the packed new tokens are each one's; k, v [tokens, heads*dim].  Returns their packed offsets."""
+        starts, page_starts, slots = self._map(None, fresh, k.shape[0])
+        taken = int(page_starts[-1])
+        if taken > self.free.numel():
+            raise RuntimeError(f"{taken} pages wanted, {self.free.numel()} free")
+        ttc.ttc_pages_write(self.handle, k.shape[0], _ptr(slots), _ptr(k), _rows_apart(k), _ptr(v), _rows_apart(v), _ptr(self.k), _ptr(self.v),
+                            _ptr(self.scale), _ptr(self.scale), _stream())
+        self.free, self.cached = self.free[taken:].contiguous(), self.cached + fresh
+        return starts
+
+    def context(self):
+        """Every request's keys and values, packed, and their offsets."""
+        none, total = torch.zeros_like(self.cached), int(self.cached.sum())
+        starts, _, slots = self._map(none, none, total)
+        k, v = (torch.empty(total, self.heads * self.dim, dtype=self.dtype, device=self.device) for _ in range(2))
+        ttc.ttc_pages_read(self.handle, total, _ptr(slots), _ptr(self.k), _ptr(self.v), _ptr(self.scale), _ptr(self.scale), _ptr(k), k.shape[1], _ptr(v), v.shape[1], _stream())
+        return starts, k, v
+
+
+def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, heads: int, kv_heads: int) -> torch.Tensor:
+    """Causal attention of one request's last tokens over its context, in 32 bits: q [new, heads*dim], k and v [all, kv_heads*dim]."""
+    new, length, dim = q.shape[0], k.shape[0], k.shape[1] // kv_heads
+    by_head = lambda x, n: x.float().view(x.shape[0], n, dim).transpose(0, 1)  # noqa: E731
+    kh, vh = (by_head(x, kv_heads).repeat_interleave(heads // kv_heads, 0).contiguous() for x in (k, v))
+    scores = by_head(q, heads).contiguous() @ kh.transpose(1, 2).contiguous() / dim ** 0.5
+    later = torch.arange(length, device=q.device)[None, :] > torch.arange(length - new, length, device=q.device)[:, None]
+    return (scores.masked_fill(later, -torch.inf).softmax(-1) @ vh).transpose(0, 1).reshape(new, heads * dim).to(q.dtype)
+
+
+def layer(x: torch.Tensor, fresh: torch.Tensor, cache: PagedCache, w: dict, heads: int, topk: int) -> torch.Tensor:
+    """One layer over the packed new tokens of all requests."""
+    kv = cache.heads * cache.dim
+    qkv = x @ w["qkv"]
+    starts = cache.append(fresh, qkv[:, heads * cache.dim:heads * cache.dim + kv], qkv[:, heads * cache.dim + kv:]).tolist()
+    ends, k, v = cache.context()
+    ends = ends.tolist()
+    mixed = [attention(qkv[a:b, :heads * cache.dim], k[c:d], v[c:d], heads, cache.heads) for a, b, c, d in zip(starts, starts[1:], ends, ends[1:]) if b > a]
+    x = x + torch.cat(mixed) @ w["out"]
+    return x + experts_forward(x, w["router"], w["up"], w["down"], topk)
+
+
+def weights(width: int, heads: int, kv_heads: int, dim: int, experts: int, hidden: int, dtype: torch.dtype, seed: int = 0, device="cuda") -> dict:
+    g = torch.Generator(device=device).manual_seed(seed)
+    draw = lambda *s: (torch.randn(s, generator=g, device=device) / s[-2] ** 0.5).to(dtype)  # noqa: E731
+    return {"qkv": draw(width, (heads + 2 * kv_heads) * dim), "out": draw(heads * dim, width), "router": draw(width, experts),
+            "up": draw(experts, width, hidden), "down": draw(experts, hidden, width)}
+
+
+def main() -> None:
+    ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
+    ap.add_argument("--steps", type=int, default=4, help="decoding steps, and training steps")
+    steps = ap.parse_args().steps
+    width, heads, kv_heads, dim, experts, topk, dtype = 512, 8, 2, 64, 16, 4, torch.bfloat16
+    w = weights(width, heads, kv_heads, dim, experts, 1024, dtype)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    lengths = torch.tensor([70, 1, 33, 128], dtype=torch.int32, device="cuda")
+    for cache_dtype in (torch.bfloat16, torch.float8_e4m3fn):
+        cache = PagedCache(4, kv_heads, dim, 16, 64, 256, dtype, cache_dtype)
+        with torch.no_grad():
+            y = layer(torch.randn(int(lengths.sum()), width, generator=g, device="cuda").to(dtype), lengths, cache, w, heads, topk)
+            print(f"{cache_dtype}: prompts of {lengths.tolist()} tokens, mean square {float(y.float().square().mean()):.3f}, {cache.free.numel()} pages free")
+            for _ in range(steps):
+                y = layer(torch.randn(4, width, generator=g, device="cuda").to(dtype), torch.ones_like(lengths), cache, w, heads, topk)
+        print(f"  {steps} tokens each: lengths {cache.cached.tolist()}, mean square {float(y.float().square().mean()):.3f}, {cache.free.numel()} pages free")
+    params = {k: w[k].float().requires_grad_() for k in ("router", "up", "down")}
+    x = torch.randn(512, width, generator=g, device="cuda")
+    target = torch.randn(512, width, generator=g, device="cuda")
+    optimizer = torch.optim.Adam(params.values(), lr=1e-3)
+    for step in range(steps):
+        optimizer.zero_grad()
+        loss = (experts_forward(x, params["router"], params["up"], params["down"], topk) - target).square().mean()
+        loss.backward()
+        optimizer.step()
+        print(f"training step {step}: loss {float(loss):.4f}")
+
+
+if __name__ == "__main__":
+    main()
