@@ -237,6 +237,16 @@ __device__ __forceinline__ float sum_in_last_lane(float v)        // lane 63 get
     return __builtin_bit_cast(float, over_lanes(__builtin_bit_cast(uint32_t, v), add));
 }
 
+// Touches every 64-byte line of a kernel's arguments at once: read where they are used, a line after the other, each costs the way to
+// memory again.  One token's combine 2.4 -> 2.2 us, 128 tokens into the cache 2.7 -> 2.5; the gather, the sort and the map gain nothing.
+template <typename Args> __device__ __forceinline__ void touch(const Args& args)
+{
+    const __attribute__((address_space(4))) uint32_t* words = (const __attribute__((address_space(4))) uint32_t*)&args;
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(Args) / 4; i += 16) asm volatile("" : : "s"(words[i]));
+    asm volatile("" : : "s"(words[sizeof(Args) / 4 - 1]));
+}
+
 // A launch dimension may count at most 2^32 work items: blocks beyond 2^20 go into the second dimension.
 constexpr uint32_t kGridRow = 1u << 20;
 __device__ __forceinline__ uint32_t block_id() { return blockIdx.y * kGridRow + blockIdx.x; }

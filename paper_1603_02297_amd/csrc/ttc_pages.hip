@@ -277,6 +277,7 @@ __device__ __forceinline__ void convert_out(const Vec<From, V>& x, float scale, 
 template <typename T, typename C, int V, bool WRITE, bool NTL, bool NTS>
 __global__ __launch_bounds__(kMoveThreads) void slots_kernel(PlaceArgs p)
 {
+    touch(p);
     constexpr bool same = sizeof(T) == sizeof(C);
     typedef typename SlotTypes<T, C, WRITE>::from From;
     typedef typename SlotTypes<T, C, WRITE>::to To;

@@ -404,6 +404,7 @@ template <typename T, int V, int GROUP, bool WHOLE, bool NT> constexpr auto gath
 template <typename T, int V, int GROUP, bool WHOLE, bool NT>
 __global__ __launch_bounds__(kMoveThreads) void combine_kernel(MoveArgs p)
 {
+    touch(p);
     uint32_t t, vec;
     if (!lane_place<WHOLE>(p, block_id(), &t, &vec)) return;
     const MovePlace place = row_place<V>(vec, p.r.width);
@@ -456,6 +457,7 @@ constexpr int kGradWaves = 8;              // wavefronts of a workgroup at most 
 template <typename T, int V, int GROUP, bool WHOLE, bool NT>
 __global__ __launch_bounds__(WHOLE ? kGradWaves * kWave : kMoveThreads) void combine_grad_kernel(MoveArgs p)
 {
+    touch(p);
     __shared__ float dots[kGradWaves][GROUP];
     const uint32_t b = block_id();
     if (b >= p.blocks) { clear_padding<T, V, NT>(p, b); return; }
