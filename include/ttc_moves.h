@@ -129,7 +129,8 @@ int ttc_pages_destroy(ttc_pages_t pages);
  *              values count as cached[r].
  *   cached, fresh [requests] int32; negative counts as 0, and cached[r]+fresh[r] is cut at 2^31-1.
  *   table      [ld_table, requests] int32, in and out: entry b of request r is the page of its positions b*page ...
- *              Entries below ceil(cached/page) are read, those from there to ceil((cached+fresh)/page) are written.
+ *              Entries below ceil(cached/page) are read, those from there to ceil((cached+fresh)/page) are written, each with
+ *              the first token of its page (so not those of tokens past the end of `slots`).
  *   free_list  [free_count] int32: pages to take, in order; request 0's come first.
  *   tokens     length of slots, positions and owner (a step's buffers; >= 0).
  *   starts     [requests+1] int32, out: where every request's listed positions start; starts[requests] is their number,
