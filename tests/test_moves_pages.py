@@ -68,7 +68,7 @@ def tables(rng, cached, page, width, pages):
 @gpu
 @pytest.mark.parametrize("requests,most_cached,most_fresh,page,with_first", [
     (1, 0, 1, 16, False), (1, 40, 1, 1, False), (3, 0, 700, 16, False), (17, 300, 1, 16, False), (40, 500, 90, 24, True), (255, 20, 5, 7, False), (256, 64, 64, 32, True),
-    (257, 100, 1, 128, False), (1000, 30, 30, 3, True), (4096, 50, 2, 16, False), (4097, 50, 2, 16, True), (9001, 10, 3, 8, False), (2, 5, 20000, 64, False)])
+    (257, 100, 1, 128, False), (1000, 30, 30, 3, True), (4096, 50, 2, 16, False), (4097, 50, 2, 16, True), (9001, 10, 3, 8, False), (2, 5, 20000, 64, False), (40, 100, 30000, 32, True), (4000, 20, 200, 16, False), (4001, 20, 200, 16, True)])
 def test_map(requests, most_cached, most_fresh, page, with_first):
     rng = np.random.default_rng(requests * 13 + page)
     cached = lengths(rng, requests, most_cached + 1)
@@ -217,6 +217,46 @@ def test_write_and_read(kind, cache_kind, heads, dim, page, pages, order, tokens
             # a product in 32 bits, then the type's rounding
             ref.assert_close(ref.wide(got[:, :heads * dim]), want.reshape(tokens, -1), kind, np.abs(want.reshape(tokens, -1)), 0 if scales is None else 1, "read")
             assert (got[:, heads * dim:] == 9).all() and (out[which][-4:] == 9).all()
+
+
+@gpu
+@pytest.mark.parametrize("kind,cache_kind,heads,dim,tokens,order", [
+    ("bf16", "bf16", 8, 128, 45000, "slots"), ("f16", "f16", 5, 84, 30000, "heads"), ("f32", "f32", 4, 130, 40000, "heads"), ("bf16", "f8", 8, 128, 50000, "heads"),
+    ("f32", "f8", 3, 97, 60000, "slots"), ("f16", "f8", 2, 576, 12000, "gaps")])
+def test_large_moves_of_slots(kind, cache_kind, heads, dim, tokens, order):
+    """Sizes at which stores, and then loads, are streamed; against indexing on the GPU in 64 bits."""
+    (code, dtype), (cache_code, cache_type) = ref.TYPES[kind], ref.TYPES[cache_kind]
+    page, pages = 16, tokens // 16 + 3
+    shape, perm, strides = layout(order, heads, dim, page, pages)
+    g = torch.Generator(device=DEV).manual_seed(dim)
+    slots = torch.randperm(page * pages, generator=g, device=DEV)[:tokens].to(torch.int32)
+    slots[torch.rand(tokens, generator=g, device=DEV) < 0.05] = -1
+    here = slots >= 0
+    at = slots[here].long()
+    scale = torch.rand(2, heads, generator=g, device=DEV) * 0.02 + 0.005
+    sp = [scale[0].data_ptr(), scale[1].data_ptr()] if cache_kind == "f8" else [0, 0]
+    k, v = (torch.randn(tokens, heads * dim, generator=g, device=DEV).to(dtype) for _ in range(2))
+    kc, vc = (torch.zeros(shape, dtype=torch.uint8 if cache_kind == "f8" else cache_type, device=DEV) for _ in range(2))
+    with Pages(code, cache_code, heads, dim, page, pages, strides) as h:
+        ttc.ttc_pages_write(h, tokens, slots.data_ptr(), k.data_ptr(), heads * dim, v.data_ptr(), heads * dim, kc.data_ptr(), vc.data_ptr(), *sp, stream())
+        ko, vo = (torch.full_like(k, 9.0) for _ in range(2))
+        ttc.ttc_pages_read(h, tokens, slots.data_ptr(), kc.data_ptr(), vc.data_ptr(), *sp, ko.data_ptr(), heads * dim, vo.data_ptr(), heads * dim, stream())
+        values = torch.from_numpy(ref.f8_values()).to(DEV)
+        for x, cache, out, s in ((k, kc, ko, scale[0]), (v, vc, vo, scale[1])):
+            held = cache.permute(perm)[..., :dim][at // page, at % page]
+            mine = x.view(tokens, heads, dim)[here]
+            if cache_kind == "f8":
+                held = values[held.long()]
+                quotient = (mine.double() / s.double()[:, None]).float().double().clamp(-448, 448)
+                step = torch.exp2(torch.floor(torch.log2(quotient.abs().clamp(min=2.0 ** -6))) - 3)
+                assert torch.equal(held, torch.round(quotient / step) * step)
+                product = held * s.double()[:, None]
+                rel, tiny = ref.ROUND[kind]
+                assert ((out.view(tokens, heads, dim)[here].double() - product).abs() <= (rel + ref.F32) * product.abs() * 1.01 + tiny).all()
+            else:
+                assert torch.equal(held, mine) and torch.equal(out.view(tokens, heads, dim)[here], mine)
+            assert (out[~here] == 0).all()
+        assert int((kc.permute(perm)[..., :dim].reshape(page * pages, -1) != 0).any(1).sum()) <= int(here.sum())         # no other slot was touched
 
 
 @gpu

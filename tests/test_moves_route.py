@@ -60,7 +60,8 @@ def run_sort(h, ids, experts, ld=None, source=True):
     (63, 1, 5, 0, 1, np.int32), (64, 1, 64, 0, 16, np.int64), (65, 3, 65, 0, 1, np.int64), (128, 8, 1024, 0, 1, np.int64), (341, 3, 7, 2, 128, np.int32),
     (1024, 1, 33, 0, 1, np.int64), (1025, 1, 33, 0, 1, np.int64), (1024, 8, 128, 64, 16, np.int32), (2731, 3, 1000, 0, 3, np.int64),
     (4097, 2, 16, 16, 64, np.int64), (16384, 4, 64, 0, 128, np.int64), (30011, 5, 129, 3, 1, np.int32), (100003, 7, 255, 0, 16, np.int64),
-    (140001, 8, 8, 4, 1, np.int64), (140001, 8, 1024, 0, 2, np.int32)])
+    (140001, 8, 8, 4, 1, np.int64), (140001, 8, 1024, 0, 2, np.int32), (70001, 5, 300, 0, 64, np.int64),
+    (341, 6, 40, 0, 1, np.int64), (2049, 1, 2, 0, 1, np.int32), (131073, 1, 17, 0, 1, np.int64)])
 def test_sort(tokens, topk, experts, first, align, id_type):
     rng = np.random.default_rng(tokens * 31 + topk)
     ids = (choose(rng, tokens, topk, experts + first + 2) if tokens < 20000 else rng.integers(-1, experts + first + 2, (tokens, topk))).astype(id_type)
@@ -181,6 +182,57 @@ def test_moves(kind, tokens, topk, experts, first, align, width, extra, shift, w
                 # a lane's chain, the shuffles, the wavefronts and the factor alpha: fewer roundings than the terms there are
                 ref.assert_close(ref.wide(dw[:tokens * topk]).reshape(tokens, topk), want_w, "f32", mag_w, width + 20, "dweights")
             assert (dw[-4:] == 77).all()
+
+
+@gpu
+@pytest.mark.parametrize("kind,tokens,topk,experts,first,align,width,beta", [
+    ("bf16", 3000, 8, 32, 0, 16, 4128, 1.0), ("f32", 6001, 3, 5, 1, 1, 2049, 0.0), ("f16", 4000, 4, 9, 0, 64, 4100, 1.0), ("bf16", 2500, 9, 12, 3, 1, 2880, 0.0),
+    ("bf16", 20000, 2, 4, 4, 1, 2056, 0.0), ("f32", 90000, 2, 8, 0, 128, 130, 0.5), ("f16", 200000, 5, 64, 0, 8, 48, 0.0), ("bf16", 1500, 1, 8, 0, 1, 40000, 1.0)])
+def test_moves_of_large_batches(kind, tokens, topk, experts, first, align, width, beta):
+    """Sizes at which rows are streamed and rows take several rounds, against 64 bits on the GPU; some choices elsewhere, some tokens empty."""
+    code, dtype = ref.TYPES[kind]
+    rel, tiny = ref.ROUND[kind]
+    g = torch.Generator(device=DEV).manual_seed(width)
+    ids = torch.rand(tokens, experts + first + 2, generator=g, device=DEV).topk(topk, dim=1).indices.contiguous()
+    ids[torch.rand(tokens, generator=g, device=DEV) < 0.1] = -1
+    draw = lambda *shape: torch.randn(shape, generator=g, device=DEV).to(dtype)  # noqa: E731
+    weights = torch.randn(tokens, topk, generator=g, device=DEV)
+    with Route(code, width, topk, experts, first, align, 8, 1.0, beta) as h:
+        n = ttc.ttc_route_rows(h, tokens)
+        i32 = lambda k: torch.empty(k, dtype=torch.int32, device=DEV)  # noqa: E731
+        offsets, counts, position, source, work = i32(experts + 1), i32(experts), i32(tokens * topk), i32(n), i32(ttc.ttc_route_workspace(h, tokens) // 4 + 1)
+        ttc.ttc_route_sort(h, tokens, ids.data_ptr(), topk, offsets.data_ptr(), counts.data_ptr(), position.data_ptr(), source.data_ptr(), work.data_ptr(), stream())
+        pos = position.view(tokens, topk).long()
+        here = pos >= 0
+        assert torch.equal(here, (ids >= first) & (ids < first + experts)) and torch.equal(source[pos[here]].long(), torch.nonzero(here.reshape(-1)).reshape(-1))
+        x, rows = draw(tokens, width), torch.full((n, width), 3.0, dtype=dtype, device=DEV)
+        ttc.ttc_route_gather(h, tokens, x.data_ptr(), width, 0, position.data_ptr(), offsets.data_ptr(), counts.data_ptr(), rows.data_ptr(), width, stream())
+        want = torch.where((torch.arange(n, device=DEV) < offsets[-1])[:, None], 0.0, torch.full_like(rows, 3.0))
+        want[pos[here]] = x[torch.nonzero(here)[:, 0]]
+        assert torch.equal(rows, want)
+        del want
+        rows = draw(n, width)
+        rows[source < 0] = float("nan")
+        y = draw(tokens, width)
+        exact, mag = beta * y.double(), abs(beta) * y.double().abs()
+        for k in range(topk):
+            term = torch.where(here[:, k, None], weights[:, k, None].double() * rows[pos[:, k].clamp(min=0)].double(), 0.0)
+            exact, mag = exact + term, mag + term.abs()
+        ttc.ttc_route_combine(h, tokens, rows.data_ptr(), width, weights.data_ptr(), position.data_ptr(), y.data_ptr(), width, stream())
+        err = (topk + 3) * ref.F32 * mag
+        assert ((y.double() - exact).abs() <= err * 1.01 + rel * (exact.abs() + err) + tiny).all()
+        del exact, mag, err
+        dy, drows, dweights = draw(tokens, width), torch.full((n, width), 3.0, dtype=dtype, device=DEV), torch.empty(tokens, topk, device=DEV)
+        ttc.ttc_route_combine_grad(h, tokens, dy.data_ptr(), width, rows.data_ptr(), width, weights.data_ptr(), position.data_ptr(), offsets.data_ptr(), counts.data_ptr(),
+                                   drows.data_ptr(), width, dweights.data_ptr(), stream())
+        assert (drows[(source < 0) & (torch.arange(n, device=DEV) < offsets[-1])] == 0).all() and (drows[int(offsets[-1]):] == 3).all()
+        for k in range(topk):
+            at, mine = pos[here[:, k], k], dy[here[:, k]].double()
+            want = weights[here[:, k], k, None].double() * mine
+            assert ((drows[at].double() - want).abs() <= (rel + 2 * ref.F32) * want.abs() * 1.01 + tiny).all()
+            product = mine * rows[at].double()
+            assert ((dweights[here[:, k], k].double() - product.sum(1)).abs() <= (width + 20) * ref.F32 * product.abs().sum(1)).all()
+        assert (dweights[~here] == 0).all()
 
 
 @gpu
