@@ -12,7 +12,7 @@
  * Conventions as in ttc.h: column-major (leftmost index has stride 1), DEVICE pointers owned by the caller, integer
  * status codes, nothing throws or aborts across this boundary.  A handle is made once for what stays (types, widths,
  * scalars), touches no device, may be used from several streams at a time, and is freed by its destroy function.
- * Every other call is asynchronous: it enqueues one to three kernels on `stream` (hipStream_t as void*, NULL is the
+ * Every other call is asynchronous: it enqueues a few kernels (mostly one) on `stream` (hipStream_t as void*, NULL is the
  * default stream), allocates nothing, never synchronises and can be captured into a graph.
  *
  * Maps are checked on the GPU before they are followed: an entry that points outside its tensor counts as "nowhere",

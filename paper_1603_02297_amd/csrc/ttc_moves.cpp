@@ -19,7 +19,7 @@ SortShape sort_shape(int64_t n, int experts)
     } else if (n <= kSortOne) {
         s.blocks = kSortOneBlocks;
     } else {                                // as many workgroups as may add up each other's counts, and beyond that as few as can be
-        while (s.blocks < kSortBlocks && (n + s.blocks * s.threads - 1) / (s.blocks * s.threads) > kSortSums) s.blocks *= 2;
+        while (s.blocks < kSortBlocks && !sort_adds((n + s.blocks * s.threads - 1) / (s.blocks * s.threads), experts)) s.blocks *= 2;
     }
     s.chunk = (int64_t)s.threads * s.blocks;
     s.chunks = std::max<int64_t>(1, (n + s.chunk - 1) / s.chunk);
@@ -73,7 +73,7 @@ int64_t route_workspace(const ttc_route_s* r, int64_t tokens)
 {
     const SortShape s = sort_shape(tokens * r->topk, r->experts);
     if (s.chunks <= 1) return 0;
-    return (s.chunks + (s.chunks > kSortSums ? 1 : 0)) * r->experts * (int64_t)sizeof(int32_t);
+    return (s.chunks + (sort_adds(s.chunks, r->experts) ? 0 : 1)) * r->experts * (int64_t)sizeof(int32_t);
 }
 
 // What the three row moves share: the token count, and the offsets that padding needs.

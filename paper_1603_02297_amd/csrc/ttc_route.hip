@@ -132,7 +132,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(SortArgs p)
     }
 }
 
-// Counts of the chunks before, per expert, in place; totals behind the last chunk.  Only for more than kSortSums chunks:
+// Counts of the chunks before, per expert, in place; totals behind the last chunk.  Only where sort_adds() says no:
 // 64 experts a workgroup, the chunks in as many ranges as it has wavefronts.
 __global__ __launch_bounds__(kSortThreads) void sum_kernel(int32_t* hist, int64_t chunks, int experts)
 {
@@ -238,7 +238,7 @@ template <int B> int launch_sort_blocks(const SortArgs& p, const SortShape& s, v
     void* sort_args[] = {&a};
     void* sum_args[] = {&a.hist, &chunks64, &experts};
     void* place_args[] = {&a, &chunks};
-    const bool summed = s.chunks > kSortSums;
+    const bool summed = !sort_adds(s.chunks, p.experts);
     if (hipLaunchKernel(reinterpret_cast<const void*>(&sort_kernel<B, false>), dim3((uint32_t)chunks), dim3(s.threads), sort_args, lds, st) != hipSuccess) return TTC_ERR_HIP;
     if (summed && hipLaunchKernel(reinterpret_cast<const void*>(&sum_kernel), dim3((uint32_t)((experts + kWave - 1) / kWave)), dim3(kSortThreads), sum_args, 0, st) != hipSuccess)
         return TTC_ERR_HIP;

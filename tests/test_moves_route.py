@@ -61,7 +61,8 @@ def run_sort(h, ids, experts, ld=None, source=True):
     (1024, 1, 33, 0, 1, np.int64), (1025, 1, 33, 0, 1, np.int64), (1024, 8, 128, 64, 16, np.int32), (2731, 3, 1000, 0, 3, np.int64),
     (4097, 2, 16, 16, 64, np.int64), (16384, 4, 64, 0, 128, np.int64), (30011, 5, 129, 3, 1, np.int32), (100003, 7, 255, 0, 16, np.int64),
     (140001, 8, 8, 4, 1, np.int64), (140001, 8, 1024, 0, 2, np.int32), (70001, 5, 300, 0, 64, np.int64),
-    (341, 6, 40, 0, 1, np.int64), (2049, 1, 2, 0, 1, np.int32), (131073, 1, 17, 0, 1, np.int64)])
+    (341, 6, 40, 0, 1, np.int64), (2049, 1, 2, 0, 1, np.int32), (131073, 1, 17, 0, 1, np.int64), (150000, 8, 40, 0, 1, np.int32),
+    (600000, 8, 700, 0, 1, np.int32), (70000, 8, 900, 0, 16, np.int64), (300000, 8, 30, 1, 1, np.int32)])
 def test_sort(tokens, topk, experts, first, align, id_type):
     rng = np.random.default_rng(tokens * 31 + topk)
     ids = (choose(rng, tokens, topk, experts + first + 2) if tokens < 20000 else rng.integers(-1, experts + first + 2, (tokens, topk))).astype(id_type)
@@ -187,7 +188,8 @@ def test_moves(kind, tokens, topk, experts, first, align, width, extra, shift, w
 @gpu
 @pytest.mark.parametrize("kind,tokens,topk,experts,first,align,width,beta", [
     ("bf16", 3000, 8, 32, 0, 16, 4128, 1.0), ("f32", 6001, 3, 5, 1, 1, 2049, 0.0), ("f16", 4000, 4, 9, 0, 64, 4100, 1.0), ("bf16", 2500, 9, 12, 3, 1, 2880, 0.0),
-    ("bf16", 20000, 2, 4, 4, 1, 2056, 0.0), ("f32", 90000, 2, 8, 0, 128, 130, 0.5), ("f16", 200000, 5, 64, 0, 8, 48, 0.0), ("bf16", 1500, 1, 8, 0, 1, 40000, 1.0)])
+    ("bf16", 20000, 2, 4, 4, 1, 2056, 0.0), ("f32", 90000, 2, 8, 0, 128, 130, 0.5), ("f16", 200000, 5, 64, 0, 8, 48, 0.0), ("bf16", 1500, 1, 8, 0, 1, 40000, 1.0),
+    ("bf16", 5000, 4, 8, 0, 1, 4097, 1.0), ("f16", 3000, 6, 8, 2, 32, 3333, 0.0)])
 def test_moves_of_large_batches(kind, tokens, topk, experts, first, align, width, beta):
     """Sizes at which rows are streamed and rows take several rounds, against 64 bits on the GPU; some choices elsewhere, some tokens empty."""
     code, dtype = ref.TYPES[kind]
