@@ -18,8 +18,8 @@ SortShape sort_shape(int64_t n, int experts)
         s.threads = (int)((need + kWave - 1) / kWave * kWave);
     } else if (n <= kSortOne) {
         s.blocks = kSortOneBlocks;
-    } else {                                // as many workgroups as may add up each other's counts, and beyond that as few as can be
-        while (s.blocks < kSortBlocks && !sort_adds((n + s.blocks * s.threads - 1) / (s.blocks * s.threads), experts)) s.blocks *= 2;
+    } else {                                // several workgroups, a lane with as few ids as kSortChunks allows
+        while (s.blocks < kSortBlocks && (n + s.blocks * s.threads - 1) / (s.blocks * s.threads) > kSortChunks) s.blocks *= 2;
     }
     s.chunk = (int64_t)s.threads * s.blocks;
     s.chunks = std::max<int64_t>(1, (n + s.chunk - 1) / s.chunk);

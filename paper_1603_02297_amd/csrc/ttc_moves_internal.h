@@ -32,11 +32,11 @@ constexpr int kSortBlocks = 8;             // ids a lane of the sort holds at mo
 constexpr int kSortOneBlocks = 2;          // and where one workgroup sorts alone: 2048 ids in 4.7 us, two kernels of two workgroups 3.4 + 3.2 and the
                                            // way from one to the other; 4000 ids the other way round (7.5 us alone)
 constexpr int kSortOne = kSortOneBlocks * kSortThreads;
-// Chunks, and counts in all, up to which every workgroup adds up the counts of the others by itself; beyond them a lane takes more ids, and at
-// last a kernel between does it.  1,048,576 ids of 64 experts with limits of 64, 128 and 512 chunks 28, 25 and 20 us, of 256 experts 31,
-// 34, 34; 524,288 ids of 1024 experts 43, 28 and 79 (512 chunks of so many counts are what the second limit is for).
-constexpr int64_t kSortSums = 512, kSortCounts = 1 << 17;
-inline bool sort_adds(int64_t chunks, int experts) { return chunks <= kSortSums && chunks * experts <= kSortCounts; }
+// Chunks up to which a lane takes no more ids, and counts (chunks times experts) up to which every workgroup adds up those of the others by
+// itself; beyond them a kernel between does it.  us for 1,048,576 ids of 64 and 256 experts with 128, 256 and 512 chunks 25, 18, 20 and 34, 24, 34;
+// 262,144 ids of 256 experts (256 chunks) 14 without the kernel between, 17 with it; 524,288 ids of 1024 experts 28 (128 chunks) and 23.
+constexpr int64_t kSortChunks = 256, kSortCounts = 1 << 16;
+inline bool sort_adds(int64_t chunks, int experts) { return chunks * experts <= kSortCounts; }
 
 inline int elem_bytes(int dtype) { return dtype == TTC_F32 ? 4 : dtype == TTC_F8 ? 1 : 2; }
 

@@ -156,7 +156,7 @@ __global__ __launch_bounds__(kSortThreads) void sum_kernel(int32_t* hist, int64_
 }
 
 // Ranks within a chunk become rows.  SUMMED: sum_kernel has been over the counts; otherwise every workgroup adds up
-// those of the other chunks by itself (a few 64 KB out of L2), which saves a launch.
+// those of the other chunks by itself (up to 256 KB out of L2), which saves a launch.
 template <int B, bool SUMMED>
 __global__ __launch_bounds__(kSortThreads) void place_kernel(SortArgs p, int32_t chunks)
 {

@@ -62,7 +62,8 @@ def run_sort(h, ids, experts, ld=None, source=True):
     (4097, 2, 16, 16, 64, np.int64), (16384, 4, 64, 0, 128, np.int64), (30011, 5, 129, 3, 1, np.int32), (100003, 7, 255, 0, 16, np.int64),
     (140001, 8, 8, 4, 1, np.int64), (140001, 8, 1024, 0, 2, np.int32), (70001, 5, 300, 0, 64, np.int64),
     (341, 6, 40, 0, 1, np.int64), (2049, 1, 2, 0, 1, np.int32), (131073, 1, 17, 0, 1, np.int64), (150000, 8, 40, 0, 1, np.int32),
-    (600000, 8, 700, 0, 1, np.int32), (70000, 8, 900, 0, 16, np.int64), (300000, 8, 30, 1, 1, np.int32)])
+    (600000, 8, 700, 0, 1, np.int32), (70000, 8, 900, 0, 16, np.int64), (300000, 8, 30, 1, 1, np.int32),
+    (20000, 8, 1000, 0, 1, np.int64), (60000, 8, 400, 0, 128, np.int32)])
 def test_sort(tokens, topk, experts, first, align, id_type):
     rng = np.random.default_rng(tokens * 31 + topk)
     ids = (choose(rng, tokens, topk, experts + first + 2) if tokens < 20000 else rng.integers(-1, experts + first + 2, (tokens, topk))).astype(id_type)
