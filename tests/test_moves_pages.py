@@ -222,7 +222,8 @@ def test_write_and_read(kind, cache_kind, heads, dim, page, pages, order, tokens
 @gpu
 @pytest.mark.parametrize("kind,cache_kind,heads,dim,tokens,order", [
     ("bf16", "bf16", 8, 128, 45000, "slots"), ("f16", "f16", 5, 84, 30000, "heads"), ("f32", "f32", 4, 130, 40000, "heads"), ("bf16", "f8", 8, 128, 50000, "heads"),
-    ("f32", "f8", 3, 97, 60000, "slots"), ("f16", "f8", 2, 576, 12000, "gaps")])
+    ("f32", "f8", 3, 97, 60000, "slots"), ("f16", "f8", 2, 576, 12000, "gaps"),
+    ("bf16", "f8", 15, 80, 20000, "heads"), ("bf16", "bf16", 1, 40, 300000, "slots"), ("f16", "f16", 3, 72, 60000, "heads"), ("f32", "f8", 7, 80, 60001, "gaps")])
 def test_large_moves_of_slots(kind, cache_kind, heads, dim, tokens, order):
     """Sizes at which stores, and then loads, are streamed; against indexing on the GPU in 64 bits."""
     (code, dtype), (cache_code, cache_type) = ref.TYPES[kind], ref.TYPES[cache_kind]
