@@ -309,7 +309,8 @@ template <bool WHOLE> __device__ __forceinline__ bool lane_place(const MoveArgs&
     return *vec < p.vecs;
 }
 
-// GROUP choices (2, 4 or 8, by topk) of a token from k0 on: the rows they point to, kNowhere where there is none, and their
+// GROUP choices (2, 4 or 8, by topk: 4096 x 2 rows of 1001 f32, combine and gradient 33.4 us in groups of eight, 29.2 of two; 700 x 4 of bf16
+// 13.1 of eight, 12.4 of four) of a token from k0 on: the rows they point to, kNowhere where there is none, and their
 // weights, 0 there.  All loads are under way together, none hangs on a branch: indices past the last choice read the
 // last one again.  Where the wavefront has one token they are scalar loads; the compiler would not make them by itself, for all it
 // knows the kernel's stores could change the map, and with vector loads that each wait for the one before
@@ -452,8 +453,11 @@ __global__ __launch_bounds__(kMoveThreads) void combine_kernel(MoveArgs p)
 // The gradient: `lanes` lanes walk over a whole row, because the dot products need all of it: a power of two up to a wavefront,
 // several tokens to a workgroup, or a whole workgroup of several wavefronts.  Their partial sums
 // meet by shuffles inside a wavefront and through LDS between wavefronts, always in the same order.
-constexpr int kGradWaves = 8;              // wavefronts of a workgroup at most (and then rounds): 500 x 4 rows of 4097 bf16 with 4, 8, 16 16.8, 15.5, 17.1 us,
-                                           // 8192 x 4 of 4104 176, 192, 235, of 8192 167, 162, 166, 2 x 8 of 4096 10.9, 9.0, 9.0
+// Wavefronts of a workgroup at most (beyond that they go round): 8, four from kGradMany tokens on, where five to seven of them would leave
+// slots of a compute unit empty and the many waits show that half the rows nowhere cause.  us with 8 and 4, bf16:
+//   3878 x 5 rows of 2112, one of two ranks 45.8, 31.8; 2844 x 5 of 2880 39.4, 30.6; 1996 x 5 of 4104 38.2, 33.9; all 8 rows here 82.9, 82.6
+//   (4608), at worst 87.3, 90.9 (4104); 100 x 4 rows of 8192 9.0, 10.1; 4 x 8 8.2, 9.1; 500 x 4 of 4097 15.5, 16.8.
+constexpr int kGradWaves = 8, kGradWavesMany = 4, kGradMany = 1024;
 template <typename T, int V, int GROUP, bool WHOLE, bool NT>
 __global__ __launch_bounds__(WHOLE ? kGradWaves * kWave : kMoveThreads) void combine_grad_kernel(MoveArgs p)
 {
@@ -482,7 +486,7 @@ __global__ __launch_bounds__(WHOLE ? kGradWaves * kWave : kMoveThreads) void com
             for (uint32_t vec = lane; vec < p.vecs; vec += lanes) {
                 const MovePlace place = row_place<V>(vec, p.r.width);
                 const uint32_t c = place.at;
-                            Vec<T, V> d = load_vec<T, V, false>(dy + c), x[GROUP];
+                Vec<T, V> d = load_vec<T, V, false>(dy + c), x[GROUP];
 #pragma unroll
                 for (int k = 0; k < GROUP; ++k) {
                     x[k] = {};
@@ -626,8 +630,9 @@ template <typename T> int launch_grad_type(const RowArgs& r, void* stream)
     MoveArgs p = move_args<T>(r);
     p.lanes = 1u << p.lanes_log;
     int threads = kMoveThreads;
-    if (p.vecs > (uint32_t)kWave) {         // as few rounds as kGradWaves wavefronts need, and then no more wavefronts than those rounds
-        const uint32_t pieces = (p.vecs + kWave - 1) / kWave, rounds = (pieces + kGradWaves - 1) / kGradWaves;
+    if (p.vecs > (uint32_t)kWave) {         // as few rounds as that many wavefronts need, and then no more wavefronts than those rounds
+        const uint32_t most = r.tokens >= kGradMany ? kGradWavesMany : kGradWaves;
+        const uint32_t pieces = (p.vecs + kWave - 1) / kWave, rounds = (pieces + most - 1) / most;
         p.lanes = (pieces + rounds - 1) / rounds * kWave;
         threads = (int)p.lanes;
     }
