@@ -30,19 +30,29 @@ def _ptr(x) -> int:
     return 0 if x is None else x.data_ptr()
 
 
+def _matrix(x: torch.Tensor, shape, dtype: torch.dtype, device, what: str) -> torch.Tensor:
+    """x as the moves take a matrix, by its address and leading dimension alone: of this type and shape, elements of a row next to each other,
+    rows apart from each other.  Columns in the place of rows and a row that stands for many (an expanded tensor) are copied out."""
+    if x.dtype != dtype or tuple(x.shape) != tuple(shape) or x.device != device:
+        raise ValueError(f"{what}: {x.dtype} {list(x.shape)} on {x.device}, wanted {dtype} {list(shape)} on {device}")
+    fits = (x.shape[1] <= 1 or x.stride(1) == 1) and (x.shape[0] <= 1 or x.stride(0) >= x.shape[1])
+    return x if fits else x.contiguous()
+
+
 def _rows_apart(x: torch.Tensor) -> int:
-    """The leading dimension of a row-major matrix, which may be part of a wider one."""
-    if x.stride(-1) != 1:
-        raise ValueError("the elements of a row are neighbours")
-    return max(x.stride(0), x.shape[-1])
+    """The leading dimension of such a matrix, which may be part of a wider one."""
+    return max(x.stride(0), x.shape[1])
 
 
 class Routing:
     """The rows of one batch sorted by expert: what ttc_route_sort found, and the moves along it."""
 
     def __init__(self, ids: torch.Tensor, experts: int, width: int, dtype: torch.dtype, first: int = 0, align: int = 1):
+        if ids.dim() != 2 or ids.dtype not in (torch.int32, torch.int64) or not ids.is_cuda:
+            raise ValueError(f"ids: {ids.dtype} {list(ids.shape)} on {ids.device}, wanted [tokens, topk] of int32 or int64 on the GPU")
         self.tokens, self.topk = ids.shape
         self.width, self.dtype, self.experts, self.device = width, dtype, experts, ids.device
+        ids = _matrix(ids, ids.shape, ids.dtype, ids.device, "ids")
         self.handle = ttc.ttc_route_create(CODES[dtype], width, self.topk, experts, first, align, ids.element_size())
         weakref.finalize(self, ttc.ttc_route_destroy, self.handle)
         self.row_count = ttc.ttc_route_rows(self.handle, self.tokens)
@@ -51,19 +61,32 @@ class Routing:
         work = torch.empty(ttc.ttc_route_workspace(self.handle, self.tokens), dtype=torch.uint8, device=self.device)
         ttc.ttc_route_sort(self.handle, self.tokens, _ptr(ids), _rows_apart(ids), _ptr(self.offsets), _ptr(self.counts), _ptr(self.position), 0, _ptr(work), _stream())
 
+    def _tokens(self, x: torch.Tensor, what: str) -> torch.Tensor:
+        return _matrix(x, (self.tokens, self.width), self.dtype, self.device, what)
+
+    def _rows(self, x: torch.Tensor, what: str) -> torch.Tensor:
+        return _matrix(x, (self.row_count, self.width), self.dtype, self.device, what)
+
+    def _weights(self, w: torch.Tensor) -> torch.Tensor:
+        return _matrix(w, (self.tokens, self.topk), torch.float32, self.device, "weights").contiguous()
+
     def gather(self, x: torch.Tensor) -> torch.Tensor:
         """Tokens to their rows; rows past the last segment are 0."""
+        x = self._tokens(x, "x")
         rows = torch.zeros(self.row_count, self.width, dtype=self.dtype, device=self.device)
         ttc.ttc_route_gather(self.handle, self.tokens, _ptr(x), _rows_apart(x), 0, _ptr(self.position), _ptr(self.offsets), _ptr(self.counts), _ptr(rows), self.width, _stream())
         return rows
 
     def combine(self, rows: torch.Tensor, weights) -> torch.Tensor:
+        rows, weights = self._rows(rows, "rows"), None if weights is None else self._weights(weights)
         y = torch.empty(self.tokens, self.width, dtype=self.dtype, device=self.device)
         ttc.ttc_route_combine(self.handle, self.tokens, _ptr(rows), _rows_apart(rows), _ptr(weights), _ptr(self.position), _ptr(y), self.width, _stream())
         return y
 
     def combine_grad(self, dy: torch.Tensor, rows: torch.Tensor, weights: torch.Tensor):
-        drows, dweights = torch.zeros_like(rows), torch.empty_like(weights)
+        dy, rows, weights = self._tokens(dy, "dy"), self._rows(rows, "rows"), self._weights(weights)
+        drows = torch.zeros(self.row_count, self.width, dtype=self.dtype, device=self.device)
+        dweights = torch.empty(self.tokens, self.topk, dtype=torch.float32, device=self.device)
         ttc.ttc_route_combine_grad(self.handle, self.tokens, _ptr(dy), _rows_apart(dy), _ptr(rows), _rows_apart(rows), _ptr(weights), _ptr(self.position),
                                    _ptr(self.offsets), _ptr(self.counts), _ptr(drows), self.width, _ptr(dweights), _stream())
         return drows, dweights
@@ -79,7 +102,7 @@ class Gather(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, drows):
-        return ctx.routing.combine(drows.contiguous(), None), None
+        return ctx.routing.combine(drows, None), None
 
 
 class Combine(torch.autograd.Function):
@@ -93,7 +116,7 @@ class Combine(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dy):
-        drows, dweights = ctx.routing.combine_grad(dy.contiguous(), *ctx.saved_tensors)
+        drows, dweights = ctx.routing.combine_grad(dy, *ctx.saved_tensors)
         return drows, dweights, None
 
 
@@ -101,12 +124,12 @@ def experts_forward(x: torch.Tensor, router: torch.Tensor, up: torch.Tensor, dow
     """x [tokens, width] through the experts that the router chooses: up [experts, width, hidden], down [experts, hidden, width]."""
     logits = x.float() @ router.float()
     best, ids = logits.topk(topk, dim=1)
-    routing = Routing(ids.contiguous(), up.shape[0], x.shape[1], x.dtype, align=align)
+    routing = Routing(ids, up.shape[0], x.shape[1], x.dtype, align=align)
     rows = Gather.apply(x, routing)
     ends = routing.offsets.tolist()                               # the segments' sizes shape the products
     out = [torch.nn.functional.silu(rows[a:b] @ up[e]) @ down[e] for e, (a, b) in enumerate(zip(ends, ends[1:]))]
     out.append(rows[ends[-1]:])                                   # rows that nothing points to
-    return Combine.apply(torch.cat(out), best.softmax(1).contiguous(), routing)
+    return Combine.apply(torch.cat(out), best.softmax(1), routing)
 
 
 class PagedCache:

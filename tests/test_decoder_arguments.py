@@ -1,0 +1,123 @@
+"""What the example's classes (paper_1603_02297_amd/decoder.py) hand to the library: addresses and leading dimensions that stay inside the tensors, or an error
+before the call."""
+import pytest
+import torch
+
+import paper_1603_02297_amd as ttc
+from paper_1603_02297_amd import decoder
+
+gpu = pytest.mark.gpu
+
+
+class Recorder:
+    """In place of the library's moves: what they were given."""
+
+    def __init__(self, monkeypatch):
+        self.calls = []
+        monkeypatch.setattr(decoder, "_stream", lambda: 0)
+        for name in ("ttc_route_gather", "ttc_route_combine", "ttc_route_combine_grad"):
+            monkeypatch.setattr(ttc, name, lambda *args, name=name: self.calls.append((name, args)))
+
+
+def routing(tokens, topk, width, rows, dtype=torch.float32):
+    """A routing whose maps are of no interest, on the CPU."""
+    r = decoder.Routing.__new__(decoder.Routing)
+    i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32)  # noqa: E731
+    r.tokens, r.topk, r.width, r.row_count, r.dtype, r.device, r.handle = tokens, topk, width, rows, dtype, torch.device("cpu"), 0
+    r.offsets, r.counts, r.position = i32(5), i32(4), i32(tokens, topk)
+    return r
+
+
+def matrices(width):
+    """Matrices of 6 rows whose strides are not a dense matrix's: one row for all, one column for all, columns for rows, part of a wider one, every other element."""
+    base = torch.arange(400.0)
+    return [base[:width].expand(6, width), base[:6, None].expand(6, width), base[:6 * width].view(width, 6).t(), base[:6 * (width + 3)].view(6, width + 3)[:, 1:width + 1],
+            base[:12 * width].view(6, 2 * width)[:, ::2], base[:6 * width].view(6, width)]
+
+
+@pytest.mark.parametrize("width", [1, 2, 17])
+def test_addresses_stay_inside_and_mean_the_tensor(monkeypatch, width):
+    """What a call would read, by address and leading dimension, is the tensor's own elements."""
+    def read(x, ld, address, rows, kept):
+        owner = next((t for t in kept if t.untyped_storage().data_ptr() <= address < t.untyped_storage().data_ptr() + t.untyped_storage().nbytes()), None)
+        assert owner is not None
+        flat = torch.empty(0, dtype=torch.float32).set_(owner.untyped_storage())
+        first = (address - owner.untyped_storage().data_ptr()) // 4
+        assert first + (rows - 1) * ld + width <= flat.numel()
+        assert torch.equal(torch.as_strided(flat, (rows, width), (ld, 1), first), x)
+
+    kept = []
+    whole = torch.Tensor.contiguous
+    monkeypatch.setattr(torch.Tensor, "contiguous", lambda t: kept.append(whole(t)) or kept[-1])      # copies live as long as the test
+    for x in matrices(width):
+        kept[:] = [x]
+        seen = Recorder(monkeypatch)
+        r = routing(6, 2, width, 6)
+        r.gather(x)
+        r.combine(x, None)
+        r.combine_grad(x, x, torch.ones(6, 2))
+        (_, g), (_, c), (_, d) = seen.calls
+        for address, ld in ((g[2], g[3]), (c[2], c[3]), (d[2], d[3]), (d[4], d[5])):
+            read(x, ld, address, 6, kept)
+
+
+def test_weights_and_their_gradient_are_dense(monkeypatch):
+    seen, r = Recorder(monkeypatch), routing(6, 3, 4, 18)
+    w = torch.arange(18.0).view(3, 6).t()
+    kept, whole = [], torch.Tensor.contiguous
+    monkeypatch.setattr(torch.Tensor, "contiguous", lambda t: kept.append(whole(t)) or kept[-1])
+    _, dw = r.combine_grad(torch.ones(6, 4), torch.ones(18, 4), w)
+    assert dw.is_contiguous() and dw.shape == w.shape
+    assert any(t.data_ptr() == seen.calls[0][1][6] and torch.equal(t, w) and t.is_contiguous() for t in kept)
+
+
+def test_other_types_and_shapes_are_refused(monkeypatch):
+    seen, r = Recorder(monkeypatch), routing(6, 2, 8, 12)
+    x, rows, w = torch.ones(6, 8), torch.ones(12, 8), torch.ones(6, 2)
+    for bad in (x.bfloat16(), x.double(), x[:5], x[:, :7], x.view(48), torch.ones(6, 9), x.to("meta")):
+        for call in (lambda: r.gather(bad), lambda: r.combine_grad(bad, rows, w)):
+            with pytest.raises(ValueError):
+                call()
+    for bad in (rows.half(), rows[:11], torch.ones(13, 8), rows[:, 1:]):
+        for call in (lambda: r.combine(bad, w), lambda: r.combine_grad(x, bad, w)):
+            with pytest.raises(ValueError):
+                call()
+    for bad in (w.double(), w.bfloat16(), w[:, :1], w[:5], torch.ones(6, 3)):
+        for call in (lambda: r.combine(rows, bad), lambda: r.combine_grad(x, rows, bad)):
+            with pytest.raises(ValueError):
+                call()
+    assert not seen.calls
+
+
+def test_ids_are_whole_numbers_on_the_gpu():
+    for ids in (torch.zeros(4, 2, dtype=torch.int64), torch.zeros(4, 2), torch.zeros(4, dtype=torch.int64)):
+        with pytest.raises(ValueError):
+            decoder.Routing(ids, 4, 8, torch.float32)
+
+
+@gpu
+def test_broadcast_tokens_and_gradients():
+    """One token for many, and the gradient of a sum (one number for all): as for the same values written out."""
+    torch.manual_seed(5)
+    tokens, topk, width, experts = 37, 3, 24, 5
+    ids = torch.rand(tokens, experts, device="cuda").topk(topk, dim=1).indices
+    for made in (ids, ids.t().contiguous().t(), ids.to(torch.int32)):
+        r = decoder.Routing(made, experts, width, torch.float32, align=4)
+        weights, one = torch.randn(tokens, topk, device="cuda"), torch.randn(1, width, device="cuda")
+        results = []
+        for form in (lambda t: t.expand(tokens, width), lambda t: t.expand(tokens, width).contiguous()):
+            x, w = one.clone().requires_grad_(), weights.clone().requires_grad_()
+            rows = decoder.Gather.apply(form(x), r)
+            y = decoder.Combine.apply(rows * 2, w, r)
+            scale = form(torch.full((1, 1), 3.0, device="cuda"))
+            gx, gw = torch.autograd.grad(y, (x, w), scale)
+            results.append((rows, y, gx, gw))
+        for a, b in zip(*results):
+            assert torch.equal(a, b)
+        assert torch.equal(results[0][0][r.position.long().reshape(-1)], one.expand(tokens * topk, width))
+    with pytest.raises(ValueError):
+        decoder.Routing(torch.zeros(4, 2, device="cuda"), 4, 8, torch.float32)
+    with pytest.raises(ValueError):
+        r.gather(torch.zeros(tokens, width, device="cuda", dtype=torch.bfloat16))
+    with pytest.raises(ValueError):
+        r.combine(torch.zeros(r.row_count - 1, width, device="cuda"), weights)
