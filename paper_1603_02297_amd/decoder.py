@@ -154,12 +154,23 @@ class PagedCache:
         return starts, page_starts, slots
 
     def append(self, fresh: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> torch.Tensor:
-        """fresh [requests]: how many of the packed new tokens are each one's; k, v [tokens, heads*dim].  Returns their packed offsets."""
-        starts, page_starts, slots = self._map(None, fresh, k.shape[0])
-        taken = int(page_starts[-1])
+        """fresh [requests]: how many of the packed new tokens are each one's; k, v [tokens, heads*dim].  Returns their packed offsets.  What does
+        not fit is refused before anything is mapped: a position past the table has no slot, and the write would leave its token out."""
+        tokens, device = k.shape[0], self.k.device
+        k, v = (_matrix(x, (tokens, self.heads * self.dim), self.dtype, device, "keys and values") for x in (k, v))
+        if fresh.dtype != torch.int32 or tuple(fresh.shape) != (self.requests,) or fresh.device != device:
+            raise ValueError(f"fresh: {fresh.dtype} {list(fresh.shape)} on {fresh.device}, wanted int32 [{self.requests}] on {device}")
+        fresh, end, limit = fresh.contiguous(), self.cached.long() + fresh, self.table.shape[1] * self.page
+        blocks = lambda n: (n + (self.page - 1)) // self.page  # noqa: E731
+        total, negative, over, taken = torch.stack([fresh.sum(), (fresh < 0).any(), (end > limit).sum(), (blocks(end) - blocks(self.cached.long())).sum()]).tolist()
+        if negative or total != tokens:
+            raise ValueError(f"fresh: {total} tokens, the keys are of {tokens}" if not negative else "fresh: a negative length")
+        if over:
+            raise RuntimeError(f"{over} requests would hold more than the {limit} tokens that the table has entries for")
         if taken > self.free.numel():
             raise RuntimeError(f"{taken} pages wanted, {self.free.numel()} free")
-        ttc.ttc_pages_write(self.handle, k.shape[0], _ptr(slots), _ptr(k), _rows_apart(k), _ptr(v), _rows_apart(v), _ptr(self.k), _ptr(self.v),
+        starts, _, slots = self._map(None, fresh, tokens)
+        ttc.ttc_pages_write(self.handle, tokens, _ptr(slots), _ptr(k), _rows_apart(k), _ptr(v), _rows_apart(v), _ptr(self.k), _ptr(self.v),
                             _ptr(self.scale), _ptr(self.scale), _stream())
         self.free, self.cached = self.free[taken:].contiguous(), self.cached + fresh
         return starts
@@ -209,9 +220,11 @@ def main() -> None:
     width, heads, kv_heads, dim, experts, topk, dtype = 512, 8, 2, 64, 16, 4, torch.bfloat16
     w = weights(width, heads, kv_heads, dim, experts, 1024, dtype)
     g = torch.Generator(device="cuda").manual_seed(1)
-    lengths = torch.tensor([70, 1, 33, 128], dtype=torch.int32, device="cuda")
+    prompts, page = [70, 1, 33, 128], 16
+    longest, pages = max(prompts) + steps, sum(-(-(n + steps) // page) for n in prompts)
+    lengths = torch.tensor(prompts, dtype=torch.int32, device="cuda")
     for cache_dtype in (torch.bfloat16, torch.float8_e4m3fn):
-        cache = PagedCache(4, kv_heads, dim, 16, 64, 256, dtype, cache_dtype)
+        cache = PagedCache(len(prompts), kv_heads, dim, page, max(pages, 64), longest, dtype, cache_dtype)
         with torch.no_grad():
             y = layer(torch.randn(int(lengths.sum()), width, generator=g, device="cuda").to(dtype), lengths, cache, w, heads, topk)
             print(f"{cache_dtype}: prompts of {lengths.tolist()} tokens, mean square {float(y.float().square().mean()):.3f}, {cache.free.numel()} pages free")

@@ -1,5 +1,8 @@
 """What the example's classes (paper_1603_02297_amd/decoder.py) hand to the library: addresses and leading dimensions that stay inside the tensors, or an error
 before the call."""
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -121,3 +124,79 @@ def test_broadcast_tokens_and_gradients():
         r.gather(torch.zeros(tokens, width, device="cuda", dtype=torch.bfloat16))
     with pytest.raises(ValueError):
         r.combine(torch.zeros(r.row_count - 1, width, device="cuda"), weights)
+
+
+# ---- the paged cache: what does not fit changes nothing ----------------------------------------------------------
+
+def filled_cache(device, pages=9, longest=24, dtype=torch.float32):
+    """Three requests that hold 20, 0 and 9 tokens in pages of 8."""
+    c = decoder.PagedCache(3, 2, 4, 8, pages, longest, dtype, dtype, device=device)
+    return c, torch.tensor([20, 0, 9], dtype=torch.int32, device=device)
+
+
+BAD = [  # fresh, tokens, error
+    ([5, 0, 0], 5, RuntimeError), ([0, 25, 0], 25, RuntimeError), ([4, 24, 16], 44, RuntimeError), ([4, 24, 15], 43, RuntimeError), ([2 ** 31 - 1, 2 ** 31 - 1, 2], 0, ValueError), ([1, 1, 1], 2, ValueError),
+    ([1, 1, 1], 4, ValueError), ([3, -1, 0], 2, ValueError), ([0, 0, 0], 1, ValueError)]
+
+
+@pytest.mark.parametrize("fresh,tokens,error", BAD)
+def test_what_does_not_fit_the_table_or_the_pages_is_not_appended(monkeypatch, fresh, tokens, error):
+    called = []
+    for name in ("ttc_pages_map", "ttc_pages_write"):
+        monkeypatch.setattr(ttc, name, lambda *args: called.append(args))
+    monkeypatch.setattr(decoder, "_stream", lambda: 0)
+    c, c.cached = filled_cache("cpu", pages=3 if sum(fresh) == 43 else 99)
+    free, cached = c.free.clone(), c.cached.clone()
+    with pytest.raises(error) as e:
+        c.append(torch.tensor(fresh, dtype=torch.int32), torch.ones(tokens, 8), torch.ones(tokens, 8))
+    assert not isinstance(e.value, ttc.TtcError) and not called
+    assert torch.equal(c.free, free) and torch.equal(c.cached, cached)
+
+
+def test_appended_tensors_are_checked(monkeypatch):
+    called = []
+    for name in ("ttc_pages_map", "ttc_pages_write"):
+        monkeypatch.setattr(ttc, name, lambda *args: called.append(args))
+    c, _ = filled_cache("cpu")
+    one, k = torch.ones(3, dtype=torch.int32), torch.ones(3, 8)
+    for fresh, a, b in ((one.long(), k, k), (one[:2], k, k), (one.view(3, 1), k, k), (one, k.half(), k), (one, k, k[:2]), (one, k[:, :7], k), (one, k, torch.ones(3, 9)), (one.to("meta"), k, k)):
+        with pytest.raises(ValueError):
+            c.append(fresh, a, b)
+    assert not called
+
+
+@gpu
+def test_a_cache_filled_to_its_last_place_and_beyond():
+    """Up to the table's end everything is kept; one token more is an error that leaves the cache as it was."""
+    torch.manual_seed(6)
+    c, lengths = filled_cache("cuda")
+    draw = lambda n: torch.randn(n, 8, device="cuda")  # noqa: E731
+    k, v = draw(29), draw(29)
+    c.append(lengths, k, v)
+    more = torch.tensor([4, 24, 15], dtype=torch.int32, device="cuda")
+    k2, v2 = draw(43), draw(43)
+    c.append(more, k2, v2)
+    assert c.cached.tolist() == [24, 24, 24] and c.free.numel() == 0
+
+    def check():
+        starts, got_k, got_v = c.context()
+        assert starts.tolist() == [0, 24, 48, 72]
+        for got, a, b in ((got_k, k, k2), (got_v, v, v2)):
+            assert torch.equal(got, torch.cat([a[:20], b[:4], b[4:28], a[20:], b[28:]]))
+
+    check()
+    for r in range(3):
+        fresh = torch.zeros(3, dtype=torch.int32, device="cuda")
+        fresh[r] = 1
+        with pytest.raises(RuntimeError):
+            c.append(fresh, draw(1), draw(1))
+    assert c.cached.tolist() == [24, 24, 24] and c.free.numel() == 0
+    check()
+
+
+@gpu
+def test_the_command_serves_as_many_steps_as_it_is_asked_for():
+    """The cache is sized by the prompts and the steps: 140 steps take the longest request past 256 tokens."""
+    done = subprocess.run([sys.executable, "-m", "paper_1603_02297_amd.decoder", "--steps", "140"], capture_output=True, text=True, timeout=110)
+    assert done.returncode == 0, done.stderr[-2000:]
+    assert done.stdout.count("lengths [210, 141, 173, 268]") == 2
