@@ -93,7 +93,8 @@ class Routing:
 
 
 class Gather(torch.autograd.Function):
-    """Tokens to their rows; the gradient adds the rows up again."""
+    """Tokens to their rows; the gradient adds the rows up again.  The moves go by address and record no graph of their own, so that every
+    backward pass here is written in these functions again and can be differentiated in its turn."""
 
     @staticmethod
     def forward(ctx, x, routing):
@@ -102,11 +103,11 @@ class Gather(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, drows):
-        return ctx.routing.combine(drows, None), None
+        return Combine.apply(drows, None, ctx.routing), None
 
 
 class Combine(torch.autograd.Function):
-    """Rows back to their tokens, weighted; the gradients of rows and weights in one pass."""
+    """Rows back to their tokens, weighted (weights None: all 1); the gradients of rows and weights in one pass."""
 
     @staticmethod
     def forward(ctx, rows, weights, routing):
@@ -116,8 +117,26 @@ class Combine(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, dy):
-        drows, dweights = ctx.routing.combine_grad(dy, *ctx.saved_tensors)
-        return drows, dweights, None
+        rows, weights = ctx.saved_tensors
+        if weights is None:
+            return Gather.apply(dy, ctx.routing), None, None
+        return (*CombineGrad.apply(dy, rows, weights, ctx.routing), None)
+
+
+class CombineGrad(torch.autograd.Function):
+    """drows = weights * dy and dweights = <dy, rows>, along the map: both are linear in dy, the one in weights, the other in rows."""
+
+    @staticmethod
+    def forward(ctx, dy, rows, weights, routing):
+        ctx.routing = routing
+        ctx.save_for_backward(dy, rows, weights)
+        return routing.combine_grad(dy, rows, weights)
+
+    @staticmethod
+    def backward(ctx, to_rows, to_weights):
+        dy, rows, weights = ctx.saved_tensors
+        back = Combine.apply(to_rows, weights, ctx.routing) + Combine.apply(rows, to_weights, ctx.routing)
+        return (back, *CombineGrad.apply(dy, to_rows, to_weights, ctx.routing), None)
 
 
 def experts_forward(x: torch.Tensor, router: torch.Tensor, up: torch.Tensor, down: torch.Tensor, topk: int, align: int = 16) -> torch.Tensor:

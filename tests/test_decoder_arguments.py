@@ -126,6 +126,69 @@ def test_broadcast_tokens_and_gradients():
         r.combine(torch.zeros(r.row_count - 1, width, device="cuda"), weights)
 
 
+# ---- derivatives of derivatives -------------------------------------------------------------------------------
+
+class PlainRouting:
+    """The moves of Routing in torch operations on the CPU, detached as the library's calls are."""
+
+    def __init__(self, position, rows):
+        self.position, self.rows = position, rows
+
+    def gather(self, x):
+        out = torch.zeros(self.rows, x.shape[1], dtype=x.dtype)
+        out[self.position.reshape(-1)] = x.detach().repeat_interleave(self.position.shape[1], 0)
+        return out
+
+    def combine(self, rows, weights):
+        w = torch.ones(self.position.shape, dtype=rows.dtype) if weights is None else weights.detach()
+        return (rows.detach()[self.position] * w[:, :, None]).sum(1)
+
+    def combine_grad(self, dy, rows, weights):
+        drows = torch.zeros_like(rows)
+        drows[self.position.reshape(-1)] = (dy.detach()[:, None, :] * weights.detach()[:, :, None]).reshape(-1, dy.shape[1])
+        return drows, (dy.detach()[:, None, :] * rows.detach()[self.position]).sum(2)
+
+
+def test_derivatives_of_derivatives():
+    """First, second and third derivatives through Gather and Combine agree with those through torch's operations."""
+    torch.manual_seed(1)
+    position = torch.randperm(12).view(6, 2)
+    r, up = PlainRouting(position, 12), torch.randn(5, 5, dtype=torch.float64, requires_grad=True)
+    x, w = torch.randn(6, 5, dtype=torch.float64, requires_grad=True), torch.randn(6, 2, dtype=torch.float64, requires_grad=True)
+
+    def through(moves):
+        rows = decoder.Gather.apply(x, r) if moves else torch.zeros(12, 5, dtype=torch.float64).index_put((position.reshape(-1),), x.repeat_interleave(2, 0))
+        rows = torch.tanh(rows @ up)
+        y, levels = decoder.Combine.apply(rows, w, r) if moves else (rows[position] * w[:, :, None]).sum(1), []
+        value = (y ** 2).sum()
+        for _ in range(3):
+            levels.append(torch.autograd.grad(value, (x, w, up), create_graph=True))
+            value = sum((g ** 2).sum() for g in levels[-1])
+        return levels
+
+    for mine, exact in zip(through(True), through(False)):
+        assert all(torch.allclose(a, b, rtol=1e-9) for a, b in zip(mine, exact))
+
+
+@gpu
+def test_gradient_of_a_gradient_norm_through_the_experts():
+    """In 32 bits through the moves, against torch's operations in 64 bits."""
+    from test_decoder import plain_experts
+    torch.manual_seed(3)
+    tokens, width, hidden, experts, topk = 29, 52, 24, 7, 3
+    exact = [torch.randn(tokens, width), torch.randn(width, experts) / width ** 0.5, torch.randn(experts, width, hidden) / width ** 0.5, torch.randn(experts, hidden, width) / hidden ** 0.5]
+    mine = [p.cuda().requires_grad_() for p in exact]
+    exact = [p.double().requires_grad_() for p in exact]
+    results = []
+    for f, p in ((plain_experts, exact), (decoder.experts_forward, mine)):
+        first = torch.autograd.grad((f(*p, topk) ** 2).sum(), p, create_graph=True)
+        results.append(torch.autograd.grad(sum((g ** 2).sum() for g in first), p))
+    # chains of products over at most 52 terms and sums over at most 29 tokens, each off by their length in units of 2^-24, some ten of them one
+    # after another: below 1e-4 of the largest value; a part that is missing is some tenths of it
+    for a, b in zip(*results):
+        assert float((b.cpu().double() - a).abs().max()) <= 1e-3 * float(a.abs().max())
+
+
 # ---- the paged cache: what does not fit changes nothing ----------------------------------------------------------
 
 def filled_cache(device, pages=9, longest=24, dtype=torch.float32):
