@@ -24,17 +24,29 @@ __all__ = [*MOVE_EXPORTS, "MOVE_EXPORTS", "TTC_BF16", "TTC_F16", "TTC_F8", "TTC_
 _MOVES = ("ttc_route_sort", "ttc_route_gather", "ttc_route_combine", "ttc_route_combine_grad", "ttc_pages_map", "ttc_pages_write", "ttc_pages_read")
 
 
+class _Address(ctypes.c_void_p):
+    """An address: an int, None, a c_void_p, or an object whose _as_parameter_ is one.  ctypes by itself would also take a str, bytes or an array for one and hand on where those lie in
+    host memory, which no check of the library can tell from a device address."""
+
+    @classmethod
+    def from_param(cls, value):
+        value = getattr(value, "_as_parameter_", value)
+        if value is None or isinstance(value, (int, ctypes.c_void_p)):
+            return ctypes.c_void_p.from_param(value)
+        raise TypeError(f"an address is an int or None, not {type(value).__name__}")
+
+
 def _declare(L: ctypes.CDLL) -> None:
-    vp, i, n = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64
+    vp, ret, i, n = _Address, ctypes.c_void_p, ctypes.c_int, ctypes.c_int64
     fp, np = ctypes.POINTER(ctypes.c_float), ctypes.POINTER(ctypes.c_int64)
     for name, restype, argtypes in (
-            ("ttc_route_create", vp, [i, n, i, i, n, i, i, fp, fp]), ("ttc_route_destroy", i, [vp]),
+            ("ttc_route_create", ret, [i, n, i, i, n, i, i, fp, fp]), ("ttc_route_destroy", i, [vp]),
             ("ttc_route_rows", n, [vp, n]), ("ttc_route_workspace", n, [vp, n]),
             ("ttc_route_sort", i, [vp, n, vp, n, vp, vp, vp, vp, vp, vp]),
             ("ttc_route_gather", i, [vp, n, vp, n, vp, vp, vp, vp, vp, n, vp]),
             ("ttc_route_combine", i, [vp, n, vp, n, vp, vp, vp, n, vp]),
             ("ttc_route_combine_grad", i, [vp, n, vp, n, vp, n, vp, vp, vp, vp, vp, n, vp, vp]),
-            ("ttc_pages_create", vp, [i, i, n, n, n, n, np]), ("ttc_pages_destroy", i, [vp]),
+            ("ttc_pages_create", ret, [i, i, n, n, n, n, np]), ("ttc_pages_destroy", i, [vp]),
             ("ttc_pages_map", i, [vp, n, vp, vp, vp, vp, n, vp, n, n, vp, vp, vp, vp, vp, vp]),
             ("ttc_pages_write", i, [vp, n, vp, vp, n, vp, n, vp, vp, vp, vp, vp]),
             ("ttc_pages_read", i, [vp, n, vp, vp, vp, vp, vp, vp, n, vp, n, vp])):
@@ -42,7 +54,7 @@ def _declare(L: ctypes.CDLL) -> None:
         f.restype, f.argtypes = restype, argtypes
     if _fast is not None:
         for k, name in enumerate(_MOVES):
-            _fast.bind_move(k, ctypes.cast(getattr(L, name), vp).value)
+            _fast.bind_move(k, ctypes.cast(getattr(L, name), ret).value)
 
 
 binding._on_load.append(_declare)
