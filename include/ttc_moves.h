@@ -152,12 +152,14 @@ int ttc_pages_map(ttc_pages_t pages, int64_t requests, const int32_t* first, con
  *   k_scale, v_scale [heads] float or NULL (1): with TTC_F8 the cache holds k / k_scale[h], cut at +-448 and rounded to
  *              nearest even; a NaN stays one.  Refused (TTC_ERR_INVALID_VALUE) with another cache type.
  * A token whose slot is nowhere (negative, or past the cache) is left out.  Two tokens must not have one slot.
+ * k_cache and v_cache may be parts of one tensor, their vectors between each other's; sharing an element is TTC_ERR_ALIAS.
  */
 int ttc_pages_write(ttc_pages_t pages, int64_t tokens, const int32_t* slots, const void* k, int64_t ldk, const void* v, int64_t ldv,
                     void* k_cache, void* v_cache, const float* k_scale, const float* v_scale, void* stream);
 
 /*
  * And out of it:  k[:, h, i] <- k_cache[:, h, slots[i]] (* k_scale[h]), 0 where the slot is nowhere.
+ * k and v may be parts of one tensor, with ldk == ldv where one lies within the other's rows; sharing an element is TTC_ERR_ALIAS.
  */
 int ttc_pages_read(ttc_pages_t pages, int64_t tokens, const int32_t* slots, const void* k_cache, const void* v_cache,
                    const float* k_scale, const float* v_scale, void* k, int64_t ldk, void* v, int64_t ldv, void* stream);

@@ -60,6 +60,27 @@ template <int N> int check_operands(const Operand (&o)[N])
     return TTC_OK;
 }
 
+// Keys and values are written by one call and may be parts of one tensor, so that their spans interleave: whether two tensors of one layout,
+// `apart` bytes from each other, share a byte.  Levels go from the largest stride down, each stride no smaller than all that lies below it
+// spans, so that only the two steps next to apart / stride bring them that close.
+struct Level {
+    int64_t stride, extent;                 // bytes, entries
+};
+bool share(int64_t apart, const Level* l, int levels, int64_t bytes)
+{
+    if (levels == 0) return -bytes < apart && apart < bytes;
+    const int64_t step = apart / l->stride - (apart % l->stride < 0);
+    for (int64_t t = step; t <= step + 1; ++t)
+        if (-l->extent < t && t < l->extent && share(apart - t * l->stride, l + 1, levels - 1, bytes)) return true;
+    return false;
+}
+bool share(const void* a, const void* b, uint64_t span, const Level* l, int levels, int64_t bytes)
+{
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    if ((x < y ? y - x : x - y) >= span) return false;
+    return share((int64_t)(y - x), l, levels, bytes);
+}
+
 int64_t route_rows(const ttc_route_s* r, int64_t tokens)
 {
     if (tokens < 0) return -TTC_ERR_INVALID_VALUE;
@@ -322,13 +343,28 @@ static int move_slots(ttc_pages_t pages, bool write, int64_t tokens, const int32
     uint64_t bk, bv = 0;
     if (!span_bytes(tokens, ldk, row, eb, &bk) || (v && !span_bytes(tokens, ldv, row, eb, &bv))) return TTC_ERR_OVERFLOW;
     const uint64_t bc = (uint64_t)pages->span * cb, bs = 4 * (uint64_t)pages->heads;
-    // keys and values may be parts of one tensor, on either side: they are checked against the other side, and for being the same
+    // keys and values may be parts of one tensor, on either side: they are checked against the other side, for being the same, and where they
+    // are written for sharing elements
     if (v && (k == v || k_cache == v_cache)) return TTC_ERR_ALIAS;
     int st = check_operands({Operand{k, bk, eb, !write}, {k_cache, bc, cb, write}, {slots, 4 * (uint64_t)tokens, 4, false}, {k_scale, bs, 4, false}, {v_scale, bs, 4, false}});
     if (st == TTC_OK && v) {
         st = check_operands({Operand{v, bv, eb, !write}, {v_cache, bc, cb, write}, {slots, 4 * (uint64_t)tokens, 4, false}, {k_scale, bs, 4, false}, {v_scale, bs, 4, false}});
         if (st == TTC_OK) st = check_operands({Operand{k, bk, eb, !write}, {v_cache, bc, cb, write}});
         if (st == TTC_OK) st = check_operands({Operand{v, bv, eb, !write}, {k_cache, bc, cb, write}});
+        Level level[3];
+        int levels = 0;
+        bool shared;
+        if (write) {
+            for (const Level& l : {Level{pages->stride_head, pages->heads}, {pages->stride_slot, pages->page}, {pages->stride_page, pages->pages}})
+                if (l.extent > 1) level[levels++] = {l.stride * cb, l.extent};
+            std::sort(level, level + levels, [](const Level& a, const Level& b) { return a.stride > b.stride; });
+            shared = share(k_cache, v_cache, bc, level, levels, pages->dim * cb);
+        } else {
+            if (tokens > 1) level[levels++] = {ldk * eb, tokens};
+            // rows of two different distances in one span: taken to meet
+            shared = ldk == ldv || tokens == 1 ? share(k, v, bk, level, levels, row * eb) : (uintptr_t)k < (uintptr_t)v + bv && (uintptr_t)v < (uintptr_t)k + bk;
+        }
+        if (st == TTC_OK && shared) st = TTC_ERR_ALIAS;
     }
     if (st != TTC_OK) return st;
     SlotArgs a = {};
