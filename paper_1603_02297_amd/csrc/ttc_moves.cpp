@@ -46,14 +46,14 @@ struct Operand {
     bool        written;
 };
 
-// Every pointer aligned to its element, nothing written overlaps anything else.
+// Every pointer aligned to its element, nothing written overlaps anything else.  A tensor without elements overlaps nothing, wherever it points.
 template <int N> int check_operands(const Operand (&o)[N])
 {
     for (int i = 0; i < N; ++i)
         if (o[i].p && (uintptr_t)o[i].p % (uintptr_t)o[i].align) return TTC_ERR_MISALIGNED;
     for (int i = 0; i < N; ++i)
         for (int j = 0; j < N; ++j) {
-            if (i == j || !o[i].written || !o[i].p || !o[j].p) continue;
+            if (i == j || !o[i].written || !o[i].p || !o[j].p || !o[i].bytes || !o[j].bytes) continue;
             const uintptr_t a = (uintptr_t)o[i].p, b = (uintptr_t)o[j].p;
             if (a < b + o[j].bytes && b < a + o[i].bytes) return TTC_ERR_ALIAS;
         }

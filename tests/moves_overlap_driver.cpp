@@ -35,7 +35,7 @@ int main()
     std::mt19937 rng(7);
     auto pick = [&](int lo, int hi) { return (int64_t)(lo + (int)(rng() % (unsigned)(hi - lo + 1))); };
     const uint64_t base = 1 << 20, far = uint64_t(1) << 30;
-    for (int round = 0; round < 1500; ++round) {
+    for (int round = 0; round < 300; ++round) {
         const int type = round % 3 == 0 ? TTC_F32 : TTC_BF16, cache = round % 3 == 1 ? TTC_F8 : type;
         const int eb = elem_bytes(type), cb = elem_bytes(cache);
         int64_t extent[3] = {pick(1, 3), pick(1, 4), pick(1, 4)}, stride[3], dim = pick(1, 5);
@@ -75,6 +75,18 @@ int main()
         }
         ttc_pages_destroy(h);
     }
+    // tensors without elements, inside of what the call writes
+    ttc_pages_t h = ttc_pages_create(TTC_BF16, TTC_BF16, 2, 8, 4, 9, nullptr);
+    int32_t *a = (int32_t*)at(base), *b = (int32_t*)at(2 * base), *c = (int32_t*)at(3 * base), *d = (int32_t*)at(4 * base), *e = (int32_t*)at(5 * base);
+    expect(ttc_pages_map(h, 4, nullptr, a, b, c, 6, c + 3, 0, 0, d, e, d + 1, d + 2, e + 1, nullptr), false, "no tokens, no free pages", 0, 0, 0, 0);
+    expect(ttc_pages_map(h, 4, nullptr, a, b, c, 6, c + 3, 1, 0, d, e, d + 1, d + 2, e + 1, nullptr), true, "a free page", 0, 0, 0, 0);
+    expect(ttc_pages_map(h, 4, nullptr, a, b, c, 6, nullptr, 0, 1, d, e, d + 1, nullptr, nullptr, nullptr), true, "a token", 0, 0, 0, 0);
+    expect(ttc_pages_map(h, 0, c + 1, c + 2, c + 3, c + 4, 6, nullptr, 0, 30, d, e, c, nullptr, nullptr, nullptr), false, "no requests", 0, 0, 0, 0);
+    ttc_pages_destroy(h);
+    ttc_route_t r = ttc_route_create(TTC_F32, 8, 2, 40, 0, 1, 8, nullptr, nullptr);
+    expect(ttc_route_sort(r, 0, a + 2, 2, a, b, a + 5, b + 6, nullptr, nullptr), false, "nothing to sort", 0, 0, 0, 0);
+    expect(ttc_route_sort(r, 1, a + 2, 2, a, b, c, d, nullptr, nullptr), true, "ids", 0, 0, 0, 0);
+    ttc_route_destroy(r);
     std::printf(failures ? "%d failures\n" : "overlap driver ok (%d)\n", failures ? failures : accepted + refused);
-    return failures != 0 || accepted < 10000 || refused < 10000;
+    return failures != 0 || accepted < 3000 || refused < 3000;
 }
