@@ -244,7 +244,7 @@ template <typename T, typename C> struct SlotTypes<T, C, false> { typedef C from
 // Into the narrower cache: x / scale.  Divisions cost a dozen instructions each, enough to bound the kernel by arithmetic (524 MB
 // in 97 us with them, 89 without; 33 MB 5.9 and 5.2).  With r = 1 / scale rounded once, q = x * r is off by two units at most, and q + (x - q * scale) * r rounds the quotient
 // itself: ties of the 8-bit format, which are quotients that 32 bits hold, stay ties.  q is held to +-512 before that, so that an infinite
-// one does not become a NaN; beyond 448 the cut follows anyhow.  Scales outside 2^-60 .. 2^60, where r or the remainder could leave the
+// one does not become a NaN; beyond 448 the cut follows anyhow.  A zero's remainder is +0, which would leave no -0: the sign is x * r's.  Scales outside 2^-60 .. 2^60, where r or the remainder could leave the
 // normal range, take the division.
 template <typename From, typename To, int V>
 __device__ __forceinline__ void convert_in(const Vec<From, V>& x, float scale, Vec<To, V>& r)
@@ -256,8 +256,8 @@ __device__ __forceinline__ void convert_in(const Vec<From, V>& x, float scale, V
         const float inverse = 1.f / scale;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float q = __builtin_fminf(__builtin_fmaxf(f[i] * inverse, -512.f), 512.f);
-            f[i] = __builtin_fmaf(__builtin_fmaf(-q, scale, f[i]), inverse, q);
+            const float near = f[i] * inverse, q = __builtin_fminf(__builtin_fmaxf(near, -512.f), 512.f);
+            f[i] = __builtin_copysignf(__builtin_fmaf(__builtin_fmaf(-q, scale, f[i]), inverse, q), near);
         }
     } else {
 #pragma unroll
