@@ -237,14 +237,16 @@ __device__ __forceinline__ float sum_in_last_lane(float v)        // lane 63 get
     return __builtin_bit_cast(float, over_lanes(__builtin_bit_cast(uint32_t, v), add));
 }
 
-// Touches every 64-byte line of a kernel's arguments at once: read where they are used, a line after the other, each costs the way to
-// memory again.  One token's combine 2.4 -> 2.2 us, 128 tokens into the cache 2.7 -> 2.5; the gather, the sort and the map gain nothing.
-template <typename Args> __device__ __forceinline__ void touch(const Args& args)
+// Touches every 64-byte line of a kernel's arguments (its first parameter, of type Args) at once: read where they are used, a line after the other,
+// each costs the way to memory again.  One token's combine 2.4 -> 2.2 us, 128 tokens into the cache 2.7 -> 2.5; the gather, the sort and the map
+// gain nothing.  It goes by the segment that the launch put them in: the parameter's own address is that of a private copy
+// until the compiler has dropped it.
+template <typename Args> __device__ __forceinline__ void touch()
 {
-    const __attribute__((address_space(4))) uint32_t* words = (const __attribute__((address_space(4))) uint32_t*)&args;
-#pragma unroll
-    for (unsigned i = 0; i < sizeof(Args) / 4; i += 16) asm volatile("" : : "s"(words[i]));
-    asm volatile("" : : "s"(words[sizeof(Args) / 4 - 1]));
+    constexpr unsigned last = sizeof(Args) / 4 - 1;
+    static_assert(last < 64, "four lines are touched here");
+    const __attribute__((address_space(4))) uint32_t* words = (const __attribute__((address_space(4))) uint32_t*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : : "s"(words[1]), "s"(words[17 < last ? 17 : last]), "s"(words[33 < last ? 33 : last]), "s"(words[49 < last ? 49 : last]));
 }
 
 // A launch dimension may count at most 2^32 work items: blocks beyond 2^20 go into the second dimension.

@@ -291,7 +291,7 @@ __device__ __forceinline__ uint32_t near_block(uint32_t near)
 template <typename T, typename C, int V, bool WRITE, bool NTL, bool NTS>
 __global__ __launch_bounds__(kMoveThreads) void slots_kernel(PlaceArgs p)
 {
-    touch(p);
+    touch<PlaceArgs>();
     constexpr bool same = sizeof(T) == sizeof(C);
     typedef typename SlotTypes<T, C, WRITE>::from From;
     typedef typename SlotTypes<T, C, WRITE>::to To;

@@ -405,7 +405,7 @@ template <typename T, int V, int GROUP, bool WHOLE, bool NT> constexpr auto gath
 template <typename T, int V, int GROUP, bool WHOLE, bool NT>
 __global__ __launch_bounds__(kMoveThreads) void combine_kernel(MoveArgs p)
 {
-    touch(p);
+    touch<MoveArgs>();
     uint32_t t, vec;
     if (!lane_place<WHOLE>(p, block_id(), &t, &vec)) return;
     const MovePlace place = row_place<V>(vec, p.r.width);
@@ -461,7 +461,7 @@ constexpr int kGradWaves = 8, kGradWavesMany = 4, kGradMany = 1024;
 template <typename T, int V, int GROUP, bool WHOLE, bool NT>
 __global__ __launch_bounds__(WHOLE ? kGradWaves * kWave : kMoveThreads) void combine_grad_kernel(MoveArgs p)
 {
-    touch(p);
+    touch<MoveArgs>();
     __shared__ float dots[kGradWaves][GROUP];
     const uint32_t b = block_id();
     if (b >= p.blocks) { clear_padding<T, V, NT>(p, b); return; }
