@@ -242,28 +242,37 @@ template <typename T, typename C, bool WRITE> struct SlotTypes { typedef T from;
 template <typename T, typename C> struct SlotTypes<T, C, false> { typedef C from; typedef T to; };
 
 // Into the narrower cache: x / scale.  Divisions cost a dozen instructions each, enough to bound the kernel by arithmetic (524 MB
-// in 97 us with them, 89 without; 33 MB 5.9 and 5.2).  With r = 1 / scale rounded once, q = x * r is off by two units at most, and q + (x - q * scale) * r rounds the quotient
-// itself: ties of the 8-bit format, which are quotients that 32 bits hold, stay ties.  q is held to +-512 before that, so that an infinite
-// one does not become a NaN; beyond 448 the cut follows anyhow.  A zero's remainder is +0, which would leave no -0: the sign is x * r's.  Scales outside 2^-60 .. 2^60, where r or the remainder could leave the
-// normal range, take the division.
-template <typename From, typename To, int V>
-__device__ __forceinline__ void convert_in(const Vec<From, V>& x, float scale, Vec<To, V>& r)
+// in 97 us with them, 89 without; 33 MB 5.9 and 5.2).  With r = 1 / |scale| rounded once, q = x * r is off by two units at most, and q - (q * |scale| - x) * r rounds
+// the quotient itself: ties of the 8-bit format, which are quotients that 32 bits hold, stay ties.  Subtracted in that order a remainder of nothing, which is +0,
+// leaves q as it is, -0 among others.  q is held to +-512 before that, so that an infinite
+// one does not become a NaN; beyond 448 the cut follows anyhow.  A negative scale turns the signs of the result, four at a time.  Scales outside
+// 2^-60 .. 2^60, where r or the remainder could leave the normal range, take the division.
+__device__ __forceinline__ void turn_signs(Vec<f8, 1>& r) { r.e.bits ^= 0x80; }
+template <int V> __device__ __forceinline__ void turn_signs(Vec<f8, V>& r)
+{
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) r.w[i] ^= 0x80808080u;
+}
+template <typename From, int V>
+__device__ __forceinline__ void convert_in(const Vec<From, V>& x, float scale, Vec<f8, V>& r)
 {
     float f[V];
     widen(x, f);
     const float size = __builtin_fabsf(scale);
     if (size >= 0x1p-60f && size <= 0x1p60f) {
-        const float inverse = 1.f / scale;
+        const float inverse = 1.f / size;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float near = f[i] * inverse, q = __builtin_fminf(__builtin_fmaxf(near, -512.f), 512.f);
-            f[i] = __builtin_copysignf(__builtin_fmaf(__builtin_fmaf(-q, scale, f[i]), inverse, q), near);
+            const float q = __builtin_fminf(__builtin_fmaxf(f[i] * inverse, -512.f), 512.f);
+            f[i] = __builtin_fmaf(-__builtin_fmaf(q, size, -f[i]), inverse, q);
         }
+        narrow(f, r);
+        if (scale < 0.f) turn_signs(r);
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i) f[i] = f[i] / scale;
+        narrow(f, r);
     }
-    narrow(f, r);
 }
 
 // And out of it.
