@@ -221,7 +221,8 @@ def layer(x: torch.Tensor, fresh: torch.Tensor, cache: PagedCache, w: dict, head
     ends, k, v = cache.context()
     ends = ends.tolist()
     mixed = [attention(qkv[a:b, :heads * cache.dim], k[c:d], v[c:d], heads, cache.heads) for a, b, c, d in zip(starts, starts[1:], ends, ends[1:]) if b > a]
-    x = x + torch.cat(mixed) @ w["out"]
+    if mixed:                                                     # a step may bring nothing
+        x = x + torch.cat(mixed) @ w["out"]
     return x + experts_forward(x, w["router"], w["up"], w["down"], topk)
 
 

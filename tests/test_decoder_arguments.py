@@ -263,3 +263,21 @@ def test_the_command_serves_as_many_steps_as_it_is_asked_for():
     done = subprocess.run([sys.executable, "-m", "paper_1603_02297_amd.decoder", "--steps", "140"], capture_output=True, text=True, timeout=110)
     assert done.returncode == 0, done.stderr[-2000:]
     assert done.stdout.count("lengths [210, 141, 173, 268]") == 2
+
+
+@gpu
+def test_a_step_without_tokens():
+    """Nothing new for any request: no rows come out, nothing is taken; the next step goes on from there."""
+    torch.manual_seed(7)
+    w = decoder.weights(32, 2, 1, 16, 4, 16, torch.float32)
+    for before in ([0, 0], [9, 3]):
+        c = decoder.PagedCache(2, 1, 16, 8, 6, 24, torch.float32, torch.float32)
+        step = lambda n: decoder.layer(torch.randn(sum(n), 32, device="cuda"), torch.tensor(n, dtype=torch.int32, device="cuda"), c, w, 2, 2)  # noqa: E731
+        step(before)
+        free = c.free.clone()
+        assert step([0, 0]).shape == (0, 32)
+        assert c.cached.tolist() == before and torch.equal(c.free, free)
+        assert step([1, 0]).shape == (1, 32) and c.cached.tolist() == [before[0] + 1, before[1]]
+    x = torch.zeros(0, 32, device="cuda", requires_grad=True)
+    decoder.experts_forward(x, w["router"], w["up"], w["down"], 2).sum().backward()
+    assert x.grad.shape == (0, 32)
