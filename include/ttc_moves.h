@@ -89,8 +89,8 @@ int ttc_route_gather(ttc_route_t route, int64_t tokens, const void* x, int64_t l
 /*
  * Rows back to their tokens:  y[:, t] <- alpha * sum_k weights[k,t] * rows[:, position[k,t]]  +  beta * y[:, t].
  * Choices that are nowhere add nothing (a token with no other becomes beta * y); weights NULL: all 1.  The sum runs
- * over k in order; with beta == 0 y is never read.  With weights NULL this is the gradient of ttc_route_gather (of the
- * weighted one with its weights).
+ * over k in order; with beta == 0 y is never read.  By a handle with alpha = 1 and beta = 0, whatever those of the layer's own
+ * handle are, this is the gradient of ttc_route_gather: with weights NULL, or of the weighted one with its weights.
  */
 int ttc_route_combine(ttc_route_t route, int64_t tokens, const void* rows, int64_t ld_rows, const float* weights, const int32_t* position,
                       void* y, int64_t ldy, void* stream);
@@ -100,7 +100,8 @@ int ttc_route_combine(ttc_route_t route, int64_t tokens, const void* rows, int64
  *   drows[:, position[k,t]] <- (alpha * weights[k,t]) * dy[:, t]       (padding rows 0, rows past the end not touched)
  *   dweights[k,t]           <- alpha * sum_i dy[i, t] * rows[i, position[k,t]]        (0 where the choice is nowhere)
  * dweights NULL: no gradient of the weights; rows is not read then and may be NULL.  drows NULL: that of the weights only
- * (with x as dy and the gradient of ttc_route_gather's rows as rows, its weights' gradient).  weights NULL: all 1.
+ * (with x as dy and the gradient of ttc_route_gather's rows as rows, by a handle with alpha = 1, its weights' gradient).  weights
+ * NULL: all 1.
  */
 int ttc_route_combine_grad(ttc_route_t route, int64_t tokens, const void* dy, int64_t ld_dy, const void* rows, int64_t ld_rows,
                            const float* weights, const int32_t* position, const int32_t* offsets, const int32_t* counts,
@@ -136,7 +137,8 @@ int ttc_pages_destroy(ttc_pages_t pages);
  *   starts     [requests+1] int32, out: where every request's listed positions start; starts[requests] is their number,
  *              also where it exceeds `tokens` (cut at 2^31-1).
  *   page_starts [requests+1] int32, out: the same for the pages taken; page_starts[requests] > free_count says that there
- *              were too few: entries without a page become -1.
+ *              were too few: entries without a page become -1.  Pages are counted for every block that a request needs, those past
+ *              the table's width, which nothing will point to, among them.
  *   slots      [tokens] int32, out: the slot of every listed position; -1 past the end, where the table has no entry
  *              (position >= ld_table*page), and where the entry is no page (0 .. pages-1).
  *   positions, owner [tokens] int32, out, each may be NULL: position within its request, and the request; -1 past the end.

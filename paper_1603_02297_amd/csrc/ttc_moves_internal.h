@@ -47,7 +47,8 @@ struct SortShape {
 };
 SortShape sort_shape(int64_t n, int experts);
 
-// Kernel launchers; the callers have checked every argument.  They return TTC_OK or TTC_ERR_HIP.
+// Kernel launchers; the callers have checked every argument.  They return TTC_OK or TTC_ERR_HIP; the row moves TTC_ERR_OVERFLOW, with nothing
+// launched, where tokens times pieces of a row (64 vectors) exceed 2^31-1, which takes a tensor of 1 TB.
 struct SortArgs {
     const void* ids;
     int64_t     ld_ids;

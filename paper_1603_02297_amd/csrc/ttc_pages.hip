@@ -234,15 +234,16 @@ struct PlaceArgs {
     uint32_t near;                         // workgroups before this one are numbered by near_block
 };
 
-// Sixteen bytes a lane of the type outside the cache.  (f32 as two accesses of 16 bytes and 8 bytes of an 8-bit cache: 64 x 1333 tokens of 8
-// heads of 128 out of it 140 us instead of 86, into it 82 and 74; 16 elements of a 16-bit type: out of it 105 and 89.)
+// Sixteen bytes a lane of the type outside the cache.  With 32 (f32 as two accesses of 16 bytes, and 8 bytes of an 8-bit cache), keys and values of
+// 28,448 tokens of 8 heads of 128: f32 out of an 8-bit cache (291 MB) 88 us instead of 52, into it 55 and 52; out of one of f32 (466 MB) 90 and 75, into it 107
+// and 79; 55,472 tokens of bf16 out of 8 bits (341 MB) 76 and 57, into them 63 and 59.
 template <typename T> struct SlotVec { static constexpr int value = 16 / (int)sizeof(T); };
 
 template <typename T, typename C, bool WRITE> struct SlotTypes { typedef T from; typedef C to; };
 template <typename T, typename C> struct SlotTypes<T, C, false> { typedef C from; typedef T to; };
 
-// Into the narrower cache: x / scale.  Divisions cost a dozen instructions each, enough to bound the kernel by arithmetic (524 MB
-// in 97 us with them, 89 without; 33 MB 5.9 and 5.2).  With r = 1 / |scale| rounded once, q = x * r is off by two units at most, and q - (q * |scale| - x) * r rounds
+// Into the narrower cache: x / scale.  Divisions cost a dozen instructions each, enough to bound the kernel by arithmetic (bf16, 682 MB
+// in 154 us with them, 124 without; 128 MB by head 24.4 and 21.2; 20 MB 6.9 and 5.9).  With r = 1 / |scale| rounded once, q = x * r is off by two units at most, and q - (q * |scale| - x) * r rounds
 // the quotient itself: ties of the 8-bit format, which are quotients that 32 bits hold, stay ties.  Subtracted in that order a remainder of nothing, which is +0,
 // leaves q as it is, -0 among others.  q is held to +-512 before that, so that an infinite
 // one does not become a NaN; beyond 448 the cut follows anyhow.  A negative scale turns the signs of the result, four at a time.  Scales outside
@@ -288,8 +289,8 @@ __device__ __forceinline__ void convert_out(const Vec<From, V>& x, float scale, 
 
 // Workgroups go to the eight dies in turn, each with an L2 of its own.  A head whose elements end inside a line shares it with the next
 // slot's, and a token's heads, where the cache is ordered by head, are lines far apart that only the tokens after it use up: on different
-// dies such a line moves several times.  So kNear successive workgroups go to the same die.  15 heads of 80, bf16 and an 8-bit cache by head:
-// 123657 tokens out of it 69.1 us with runs of 1, 59.1 of 16, 58.2 of 64, 58.1 of 256.
+// dies such a line moves several times.  So kNear successive workgroups go to the same die.  15 heads of 80, bf16 and an 8-bit cache by head,
+// keys and values of 41,239 tokens (297 MB) out of it 69.4 us with runs of 1, 59.8 of 16, 58.7 of 64, 58.9 of 256.
 constexpr uint32_t kDies = 8, kNear = 64;
 __device__ __forceinline__ uint32_t near_block(uint32_t near)
 {
@@ -344,8 +345,8 @@ __global__ __launch_bounds__(kMoveThreads) void slots_kernel(PlaceArgs p)
 }
 
 // Non-temporal hints by the bytes moved, stores from 16 MB, loads from 256 MB on.  Measured with 8 heads of 128 bf16 into (out of) pages of
-// bf16, without hints, stores only, both: 44 MB 8.1, 8.1, 10.0 us (8.4, 8.0, 9.8); 175 MB 35.4, 29.4, 31.9 (36.3, 28.6, 30.9); 700 MB
-// 130, 123, 122 (132, 123, 117); with an 8-bit cache 33 MB 9.1, 8.1, 8.5 (7.1, 6.5, 8.6); 524 MB 101, 98, 97 (96, 89, 88).
+// bf16, without hints, stores only, both: 44 MB 8.0, 8.1, 9.4 us (7.9, 7.8, 9.1); 175 MB 35.3, 29.5, 31.5 (36.2, 27.4, 29.5); 700 MB
+// 122, 114, 115 (127, 117, 113); with an 8-bit cache 33 MB 8.2, 8.0, 7.9 (7.1, 6.0, 8.0); 524 MB 98, 95, 99 (97, 89, 88).
 constexpr uint64_t kStreamStores = uint64_t(16) << 20, kStreamLoads = uint64_t(256) << 20;
 
 template <typename T, typename C, bool WRITE> int launch_slots_types(const SlotArgs& a, void* stream)
@@ -377,9 +378,10 @@ template <typename T, typename C, bool WRITE> int launch_slots_types(const SlotA
         // has less under way and wants them all
         const size_t lds = sizeof(T) == sizeof(C) && bytes >= kStreamLoads ? lds_for(5) : 0;
         // Into the cache, where heads are not whole units of 64 bytes: near each other, and without the hint, so that the L2 joins the parts of
-        // a line (as above, 128016 tokens 120 us; near each other 96; no hint 60; both 56).  Where they are whole, or tokens follow each other
-        // closely in the cache at 16 bytes a lane, both lose: 8 heads of 128, 8-bit, 86 and 104; one head of 40 bf16 47 and 52.  Out of the
-        // cache, near each other loses nowhere: 16 heads of 64, 8-bit by head 41.0 and 35.1 us, 8 of 128 bf16 106 and 106.
+        // a line (as above, 42,668 tokens, 307 MB, 119 us; near each other 92; no hint 72; both 61; 5 heads of 84 fp16 by head, 47, 42, 46 and 40).  Where
+        // they are whole, or tokens follow each other closely in the cache at 16 bytes a lane, both lose: 8 heads of 128, 8-bit by head, 58.6 and
+        // 61.8; one head of 40 bf16 27.5 and 31.3.  Out of the cache, near each other loses nowhere: 16 heads of 64, 8-bit by head 63.2 and 57.8 us, 8 of
+        // 128 bf16 112 and 112.
         const bool whole = ((a.dim | (uint64_t)a.stride_head | (uint64_t)a.stride_slot | (uint64_t)a.stride_page) * sizeof(C)
                             | (uintptr_t)a.k_out | (uintptr_t)a.v_out) % 64 == 0;
         const bool packed = a.stride_slot == (int64_t)a.heads * a.dim && (a.heads == 1 || a.stride_head == (int64_t)a.dim);

@@ -454,9 +454,10 @@ __global__ __launch_bounds__(kMoveThreads) void combine_kernel(MoveArgs p)
 // several tokens to a workgroup, or a whole workgroup of several wavefronts.  Their partial sums
 // meet by shuffles inside a wavefront and through LDS between wavefronts, always in the same order.
 // Wavefronts of a workgroup at most (beyond that they go round): 8, four from kGradMany tokens on, where five to seven of them would leave
-// slots of a compute unit empty and the many waits show that half the rows nowhere cause.  us with 8 and 4, bf16:
-//   3878 x 5 rows of 2112, one of two ranks 45.8, 31.8; 2844 x 5 of 2880 39.4, 30.6; 1996 x 5 of 4104 38.2, 33.9; all 8 rows here 82.9, 82.6
-//   (4608), at worst 87.3, 90.9 (4104); 100 x 4 rows of 8192 9.0, 10.1; 4 x 8 8.2, 9.1; 500 x 4 of 4097 15.5, 16.8.
+// slots of a compute unit empty and the many waits show that half the rows nowhere cause.  This kernel's us with 8 and 4, bf16:
+//   3878 x 5 rows of 2112, one of two ranks 36.9, 22.3; 2844 x 5 of 2880 30.3, 21.4; 1996 x 5 of 4104 28.6, 24.9; all rows here 1024 x 8 of 4608 35.8,
+//   33.7, of 4104 34.8, 34.0, but 8192 x 4 of 4100 112, 122; below 100 x 4 rows of 8192 6.7, 7.8; 4 x 8 of 4096 5.0, 5.6; 500 x 4 of 4097 9.8, 9.6;
+//   900 x 5 of 4104, one of two ranks 16.5, 14.5.
 constexpr int kGradWaves = 8, kGradWavesMany = 4, kGradMany = 1024;
 template <typename T, int V, int GROUP, bool WHOLE, bool NT>
 __global__ __launch_bounds__(WHOLE ? kGradWaves * kWave : kMoveThreads) void combine_grad_kernel(MoveArgs p)
@@ -561,10 +562,11 @@ template <typename T> MoveArgs move_args(const RowArgs& r)
 }
 
 // Non-temporal accesses to the sorted rows, by their size: what will not stay in the last-level cache anyhow does better
-// without pushing the rest out.  Measured at 4096 bf16, 256 to 8192 tokens, three sets of tensors in turn:
-//   gather (stores of rows; x stays plain): 8 choices, 512 tokens 15.9 us with the hint, 17.2 without; 2048: 35.0, 39.8; 8192: 109, 119
-//   combine (rows and y): 8 choices, 1024 tokens 13.5, 12.5; 2048: 26.2, 30.8; 8192: 104, 117
-//   gradient (rows and drows; dy stays plain): 4 choices, 512 tokens 15.5, 15.5; 1024: 26.9, 31.6; 8192: 173, 193
+// without pushing the rest out.  Kernel times at 4096 bf16, 256 to 8192 tokens, three sets of tensors in turn, with the hint and without:
+//   gather (stores of rows; x stays plain): 8 choices, 512 tokens 7.4, 8.0 us; 2048: 25.3, 30.0; 8192: 98, 118
+//   combine (rows and y): 8 choices, 1024 tokens 13.8, 12.8; 2048: 26.2, 30.8; 8192: 104, 117
+//   gradient (rows and drows; dy stays plain), 4 choices: 512 tokens 9.1, 8.3; 1024: 15.3, 15.2, and the combine behind it, which finds its rows still
+//   in the cache or not, 7.5, 11.4; 8192: 101, 105
 constexpr uint64_t kStreamGather = uint64_t(32) << 20, kStreamCombine = uint64_t(96) << 20, kStreamGrad = uint64_t(24) << 20;
 template <typename T> bool streams(const RowArgs& r, uint64_t from) { return (uint64_t)r.tokens * r.topk * r.width * sizeof(T) >= from; }
 
