@@ -1,0 +1,91 @@
+/*
+ * ttc_attention.h -- C ABI of the way of a layer's queries, keys and values around the paged cache of ttc_moves.h.
+ *
+ *   ttc_heads_*        norms of queries and keys for each head, with the rotation by position in the same pass; with the gradients
+ *   ttc_pages_append   the same on the way of new tokens into the cache
+ *
+ * Conventions as in ttc_moves.h: column-major, DEVICE pointers owned by the caller, integer status codes, nothing throws or aborts
+ * across this boundary; handles are made once, touch no device, may be used from several streams at a time; every other
+ * call enqueues a few kernels on `stream`, allocates nothing, never synchronises and can be captured into a graph.  A call works on the
+ * current device, which its tensors and its stream belong to.  A workspace belongs to the calls of one stream (or of one graph) at a time.
+ * Entries of slots, tables and lengths are checked on the GPU before they are followed.  Sums run in 32 bits in a fixed order: the same
+ * inputs give the same bits.
+ */
+#ifndef TTC_ATTENTION_H_
+#define TTC_ATTENTION_H_
+
+#include "ttc_moves.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Limits of a handle (TTC_ERR_INVALID_VALUE beyond them). */
+enum { TTC_HEADS_MAX_DIM = 512, TTC_HEADS_MAX_ROTATED = 256 };
+
+/* ---- norms of the heads, and their rotation ------------------------------------------------------------------ */
+
+typedef struct ttc_heads_s* ttc_heads_t;
+
+/*
+ * A handle for the heads of one layer.  For a vector x of `dim` elements at position p, with weights w:
+ *     u = x / sqrt(mean(x^2) + eps) * w            (norm != 0; else u = x)
+ *     y = u with its first `rotated` elements turned, pair i by the angle p * angles[i]:
+ *         (y_a, y_b) = (u_a cos - u_b sin, u_b cos + u_a sin)
+ * where pair i is elements (i, i + rotated/2), or its neighbours (2i, 2i+1) if paired != 0.
+ *   dtype      TTC_F32, TTC_BF16 or TTC_F16: the type of every tensor but weights.  Everything between is 32 bits, rounded once.
+ *   q_heads, kv_heads  heads of queries and of keys.
+ *   dim        1 .. TTC_HEADS_MAX_DIM.
+ *   rotated    even, 0 .. min(dim, TTC_HEADS_MAX_ROTATED).
+ *   angles     HOST array of rotated/2 doubles (radians for each position, finite), copied; NULL if rotated is 0.  Products with the position
+ *              are exact to 2^-31 of a turn, however far the position.
+ *   eps        >= 0, finite; not read without norm.
+ * Returns NULL on error; ttc_last_status() says why.
+ */
+ttc_heads_t ttc_heads_create(int dtype, int64_t q_heads, int64_t kv_heads, int64_t dim, int64_t rotated, int paired, const double* angles,
+                             int norm, float eps);
+int ttc_heads_destroy(ttc_heads_t heads);
+
+/*
+ * Queries and keys of packed tokens:  q_out <- y(q), k_out <- y(k).
+ *   positions  [tokens] int32; a token with a negative one is padding, whose results are left as they were.  NULL only if nothing is rotated.
+ *   q, k       [dim, heads, tokens], ldq, ldk >= heads*dim elements between tokens (parts of one fused projection).  k and k_out NULL: queries
+ *              only; q and q_out NULL: keys only.
+ *   q_weight, k_weight  [dim] float, or NULL (1).  Refused (TTC_ERR_INVALID_VALUE) without norm.
+ *   q_out, k_out  as q and k; each may be the tensor that it is made of, in its place (same address, same distance).
+ */
+int ttc_heads_rotate(ttc_heads_t heads, int64_t tokens, const int32_t* positions, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                     const float* q_weight, const float* k_weight, void* q_out, int64_t ld_qo, void* k_out, int64_t ld_ko, void* stream);
+
+/* Bytes of workspace for ttc_heads_rotate_grad (0 where it needs none), or a negative status. */
+int64_t ttc_heads_workspace(ttc_heads_t heads, int64_t tokens);
+
+/*
+ * The gradients of ttc_heads_rotate, from those of its results (dq_out, dk_out) and its inputs:
+ *     du = dy turned back,  dw = sum over tokens and heads of x/s * du,  g = du * w,  dx = g/s - x * mean(g * x) / s^3,   s = sqrt(mean(x^2) + eps)
+ *   q, k       not read, and may be NULL, without norm.
+ *   dq, dk     as dq_out and dk_out; each may be its tensor of gradients, in its place.  Padding is left as it was and adds nothing.
+ *   dq_weight, dk_weight  [dim] float, each may be NULL; refused without norm.  0 where no token is left.
+ *   workspace  ttc_heads_workspace bytes, aligned to 4; not used, and may be NULL, where neither is wanted.
+ */
+int ttc_heads_rotate_grad(ttc_heads_t heads, int64_t tokens, const int32_t* positions, const void* dq_out, int64_t ld_dqo, const void* dk_out,
+                          int64_t ld_dko, const void* q, int64_t ldq, const void* k, int64_t ldk, const float* q_weight, const float* k_weight,
+                          void* dq, int64_t ld_dq, void* dk, int64_t ld_dk, float* dq_weight, float* dk_weight, void* workspace, void* stream);
+
+/* ---- new tokens into the cache -------------------------------------------------------------------------------- */
+
+/*
+ * q_out <- y(q),  k_cache[:, h, slots[i]] <- y(k)[:, h, i],  v_cache[:, h, slots[i]] <- v[:, h, i]
+ * in one pass, for a cache and heads of one type, one dim and one number of kv_heads.  What goes into 8 or 4 bits is y itself, rounded once; scales as for
+ * ttc_pages_write.  A token with a negative position is left out; one whose slot is nowhere gets its queries only.  q and q_out may both be NULL; q_out may be q
+ * in its place.  Two tokens must not have one slot.  A cache in 4 bits takes vectors whose rotated part is a multiple of 16 (TTC_ERR_INVALID_VALUE: rotate first, then
+ * ttc_pages_write).
+ */
+int ttc_pages_append(ttc_pages_t pages, ttc_heads_t heads, int64_t tokens, const int32_t* slots, const int32_t* positions, const void* q, int64_t ldq,
+                     const void* k, int64_t ldk, const void* v, int64_t ldv, const float* q_weight, const float* k_weight, void* q_out, int64_t ld_qo,
+                     void* k_cache, void* v_cache, const float* k_scale, const float* v_scale, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* TTC_ATTENTION_H_ */

@@ -30,8 +30,13 @@ extern "C" {
 #endif
 
 /* Element types beside TTC_F32 that these moves take (ttc_plan_create takes none of them).  TTC_F8 is the 8-bit format
- * with four exponent and three mantissa bits, largest value 448, no infinities; it is a type of the cache only. */
-enum { TTC_BF16 = 8, TTC_F16 = 9, TTC_F8 = 10 };
+ * with four exponent and three mantissa bits, largest value 448, no infinities; it is a type of the cache only.
+ * So is TTC_Q4: a vector of `dim` elements (a multiple of 8, at most 512) is a record of 4 + dim/2 bytes, a step and a minimum in bf16 (in this order) and the
+ * codes, element 2i in the low and 2i+1 in the high half of byte i; element = minimum + code * step.  Written are the largest
+ * minimum of bf16 that is no larger than the vector's, the smallest step of bf16 that reaches its maximum with code 15, and the nearest codes (to the even one in the middle): no
+ * element is off by more than half a step.  A vector with a NaN, an infinity, an element beyond the range of bf16, or
+ * elements further apart than 32 bits can say becomes all NaN. */
+enum { TTC_BF16 = 8, TTC_F16 = 9, TTC_F8 = 10, TTC_Q4 = 11 };
 
 /* Limits of a handle (TTC_ERR_INVALID_VALUE beyond them). */
 enum { TTC_ROUTE_MAX_EXPERTS = 1024, TTC_ROUTE_MAX_TOPK = 64, TTC_ROUTE_MAX_ALIGN = 65536 };
@@ -115,9 +120,9 @@ typedef struct ttc_pages_s* ttc_pages_t;
  * A handle for a cache of `pages` pages with `page` slots each; a slot holds `heads` vectors of `dim` elements (keys or
  * values of one token).  Slot s is place s % page of page s / page.
  *   dtype        type of keys and values outside the cache: TTC_F32, TTC_BF16 or TTC_F16.
- *   cache_dtype  the same, or TTC_F8.
- *   strides      HOST array of three: elements between neighbouring heads, slots and pages in the cache (elements of a
- *                vector are neighbours).  NULL: [dim, heads, page, pages] dense.  No two elements may share a place.
+ *   cache_dtype  the same, or TTC_F8, or TTC_Q4.
+ *   strides      HOST array of three: elements (TTC_Q4: bytes) between neighbouring heads, slots and pages in the cache (elements of a
+ *                vector are neighbours).  NULL: [dim, heads, page, pages] dense, with records in the place of vectors for TTC_Q4.  No two elements may share a place.
  * Returns NULL on error; ttc_last_status() says why.
  */
 ttc_pages_t ttc_pages_create(int dtype, int cache_dtype, int64_t heads, int64_t dim, int64_t page, int64_t pages, const int64_t* strides);

@@ -4,7 +4,7 @@
 #include <climits>
 #include <new>
 
-#include "ttc_moves_internal.h"
+#include "ttc_moves_checks.h"
 
 namespace ttc {
 
@@ -27,59 +27,6 @@ SortShape sort_shape(int64_t n, int experts)
 }
 
 namespace {
-
-// Bytes from the first to the last element of `cols` columns of `len` elements, ld apart; false if that is no size.
-bool span_bytes(int64_t cols, int64_t ld, int64_t len, int bytes, uint64_t* out)
-{
-    if (cols == 0 || len == 0) { *out = 0; return true; }
-    int64_t n;
-    if (__builtin_mul_overflow(cols - 1, ld, &n) || __builtin_add_overflow(n, len, &n) || n > (INT64_MAX >> 4)) return false;
-    *out = (uint64_t)n * (uint64_t)bytes;
-    return true;
-}
-
-// One tensor of a call: where it is, how long, and whether the call writes it.
-struct Operand {
-    const void* p;
-    uint64_t    bytes;
-    int         align;
-    bool        written;
-};
-
-// Every pointer aligned to its element, nothing written overlaps anything else.  A tensor without elements overlaps nothing, wherever it points.
-template <int N> int check_operands(const Operand (&o)[N])
-{
-    for (int i = 0; i < N; ++i)
-        if (o[i].p && (uintptr_t)o[i].p % (uintptr_t)o[i].align) return TTC_ERR_MISALIGNED;
-    for (int i = 0; i < N; ++i)
-        for (int j = 0; j < N; ++j) {
-            if (i == j || !o[i].written || !o[i].p || !o[j].p || !o[i].bytes || !o[j].bytes) continue;
-            const uintptr_t a = (uintptr_t)o[i].p, b = (uintptr_t)o[j].p;
-            if (a < b + o[j].bytes && b < a + o[i].bytes) return TTC_ERR_ALIAS;
-        }
-    return TTC_OK;
-}
-
-// Keys and values are written by one call and may be parts of one tensor, so that their spans interleave: whether two tensors of one layout,
-// `apart` bytes from each other, share a byte.  Levels go from the largest stride down, each stride no smaller than all that lies below it
-// spans, so that only the two steps next to apart / stride bring them that close.
-struct Level {
-    int64_t stride, extent;                 // bytes, entries
-};
-bool share(int64_t apart, const Level* l, int levels, int64_t bytes)
-{
-    if (levels == 0) return -bytes < apart && apart < bytes;
-    const int64_t step = apart / l->stride - (apart % l->stride < 0);
-    for (int64_t t = step; t <= step + 1; ++t)
-        if (-l->extent < t && t < l->extent && share(apart - t * l->stride, l + 1, levels - 1, bytes)) return true;
-    return false;
-}
-bool share(const void* a, const void* b, uint64_t span, const Level* l, int levels, int64_t bytes)
-{
-    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    if ((x < y ? y - x : x - y) >= span) return false;
-    return share((int64_t)(y - x), l, levels, bytes);
-}
 
 int64_t route_rows(const ttc_route_s* r, int64_t tokens)
 {
@@ -119,8 +66,6 @@ RowArgs row_args(const ttc_route_s* r, int64_t tokens, int64_t rows)
     a.beta = r->beta;
     return a;
 }
-
-bool row_type(int dtype) { return dtype == TTC_F32 || dtype == TTC_BF16 || dtype == TTC_F16; }
 
 }  // namespace
 }  // namespace ttc
@@ -264,18 +209,21 @@ ttc_pages_t ttc_pages_create(int dtype, int cache_dtype, int64_t heads, int64_t 
     ttc_pages_s p = {};
     p.dtype = dtype; p.cache_dtype = cache_dtype; p.heads = heads; p.dim = dim; p.page = page; p.pages = pages;
     int64_t slots, token;
-    if (!row_type(dtype) || (cache_dtype != dtype && cache_dtype != TTC_F8)) st = TTC_ERR_UNSUPPORTED_DTYPE;
-    else if (heads < 1 || dim < 1 || page < 1 || pages < 1) st = TTC_ERR_INVALID_VALUE;
+    const bool records = cache_dtype == TTC_Q4;
+    const int64_t vec = records ? kRecordHead + dim / 2 : dim;              // elements (bytes of a record) between the first and the last of a vector
+    if (!row_type(dtype) || (cache_dtype != dtype && cache_dtype != TTC_F8 && !records)) st = TTC_ERR_UNSUPPORTED_DTYPE;
+    else if (heads < 1 || dim < 1 || page < 1 || pages < 1 || (records && (dim % 8 || dim > kRecordMaxDim))) st = TTC_ERR_INVALID_VALUE;
     else if (__builtin_mul_overflow(page, pages, &slots) || slots > INT32_MAX || __builtin_mul_overflow(heads, dim, &token) || token > INT32_MAX / 2)
         st = TTC_ERR_OVERFLOW;
     if (st == TTC_OK) {
-        p.stride_head = strides ? strides[0] : dim;
-        p.stride_slot = strides ? strides[1] : heads * dim;
-        p.stride_page = strides ? strides[2] : page * heads * dim;
+        p.vec = vec;
+        p.stride_head = strides ? strides[0] : vec;
+        p.stride_slot = strides ? strides[1] : heads * vec;
+        p.stride_page = strides ? strides[2] : page * heads * vec;
         // from the smallest stride up, every index steps over all that lies below it: no two elements share a place
         struct { int64_t stride, extent; } index[3] = {{p.stride_head, heads}, {p.stride_slot, page}, {p.stride_page, pages}};
         std::sort(index, index + 3, [](const auto& a, const auto& b) { return a.stride < b.stride; });
-        int64_t span = dim;
+        int64_t span = vec;
         for (const auto& i : index) {
             if (i.extent == 1) continue;
             if (i.stride < span) { st = TTC_ERR_INVALID_VALUE; break; }
@@ -358,7 +306,7 @@ static int move_slots(ttc_pages_t pages, bool write, int64_t tokens, const int32
             for (const Level& l : {Level{pages->stride_head, pages->heads}, {pages->stride_slot, pages->page}, {pages->stride_page, pages->pages}})
                 if (l.extent > 1) level[levels++] = {l.stride * cb, l.extent};
             std::sort(level, level + levels, [](const Level& a, const Level& b) { return a.stride > b.stride; });
-            shared = share(k_cache, v_cache, bc, level, levels, pages->dim * cb);
+            shared = share(k_cache, v_cache, bc, level, levels, pages->vec * cb);
         } else {
             if (tokens > 1) level[levels++] = {ldk * eb, tokens};
             // rows of two different distances in one span: taken to meet

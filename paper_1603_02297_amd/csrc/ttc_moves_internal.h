@@ -19,7 +19,8 @@ struct ttc_route_s {
 struct ttc_pages_s {
     int      dtype, cache_dtype;
     int64_t  heads, dim, page, pages;
-    int64_t  stride_head, stride_slot, stride_page;    // elements
+    int64_t  vec;                                      // elements of a vector in the cache: dim, or the bytes of a record (TTC_Q4)
+    int64_t  stride_head, stride_slot, stride_page;    // elements (bytes where vectors are records)
     int64_t  span;                                     // elements from the first to the last of the cache, inclusive
     ttc::FastDiv page_div;
 };
@@ -38,7 +39,9 @@ constexpr int kSortOne = kSortOneBlocks * kSortThreads;
 constexpr int64_t kSortChunks = 256, kSortCounts = 1 << 16;
 inline bool sort_adds(int64_t chunks, int experts) { return chunks * experts <= kSortCounts; }
 
-inline int elem_bytes(int dtype) { return dtype == TTC_F32 ? 4 : dtype == TTC_F8 ? 1 : 2; }
+inline int elem_bytes(int dtype) { return dtype == TTC_F32 ? 4 : dtype == TTC_F8 || dtype == TTC_Q4 ? 1 : 2; }
+
+constexpr int kRecordHead = 4, kRecordMaxDim = 512;     // TTC_Q4: bytes before the codes, and a wavefront's eight elements a lane
 
 // How a sort of n assignments is cut: `blocks` ids per lane, `chunk` assignments per workgroup.
 struct SortShape {

@@ -1,6 +1,7 @@
 // Pages of a cache (include/ttc_moves.h, ttc_pages_*), for gfx950 (MI355X): block tables and slots from request
 // lengths, and the moves of keys and values by those slots.
 #include "ttc_moves_device.h"
+#include "ttc_records.h"
 
 namespace ttc {
 
@@ -242,38 +243,13 @@ template <typename T> struct SlotVec { static constexpr int value = 16 / (int)si
 template <typename T, typename C, bool WRITE> struct SlotTypes { typedef T from; typedef C to; };
 template <typename T, typename C> struct SlotTypes<T, C, false> { typedef C from; typedef T to; };
 
-// Into the narrower cache: x / scale.  Divisions cost a dozen instructions each, enough to bound the kernel by arithmetic (bf16, 682 MB
-// in 154 us with them, 124 without; 128 MB by head 24.4 and 21.2; 20 MB 6.9 and 5.9).  With r = 1 / |scale| rounded once, q = x * r is off by two units at most, and q - (q * |scale| - x) * r rounds
-// the quotient itself: ties of the 8-bit format, which are quotients that 32 bits hold, stay ties.  Subtracted in that order a remainder of nothing, which is +0,
-// leaves q as it is, -0 among others.  q is held to +-512 before that, so that an infinite
-// one does not become a NaN; beyond 448 the cut follows anyhow.  A negative scale turns the signs of the result, four at a time.  Scales outside
-// 2^-60 .. 2^60, where r or the remainder could leave the normal range, take the division.
-__device__ __forceinline__ void turn_signs(Vec<f8, 1>& r) { r.e.bits ^= 0x80; }
-template <int V> __device__ __forceinline__ void turn_signs(Vec<f8, V>& r)
-{
-#pragma unroll
-    for (int i = 0; i < V / 4; ++i) r.w[i] ^= 0x80808080u;
-}
+// Into the narrower cache.
 template <typename From, int V>
 __device__ __forceinline__ void convert_in(const Vec<From, V>& x, float scale, Vec<f8, V>& r)
 {
     float f[V];
     widen(x, f);
-    const float size = __builtin_fabsf(scale);
-    if (size >= 0x1p-60f && size <= 0x1p60f) {
-        const float inverse = 1.f / size;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float q = __builtin_fminf(__builtin_fmaxf(f[i] * inverse, -512.f), 512.f);
-            f[i] = __builtin_fmaf(-__builtin_fmaf(q, size, -f[i]), inverse, q);
-        }
-        narrow(f, r);
-        if (scale < 0.f) turn_signs(r);
-    } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) f[i] = f[i] / scale;
-        narrow(f, r);
-    }
+    narrow_scaled(f, scale, r);
 }
 
 // And out of it.
@@ -413,7 +389,115 @@ template <bool WRITE> int launch_slots(const SlotArgs& a, void* stream)
 
 }  // namespace
 
-int launch_write(const SlotArgs& a, void* stream) { return launch_slots<true>(a, stream); }
-int launch_read(const SlotArgs& a, void* stream) { return launch_slots<false>(a, stream); }
+// ---------------------------------------------------------------------------------
+// Keys and values into and out of a cache in 4 bits: a lane has eight elements of one head's vector, of the keys and of the values, and as
+// many lanes as a vector needs, rounded up to a power of two, find its smallest and largest together.
+// ---------------------------------------------------------------------------------
+namespace {
+
+struct RecordArgs {
+    SlotArgs s;
+    uint32_t vectors;                      // tokens * heads
+    uint32_t words;                        // of eight codes, of a vector
+    int32_t  lanes_log;
+    FastDiv  heads;
+};
+
+template <typename T, bool WRITE>
+__global__ __launch_bounds__(kMoveThreads) void records_kernel(RecordArgs p)
+{
+    touch<RecordArgs>();
+    const uint64_t thread = (uint64_t)block_id() * kMoveThreads + threadIdx.x;
+    const uint64_t number = thread >> p.lanes_log;
+    const uint32_t word = (uint32_t)thread & ((1u << p.lanes_log) - 1), at = 8 * word;
+    const uint32_t vector = number < p.vectors ? (uint32_t)number : 0;
+    const uint32_t token = fdiv(vector, p.heads), head = vector - token * p.heads.div;
+    const bool mine = number < p.vectors && word < p.words;
+    const uint32_t slot = (uint32_t)p.s.slots[token];
+    const bool here = slot < p.s.slot_count;
+    const uint32_t page = here ? fdiv(slot, p.s.page) : 0, inside = here ? slot - page * p.s.page.div : 0;
+    const int64_t record = (int64_t)page * p.s.stride_page + (int64_t)inside * p.s.stride_slot + (int64_t)head * p.s.stride_head;
+    const int64_t packed = (int64_t)head * p.s.dim + at, at_k = (int64_t)token * p.s.ld_k + packed, at_v = (int64_t)token * p.s.ld_v + packed;
+    const bool both = p.s.v_out != nullptr;
+    float x[8];
+    if constexpr (WRITE) {
+        Vec<T, 8> k = {}, v = {};
+        if (mine && here) {
+            k = load_vec<T, 8, false>(static_cast<const T*>(p.s.k) + at_k);
+            if (both) v = load_vec<T, 8, false>(static_cast<const T*>(p.s.v) + at_v);
+        }
+        auto put = [&](const Vec<T, 8>& r, void* cache) {
+            widen(r, x);
+            RecordRange range;
+            if (mine) range.take(x, 8);
+            const Record made = range.record(p.lanes_log);
+            uint8_t* to = static_cast<uint8_t*>(cache) + record;
+            if (mine && here) {
+                if (word == 0) store_word(to, made.head());
+                store_word(to + kRecordHead + at / 2, made.codes(x));
+            }
+        };
+        put(k, p.s.k_out);
+        if (both) put(v, p.s.v_out);
+    } else {
+        if (!mine) return;
+        uint32_t k_head = 0, k_word = 0, v_head = 0, v_word = 0;           // nowhere: 0 * 0 + 0
+        if (here) {
+            const uint8_t* from = static_cast<const uint8_t*>(p.s.k) + record;
+            k_head = load_word(from);
+            k_word = load_word(from + kRecordHead + at / 2);
+            if (both) {
+                const uint8_t* v_from = static_cast<const uint8_t*>(p.s.v) + record;
+                v_head = load_word(v_from);
+                v_word = load_word(v_from + kRecordHead + at / 2);
+            }
+        }
+        Vec<T, 8> r;
+        widen_record(k_head, k_word, x);
+        narrow(x, r);
+        store_vec<T, 8, false>(static_cast<T*>(p.s.k_out) + at_k, r);
+        if (both) {
+            widen_record(v_head, v_word, x);
+            narrow(x, r);
+            store_vec<T, 8, false>(static_cast<T*>(p.s.v_out) + at_v, r);
+        }
+    }
+}
+
+template <bool WRITE> int launch_records(const SlotArgs& a, void* stream)
+{
+    RecordArgs p = {};
+    p.s = a;
+    p.words = a.dim / 8;
+    p.lanes_log = log2_ceil(p.words);
+    p.heads = make_fastdiv(a.heads);
+    const int eb = elem_bytes(a.dtype);
+    // vectors are counted below 2^31: very long lists go in several launches
+    const uint32_t most = (uint32_t)INT32_MAX / a.heads;
+    for (uint64_t done = 0; done < a.tokens; done += most) {
+        const uint32_t tokens = a.tokens - done < most ? (uint32_t)(a.tokens - done) : most;
+        p.s.slots = a.slots + done;
+        const int64_t skip_k = (int64_t)done * a.ld_k * eb, skip_v = (int64_t)done * a.ld_v * eb;
+        if (WRITE) {
+            p.s.k = static_cast<const char*>(a.k) + skip_k;
+            if (a.v) p.s.v = static_cast<const char*>(a.v) + skip_v;
+        } else {
+            p.s.k_out = static_cast<char*>(a.k_out) + skip_k;
+            if (a.v_out) p.s.v_out = static_cast<char*>(a.v_out) + skip_v;
+        }
+        p.vectors = tokens * a.heads;
+        const void* fn = a.dtype == TTC_F32 ? reinterpret_cast<const void*>(&records_kernel<float, WRITE>)
+                       : a.dtype == TTC_BF16 ? reinterpret_cast<const void*>(&records_kernel<__bf16, WRITE>)
+                                             : reinterpret_cast<const void*>(&records_kernel<_Float16, WRITE>);
+        const int st = launch_blocks(fn, (((uint64_t)p.vectors << p.lanes_log) + kMoveThreads - 1) / kMoveThreads, kMoveThreads, 0, &p, stream);
+        if (st != TTC_OK) return st;
+    }
+    return TTC_OK;
+}
+
+}  // namespace
+
+int launch_write(const SlotArgs& a, void* stream) { return a.cache_dtype == TTC_Q4 ? launch_records<true>(a, stream) : launch_slots<true>(a, stream); }
+int launch_read(const SlotArgs& a, void* stream) { return a.cache_dtype == TTC_Q4 ? launch_records<false>(a, stream) : launch_slots<false>(a, stream); }
 
 }  // namespace ttc

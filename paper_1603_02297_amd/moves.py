@@ -9,7 +9,7 @@ from typing import Optional, Sequence
 from . import binding
 from .binding import TTC_OK, TtcError, lib, ttc_last_status
 
-TTC_BF16, TTC_F16, TTC_F8 = 8, 9, 10
+TTC_BF16, TTC_F16, TTC_F8, TTC_Q4 = 8, 9, 10, 11
 TTC_ROUTE_MAX_EXPERTS, TTC_ROUTE_MAX_TOPK, TTC_ROUTE_MAX_ALIGN = 1024, 64, 65536
 
 MOVE_EXPORTS = (
@@ -18,7 +18,7 @@ MOVE_EXPORTS = (
     "ttc_pages_read",
 )
 
-__all__ = [*MOVE_EXPORTS, "MOVE_EXPORTS", "TTC_BF16", "TTC_F16", "TTC_F8", "TTC_ROUTE_MAX_EXPERTS", "TTC_ROUTE_MAX_TOPK", "TTC_ROUTE_MAX_ALIGN"]
+__all__ = [*MOVE_EXPORTS, "MOVE_EXPORTS", "TTC_BF16", "TTC_F16", "TTC_F8", "TTC_Q4", "TTC_ROUTE_MAX_EXPERTS", "TTC_ROUTE_MAX_TOPK", "TTC_ROUTE_MAX_ALIGN"]
 
 # the calls that enqueue work, in the order of the CPython form's table
 _MOVES = ("ttc_route_sort", "ttc_route_gather", "ttc_route_combine", "ttc_route_combine_grad", "ttc_pages_map", "ttc_pages_write", "ttc_pages_read")
