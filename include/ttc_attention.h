@@ -3,6 +3,7 @@
  *
  *   ttc_heads_*        norms of queries and keys for each head, with the rotation by position in the same pass; with the gradients
  *   ttc_pages_append   the same on the way of new tokens into the cache
+ *   ttc_attend_*       attention of new tokens over the pages of their requests
  *
  * Conventions as in ttc_moves.h: column-major, DEVICE pointers owned by the caller, integer status codes, nothing throws or aborts
  * across this boundary; handles are made once, touch no device, may be used from several streams at a time; every other
@@ -21,7 +22,7 @@ extern "C" {
 #endif
 
 /* Limits of a handle (TTC_ERR_INVALID_VALUE beyond them). */
-enum { TTC_HEADS_MAX_DIM = 512, TTC_HEADS_MAX_ROTATED = 256 };
+enum { TTC_HEADS_MAX_DIM = 512, TTC_HEADS_MAX_ROTATED = 256, TTC_ATTEND_MAX_DIM = 256 };
 
 /* ---- norms of the heads, and their rotation ------------------------------------------------------------------ */
 
@@ -84,6 +85,42 @@ int ttc_heads_rotate_grad(ttc_heads_t heads, int64_t tokens, const int32_t* posi
 int ttc_pages_append(ttc_pages_t pages, ttc_heads_t heads, int64_t tokens, const int32_t* slots, const int32_t* positions, const void* q, int64_t ldq,
                      const void* k, int64_t ldk, const void* v, int64_t ldv, const float* q_weight, const float* k_weight, void* q_out, int64_t ld_qo,
                      void* k_cache, void* v_cache, const float* k_scale, const float* v_scale, void* stream);
+
+/* ---- attention over the cache ---------------------------------------------------------------------------------- */
+
+typedef struct ttc_attend_s* ttc_attend_t;
+
+/*
+ * A handle for attention over caches like that of `pages` (what it says is copied), dim 1 .. TTC_ATTEND_MAX_DIM.
+ *   q_heads    a multiple of the cache's heads: query head h reads head h / (q_heads / heads).
+ *   scale      finite, what the products of queries and keys are multiplied with.
+ *   window     0: every position up to the query's own; else the last `window` of them, its own among them.
+ * Returns NULL on error; ttc_last_status() says why.
+ */
+ttc_attend_t ttc_attend_create(ttc_pages_t pages, int64_t q_heads, double scale, int64_t window);
+int ttc_attend_destroy(ttc_attend_t attend);
+
+/* Bytes of workspace for ttc_attend_pages with tables of ld_table entries (0 where it needs none), or a negative status. */
+int64_t ttc_attend_workspace(ttc_attend_t attend, int64_t requests, int64_t tokens, int64_t ld_table);
+
+/*
+ * out[:, h, i] <- sum_j softmax_j(scale * <q[:, h, i], k_j>) v_j  over the positions j that token i sees.
+ *   q          [dim, q_heads, tokens], ldq >= q_heads*dim: the packed new tokens.
+ *   starts     [requests+1] int32 as ttc_pages_map left it for them: request r has the tokens starts[r] .. starts[r+1]-1.  Tokens before starts[0] and from
+ *              starts[requests] on are left as they were.
+ *   cached     [requests] int32: positions that request r held before them (negative counts as 0); its token i stands at cached[r] + i - starts[r], and its keys and
+ *              values, those of the new tokens among them, are in the cache already.
+ *   table      [ld_table, requests] int32 as for ttc_pages_map.  Positions past the table (>= ld_table*page) and those whose entry is no page are not there.
+ *   k_cache, v_cache, k_scale, v_scale   as for ttc_pages_read.
+ *   out        as q; must not overlap it.
+ *   lse        [q_heads, tokens] float or NULL: the logarithm of the sum of exponentials, -inf where a token sees nothing.
+ *   workspace  ttc_attend_workspace bytes, aligned to 16.
+ * A token that sees nothing gets 0, and a score of -inf counts as not seen.  What a position that is not seen holds (NaN, infinities) has no effect.  Scores, exponentials and
+ * their sums are 32 bits; with 16-bit queries the exponentials (at most 1) are rounded to that type for their products with the values, once.
+ */
+int ttc_attend_pages(ttc_attend_t attend, int64_t requests, int64_t tokens, const void* q, int64_t ldq, const int32_t* starts, const int32_t* cached,
+                     const int32_t* table, int64_t ld_table, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                     void* out, int64_t ldo, float* lse, void* workspace, void* stream);
 
 #ifdef __cplusplus
 }

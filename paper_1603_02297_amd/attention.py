@@ -10,16 +10,17 @@ from . import binding
 from .binding import TtcError, lib, ttc_last_status
 from .moves import _Address, _checked, _failed, _fast as _moves_fast, _size
 
-TTC_HEADS_MAX_DIM, TTC_HEADS_MAX_ROTATED = 512, 256
+TTC_HEADS_MAX_DIM, TTC_HEADS_MAX_ROTATED, TTC_ATTEND_MAX_DIM = 512, 256, 256
 
 ATTENTION_EXPORTS = (
     "ttc_heads_create", "ttc_heads_destroy", "ttc_heads_rotate", "ttc_heads_workspace", "ttc_heads_rotate_grad", "ttc_pages_append",
+    "ttc_attend_create", "ttc_attend_destroy", "ttc_attend_workspace", "ttc_attend_pages",
 )
 
-__all__ = [*ATTENTION_EXPORTS, "ATTENTION_EXPORTS", "TTC_HEADS_MAX_DIM", "TTC_HEADS_MAX_ROTATED"]
+__all__ = [*ATTENTION_EXPORTS, "ATTENTION_EXPORTS", "TTC_HEADS_MAX_DIM", "TTC_HEADS_MAX_ROTATED", "TTC_ATTEND_MAX_DIM"]
 
 # the calls that enqueue work, by their numbers in the CPython form's table
-_CALLS = {"ttc_heads_rotate": 7, "ttc_heads_rotate_grad": 8, "ttc_pages_append": 9}
+_CALLS = {"ttc_heads_rotate": 7, "ttc_heads_rotate_grad": 8, "ttc_pages_append": 9, "ttc_attend_pages": 10}
 _fast = _moves_fast if all(hasattr(_moves_fast, name) for name in _CALLS) else None      # not built, or of an older source
 
 
@@ -30,7 +31,10 @@ def _declare(L: ctypes.CDLL) -> None:
             ("ttc_heads_rotate", i, [vp, n, vp, vp, n, vp, n, vp, vp, vp, n, vp, n, vp]),
             ("ttc_heads_workspace", n, [vp, n]),
             ("ttc_heads_rotate_grad", i, [vp, n, vp, vp, n, vp, n, vp, n, vp, n, vp, vp, vp, n, vp, n, vp, vp, vp, vp]),
-            ("ttc_pages_append", i, [vp, vp, n, vp, vp, vp, n, vp, n, vp, n, vp, vp, vp, n, vp, vp, vp, vp, vp])):
+            ("ttc_pages_append", i, [vp, vp, n, vp, vp, vp, n, vp, n, vp, n, vp, vp, vp, n, vp, vp, vp, vp, vp]),
+            ("ttc_attend_create", ret, [vp, n, ctypes.c_double, n]), ("ttc_attend_destroy", i, [vp]),
+            ("ttc_attend_workspace", n, [vp, n, n, n]),
+            ("ttc_attend_pages", i, [vp, n, n, vp, n, vp, vp, vp, n, vp, vp, vp, vp, vp, n, vp, vp, vp])):
         g = getattr(L, name)
         g.restype, g.argtypes = restype, argtypes
     if _fast is not None:
@@ -83,6 +87,31 @@ def ttc_pages_append(pages: int, heads: int, tokens: int, slots: int, positions:
     """The same on the way into the cache, values with the keys."""
     _checked(lib().ttc_pages_append(pages, heads, tokens, slots, positions, q, ldq, k, ldk, v, ldv, q_weight, k_weight, q_out, ld_qo, k_cache, v_cache,
                                     k_scale, v_scale, stream or None), "ttc_pages_append")
+
+
+def ttc_attend_create(pages: int, q_heads: int, scale: float, window: int = 0) -> int:
+    """Returns the handle.  window: positions that a query sees, its own among them; 0: all before it."""
+    h = lib().ttc_attend_create(pages, int(q_heads), float(scale), int(window))
+    if not h:
+        raise TtcError(ttc_last_status(), "ttc_attend_create")
+    return h
+
+
+def ttc_attend_destroy(attend: Optional[int]) -> None:
+    lib().ttc_attend_destroy(attend)
+
+
+def ttc_attend_workspace(attend: int, requests: int, tokens: int, ld_table: int) -> int:
+    """Bytes of workspace for ttc_attend_pages."""
+    return _size(lib().ttc_attend_workspace(attend, int(requests), int(tokens), int(ld_table)), "ttc_attend_workspace")
+
+
+def ttc_attend_pages(attend: int, requests: int, tokens: int, q: int, ldq: int, starts: int, cached: int, table: int, ld_table: int, k_cache: int, v_cache: int,
+                     k_scale: Optional[int], v_scale: Optional[int], out: int, ldo: int, lse: Optional[int], workspace: Optional[int],
+                     stream: Optional[int] = None) -> None:
+    """Attention of packed new tokens over the pages of their requests."""
+    _checked(lib().ttc_attend_pages(attend, requests, tokens, q, ldq, starts, cached, table, ld_table, k_cache, v_cache, k_scale, v_scale, out, ldo, lse,
+                                    workspace, stream or None), "ttc_attend_pages")
 
 
 _ctypes_forms = {name: globals()[name] for name in _CALLS}

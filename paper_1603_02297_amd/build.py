@@ -20,7 +20,8 @@ LIB = os.path.join(HERE, "libttc.so")
 CALL = os.path.join(HERE, "_call" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))      # the binding's ttc_execute
 SOURCES = ["ttc_launch_f32.hip", "ttc_launch_mixed_real.hip", "ttc_launch_f64.hip", "ttc_launch_c64.hip",
            "ttc_launch_mixed_complex.hip", "ttc_launch_c128.hip", "ttc_plan.cpp", "ttc_cache.cpp", "ttc_device.hip",
-           "ttc_moves.cpp", "ttc_route.hip", "ttc_pages.hip", "ttc_attention.cpp", "ttc_heads.hip"]
+           "ttc_moves.cpp", "ttc_route.hip", "ttc_pages.hip", "ttc_attention.cpp", "ttc_heads.hip", "ttc_attend.hip",
+           "ttc_attend_f32.hip", "ttc_attend_bf16.hip", "ttc_attend_f16.hip"]
 
 
 def _flags(verbose: bool):

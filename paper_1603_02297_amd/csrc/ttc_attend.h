@@ -1,0 +1,721 @@
+// Attention of new tokens over the pages of their requests (include/ttc_attention.h, ttc_attend_pages), for gfx950 (MI355X): the kernel, instantiated per
+// type of the queries in ttc_attend_f32.hip, ttc_attend_bf16.hip and ttc_attend_f16.hip.
+//
+// The query heads that share a head of the cache are rows of one matrix product, token by token, so that a position's key and value are fetched once for
+// them all.  A wavefront has 32 rows.  It makes scores transposed, S^T = K Q^T, with the 32 x 32 matrix instructions: their result has a row in two lanes, half a wavefront
+// apart, and its positions in their registers.  The softmax's maximum and sum are then registers, too (one exchange between the two lanes for the
+// maximum of a tile, one for the sum at the end), and the exponentials are, without a move, what O^T = V^T P^T takes as its right operand: a product's
+// order of positions is free as long as both sides have the same one.  V^T is read from the tile by the transposing LDS loads, in that order.
+//
+//   FEW   at most some 32 rows to a request (tokens that are generated one by one): the wavefronts of a workgroup have the same rows and every one its own tiles of 32
+//         positions, in LDS of its own; no barrier until they add up their results.  Bound by the cache's bytes.
+//   else  prompts: wavefronts have 32 rows each of the same 128 and share the tiles.  Bound by the matrix instructions, and the exponentials beside them.
+//
+// A tile's loads are under way while the one before it is used, its entries of the block table one tile earlier.
+#pragma once
+
+#include <type_traits>
+
+#include "ttc_attention_internal.h"
+#include "ttc_moves_device.h"
+#include "ttc_records.h"
+
+namespace ttc {
+namespace attend {
+
+typedef float Acc __attribute__((ext_vector_type(16)));
+typedef short Short4 __attribute__((ext_vector_type(4)));
+typedef short Short8 __attribute__((ext_vector_type(8)));
+#define TTC_LDS __attribute__((address_space(3)))
+
+// What a lane holds of an operand: 16 bytes, kDims of the contracted index over the two lanes of a row.
+template <typename E> struct Fragment;
+template <> struct Fragment<__bf16> {
+    typedef __bf16 type __attribute__((ext_vector_type(8)));
+    static constexpr int kDims = 16;
+    static __device__ __forceinline__ void mul(type a, type b, Acc& c) { c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Fragment<_Float16> {
+    typedef _Float16 type __attribute__((ext_vector_type(8)));
+    static constexpr int kDims = 16;
+    static __device__ __forceinline__ void mul(type a, type b, Acc& c) { c = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct Fragment<float> {
+    typedef float type __attribute__((ext_vector_type(4)));
+    static constexpr int kDims = 8;
+    static __device__ __forceinline__ void mul(type a, type b, Acc& c)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
+    }
+};
+
+// T: queries and results; C: the cache; DP: dim rounded up to what the kernel is compiled for.
+template <typename T, typename C, int DP, bool FEW> struct Plan {
+    typedef T K;                                                            // keys in LDS
+    // Values in LDS, and the exponentials.  Codes of 4 bits are multiplied by exponentials times steps, of which fp16 would lose the small ones: bf16.
+    typedef typename std::conditional<std::is_same<C, q4>::value && !std::is_same<T, float>::value, __bf16, T>::type V;
+    static constexpr bool kRecords = std::is_same<C, q4>::value;
+    // records as codes (integers that 16 bits hold), step and minimum applied to scores and exponentials; in 32 bits as what they stand for
+    static constexpr bool kCodes = kRecords && sizeof(T) == 2;
+    static constexpr bool kWide = sizeof(T) == 4;
+    static constexpr int  kWaves = FEW && kWide && DP > 128 ? 2 : 4;
+    static constexpr int  kThreads = kWaves * kWave;
+    static constexpr int  kTeams = FEW ? kWaves : 1;
+    static constexpr int  kTeam = FEW ? kWave : kThreads;                    // threads that load a tile together
+    static constexpr int  kKeys = FEW || (kWide && DP > 128) ? 32 : 64;      // positions of a tile
+    static constexpr int  kStep = kKeys * kTeams;
+    static constexpr int  kChunks = DP / 8;                                  // of eight elements, of a vector
+    static constexpr int  kMine = kKeys * kChunks / kTeam;                   // chunks of a tile that a thread loads
+    static constexpr bool kAhead = !(FEW && kWide && DP > 128);              // loads of the next tile under way beside the products of this one
+    // rows in LDS end 16 and 32 bytes later than their elements, so that eight rows (four, of values) meet all banks
+    static constexpr int  kKeyRow = DP * (int)sizeof(K) + 16, kValueRow = DP * (int)sizeof(V) + (kWide ? 16 : 32);
+    static constexpr int  kTile = kKeys * (kKeyRow + kValueRow) + (kCodes ? 4 * kKeys * 4 : 0);
+    static constexpr int  kMergeRow = DP + 4;                                // floats
+    static constexpr int  kMerge = FEW ? kWaves * 32 * kMergeRow * 4 + 3 * kWaves * 32 * 4 : 0;
+    static constexpr int  kLds = kTile * kTeams > kMerge ? kTile * kTeams : kMerge;
+    static_assert(kKeys * kChunks % kTeam == 0 && DP % 32 == 0 && kLds <= kMaxLdsBytes, "a tile is loaded in whole chunks");
+};
+
+// Eight elements of the cache in registers, as they lie there.
+template <typename C> struct Chunk8 { Vec<C, 8> v; };
+template <> struct Chunk8<q4> { uint32_t word, head; };
+
+template <typename C> __device__ __forceinline__ Chunk8<C> load_chunk(const char* vector, uint32_t at, uint32_t dim)
+{
+    Chunk8<C> r = {};
+    const C* p = reinterpret_cast<const C*>(vector) + at;
+    if (at + 8 <= dim) {
+        r.v = load_vec<C, 8, false>(p);
+    } else if (at < dim) {                                                  // dims that are no multiple of eight: the last chunk
+        C e[8] = {};
+        for (uint32_t i = 0; i < 8; ++i)
+            if (at + i < dim) e[i] = p[i];
+        __builtin_memcpy(&r.v, e, sizeof(r.v));
+    }
+    return r;
+}
+template <> __device__ __forceinline__ Chunk8<q4> load_chunk<q4>(const char* vector, uint32_t at, uint32_t dim)
+{
+    Chunk8<q4> r = {};
+    const uint8_t* p = reinterpret_cast<const uint8_t*>(vector);
+    r.head = load_word(p);
+    if (at < dim) r.word = load_word(p + kRecordHead + at / 2);
+    return r;
+}
+
+// Whether one of eight elements is an infinity or a NaN.
+__device__ __forceinline__ bool any_bad(const Vec<float, 8>& v)
+{
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) bad |= (v.w[i] & 0x7f800000u) == 0x7f800000u;
+    return bad;
+}
+__device__ __forceinline__ bool any_bad(const Vec<__bf16, 8>& v)
+{
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bad |= (v.w[i] & 0x7f80u) == 0x7f80u || (v.w[i] & 0x7f800000u) == 0x7f800000u;
+    return bad;
+}
+__device__ __forceinline__ bool any_bad(const Vec<_Float16, 8>& v)
+{
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bad |= (v.w[i] & 0x7c00u) == 0x7c00u || (v.w[i] & 0x7c000000u) == 0x7c000000u;
+    return bad;
+}
+__device__ __forceinline__ bool any_bad(const Vec<f8, 8>& v)
+{
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) bad |= (v.w[i] >> (8 * j) & 0x7fu) == 0x7fu;
+    return bad;
+}
+template <typename C> __device__ __forceinline__ bool any_bad(const Chunk8<C>& c) { return any_bad(c.v); }
+__device__ __forceinline__ bool any_bad(const Chunk8<q4>& c)
+{
+    return (c.head & 0x7f80u) == 0x7f80u || (c.head & 0x7f800000u) == 0x7f800000u;
+}
+
+// Eight codes as 16 + code, which 16 bits hold.  Scores take the 16 back with the minimum; values have 24 times the sum of their weights, as they were
+// rounded, taken back, so that a weight's rounding is off by that of code - 8 times the step.
+__device__ __forceinline__ void codes_of(uint32_t word, uint32_t one, int shift, uint32_t* w)
+{
+    const uint32_t even = word & 0x0f0f0f0fu, odd = word >> 4 & 0x0f0f0f0fu;
+#pragma unroll
+    for (uint32_t k = 0; k < 4; ++k) w[k] = __builtin_amdgcn_perm(odd, even, 0x0c000c00u | (4 + k) << 16 | k) << shift | one;
+}
+__device__ __forceinline__ void codes_of(uint32_t word, Vec<__bf16, 8>& r) { codes_of(word, 0x41804180u, 3, r.w); }
+__device__ __forceinline__ void codes_of(uint32_t word, Vec<_Float16, 8>& r) { codes_of(word, 0x4c004c00u, 6, r.w); }
+
+__device__ __forceinline__ void widen_eight(const Vec<f8, 8>& c, Vec<float, 8>& r)
+{
+    float x[8];
+    widen(c, x);
+    narrow(x, r);
+}
+__device__ __forceinline__ void widen_eight(const Vec<f8, 8>& c, Vec<__bf16, 8>& r)
+{
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        r.w[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c.w[i], 1.f, false));
+        r.w[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)c.w[i], 1.f, true));
+    }
+}
+__device__ __forceinline__ void widen_eight(const Vec<f8, 8>& c, Vec<_Float16, 8>& r)
+{
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        r.w[2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)c.w[i], 1.f, false));
+        r.w[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)c.w[i], 1.f, true));
+    }
+}
+
+// A chunk as the tile holds it.  16-bit caches are of the queries' type, and 8 bits widen exactly.
+template <typename E, typename C> __device__ __forceinline__ void store_chunk(char* lds, const Chunk8<C>& c)
+{
+    Vec<E, 8> r;
+    if constexpr (std::is_same<C, q4>::value) {
+        if constexpr (sizeof(E) == 4) {
+            float x[8];
+            widen_record(c.head, c.word, x);
+            narrow(x, r);
+        } else {
+            codes_of(c.word, r);
+        }
+    } else if constexpr (std::is_same<E, C>::value) {
+        r = c.v;
+    } else {
+        widen_eight(c.v, r);
+    }
+    typedef uint32_t Word4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int i = 0; i < Vec<E, 8>::kWords / 4; ++i) {
+        Word4 w;
+        __builtin_memcpy(&w, r.w + 4 * i, 16);
+        reinterpret_cast<Word4*>(lds)[i] = w;
+    }
+}
+
+template <bool WAVE> __device__ __forceinline__ void team_sync()
+{
+    if constexpr (WAVE) {                                                   // a wavefront's LDS accesses happen in order: only the compiler has to keep it
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    } else {
+        __syncthreads();
+    }
+}
+
+// The tile of rows of a workgroup, the positions that it goes over, and which of the parts of these it is.
+struct Work {
+    uint32_t request, row0, rows;          // rows: of the request
+    uint32_t first_token;                  // of the request
+    uint32_t cached;
+    uint32_t lo, hi;                       // of this part
+    uint32_t part, parts;
+};
+
+// Tile number `slot` is request r's with starts[r] * group / tile + r <= slot: these numbers grow with r, so that the wavefront counts, 64 requests at a time.
+__device__ __forceinline__ uint32_t first_slot(const AttendArgs& p, uint32_t r, uint32_t tile)
+{
+    const int32_t s = p.starts[r];
+    return ((s < 0 ? 0u : (uint32_t)s < p.tokens ? (uint32_t)s : p.tokens) * p.group) / tile + r;
+}
+
+template <typename P, int TILE> __device__ __forceinline__ bool find_work(const AttendArgs& p, uint32_t slot, uint32_t split, Work& w)
+{
+    const uint32_t lane = threadIdx.x & (kWave - 1);
+    uint32_t lo = 0, n = p.requests;
+    while (n > 1) {
+        const uint32_t step = (n + kWave - 1) / kWave, r = lo + lane * step;
+        const uint64_t before = __ballot(lane * step < n && first_slot(p, r < p.requests ? r : 0, TILE) <= slot);
+        const uint32_t count = (uint32_t)__builtin_popcountll(before);
+        if (count == 0) return false;
+        lo += (count - 1) * step;
+        n = n - (count - 1) * step < step ? n - (count - 1) * step : step;
+        if (step == 1) n = 1;
+    }
+    const uint32_t base = first_slot(p, lo, TILE);
+    if (slot < base) return false;
+    auto cut = [&](int32_t s) { return s < 0 ? 0u : (uint32_t)s < p.tokens ? (uint32_t)s : p.tokens; };
+    const uint32_t begin = cut(p.starts[lo]), end = cut(p.starts[lo + 1]);
+    w.request = lo;
+    w.first_token = begin;
+    w.row0 = (slot - base) * TILE;
+    w.rows = end > begin ? (end - begin) * p.group : 0;
+    if (w.row0 >= w.rows) return false;
+    const int32_t c = p.cached[lo];
+    w.cached = c < 0 ? 0 : (uint32_t)c;
+    // what the tile's rows see, within the table
+    const uint32_t last = w.row0 + TILE < w.rows ? w.row0 + TILE - 1 : w.rows - 1;
+    const uint64_t entries = (uint64_t)p.ld_table * p.page.div;
+    uint64_t hi = (uint64_t)w.cached + fdiv(last, p.group_div) + 1;
+    hi = hi < entries ? hi : entries;
+    const uint32_t top = hi < 0x7fffffffu ? (uint32_t)hi : 0x7fffffffu, first = w.cached + fdiv(w.row0, p.group_div) + 1;
+    const uint32_t bottom = p.window && first > p.window ? first - p.window : 0;
+    const uint32_t count = top > bottom ? top - bottom : 0;
+    constexpr uint32_t kUnit = P::kStep > 128 ? P::kStep : 128;
+    w.parts = (count + kUnit - 1) / kUnit;
+    w.parts = w.parts < p.splits ? w.parts : p.splits;
+    w.part = split;
+    if (w.parts <= 1) {
+        w.parts = 1;
+        w.lo = bottom;
+        w.hi = top > bottom ? top : bottom;
+        return split == 0;
+    }
+    const uint32_t each = ((count + w.parts - 1) / w.parts + P::kStep - 1) / P::kStep * P::kStep;
+    w.parts = (count + each - 1) / each;
+    w.lo = bottom + split * each;
+    w.hi = top - w.lo < each ? top : w.lo + each;
+    return split < w.parts;
+}
+
+// The larger, and the sum, of the two lanes of a row.
+__device__ __forceinline__ float max_of_row(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    return __builtin_fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float sum_of_row(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+
+// The weights of a value's element in the count of what is neither finite: at most 64 of each in a tile.
+constexpr int kPlus = 1, kMinus = 128, kNan = 16384;
+
+// A fragment of values taken apart: what is finite, and marks where it is not.
+template <typename E> struct Bad;
+template <typename E, int EXP, int SIGN, int PLUS, int MINUS, int NAN_> struct Bad16 {
+    typedef typename Fragment<E>::type Frag;
+    static __device__ __forceinline__ Frag marks(Frag& v)
+    {
+        const Short8 b = __builtin_bit_cast(Short8, v);
+        const Short8 bad = (b & (short)EXP) == (short)EXP, nan = bad & ((b & (short)(0x7fff & ~EXP)) != (short)0), minus = (b & (short)SIGN) != (short)0;
+        v = __builtin_bit_cast(Frag, b & ~bad);
+        return __builtin_bit_cast(Frag, bad & ((nan & (short)NAN_) | (~nan & ((minus & (short)MINUS) | (~minus & (short)PLUS)))));
+    }
+};
+template <> struct Bad<__bf16> : Bad16<__bf16, 0x7f80, 0x8000, 0x3f80, 0x4300, 0x4680> {};
+template <> struct Bad<_Float16> : Bad16<_Float16, 0x7c00, 0x8000, 0x3c00, 0x5800, 0x7400> {};
+template <> struct Bad<float> {
+    typedef typename Fragment<float>::type Frag;
+    static __device__ __forceinline__ Frag marks(Frag& v)
+    {
+        Frag m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float x = v[i];
+            m[i] = x != x ? (float)kNan : __builtin_isinf(x) ? (x > 0 ? (float)kPlus : (float)kMinus) : 0.f;
+            v[i] = m[i] != 0.f ? 0.f : x;
+        }
+        return m;
+    }
+};
+
+template <typename T, typename C, int DP, bool FEW>
+__global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), 1) void attend_kernel(AttendArgs p)
+{
+    typedef Plan<T, C, DP, FEW> P;
+    typedef typename P::K KE;
+    typedef typename P::V VE;
+    typedef typename Fragment<KE>::type KFrag;
+    typedef typename Fragment<VE>::type VFrag;
+    constexpr int kTileRows = FEW ? kTileFew : kTileMany, kBlocks = P::kKeys / 32, kSteps = DP / Fragment<KE>::kDims, kOut = DP / 32;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const uint32_t lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, half = lane >> 5, column = lane & 31;
+    const uint32_t head = blockIdx.y, slot = blockIdx.x, split = blockIdx.z;
+    Work w;
+    if (!find_work<P, kTileRows>(p, p.slots_of_tiles - 1 - slot, split, w)) return;        // the last tiles see most: first
+
+    // this lane's row; behind the request's last one, that one again
+    const uint32_t own = w.row0 + (FEW ? 0 : wave * 32) + column, row = own < w.rows ? own : w.rows - 1;
+    const uint32_t in_request = fdiv(row, p.group_div), q_head = head * p.group + (row - in_request * p.group);
+    const uint32_t token = w.first_token + in_request, position = w.cached + in_request;
+    uint32_t first_row = w.row0 + (FEW ? 0 : wave * 32);
+    const bool idle = first_row >= w.rows;                                  // no row of this wavefront's is one
+    first_row = first_row < w.rows ? first_row : w.rows - 1;
+    const uint32_t last_row = first_row + 31 < w.rows ? first_row + 31 : w.rows - 1;
+    const uint32_t lowest = w.cached + fdiv(first_row, p.group_div), highest = w.cached + fdiv(last_row, p.group_div);
+
+    // scores times `scale` are exponents of 2; its sign goes into the queries, so that the largest product has the largest exponent
+    float scale = p.scale;
+    if (std::is_same<C, f8>::value && p.k_scale) scale *= p.k_scale[head];
+    const float sign = scale < 0.f ? -1.f : scale == 0.f ? 0.f : 1.f;
+    scale = scale < 0.f ? -scale : scale == 0.f ? 1.f : scale;
+    KFrag query[kSteps];
+    float query_sum = 0.f;
+    {
+        const T* from = static_cast<const T*>(p.q) + (int64_t)token * p.ld_q + (int64_t)q_head * p.dim;
+        constexpr int E = 16 / (int)sizeof(T);
+        const KFrag none = {};
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            const uint32_t at = i * Fragment<KE>::kDims + half * E;
+            query[i] = none;
+            if (at + E <= p.dim) query[i] = __builtin_bit_cast(KFrag, load_vec<T, E, false>(from + at));
+            else
+                for (int j = 0; j < E; ++j)
+                    if (at + j < p.dim) query[i][j] = from[at + j];
+        }
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                if (sign != 1.f) query[i][j] = (T)((float)query[i][j] * sign);
+                if (P::kCodes) query_sum += (float)query[i][j];
+            }
+        if (P::kCodes) query_sum = sum_of_row(query_sum);
+    }
+
+    char* tile = lds + (FEW ? wave * P::kTile : 0);
+    char *keys = tile, *values = tile + P::kKeys * P::kKeyRow;
+    float* key_step = reinterpret_cast<float*>(values + P::kKeys * P::kValueRow);           // kCodes: four arrays of kKeys
+    float *key_low = key_step + P::kKeys, *value_step = key_low + P::kKeys, *value_low = value_step + P::kKeys;
+    const uint32_t member = FEW ? lane : threadIdx.x;
+    const char* k_cache = static_cast<const char*>(p.k_cache) + (int64_t)head * p.stride_head * (int64_t)sizeof(C);
+    const char* v_cache = static_cast<const char*>(p.v_cache) + (int64_t)head * p.stride_head * (int64_t)sizeof(C);
+    const int32_t* table = p.table + (int64_t)w.request * p.ld_table;
+
+    // lane j of every wavefront has position j of a tile: its entry of the table, then where its vectors are
+    auto look_up = [&](uint32_t at) -> int32_t {
+        const uint32_t key = at + (lane & (P::kKeys - 1));
+        return key < w.hi ? table[fdiv(key, p.page)] : -1;
+    };
+    struct Spot { int64_t offset; bool here; };
+    auto spot_of = [&](uint32_t at, int32_t entry) -> Spot {
+        const uint32_t key = at + (lane & (P::kKeys - 1)), inside = key - fdiv(key, p.page) * p.page.div;
+        const bool here = (uint32_t)entry < p.pages;
+        return {here ? ((int64_t)entry * p.stride_page + (int64_t)inside * p.stride_slot) * (int64_t)sizeof(C) : -1, here};
+    };
+    Chunk8<C> raw_k[P::kMine], raw_v[P::kAhead ? P::kMine : 1];
+    auto load = [&](const char* cache, int64_t offset, Chunk8<C>* raw) {
+#pragma unroll
+        for (int i = 0; i < P::kMine; ++i) {
+            const uint32_t id = member + i * P::kTeam, key = id / P::kChunks, at = id % P::kChunks * 8;
+            const uint32_t low = __shfl((uint32_t)offset, key), high = __shfl((uint32_t)(offset >> 32), key);
+            const int64_t place = (int64_t)((uint64_t)high << 32 | low);
+            raw[i] = {};
+            if (place >= 0) raw[i] = load_chunk<C>(cache + place, at, p.dim);
+        }
+    };
+    auto put_keys = [&](const Chunk8<C>* raw) {
+#pragma unroll
+        for (int i = 0; i < P::kMine; ++i) {
+            const uint32_t id = member + i * P::kTeam, key = id / P::kChunks, at = id % P::kChunks;
+            store_chunk<KE, C>(keys + key * P::kKeyRow + at * 8 * sizeof(KE), raw[i]);
+            if constexpr (P::kCodes)
+                if (at == 0) {
+                    const float step = __builtin_bit_cast(float, raw[i].head << 16);
+                    key_step[key] = step;
+                    key_low[key] = __builtin_fmaf(-16.f, step, __builtin_bit_cast(float, raw[i].head & 0xffff0000u));
+                }
+        }
+    };
+    auto put_values = [&](const Chunk8<C>* raw, bool look) -> bool {
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < P::kMine; ++i) {
+            const uint32_t id = member + i * P::kTeam, key = id / P::kChunks, at = id % P::kChunks;
+            store_chunk<VE, C>(values + key * P::kValueRow + at * 8 * sizeof(VE), raw[i]);
+            if constexpr (P::kCodes) {
+                if (at == 0) {
+                    const float step = __builtin_bit_cast(float, raw[i].head << 16);
+                    value_step[key] = step;
+                    value_low[key] = __builtin_fmaf(8.f, step, __builtin_bit_cast(float, raw[i].head & 0xffff0000u));
+                }
+            } else if (look) {
+                bad |= any_bad(raw[i]);
+            }
+        }
+        return bad;
+    };
+
+    Acc out[kOut] = {};
+    float top = -__builtin_inff(), sum = 0.f, low_sum = 0.f;                // of this lane's row (sums: its half of the positions); top times scale
+    const uint32_t team = FEW ? wave : 0;
+    uint32_t at = w.lo + team * P::kKeys;
+    int32_t entry = look_up(at);
+    Spot spot = spot_of(at, entry);
+    uint64_t here = __ballot(spot.here);
+    if constexpr (P::kAhead) {
+        load(k_cache, spot.offset, raw_k);
+        load(v_cache, spot.offset, raw_v);
+        entry = look_up(at + P::kStep);
+    }
+    for (; at < w.hi; at += P::kStep) {
+        // positions of the tile that some row of the workgroup's does not see
+        const uint32_t end = at + P::kKeys;
+        const uint64_t now = here;
+        constexpr uint64_t kAll = P::kKeys == 64 ? ~0ull : (1ull << P::kKeys) - 1;
+        const bool holes = (now & kAll) != kAll;
+        const uint32_t tile_lowest = w.cached + fdiv(w.row0, p.group_div);
+        const bool look = holes || end > tile_lowest + 1 || (p.window && at + p.window <= w.cached + fdiv(w.row0 + kTileRows < w.rows ? w.row0 + kTileRows - 1 : w.rows - 1, p.group_div));
+        bool bad;
+        team_sync<FEW>();                                                   // the tile before has been used
+        if constexpr (P::kAhead) {
+            put_keys(raw_k);
+            bad = put_values(raw_v, look);
+            if (at + P::kStep < w.hi) {
+                spot = spot_of(at + P::kStep, entry);
+                here = __ballot(spot.here);
+                load(k_cache, spot.offset, raw_k);
+                load(v_cache, spot.offset, raw_v);
+                entry = look_up(at + 2 * P::kStep);
+            }
+        } else {
+            load(k_cache, spot.offset, raw_k);
+            put_keys(raw_k);
+            load(v_cache, spot.offset, raw_k);
+            bad = put_values(raw_k, look);
+            if (at + P::kStep < w.hi) {
+                spot = spot_of(at + P::kStep, look_up(at + P::kStep));
+                here = __ballot(spot.here);
+            }
+        }
+        if constexpr (FEW) {
+            bad = __ballot(bad) != 0;
+            team_sync<FEW>();
+        } else if (look) {
+            bad = __syncthreads_or(bad);
+        } else {
+            __syncthreads();
+        }
+        if (idle || at > highest || (p.window && (uint64_t)end + p.window <= (uint64_t)lowest + 1)) continue;       // nothing that this wavefront's rows see
+
+        Acc score[kBlocks] = {};
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) {
+            const char* from = keys + (b * 32 + column) * P::kKeyRow + half * 16;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) Fragment<KE>::mul(*reinterpret_cast<const KFrag*>(from + i * Fragment<KE>::kDims * sizeof(KE)), query[i], score[b]);
+        }
+        // register i of block b is position 32 b + 8 (i / 4) + 4 half + i % 4
+        if constexpr (P::kCodes) {
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float4 step = *reinterpret_cast<const float4*>(key_step + b * 32 + j * 8 + half * 4), low = *reinterpret_cast<const float4*>(key_low + b * 32 + j * 8 + half * 4);
+                    const float steps[4] = {step.x, step.y, step.z, step.w}, lows[4] = {low.x, low.y, low.z, low.w};
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) score[b][4 * j + c] = __builtin_fmaf(score[b][4 * j + c], steps[c], lows[c] * query_sum);
+                }
+        }
+        const bool masked = holes || end > lowest + 1 || (p.window && at + p.window <= highest);
+        uint32_t seen = ~0u;                                                // bit 16 b + i
+        if (masked) {
+            seen = 0;
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const uint32_t in_tile = b * 32 + 8 * (i / 4) + 4 * half + i % 4, key = at + in_tile;
+                    const bool sees = key <= position && (!p.window || position - key < p.window) && (now >> in_tile & 1);
+                    score[b][i] = sees ? score[b][i] : -__builtin_inff();
+                    seen |= (sees && score[b][i] != -__builtin_inff() ? 1u : 0u) << (16 * b + i);
+                }
+        }
+        float most = -__builtin_inff();
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) most = __builtin_fmaxf(most, score[b][i]);
+        most = max_of_row(most) * scale;
+        if (__ballot(most > top)) {
+            const float higher = __builtin_fmaxf(top, most), factor = higher == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(top - higher);
+            top = higher;
+            sum *= factor;
+            low_sum *= factor;
+#pragma unroll
+            for (int d = 0; d < kOut; ++d) out[d] *= factor;
+        }
+        const float base = top == -__builtin_inff() ? 0.f : top;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                score[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[b][i], scale, -base));
+                sum += score[b][i];
+            }
+        if constexpr (P::kCodes) {
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float4 step = *reinterpret_cast<const float4*>(value_step + b * 32 + j * 8 + half * 4), low = *reinterpret_cast<const float4*>(value_low + b * 32 + j * 8 + half * 4);
+                    const float steps[4] = {step.x, step.y, step.z, step.w}, lows[4] = {low.x, low.y, low.z, low.w};
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const bool sees = !masked || (seen >> (16 * b + 4 * j + c) & 1);    // not seen: 0, whatever the record says
+                        low_sum = sees ? __builtin_fmaf(score[b][4 * j + c], lows[c], low_sum) : low_sum;
+                        score[b][4 * j + c] = sees ? score[b][4 * j + c] * steps[c] : 0.f;
+                    }
+                }
+        }
+        // O^T += V^T P^T, 16 positions at a time (32 bits: eight)
+        constexpr int kParts = P::kKeys / Fragment<VE>::kDims, kEach = 16 / (int)sizeof(VE);
+        VFrag weight[kParts];
+#pragma unroll
+        for (int k = 0; k < kParts; ++k)
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) weight[k][e] = (VE)score[k * kEach / 16][k * kEach % 16 + e];
+        if constexpr (P::kCodes) {
+            typedef __bf16 Two __attribute__((ext_vector_type(2)));
+            const Two back = {(__bf16)-24.f, (__bf16)-24.f};
+#pragma unroll
+            for (int k = 0; k < kParts; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) low_sum = __builtin_amdgcn_fdot2_f32_bf16(Two{weight[k][2 * e], weight[k][2 * e + 1]}, back, low_sum, false);
+        }
+        auto value = [&](int k, int d) -> VFrag {
+            if constexpr (sizeof(VE) == 4) {
+                VFrag r;
+                const char* from = values + (k * 8 + half * 4) * P::kValueRow + (d * 32 + column) * 4;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) r[e] = *reinterpret_cast<const float*>(from + e * P::kValueRow);
+                return r;
+            } else {
+                // four rows of 16 elements for each 16 lanes, which get a column of them each
+                const char* from = values + (k * 16 + half * 4 + (lane & 15) / 4) * P::kValueRow + (d * 32 + (lane >> 4 & 1) * 16 + (lane & 3) * 4) * 2;
+                const Short4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((TTC_LDS Short4*)from), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((TTC_LDS Short4*)(from + 8 * P::kValueRow));
+                return __builtin_bit_cast(VFrag, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+        };
+        if (!P::kCodes && masked && bad) {
+            // An infinity or a NaN among the values, which zero weights would not keep from the rows that do not see it: products with what is finite, and a
+            // count of the rest for each result, by the rows that see it.
+            VFrag sees[kParts];
+#pragma unroll
+            for (int k = 0; k < kParts; ++k)
+#pragma unroll
+                for (int e = 0; e < kEach; ++e) sees[k][e] = (VE)(seen >> (k * kEach + e) & 1 ? 1.f : 0.f);
+#pragma unroll
+            for (int d = 0; d < kOut; ++d) {
+                Acc count = {};
+#pragma unroll
+                for (int k = 0; k < kParts; ++k) {
+                    VFrag v = value(k, d);
+                    const VFrag marks = Bad<VE>::marks(v);
+                    Fragment<VE>::mul(v, weight[k], out[d]);
+                    Fragment<VE>::mul(marks, sees[k], count);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int n = (int)count[i];
+                    const bool plus = n & (kMinus - 1), minus = n & (kNan - kMinus), nan = n >= kNan;
+                    out[d][i] += nan || (plus && minus) ? __builtin_nanf("") : plus ? __builtin_inff() : minus ? -__builtin_inff() : 0.f;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int d = 0; d < kOut; ++d)
+#pragma unroll
+                for (int k = 0; k < kParts; ++k) Fragment<VE>::mul(value(k, d), weight[k], out[d]);
+        }
+    }
+
+    sum = sum_of_row(sum);
+    low_sum = sum_of_row(low_sum);
+    const float v_scale = std::is_same<C, f8>::value && p.v_scale ? p.v_scale[head] : 1.f;
+    // Writes four neighbouring elements of a row's result, normalized: to the result, or to this part's place.
+    auto write = [&](uint32_t to_token, uint32_t to_head, uint32_t d, const float* x) {
+        if (d >= p.dim) return;
+        const int64_t r = (int64_t)to_token * p.q_heads + to_head;
+        const uint32_t left = p.dim - d;
+        if (w.parts > 1) {
+            float* to = p.partial + (r * p.splits + w.part) * p.dim + d;
+            if (left >= 4) { Vec<float, 4> v; narrow(x, v); store_vec<float, 4, false>(to, v); }
+            else for (uint32_t i = 0; i < left; ++i) to[i] = x[i];
+        } else {
+            T* to = static_cast<T*>(p.out) + (int64_t)to_token * p.ld_o + (int64_t)to_head * p.dim + d;
+            if (left >= 4) { Vec<T, 4> v; narrow(x, v); store_vec<T, 4, false>(to, v); }
+            else for (uint32_t i = 0; i < left; ++i) to[i] = (T)x[i];
+        }
+    };
+    auto write_lse = [&](uint32_t to_token, uint32_t to_head, float m, float l) {
+        const int64_t r = (int64_t)to_token * p.q_heads + to_head;
+        const float value = l > 0.f || l != l ? m * 0.693147180559945f + __builtin_logf(l) : -__builtin_inff();
+        if (w.parts > 1) p.partial_lse[r * p.splits + w.part] = value;
+        else if (p.lse) p.lse[r] = value;
+        if (w.part == 0 && p.parts) p.parts[r] = (int32_t)w.parts;
+    };
+    if constexpr (FEW) {
+        // the wavefronts' results to the largest of their maxima, then added up
+        __syncthreads();
+        float* merged = reinterpret_cast<float*>(lds);
+        float *tops = merged + P::kWaves * 32 * P::kMergeRow, *sums = tops + P::kWaves * 32, *lows = sums + P::kWaves * 32;
+        if (half == 0) { tops[wave * 32 + column] = top; sums[wave * 32 + column] = sum; lows[wave * 32 + column] = low_sum; }
+        if (own < w.rows) {
+#pragma unroll
+            for (int d = 0; d < kOut; ++d)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    *reinterpret_cast<float4*>(merged + (wave * 32 + column) * P::kMergeRow + d * 32 + j * 8 + half * 4) =
+                        make_float4(out[d][4 * j], out[d][4 * j + 1], out[d][4 * j + 2], out[d][4 * j + 3]);
+        }
+        __syncthreads();
+        const uint32_t rows = w.rows - w.row0 < 32 ? w.rows - w.row0 : 32;
+        for (uint32_t i = threadIdx.x; i < rows * (DP / 4); i += P::kThreads) {
+            const uint32_t r = i / (DP / 4), d = i % (DP / 4) * 4;
+            float m = -__builtin_inff(), l = 0.f, low = 0.f, x[4] = {};
+#pragma unroll
+            for (int k = 0; k < P::kWaves; ++k) m = __builtin_fmaxf(m, tops[k * 32 + r]);
+#pragma unroll
+            for (int k = 0; k < P::kWaves; ++k) {
+                const float t = tops[k * 32 + r], factor = t == -__builtin_inff() ? (sums[k * 32 + r] != sums[k * 32 + r] ? 1.f : 0.f) : __builtin_amdgcn_exp2f(t - m);
+                const float4 v = *reinterpret_cast<const float4*>(merged + (k * 32 + r) * P::kMergeRow + d);
+                if (factor == 0.f) continue;
+                l = __builtin_fmaf(sums[k * 32 + r], factor, l);
+                low = __builtin_fmaf(lows[k * 32 + r], factor, low);
+                x[0] = __builtin_fmaf(v.x, factor, x[0]); x[1] = __builtin_fmaf(v.y, factor, x[1]);
+                x[2] = __builtin_fmaf(v.z, factor, x[2]); x[3] = __builtin_fmaf(v.w, factor, x[3]);
+            }
+            const uint32_t in = fdiv(w.row0 + r, p.group_div), h = head * p.group + (w.row0 + r - in * p.group);
+            const float inverse = l == 0.f ? 0.f : v_scale / l;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = (x[j] + low) * inverse;
+            write(w.first_token + in, h, d, x);
+            if (d == 0) write_lse(w.first_token + in, h, m, l);
+        }
+    } else {
+        if (own >= w.rows) return;
+        const float inverse = sum == 0.f ? 0.f : v_scale / sum;
+#pragma unroll
+        for (int d = 0; d < kOut; ++d)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float x[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) x[c] = (out[d][4 * j + c] + low_sum) * inverse;
+                write(token, q_head, d * 32 + j * 8 + half * 4, x);
+            }
+        if (half == 0) write_lse(token, q_head, top, sum);
+    }
+}
+
+template <typename T, typename C, int DP> AttendKernel kernel_of(bool few)
+{
+    if (few) return {reinterpret_cast<const void*>(&attend_kernel<T, C, DP, true>), Plan<T, C, DP, true>::kThreads, Plan<T, C, DP, true>::kLds};
+    return {reinterpret_cast<const void*>(&attend_kernel<T, C, DP, false>), Plan<T, C, DP, false>::kThreads, Plan<T, C, DP, false>::kLds};
+}
+template <typename T, typename C> AttendKernel kernel_of(int dim, bool few)
+{
+    return dim <= 64 ? kernel_of<T, C, 64>(few) : dim <= 96 ? kernel_of<T, C, 96>(few) : dim <= 128 ? kernel_of<T, C, 128>(few)
+         : dim <= 192 ? kernel_of<T, C, 192>(few) : kernel_of<T, C, 256>(few);
+}
+template <typename T> AttendKernel kernel_of(int cache_dtype, int dim, bool few)
+{
+    return cache_dtype == TTC_F8 ? kernel_of<T, f8>(dim, few) : cache_dtype == TTC_Q4 ? kernel_of<T, q4>(dim, few) : kernel_of<T, T>(dim, few);
+}
+
+}  // namespace attend
+}  // namespace ttc

@@ -1,0 +1,8 @@
+// Attention over pages: queries of float (see ttc_attend.h).
+#include "ttc_attend.h"
+
+namespace ttc {
+
+AttendKernel attend_kernel_f32(int cache_dtype, int dim, bool few) { return attend::kernel_of<float>(cache_dtype, dim, few); }
+
+}  // namespace ttc

@@ -35,6 +35,20 @@ HeadsShape cut_heads(HeadsArgs& a)
     return s;
 }
 
+AttendShape attend_shape(int64_t requests, int64_t tokens, int64_t heads, int64_t group, int64_t longest)
+{
+    AttendShape s = {};
+    const int64_t rows = tokens * group;
+    s.few = rows <= (int64_t)kTileFew * 3 / 2 * requests;
+    s.tile = s.few ? kTileFew : kTileMany;
+    // request r's tiles are numbered from starts[r] * group / tile + r on: always enough, and found without a sum over the requests
+    s.slots = (uint32_t)(rows / s.tile + requests);
+    // where tiles alone do not fill the device, several workgroups share a tile's positions, 128 of them at least
+    const int64_t groups = std::max<int64_t>((int64_t)s.slots * heads, 1), wanted = s.few ? 4096 : 1024;
+    s.splits = (uint32_t)std::min<int64_t>({std::max<int64_t>(wanted / groups, 1), (longest + 127) / 128 + (longest < 1), kAttendMaxSplits});
+    return s;
+}
+
 namespace {
 
 constexpr int64_t kGradPartials = kHeadsGroups;
@@ -124,6 +138,21 @@ HeadsArgs heads_args(const ttc_heads_s* h, int64_t tokens)
 
 // Tokens times groups of heads are counted in 32 bits.
 bool countable(const ttc_heads_s* h, int64_t tokens) { return tokens <= INT32_MAX && (__int128)tokens * (h->q_heads + 2 * h->kv_heads) <= INT32_MAX; }
+
+// Rows and tiles are counted in 32 bits, and so is a row of the table.
+bool attend_sizes(const ttc_attend_s* a, int64_t requests, int64_t tokens, int64_t ld_table)
+{
+    return requests <= INT32_MAX / 4 && tokens <= INT32_MAX / 4 && (__int128)tokens * a->q_heads <= INT32_MAX / 4 &&
+           (__int128)(requests + tokens * a->q_heads) * a->heads <= INT32_MAX && ld_table <= (int64_t)1 << 40;
+}
+
+int64_t longest_context(const ttc_attend_s* a, int64_t ld_table)
+{
+    int64_t n;
+    if (__builtin_mul_overflow(ld_table, a->page, &n)) n = INT32_MAX;
+    n = std::min<int64_t>(n, INT32_MAX);
+    return a->window ? std::min<int64_t>(n, a->window + kTileMany) : n;
+}
 
 // An angle as a fraction of a turn in units of 2^-64, whole turns dropped.
 uint64_t turn_of(double angle)
@@ -276,6 +305,86 @@ int ttc_pages_append(ttc_pages_t pages, ttc_heads_t heads, int64_t tokens, const
     a.page = pages->page_div;
     a.cache_dtype = pages->cache_dtype;
     return launch_heads(a, stream);
+}
+
+ttc_attend_t ttc_attend_create(ttc_pages_t pages, int64_t q_heads, double scale, int64_t window)
+{
+    int st = TTC_OK;
+    if (!pages) st = TTC_ERR_NULL_POINTER;
+    else if (pages->dim > TTC_ATTEND_MAX_DIM || q_heads < 1 || q_heads % pages->heads || window < 0 || !std::isfinite((float)(scale * 1.4426950408889634)))
+        st = TTC_ERR_INVALID_VALUE;
+    else if (q_heads > (int64_t)1 << 20 || pages->heads > 65535) st = TTC_ERR_OVERFLOW;
+    ttc_attend_s* a = st == TTC_OK ? new (std::nothrow) ttc_attend_s : nullptr;
+    if (st == TTC_OK && !a) st = TTC_ERR_ALLOC;
+    if (a)
+        *a = {pages->dtype, pages->cache_dtype, q_heads, pages->heads, pages->dim, pages->page, pages->pages, pages->vec, pages->span,
+              pages->stride_head, pages->stride_slot, pages->stride_page, (float)(scale * 1.4426950408889634), std::min<int64_t>(window, INT32_MAX), pages->page_div};
+    set_last_status(st);
+    return a;
+}
+
+int ttc_attend_destroy(ttc_attend_t attend)
+{
+    delete attend;
+    return TTC_OK;
+}
+
+int64_t ttc_attend_workspace(ttc_attend_t attend, int64_t requests, int64_t tokens, int64_t ld_table)
+{
+    if (!attend) return -TTC_ERR_NULL_POINTER;
+    if (requests < 0 || tokens < 0 || ld_table < 0) return -TTC_ERR_INVALID_VALUE;
+    if (!attend_sizes(attend, requests, tokens, ld_table)) return -TTC_ERR_OVERFLOW;
+    if (requests == 0 || tokens == 0) return 0;
+    const AttendShape s = attend_shape(requests, tokens, attend->heads, attend->q_heads / attend->heads, longest_context(attend, ld_table));
+    const int64_t rows = tokens * attend->q_heads;
+    return s.splits > 1 ? rows * s.splits * (attend->dim + 1) * 4 + rows * 4 : 0;
+}
+
+int ttc_attend_pages(ttc_attend_t attend, int64_t requests, int64_t tokens, const void* q, int64_t ldq, const int32_t* starts, const int32_t* cached,
+                     const int32_t* table, int64_t ld_table, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                     void* out, int64_t ldo, float* lse, void* workspace, void* stream)
+{
+    const int64_t work = ttc_attend_workspace(attend, requests, tokens, ld_table);
+    if (work < 0) return (int)-work;
+    const int64_t row = attend->q_heads * attend->dim;
+    if (ldq < row || ldo < row || ((k_scale || v_scale) && attend->cache_dtype != TTC_F8)) return TTC_ERR_INVALID_VALUE;
+    if (requests == 0 || tokens == 0) return TTC_OK;
+    if (!q || !starts || !cached || (ld_table && !table) || !k_cache || !v_cache || !out || (work && !workspace)) return TTC_ERR_NULL_POINTER;
+    const int eb = elem_bytes(attend->dtype), cb = elem_bytes(attend->cache_dtype);
+    uint64_t table_bytes;
+    if (!span_bytes(requests, ld_table, ld_table, 4, &table_bytes)) return TTC_ERR_OVERFLOW;
+    Rows rows[] = {{q, ldq, row, false, -1, 0}, {out, ldo, row, true, -1, 0}};
+    int st = check_rows(rows, tokens, eb);
+    const uint64_t bc = (uint64_t)attend->span * cb, bs = 4 * (uint64_t)attend->heads;
+    if (st == TTC_OK)
+        st = check_beside(rows, {Beside{starts, 4 * (uint64_t)requests + 4, 4, false}, {cached, 4 * (uint64_t)requests, 4, false}, {table, table_bytes, 4, false},
+                                 {k_cache, bc, cb, false}, {v_cache, bc, cb, false}, {k_scale, bs, 4, false}, {v_scale, bs, 4, false},
+                                 {lse, 4 * (uint64_t)(tokens * attend->q_heads), 4, true}, {work ? workspace : nullptr, (uint64_t)work, 16, true}});
+    if (st != TTC_OK) return st;
+    const int64_t group = attend->q_heads / attend->heads;
+    const AttendShape s = attend_shape(requests, tokens, attend->heads, group, longest_context(attend, ld_table));
+    AttendArgs a = {};
+    a.q = q; a.k_cache = k_cache; a.v_cache = v_cache; a.out = out; a.lse = lse;
+    if (work) {
+        const int64_t n = tokens * attend->q_heads;
+        a.partial = static_cast<float*>(workspace);
+        a.partial_lse = a.partial + n * s.splits * attend->dim;
+        a.parts = reinterpret_cast<int32_t*>(a.partial_lse + n * s.splits);
+    }
+    a.k_scale = k_scale; a.v_scale = v_scale;
+    a.starts = starts; a.cached = cached; a.table = table;
+    a.ld_q = ldq; a.ld_o = ldo; a.ld_table = ld_table;
+    a.stride_head = attend->stride_head; a.stride_slot = attend->stride_slot; a.stride_page = attend->stride_page;
+    a.tokens = (uint32_t)tokens; a.requests = (uint32_t)requests;
+    a.q_heads = (uint32_t)attend->q_heads; a.heads = (uint32_t)attend->heads; a.group = (uint32_t)group;
+    a.dim = (uint32_t)attend->dim; a.pages = (uint32_t)attend->pages;
+    a.splits = s.splits; a.slots_of_tiles = s.slots;
+    a.window = (uint32_t)attend->window;
+    a.page = attend->page_div;
+    a.group_div = make_fastdiv((uint32_t)group);
+    a.scale = attend->scale;
+    a.dtype = attend->dtype; a.cache_dtype = attend->cache_dtype;
+    return launch_attend(a, s, stream);
 }
 
 }  // extern "C"

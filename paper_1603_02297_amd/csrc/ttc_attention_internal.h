@@ -13,6 +13,15 @@ struct ttc_heads_s {
     uint64_t turns[TTC_HEADS_MAX_ROTATED / 2];         // angles in units of 2^-64 of a turn: products with a position wrap at whole turns
 };
 
+struct ttc_attend_s {
+    int      dtype, cache_dtype;
+    int64_t  q_heads, heads, dim, page, pages, vec, span;
+    int64_t  stride_head, stride_slot, stride_page;    // as of the cache
+    float    scale;
+    int64_t  window;
+    ttc::FastDiv page_div;
+};
+
 namespace ttc {
 
 constexpr int kHeadsThreads = 256;
@@ -51,5 +60,42 @@ struct HeadsShape {
     uint32_t splits;
 };
 HeadsShape cut_heads(HeadsArgs& a);          // sets what the cut says of a, too
+
+// Attention.  The rows of a request are its new tokens' query heads that share a head of the cache, token by token; a workgroup has `tile` rows of them
+// and a part of the positions that they see.
+struct AttendArgs {
+    const void    *q, *k_cache, *v_cache;
+    void          *out;
+    float         *lse, *partial, *partial_lse;        // partial results: [row][split][dim], [row][split], of row = token * q_heads + head
+    int32_t       *parts;                              // [row]: how many parts it has
+    const float   *k_scale, *v_scale;
+    const int32_t *starts, *cached, *table;
+    int64_t        ld_q, ld_o, ld_table;
+    int64_t        stride_head, stride_slot, stride_page;
+    uint32_t       tokens, requests, q_heads, heads, group, dim, pages, splits, slots_of_tiles;
+    uint32_t       window;                             // 0: none
+    FastDiv        page, group_div;
+    float          scale;                              // with log2(e)
+    int32_t        dtype, cache_dtype;
+};
+
+constexpr int kTileFew = 32, kTileMany = 128;          // rows of a workgroup: one wavefront's, its four each with other positions; or four wavefronts', with the same
+constexpr int kAttendMaxSplits = 32;
+
+struct AttendShape {
+    bool     few;
+    uint32_t tile, slots, splits;          // rows of a tile, tiles at most, parts of the positions at most
+};
+AttendShape attend_shape(int64_t requests, int64_t tokens, int64_t heads, int64_t group, int64_t longest);
+
+int launch_attend(const AttendArgs& a, const AttendShape& s, void* stream);
+// The kernel of a type, and what it needs; one file each.
+struct AttendKernel {
+    const void* fn;
+    int         threads, lds;
+};
+AttendKernel attend_kernel_f32(int cache_dtype, int dim, bool few);
+AttendKernel attend_kernel_bf16(int cache_dtype, int dim, bool few);
+AttendKernel attend_kernel_f16(int cache_dtype, int dim, bool few);
 
 }  // namespace ttc

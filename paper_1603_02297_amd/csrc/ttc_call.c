@@ -59,7 +59,7 @@ static PyObject* bind(PyObject* self, PyObject* const* args, Py_ssize_t nargs)
    of eleven that has nothing to move takes 1.4 us through ctypes and 0.2 us here. */
 #define MOVE_ARGS 21
 typedef uint64_t U;
-#define MOVES 10
+#define MOVES 11
 static struct { void* entry; PyObject *slow, *fail; } moves[MOVES];
 
 static PyObject* move(int which, int count, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames)
@@ -87,6 +87,7 @@ static PyObject* move(int which, int count, PyObject* const* args, Py_ssize_t na
     case 12: status = ((int (*)(U, U, U, U, U, U, U, U, U, U, U, U))f)(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], p[10], p[11]); break;
     case 14: status = ((int (*)(U, U, U, U, U, U, U, U, U, U, U, U, U, U))f)(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], p[10], p[11], p[12], p[13]); break;
     case 16: status = ((int (*)(U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U))f)(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], p[10], p[11], p[12], p[13], p[14], p[15]); break;
+    case 18: status = ((int (*)(U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U))f)(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], p[10], p[11], p[12], p[13], p[14], p[15], p[16], p[17]); break;
     case 20: status = ((int (*)(U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U))f)(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], p[10], p[11], p[12], p[13], p[14], p[15], p[16], p[17], p[18], p[19]); break;
     case 21: status = ((int (*)(U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U, U))f)(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], p[10], p[11], p[12], p[13], p[14], p[15], p[16], p[17], p[18], p[19], p[20]); break;
     }
@@ -111,6 +112,7 @@ MOVE(6, pages_read, 12)
 MOVE(7, heads_rotate, 14)
 MOVE(8, heads_rotate_grad, 21)
 MOVE(9, pages_append, 20)
+MOVE(10, attend_pages, 18)
 
 /* bind_move(which, slow, fail): the Python side of one move; bind_move(which, address): the library's entry point. */
 static PyObject* bind_move(PyObject* self, PyObject* const* args, Py_ssize_t nargs)
@@ -139,7 +141,7 @@ static PyObject* bind_move(PyObject* self, PyObject* const* args, Py_ssize_t nar
 
 static PyMethodDef methods[] = {
     METHOD(route_sort), METHOD(route_gather), METHOD(route_combine), METHOD(route_combine_grad), METHOD(pages_map), METHOD(pages_write), METHOD(pages_read),
-    METHOD(heads_rotate), METHOD(heads_rotate_grad), METHOD(pages_append),
+    METHOD(heads_rotate), METHOD(heads_rotate_grad), METHOD(pages_append), METHOD(attend_pages),
     {"bind_move", (PyCFunction)(void (*)(void))bind_move, METH_FASTCALL, NULL},
     {"ttc_execute", (PyCFunction)(void (*)(void))execute, METH_FASTCALL | METH_KEYWORDS,
      "ttc_execute(plan, A, B, stream=None)\n--\n\nA, B: device addresses (tensor.data_ptr()); stream: hipStream_t as an integer or None."},
