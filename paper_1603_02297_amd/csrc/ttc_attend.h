@@ -74,6 +74,8 @@ template <typename T, typename C, int DP, bool FEW> struct Plan {
     static constexpr int  kMergeRow = DP + 4;                                // floats
     static constexpr int  kMerge = FEW ? kWaves * 32 * kMergeRow * 4 + 3 * kWaves * 32 * 4 : 0;
     static constexpr int  kLds = kTile * kTeams > kMerge ? kTile * kTeams : kMerge;
+    // workgroups that share a compute unit, and so its registers
+    static constexpr int  kResident = !kWide && DP <= 128 && 2 * kLds <= kMaxLdsBytes ? 2 : 1;
     static_assert(kKeys * kChunks % kTeam == 0 && DP % 32 == 0 && kLds <= kMaxLdsBytes, "a tile is loaded in whole chunks");
 };
 
@@ -81,26 +83,26 @@ template <typename T, typename C, int DP, bool FEW> struct Plan {
 template <typename C> struct Chunk8 { Vec<C, 8> v; };
 template <> struct Chunk8<q4> { uint32_t word, head; };
 
-template <typename C> __device__ __forceinline__ Chunk8<C> load_chunk(const char* vector, uint32_t at, uint32_t dim)
+// One load and nothing around it: joined with another path, or under a condition, the compiler would wait for each before the next (700 keys' worth of such
+// waits made a decoding step of 96 requests take 390 us instead of LATER).  Vectors shorter than a chunk (ELEMENTS) go element by element all the same.
+template <typename C, bool ELEMENTS> __device__ __forceinline__ Chunk8<C> load_chunk(const char* vector, uint32_t at, uint32_t dim)
 {
     Chunk8<C> r = {};
-    const C* p = reinterpret_cast<const C*>(vector) + at;
-    if (at + 8 <= dim) {
-        r.v = load_vec<C, 8, false>(p);
-    } else if (at < dim) {                                                  // dims that are no multiple of eight: the last chunk
-        C e[8] = {};
-        for (uint32_t i = 0; i < 8; ++i)
-            if (at + i < dim) e[i] = p[i];
-        __builtin_memcpy(&r.v, e, sizeof(r.v));
+    if constexpr (std::is_same<C, q4>::value) {
+        const uint8_t* p = reinterpret_cast<const uint8_t*>(vector);
+        r.head = load_word(p);
+        r.word = load_word(p + kRecordHead + at / 2);
+    } else {
+        const C* p = reinterpret_cast<const C*>(vector) + at;
+        if (ELEMENTS && dim < 8) {
+            C e[8] = {};
+            for (uint32_t i = 0; i < 8; ++i)
+                if (i < dim) e[i] = p[i];
+            __builtin_memcpy(&r.v, e, sizeof(r.v));
+        } else {
+            r.v = load_vec<C, 8, false>(p);
+        }
     }
-    return r;
-}
-template <> __device__ __forceinline__ Chunk8<q4> load_chunk<q4>(const char* vector, uint32_t at, uint32_t dim)
-{
-    Chunk8<q4> r = {};
-    const uint8_t* p = reinterpret_cast<const uint8_t*>(vector);
-    r.head = load_word(p);
-    if (at < dim) r.word = load_word(p + kRecordHead + at / 2);
     return r;
 }
 
@@ -176,7 +178,7 @@ __device__ __forceinline__ void widen_eight(const Vec<f8, 8>& c, Vec<_Float16, 8
 }
 
 // A chunk as the tile holds it.  16-bit caches are of the queries' type, and 8 bits widen exactly.
-template <typename E, typename C> __device__ __forceinline__ void store_chunk(char* lds, const Chunk8<C>& c)
+template <typename E, bool WHOLE, typename C> __device__ __forceinline__ void store_chunk(char* lds, const Chunk8<C>& c)
 {
     Vec<E, 8> r;
     if constexpr (std::is_same<C, q4>::value) {
@@ -192,12 +194,19 @@ template <typename E, typename C> __device__ __forceinline__ void store_chunk(ch
     } else {
         widen_eight(c.v, r);
     }
-    typedef uint32_t Word4 __attribute__((ext_vector_type(4)));
+    if constexpr (WHOLE) {
+        typedef uint32_t Word4 __attribute__((ext_vector_type(4)));
 #pragma unroll
-    for (int i = 0; i < Vec<E, 8>::kWords / 4; ++i) {
-        Word4 w;
-        __builtin_memcpy(&w, r.w + 4 * i, 16);
-        reinterpret_cast<Word4*>(lds)[i] = w;
+        for (int i = 0; i < Vec<E, 8>::kWords / 4; ++i) {
+            Word4 w;
+            __builtin_memcpy(&w, r.w + 4 * i, 16);
+            reinterpret_cast<Word4*>(lds)[i] = w;
+        }
+    } else {                                // moved back, to any element
+        E e[8];
+        __builtin_memcpy(e, r.w, sizeof(e));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) reinterpret_cast<E*>(lds)[i] = e[i];
     }
 }
 
@@ -322,7 +331,7 @@ template <> struct Bad<float> {
 };
 
 template <typename T, typename C, int DP, bool FEW>
-__global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), 1) void attend_kernel(AttendArgs p)
+__global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FEW>::kResident)) void attend_kernel(AttendArgs p)
 {
     typedef Plan<T, C, DP, FEW> P;
     typedef typename P::K KE;
@@ -357,14 +366,24 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), 1) void attend_ker
         const T* from = static_cast<const T*>(p.q) + (int64_t)token * p.ld_q + (int64_t)q_head * p.dim;
         constexpr int E = 16 / (int)sizeof(T);
         const KFrag none = {};
+        if (p.dim % E == 0) {
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            const uint32_t at = i * Fragment<KE>::kDims + half * E;
-            query[i] = none;
-            if (at + E <= p.dim) query[i] = __builtin_bit_cast(KFrag, load_vec<T, E, false>(from + at));
-            else
+            for (int i = 0; i < kSteps; ++i) {
+                const uint32_t at = i * Fragment<KE>::kDims + half * E;
+                query[i] = __builtin_bit_cast(KFrag, load_vec<T, E, false>(from + (at < p.dim ? at : 0)));
+            }
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i)
+                if (i * Fragment<KE>::kDims + half * E >= p.dim) query[i] = none;
+        } else {
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const uint32_t at = i * Fragment<KE>::kDims + half * E;
+                query[i] = none;
+#pragma unroll
                 for (int j = 0; j < E; ++j)
                     if (at + j < p.dim) query[i][j] = from[at + j];
+            }
         }
 #pragma unroll
         for (int i = 0; i < kSteps; ++i)
@@ -394,50 +413,75 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), 1) void attend_ker
     auto spot_of = [&](uint32_t at, int32_t entry) -> Spot {
         const uint32_t key = at + (lane & (P::kKeys - 1)), inside = key - fdiv(key, p.page) * p.page.div;
         const bool here = (uint32_t)entry < p.pages;
-        return {here ? ((int64_t)entry * p.stride_page + (int64_t)inside * p.stride_slot) * (int64_t)sizeof(C) : -1, here};
+        // not there: the first slot of the cache, whose values become 0 and whose scores are left out
+        return {here ? ((int64_t)entry * p.stride_page + (int64_t)inside * p.stride_slot) * (int64_t)sizeof(C) : 0, here};
     };
+    // A thread's chunks of a tile.  The last one of a vector is moved back to end with it, and those behind it are that one again.
+    const bool whole = p.dim % 8 == 0;
+    const uint32_t last_chunk = p.dim < 8 ? 0 : p.dim - 8;
+    uint32_t chunk_at[P::kMine];
+#pragma unroll
+    for (int i = 0; i < P::kMine; ++i) {
+        const uint32_t at = (member + i * P::kTeam) % P::kChunks * 8;
+        chunk_at[i] = at < last_chunk ? at : last_chunk;
+    }
+    auto key_of = [&](int i) { return (member + i * P::kTeam) / P::kChunks; };
     Chunk8<C> raw_k[P::kMine], raw_v[P::kAhead ? P::kMine : 1];
     auto load = [&](const char* cache, int64_t offset, Chunk8<C>* raw) {
 #pragma unroll
         for (int i = 0; i < P::kMine; ++i) {
-            const uint32_t id = member + i * P::kTeam, key = id / P::kChunks, at = id % P::kChunks * 8;
-            const uint32_t low = __shfl((uint32_t)offset, key), high = __shfl((uint32_t)(offset >> 32), key);
-            const int64_t place = (int64_t)((uint64_t)high << 32 | low);
-            raw[i] = {};
-            if (place >= 0) raw[i] = load_chunk<C>(cache + place, at, p.dim);
+            const uint32_t low = __shfl((uint32_t)offset, key_of(i)), high = __shfl((uint32_t)(offset >> 32), key_of(i));
+            raw[i] = load_chunk<C, DP == 32>(cache + (int64_t)((uint64_t)high << 32 | low), chunk_at[i], p.dim);
         }
     };
     auto put_keys = [&](const Chunk8<C>* raw) {
+        auto all = [&](auto is_whole) {
 #pragma unroll
-        for (int i = 0; i < P::kMine; ++i) {
-            const uint32_t id = member + i * P::kTeam, key = id / P::kChunks, at = id % P::kChunks;
-            store_chunk<KE, C>(keys + key * P::kKeyRow + at * 8 * sizeof(KE), raw[i]);
-            if constexpr (P::kCodes)
-                if (at == 0) {
+            for (int i = 0; i < P::kMine; ++i) store_chunk<KE, decltype(is_whole)::value>(keys + key_of(i) * P::kKeyRow + chunk_at[i] * sizeof(KE), raw[i]);
+        };
+        if (whole) all(std::true_type{}); else all(std::false_type{});
+        if constexpr (P::kCodes) {
+#pragma unroll
+            for (int i = 0; i < P::kMine; ++i)
+                if (chunk_at[i] == 0) {
                     const float step = __builtin_bit_cast(float, raw[i].head << 16);
-                    key_step[key] = step;
-                    key_low[key] = __builtin_fmaf(-16.f, step, __builtin_bit_cast(float, raw[i].head & 0xffff0000u));
+                    key_step[key_of(i)] = step;
+                    key_low[key_of(i)] = __builtin_fmaf(-16.f, step, __builtin_bit_cast(float, raw[i].head & 0xffff0000u));
                 }
         }
     };
-    auto put_values = [&](const Chunk8<C>* raw, bool look) -> bool {
+    auto put_values = [&](Chunk8<C>* raw, uint64_t there, bool holes, bool look) -> bool {
         bool bad = false;
+        if (holes) {
 #pragma unroll
-        for (int i = 0; i < P::kMine; ++i) {
-            const uint32_t id = member + i * P::kTeam, key = id / P::kChunks, at = id % P::kChunks;
-            store_chunk<VE, C>(values + key * P::kValueRow + at * 8 * sizeof(VE), raw[i]);
-            if constexpr (P::kCodes) {
-                if (at == 0) {
+            for (int i = 0; i < P::kMine; ++i)
+                if (!(there >> key_of(i) & 1)) raw[i] = {};
+        }
+        if (!P::kCodes && look) {
+#pragma unroll
+            for (int i = 0; i < P::kMine; ++i) bad |= any_bad(raw[i]);
+        }
+        auto all = [&](auto is_whole) {
+#pragma unroll
+            for (int i = 0; i < P::kMine; ++i) store_chunk<VE, decltype(is_whole)::value>(values + key_of(i) * P::kValueRow + chunk_at[i] * sizeof(VE), raw[i]);
+        };
+        if (whole) all(std::true_type{}); else all(std::false_type{});
+        if constexpr (P::kCodes) {
+#pragma unroll
+            for (int i = 0; i < P::kMine; ++i)
+                if (chunk_at[i] == 0) {
                     const float step = __builtin_bit_cast(float, raw[i].head << 16);
-                    value_step[key] = step;
-                    value_low[key] = __builtin_fmaf(8.f, step, __builtin_bit_cast(float, raw[i].head & 0xffff0000u));
+                    value_step[key_of(i)] = step;
+                    value_low[key_of(i)] = __builtin_fmaf(8.f, step, __builtin_bit_cast(float, raw[i].head & 0xffff0000u));
                 }
-            } else if (look) {
-                bad |= any_bad(raw[i]);
-            }
         }
         return bad;
     };
+    // what lies behind the vectors' ends in the tile's rows: 0, once
+    if (p.dim < DP) {
+        for (uint32_t key = member / 32; key < P::kKeys; key += P::kTeam / 32)
+            for (uint32_t d = p.dim + member % 32; d < DP; d += 32) reinterpret_cast<KE*>(keys + key * P::kKeyRow)[d] = (KE)0.f;
+    }
 
     Acc out[kOut] = {};
     float top = -__builtin_inff(), sum = 0.f, low_sum = 0.f;                // of this lane's row (sums: its half of the positions); top times scale
@@ -463,7 +507,7 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), 1) void attend_ker
         team_sync<FEW>();                                                   // the tile before has been used
         if constexpr (P::kAhead) {
             put_keys(raw_k);
-            bad = put_values(raw_v, look);
+            bad = put_values(raw_v, now, holes, look);
             if (at + P::kStep < w.hi) {
                 spot = spot_of(at + P::kStep, entry);
                 here = __ballot(spot.here);
@@ -475,7 +519,7 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), 1) void attend_ker
             load(k_cache, spot.offset, raw_k);
             put_keys(raw_k);
             load(v_cache, spot.offset, raw_k);
-            bad = put_values(raw_k, look);
+            bad = put_values(raw_k, now, holes, look);
             if (at + P::kStep < w.hi) {
                 spot = spot_of(at + P::kStep, look_up(at + P::kStep));
                 here = __ballot(spot.here);
@@ -511,18 +555,20 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), 1) void attend_ker
                 }
         }
         const bool masked = holes || end > lowest + 1 || (p.window && at + p.window <= highest);
-        uint32_t seen = ~0u;                                                // bit 16 b + i
+        uint32_t seen[kBlocks];                                             // bit 8 (i / 4) + i % 4 of block b: what register i is of
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b) seen[b] = ~0u;
         if (masked) {
-            seen = 0;
+            // positions of the tile up to the row's own, less those before its window, and those that are there
+            const uint64_t upto = position < at ? 0 : position - at >= 63 ? ~0ull : (2ull << (position - at)) - 1;
+            const uint32_t out_of = p.window && position >= p.window && position - p.window >= at ? (position - p.window - at >= 63 ? 64 : position - p.window - at + 1) : 0;
+            const uint64_t sees = upto & now & (out_of >= 64 ? 0 : ~0ull << out_of);
 #pragma unroll
-            for (int b = 0; b < kBlocks; ++b)
+            for (int b = 0; b < kBlocks; ++b) {
+                seen[b] = (uint32_t)(sees >> (32 * b)) >> (4 * half);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const uint32_t in_tile = b * 32 + 8 * (i / 4) + 4 * half + i % 4, key = at + in_tile;
-                    const bool sees = key <= position && (!p.window || position - key < p.window) && (now >> in_tile & 1);
-                    score[b][i] = sees ? score[b][i] : -__builtin_inff();
-                    seen |= (sees && score[b][i] != -__builtin_inff() ? 1u : 0u) << (16 * b + i);
-                }
+                for (int i = 0; i < 16; ++i) score[b][i] = seen[b] >> (8 * (i / 4) + i % 4) & 1 ? score[b][i] : -__builtin_inff();
+            }
         }
         float most = -__builtin_inff();
 #pragma unroll
@@ -555,7 +601,7 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), 1) void attend_ker
                     const float steps[4] = {step.x, step.y, step.z, step.w}, lows[4] = {low.x, low.y, low.z, low.w};
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const bool sees = !masked || (seen >> (16 * b + 4 * j + c) & 1);    // not seen: 0, whatever the record says
+                        const bool sees = seen[b] >> (8 * j + c) & 1;    // not seen: 0, whatever the record says
                         low_sum = sees ? __builtin_fmaf(score[b][4 * j + c], lows[c], low_sum) : low_sum;
                         score[b][4 * j + c] = sees ? score[b][4 * j + c] * steps[c] : 0.f;
                     }
@@ -593,11 +639,6 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), 1) void attend_ker
         if (!P::kCodes && masked && bad) {
             // An infinity or a NaN among the values, which zero weights would not keep from the rows that do not see it: products with what is finite, and a
             // count of the rest for each result, by the rows that see it.
-            VFrag sees[kParts];
-#pragma unroll
-            for (int k = 0; k < kParts; ++k)
-#pragma unroll
-                for (int e = 0; e < kEach; ++e) sees[k][e] = (VE)(seen >> (k * kEach + e) & 1 ? 1.f : 0.f);
 #pragma unroll
             for (int d = 0; d < kOut; ++d) {
                 Acc count = {};
@@ -606,7 +647,13 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), 1) void attend_ker
                     VFrag v = value(k, d);
                     const VFrag marks = Bad<VE>::marks(v);
                     Fragment<VE>::mul(v, weight[k], out[d]);
-                    Fragment<VE>::mul(marks, sees[k], count);
+                    VFrag sees;
+#pragma unroll
+                    for (int e = 0; e < kEach; ++e) {
+                        const int i = k * kEach % 16 + e;
+                        sees[e] = (VE)(seen[k * kEach / 16] >> (8 * (i / 4) + i % 4) & 1 ? 1.f : 0.f);
+                    }
+                    Fragment<VE>::mul(marks, sees, count);
                 }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -709,7 +756,7 @@ template <typename T, typename C, int DP> AttendKernel kernel_of(bool few)
 }
 template <typename T, typename C> AttendKernel kernel_of(int dim, bool few)
 {
-    return dim <= 64 ? kernel_of<T, C, 64>(few) : dim <= 96 ? kernel_of<T, C, 96>(few) : dim <= 128 ? kernel_of<T, C, 128>(few)
+    return dim <= 32 ? kernel_of<T, C, 32>(few) : dim <= 64 ? kernel_of<T, C, 64>(few) : dim <= 96 ? kernel_of<T, C, 96>(few) : dim <= 128 ? kernel_of<T, C, 128>(few)
          : dim <= 192 ? kernel_of<T, C, 192>(few) : kernel_of<T, C, 256>(few);
 }
 template <typename T> AttendKernel kernel_of(int cache_dtype, int dim, bool few)
