@@ -71,9 +71,12 @@ template <typename T, typename C, int DP, bool FEW> struct Plan {
     // rows in LDS end 16 and 32 bytes later than their elements, so that eight rows (four, of values) meet all banks
     static constexpr int  kKeyRow = DP * (int)sizeof(K) + 16, kValueRow = DP * (int)sizeof(V) + (kWide ? 16 : 32);
     static constexpr int  kTile = kKeys * (kKeyRow + kValueRow) + (kCodes ? 4 * kKeys * 4 : 0);
+    // The queries' fragments in LDS, the same for all wavefronts, where keys and values on their way take the registers.
+    static constexpr bool kQueriesInLds = FEW && sizeof(C) == 2;
+    static constexpr int  kQueries = kQueriesInLds ? DP / Fragment<K>::kDims * kWave * 16 : 0;
     static constexpr int  kMergeRow = DP + 4;                                // floats
     static constexpr int  kMerge = FEW ? kWaves * 32 * kMergeRow * 4 + 3 * kWaves * 32 * 4 : 0;
-    static constexpr int  kLds = kTile * kTeams > kMerge ? kTile * kTeams : kMerge;
+    static constexpr int  kLds = kTile * kTeams + kQueries > kMerge ? kTile * kTeams + kQueries : kMerge;
     // workgroups that share a compute unit, and so its registers
     static constexpr int  kResident = !kWide && DP <= 128 && 2 * kLds <= kMaxLdsBytes ? 2 : 1;
     static_assert(kKeys * kChunks % kTeam == 0 && DP % 32 == 0 && kLds <= kMaxLdsBytes, "a tile is loaded in whole chunks");
@@ -250,10 +253,11 @@ template <typename P, int TILE> __device__ __forceinline__ bool find_work(const 
         n = n - (count - 1) * step < step ? n - (count - 1) * step : step;
         if (step == 1) n = 1;
     }
+    auto cut = [&](int32_t s) { return s < 0 ? 0u : (uint32_t)s < p.tokens ? (uint32_t)s : p.tokens; };
+    lo = __builtin_amdgcn_readfirstlane(lo);            // the same for all lanes, which the compiler cannot see
+    const uint32_t begin = cut(p.starts[lo]), end = cut(p.starts[lo + 1]);
     const uint32_t base = first_slot(p, lo, TILE);
     if (slot < base) return false;
-    auto cut = [&](int32_t s) { return s < 0 ? 0u : (uint32_t)s < p.tokens ? (uint32_t)s : p.tokens; };
-    const uint32_t begin = cut(p.starts[lo]), end = cut(p.starts[lo + 1]);
     w.request = lo;
     w.first_token = begin;
     w.row0 = (slot - base) * TILE;
@@ -340,7 +344,7 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FE
     typedef typename Fragment<VE>::type VFrag;
     constexpr int kTileRows = FEW ? kTileFew : kTileMany, kBlocks = P::kKeys / 32, kSteps = DP / Fragment<KE>::kDims, kOut = DP / 32;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const uint32_t lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, half = lane >> 5, column = lane & 31;
+    const uint32_t lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), half = lane >> 5, column = lane & 31;
     const uint32_t head = blockIdx.y, slot = blockIdx.x, split = blockIdx.z;
     Work w;
     if (!find_work<P, kTileRows>(p, p.slots_of_tiles - 1 - slot, split, w)) return;        // the last tiles see most: first
@@ -358,8 +362,8 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FE
     // scores times `scale` are exponents of 2; its sign goes into the queries, so that the largest product has the largest exponent
     float scale = p.scale;
     if (std::is_same<C, f8>::value && p.k_scale) scale *= p.k_scale[head];
-    const float sign = scale < 0.f ? -1.f : scale == 0.f ? 0.f : 1.f;
-    scale = scale < 0.f ? -scale : scale == 0.f ? 1.f : scale;
+    const uint32_t keep = scale == 0.f ? 0u : ~0u, flip = scale < 0.f ? (sizeof(T) == 2 ? 0x80008000u : 0x80000000u) : 0u;
+    scale = scale == 0.f ? 1.f : __builtin_fabsf(scale);
     KFrag query[kSteps];
     float query_sum = 0.f;
     {
@@ -377,21 +381,26 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FE
                 if (i * Fragment<KE>::kDims + half * E >= p.dim) query[i] = none;
         } else {
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                const uint32_t at = i * Fragment<KE>::kDims + half * E;
-                query[i] = none;
+            for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-                for (int j = 0; j < E; ++j)
-                    if (at + j < p.dim) query[i][j] = from[at + j];
-            }
+                for (int j = 0; j < E; ++j) {
+                    const uint32_t at = i * Fragment<KE>::kDims + half * E + j;
+                    const T x = from[at < p.dim ? at : 0];
+                    query[i][j] = at < p.dim ? x : (T)0.f;
+                }
         }
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i)
+        for (int i = 0; i < kSteps; ++i) {
+            uint32_t word[4];
+            __builtin_memcpy(word, &query[i], 16);
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                if (sign != 1.f) query[i][j] = (T)((float)query[i][j] * sign);
-                if (P::kCodes) query_sum += (float)query[i][j];
+            for (int j = 0; j < 4; ++j) word[j] = (word[j] & keep) ^ flip;
+            __builtin_memcpy(&query[i], word, 16);
+            if constexpr (P::kCodes) {
+#pragma unroll
+                for (int j = 0; j < E; ++j) query_sum += (float)query[i][j];
             }
+        }
         if (P::kCodes) query_sum = sum_of_row(query_sum);
     }
 
@@ -399,7 +408,7 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FE
     char *keys = tile, *values = tile + P::kKeys * P::kKeyRow;
     float* key_step = reinterpret_cast<float*>(values + P::kKeys * P::kValueRow);           // kCodes: four arrays of kKeys
     float *key_low = key_step + P::kKeys, *value_step = key_low + P::kKeys, *value_low = value_step + P::kKeys;
-    const uint32_t member = FEW ? lane : threadIdx.x;
+    uint32_t member = FEW ? lane : threadIdx.x;
     const char* k_cache = static_cast<const char*>(p.k_cache) + (int64_t)head * p.stride_head * (int64_t)sizeof(C);
     const char* v_cache = static_cast<const char*>(p.v_cache) + (int64_t)head * p.stride_head * (int64_t)sizeof(C);
     const int32_t* table = p.table + (int64_t)w.request * p.ld_table;
@@ -419,31 +428,29 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FE
     // A thread's chunks of a tile.  The last one of a vector is moved back to end with it, and those behind it are that one again.
     const bool whole = p.dim % 8 == 0;
     const uint32_t last_chunk = p.dim < 8 ? 0 : p.dim - 8;
-    uint32_t chunk_at[P::kMine];
-#pragma unroll
-    for (int i = 0; i < P::kMine; ++i) {
+    auto chunk_of = [&](int i) {
         const uint32_t at = (member + i * P::kTeam) % P::kChunks * 8;
-        chunk_at[i] = at < last_chunk ? at : last_chunk;
-    }
+        return at < last_chunk ? at : last_chunk;
+    };
     auto key_of = [&](int i) { return (member + i * P::kTeam) / P::kChunks; };
     Chunk8<C> raw_k[P::kMine], raw_v[P::kAhead ? P::kMine : 1];
     auto load = [&](const char* cache, int64_t offset, Chunk8<C>* raw) {
 #pragma unroll
         for (int i = 0; i < P::kMine; ++i) {
             const uint32_t low = __shfl((uint32_t)offset, key_of(i)), high = __shfl((uint32_t)(offset >> 32), key_of(i));
-            raw[i] = load_chunk<C, DP == 32>(cache + (int64_t)((uint64_t)high << 32 | low), chunk_at[i], p.dim);
+            raw[i] = load_chunk<C, DP == 32>(cache + (int64_t)((uint64_t)high << 32 | low), chunk_of(i), p.dim);
         }
     };
     auto put_keys = [&](const Chunk8<C>* raw) {
         auto all = [&](auto is_whole) {
 #pragma unroll
-            for (int i = 0; i < P::kMine; ++i) store_chunk<KE, decltype(is_whole)::value>(keys + key_of(i) * P::kKeyRow + chunk_at[i] * sizeof(KE), raw[i]);
+            for (int i = 0; i < P::kMine; ++i) store_chunk<KE, decltype(is_whole)::value>(keys + key_of(i) * P::kKeyRow + chunk_of(i) * sizeof(KE), raw[i]);
         };
         if (whole) all(std::true_type{}); else all(std::false_type{});
         if constexpr (P::kCodes) {
 #pragma unroll
             for (int i = 0; i < P::kMine; ++i)
-                if (chunk_at[i] == 0) {
+                if (chunk_of(i) == 0) {
                     const float step = __builtin_bit_cast(float, raw[i].head << 16);
                     key_step[key_of(i)] = step;
                     key_low[key_of(i)] = __builtin_fmaf(-16.f, step, __builtin_bit_cast(float, raw[i].head & 0xffff0000u));
@@ -463,19 +470,31 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FE
         }
         auto all = [&](auto is_whole) {
 #pragma unroll
-            for (int i = 0; i < P::kMine; ++i) store_chunk<VE, decltype(is_whole)::value>(values + key_of(i) * P::kValueRow + chunk_at[i] * sizeof(VE), raw[i]);
+            for (int i = 0; i < P::kMine; ++i) store_chunk<VE, decltype(is_whole)::value>(values + key_of(i) * P::kValueRow + chunk_of(i) * sizeof(VE), raw[i]);
         };
         if (whole) all(std::true_type{}); else all(std::false_type{});
         if constexpr (P::kCodes) {
 #pragma unroll
             for (int i = 0; i < P::kMine; ++i)
-                if (chunk_at[i] == 0) {
+                if (chunk_of(i) == 0) {
                     const float step = __builtin_bit_cast(float, raw[i].head << 16);
                     value_step[key_of(i)] = step;
                     value_low[key_of(i)] = __builtin_fmaf(8.f, step, __builtin_bit_cast(float, raw[i].head & 0xffff0000u));
                 }
         }
         return bad;
+    };
+    char* queries = lds + P::kTile * P::kTeams + lane * 16;
+    if constexpr (P::kQueriesInLds) {
+        if (wave == 0) {
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) *reinterpret_cast<KFrag*>(queries + i * kWave * 16) = query[i];
+        }
+        __syncthreads();
+    }
+    auto query_of = [&](int i) -> KFrag {
+        if constexpr (P::kQueriesInLds) return *reinterpret_cast<const KFrag*>(queries + i * kWave * 16);
+        else return query[i];
     };
     // what lies behind the vectors' ends in the tile's rows: 0, once
     if (p.dim < DP) {
@@ -496,6 +515,7 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FE
         entry = look_up(at + P::kStep);
     }
     for (; at < w.hi; at += P::kStep) {
+        asm volatile("" : "+v"(member));    // places in the tile are found again each time: kept, they would take the registers of the loads
         // positions of the tile that some row of the workgroup's does not see
         const uint32_t end = at + P::kKeys;
         const uint64_t now = here;
@@ -540,7 +560,7 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FE
         for (int b = 0; b < kBlocks; ++b) {
             const char* from = keys + (b * 32 + column) * P::kKeyRow + half * 16;
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) Fragment<KE>::mul(*reinterpret_cast<const KFrag*>(from + i * Fragment<KE>::kDims * sizeof(KE)), query[i], score[b]);
+            for (int i = 0; i < kSteps; ++i) Fragment<KE>::mul(*reinterpret_cast<const KFrag*>(from + i * Fragment<KE>::kDims * sizeof(KE)), query_of(i), score[b]);
         }
         // register i of block b is position 32 b + 8 (i / 4) + 4 half + i % 4
         if constexpr (P::kCodes) {
