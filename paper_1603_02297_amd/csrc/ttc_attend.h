@@ -11,9 +11,13 @@
 //         positions, in LDS of its own; no barrier until they add up their results.  Bound by the cache's bytes.
 //   else  prompts: wavefronts have 32 rows each of the same 128 and share the tiles.  Bound by the matrix instructions, and the exponentials beside them.
 //
+//   OWN   FEW over narrow caches, where dim is what the kernel is compiled for: a lane has half the vector of a position of its own.  Keys are never in LDS: half a vector
+//         is what the left operand of S^T holds in a lane, in an order of the dims that the queries follow.
+//
 // A tile's loads are under way while the one before it is used, its entries of the block table one tile earlier.
 #pragma once
 
+#include <atomic>
 #include <type_traits>
 
 #include "ttc_attention_internal.h"
@@ -51,7 +55,7 @@ template <> struct Fragment<float> {
 };
 
 // T: queries and results; C: the cache; DP: dim rounded up to what the kernel is compiled for.
-template <typename T, typename C, int DP, bool FEW> struct Plan {
+template <typename T, typename C, int DP, bool FEW, bool OWN> struct Plan {
     typedef T K;                                                            // keys in LDS
     // Values in LDS, and the exponentials.  Codes of 4 bits are multiplied by exponentials times steps, of which fp16 would lose the small ones: bf16.
     typedef typename std::conditional<std::is_same<C, q4>::value && !std::is_same<T, float>::value, __bf16, T>::type V;
@@ -70,15 +74,18 @@ template <typename T, typename C, int DP, bool FEW> struct Plan {
     static constexpr bool kAhead = !(FEW && kWide && DP > 128);              // loads of the next tile under way beside the products of this one
     // rows in LDS end 16 and 32 bytes later than their elements, so that eight rows (four, of values) meet all banks
     static constexpr int  kKeyRow = DP * (int)sizeof(K) + 16, kValueRow = DP * (int)sizeof(V) + (kWide ? 16 : 32);
-    static constexpr int  kTile = kKeys * (kKeyRow + kValueRow) + (kCodes ? 4 * kKeys * 4 : 0);
+    static constexpr int  kTile = kKeys * ((OWN ? 0 : kKeyRow) + kValueRow) + (kCodes ? 4 * kKeys * 4 : 0);
     // The queries' fragments in LDS, the same for all wavefronts, where keys and values on their way take the registers.
-    static constexpr bool kQueriesInLds = FEW && sizeof(C) == 2;
+    static constexpr bool kQueriesInLds = FEW && !OWN && sizeof(C) == 2;
     static constexpr int  kQueries = kQueriesInLds ? DP / Fragment<K>::kDims * kWave * 16 : 0;
+    static constexpr int  kMergeRows = 8;                                    // of the wavefronts' results that are added up at a time
     static constexpr int  kMergeRow = DP + 4;                                // floats
-    static constexpr int  kMerge = FEW ? kWaves * 32 * kMergeRow * 4 + 3 * kWaves * 32 * 4 : 0;
+    static constexpr int  kMerge = FEW ? kWaves * kMergeRows * kMergeRow * 4 + 3 * kWaves * 32 * 4 : 0;
     static constexpr int  kLds = kTile * kTeams + kQueries > kMerge ? kTile * kTeams + kQueries : kMerge;
     // workgroups that share a compute unit, and so its registers
     static constexpr int  kResident = !kWide && DP <= 128 && 2 * kLds <= kMaxLdsBytes ? 2 : 1;
+    // OWN: the words of half a vector, a lane's
+    static constexpr int  kWords = kRecords ? DP / 16 : DP / 2 * (int)sizeof(C) / 4;
     static_assert(kKeys * kChunks % kTeam == 0 && DP % 32 == 0 && kLds <= kMaxLdsBytes, "a tile is loaded in whole chunks");
 };
 
@@ -181,7 +188,7 @@ __device__ __forceinline__ void widen_eight(const Vec<f8, 8>& c, Vec<_Float16, 8
 }
 
 // A chunk as the tile holds it.  16-bit caches are of the queries' type, and 8 bits widen exactly.
-template <typename E, bool WHOLE, typename C> __device__ __forceinline__ void store_chunk(char* lds, const Chunk8<C>& c)
+template <typename E, typename C> __device__ __forceinline__ Vec<E, 8> tile_chunk(const Chunk8<C>& c)
 {
     Vec<E, 8> r;
     if constexpr (std::is_same<C, q4>::value) {
@@ -197,6 +204,16 @@ template <typename E, bool WHOLE, typename C> __device__ __forceinline__ void st
     } else {
         widen_eight(c.v, r);
     }
+    return r;
+}
+template <typename E, typename C> __device__ __forceinline__ typename Fragment<E>::type fragment_of(const Chunk8<C>& c)
+{
+    static_assert(sizeof(E) == 2, "eight elements a fragment");
+    return __builtin_bit_cast(typename Fragment<E>::type, tile_chunk<E>(c));
+}
+template <typename E, bool WHOLE, typename C> __device__ __forceinline__ void store_chunk(char* lds, const Chunk8<C>& c)
+{
+    const Vec<E, 8> r = tile_chunk<E>(c);
     if constexpr (WHOLE) {
         typedef uint32_t Word4 __attribute__((ext_vector_type(4)));
 #pragma unroll
@@ -334,10 +351,10 @@ template <> struct Bad<float> {
     }
 };
 
-template <typename T, typename C, int DP, bool FEW>
-__global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FEW>::kResident)) void attend_kernel(AttendArgs p)
+template <typename T, typename C, int DP, bool FEW, bool OWN>
+__global__ __launch_bounds__((Plan<T, C, DP, FEW, OWN>::kThreads), (Plan<T, C, DP, FEW, OWN>::kResident)) void attend_kernel(AttendArgs p)
 {
-    typedef Plan<T, C, DP, FEW> P;
+    typedef Plan<T, C, DP, FEW, OWN> P;
     typedef typename P::K KE;
     typedef typename P::V VE;
     typedef typename Fragment<KE>::type KFrag;
@@ -373,7 +390,7 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FE
         if (p.dim % E == 0) {
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                const uint32_t at = i * Fragment<KE>::kDims + half * E;
+                const uint32_t at = OWN ? half * (DP / 2) + i * E : i * Fragment<KE>::kDims + half * E;
                 query[i] = __builtin_bit_cast(KFrag, load_vec<T, E, false>(from + (at < p.dim ? at : 0)));
             }
 #pragma unroll
@@ -405,7 +422,7 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FE
     }
 
     char* tile = lds + (FEW ? wave * P::kTile : 0);
-    char *keys = tile, *values = tile + P::kKeys * P::kKeyRow;
+    char *keys = tile, *values = tile + (OWN ? 0 : P::kKeys * P::kKeyRow);
     float* key_step = reinterpret_cast<float*>(values + P::kKeys * P::kValueRow);           // kCodes: four arrays of kKeys
     float *key_low = key_step + P::kKeys, *value_step = key_low + P::kKeys, *value_low = value_step + P::kKeys;
     uint32_t member = FEW ? lane : threadIdx.x;
@@ -433,7 +450,7 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FE
         return at < last_chunk ? at : last_chunk;
     };
     auto key_of = [&](int i) { return (member + i * P::kTeam) / P::kChunks; };
-    Chunk8<C> raw_k[P::kMine], raw_v[P::kAhead ? P::kMine : 1];
+    Chunk8<C> raw_k[OWN ? 1 : P::kMine], raw_v[P::kAhead && !OWN ? P::kMine : 1];
     auto load = [&](const char* cache, int64_t offset, Chunk8<C>* raw) {
 #pragma unroll
         for (int i = 0; i < P::kMine; ++i) {
@@ -484,6 +501,49 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FE
         }
         return bad;
     };
+    // OWN: half a vector of this lane's position
+    struct Half { uint32_t w[P::kWords], head; };
+    Half half_k, half_v;
+    auto load_half = [&](const char* cache, int64_t offset, Half& r) {
+        const char* from = cache + offset + (P::kRecords ? kRecordHead : 0) + half * (P::kWords * 4);
+        r.head = P::kRecords ? load_word(reinterpret_cast<const uint8_t*>(cache + offset)) : 0;
+#pragma unroll
+        for (int i = 0; i + 4 <= P::kWords; i += 4) {
+            const typename Bits<16>::type x = *reinterpret_cast<const typename Bits<16>::type*>(from + 4 * i);
+            __builtin_memcpy(r.w + i, &x, 16);
+        }
+        if constexpr (P::kWords % 4 != 0) {
+            const typename Bits<8>::type x = *reinterpret_cast<const typename Bits<8>::type*>(from + P::kWords / 4 * 16);
+            __builtin_memcpy(r.w + P::kWords / 4 * 4, &x, 8);
+        }
+    };
+    // its eight elements number i, as LDS and the products have them
+    auto chunk_of_half = [&](const Half& r, int i) -> Chunk8<C> {
+        Chunk8<C> c;
+        if constexpr (P::kRecords) c = {r.w[i], r.head};
+        else __builtin_memcpy(&c, r.w + i * (int)sizeof(C) * 2, sizeof(c));
+        return c;
+    };
+    auto put_half = [&](Half& r, uint64_t there, bool holes, bool look) -> bool {
+        bool bad = false;
+        if (holes && !(there >> column & 1)) r = {};
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) {
+            const Chunk8<C> c = chunk_of_half(r, i);
+            store_chunk<VE, true>(values + column * P::kValueRow + (half * (DP / 2) + 8 * i) * sizeof(VE), c);
+            if (!P::kCodes && look) bad |= any_bad(c);
+        }
+        return bad;
+    };
+    auto put_steps = [&](const Half& k, const Half& v) {
+        if (half == 0) {
+            const float ks = __builtin_bit_cast(float, k.head << 16), vs = __builtin_bit_cast(float, v.head << 16);
+            key_step[column] = ks;
+            key_low[column] = __builtin_fmaf(-16.f, ks, __builtin_bit_cast(float, k.head & 0xffff0000u));
+            value_step[column] = vs;
+            value_low[column] = __builtin_fmaf(8.f, vs, __builtin_bit_cast(float, v.head & 0xffff0000u));
+        }
+    };
     char* queries = lds + P::kTile * P::kTeams + lane * 16;
     if constexpr (P::kQueriesInLds) {
         if (wave == 0) {
@@ -497,7 +557,7 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FE
         else return query[i];
     };
     // what lies behind the vectors' ends in the tile's rows: 0, once
-    if (p.dim < DP) {
+    if (!OWN && p.dim < DP) {
         for (uint32_t key = member / 32; key < P::kKeys; key += P::kTeam / 32)
             for (uint32_t d = p.dim + member % 32; d < DP; d += 32) reinterpret_cast<KE*>(keys + key * P::kKeyRow)[d] = (KE)0.f;
     }
@@ -509,7 +569,11 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FE
     int32_t entry = look_up(at);
     Spot spot = spot_of(at, entry);
     uint64_t here = __ballot(spot.here);
-    if constexpr (P::kAhead) {
+    if constexpr (OWN) {
+        load_half(k_cache, spot.offset, half_k);
+        load_half(v_cache, spot.offset, half_v);
+        entry = look_up(at + P::kStep);
+    } else if constexpr (P::kAhead) {
         load(k_cache, spot.offset, raw_k);
         load(v_cache, spot.offset, raw_v);
         entry = look_up(at + P::kStep);
@@ -525,7 +589,19 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FE
         const bool look = holes || end > tile_lowest + 1 || (p.window && at + p.window <= w.cached + fdiv(w.row0 + kTileRows < w.rows ? w.row0 + kTileRows - 1 : w.rows - 1, p.group_div));
         bool bad;
         team_sync<FEW>();                                                   // the tile before has been used
-        if constexpr (P::kAhead) {
+        Half now_k = {};
+        if constexpr (OWN) {
+            now_k = half_k;
+            if constexpr (P::kCodes) put_steps(half_k, half_v);
+            bad = put_half(half_v, now, holes, look);
+            if (at + P::kStep < w.hi) {
+                spot = spot_of(at + P::kStep, entry);
+                here = __ballot(spot.here);
+                load_half(k_cache, spot.offset, half_k);
+                load_half(v_cache, spot.offset, half_v);
+                entry = look_up(at + 2 * P::kStep);
+            }
+        } else if constexpr (P::kAhead) {
             put_keys(raw_k);
             bad = put_values(raw_v, now, holes, look);
             if (at + P::kStep < w.hi) {
@@ -559,6 +635,11 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FE
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) {
             const char* from = keys + (b * 32 + column) * P::kKeyRow + half * 16;
+            if constexpr (OWN) {
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) Fragment<KE>::mul(fragment_of<KE>(chunk_of_half(now_k, i)), query[i], score[b]);
+                continue;
+            }
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) Fragment<KE>::mul(*reinterpret_cast<const KFrag*>(from + i * Fragment<KE>::kDims * sizeof(KE)), query_of(i), score[b]);
         }
@@ -621,9 +702,8 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FE
                     const float steps[4] = {step.x, step.y, step.z, step.w}, lows[4] = {low.x, low.y, low.z, low.w};
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const bool sees = seen[b] >> (8 * j + c) & 1;    // not seen: 0, whatever the record says
-                        low_sum = sees ? __builtin_fmaf(score[b][4 * j + c], lows[c], low_sum) : low_sum;
-                        score[b][4 * j + c] = sees ? score[b][4 * j + c] * steps[c] : 0.f;
+                        low_sum = __builtin_fmaf(score[b][4 * j + c], masked && !(seen[b] >> (8 * j + c) & 1) ? 0.f : lows[c], low_sum);
+                        score[b][4 * j + c] *= masked && !(seen[b] >> (8 * j + c) & 1) ? 0.f : steps[c];        // not seen: 0, whatever the record says
                     }
                 }
         }
@@ -719,39 +799,44 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FE
         // the wavefronts' results to the largest of their maxima, then added up
         __syncthreads();
         float* merged = reinterpret_cast<float*>(lds);
-        float *tops = merged + P::kWaves * 32 * P::kMergeRow, *sums = tops + P::kWaves * 32, *lows = sums + P::kWaves * 32;
+        float *tops = merged + P::kWaves * P::kMergeRows * P::kMergeRow, *sums = tops + P::kWaves * 32, *lows = sums + P::kWaves * 32;
         if (half == 0) { tops[wave * 32 + column] = top; sums[wave * 32 + column] = sum; lows[wave * 32 + column] = low_sum; }
-        if (own < w.rows) {
-#pragma unroll
-            for (int d = 0; d < kOut; ++d)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    *reinterpret_cast<float4*>(merged + (wave * 32 + column) * P::kMergeRow + d * 32 + j * 8 + half * 4) =
-                        make_float4(out[d][4 * j], out[d][4 * j + 1], out[d][4 * j + 2], out[d][4 * j + 3]);
-        }
-        __syncthreads();
         const uint32_t rows = w.rows - w.row0 < 32 ? w.rows - w.row0 : 32;
-        for (uint32_t i = threadIdx.x; i < rows * (DP / 4); i += P::kThreads) {
-            const uint32_t r = i / (DP / 4), d = i % (DP / 4) * 4;
-            float m = -__builtin_inff(), l = 0.f, low = 0.f, x[4] = {};
+        for (uint32_t first = 0; first < rows; first += P::kMergeRows) {
+            if (first > 0) __syncthreads();
+            if (column - first < (uint32_t)P::kMergeRows) {
 #pragma unroll
-            for (int k = 0; k < P::kWaves; ++k) m = __builtin_fmaxf(m, tops[k * 32 + r]);
+                for (int d = 0; d < kOut; ++d)
 #pragma unroll
-            for (int k = 0; k < P::kWaves; ++k) {
-                const float t = tops[k * 32 + r], factor = t == -__builtin_inff() ? (sums[k * 32 + r] != sums[k * 32 + r] ? 1.f : 0.f) : __builtin_amdgcn_exp2f(t - m);
-                const float4 v = *reinterpret_cast<const float4*>(merged + (k * 32 + r) * P::kMergeRow + d);
-                if (factor == 0.f) continue;
-                l = __builtin_fmaf(sums[k * 32 + r], factor, l);
-                low = __builtin_fmaf(lows[k * 32 + r], factor, low);
-                x[0] = __builtin_fmaf(v.x, factor, x[0]); x[1] = __builtin_fmaf(v.y, factor, x[1]);
-                x[2] = __builtin_fmaf(v.z, factor, x[2]); x[3] = __builtin_fmaf(v.w, factor, x[3]);
+                    for (int j = 0; j < 4; ++j)
+                        *reinterpret_cast<float4*>(merged + (wave * P::kMergeRows + column - first) * P::kMergeRow + d * 32 + j * 8 + half * 4) =
+                            make_float4(out[d][4 * j], out[d][4 * j + 1], out[d][4 * j + 2], out[d][4 * j + 3]);
             }
-            const uint32_t in = fdiv(w.row0 + r, p.group_div), h = head * p.group + (w.row0 + r - in * p.group);
-            const float inverse = l == 0.f ? 0.f : v_scale / l;
+            __syncthreads();
+            const uint32_t some = rows - first < (uint32_t)P::kMergeRows ? rows - first : P::kMergeRows;
+            for (uint32_t i = threadIdx.x; i < some * (DP / 4); i += P::kThreads) {
+                const uint32_t r = i / (DP / 4), row_of = first + r, d = i % (DP / 4) * 4;
+                float m = -__builtin_inff(), l = 0.f, low = 0.f, x[4] = {};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = (x[j] + low) * inverse;
-            write(w.first_token + in, h, d, x);
-            if (d == 0) write_lse(w.first_token + in, h, m, l);
+                for (int k = 0; k < P::kWaves; ++k) m = __builtin_fmaxf(m, tops[k * 32 + row_of]);
+#pragma unroll
+                for (int k = 0; k < P::kWaves; ++k) {
+                    // a wavefront whose tiles none sees has no maximum, and 0 for everything else unless that is NaN
+                    const float s = sums[k * 32 + row_of], t = tops[k * 32 + row_of], factor = t == -__builtin_inff() ? (s != s ? 1.f : 0.f) : __builtin_amdgcn_exp2f(t - m);
+                    const float4 v = *reinterpret_cast<const float4*>(merged + (k * P::kMergeRows + r) * P::kMergeRow + d);
+                    const bool any = factor != 0.f;
+                    l = any ? __builtin_fmaf(s, factor, l) : l;
+                    low = any ? __builtin_fmaf(lows[k * 32 + row_of], factor, low) : low;
+                    x[0] = any ? __builtin_fmaf(v.x, factor, x[0]) : x[0]; x[1] = any ? __builtin_fmaf(v.y, factor, x[1]) : x[1];
+                    x[2] = any ? __builtin_fmaf(v.z, factor, x[2]) : x[2]; x[3] = any ? __builtin_fmaf(v.w, factor, x[3]) : x[3];
+                }
+                const uint32_t in = fdiv(w.row0 + row_of, p.group_div), h = head * p.group + (w.row0 + row_of - in * p.group);
+                const float inverse = l == 0.f ? 0.f : v_scale / l;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[j] = (x[j] + low) * inverse;
+                write(w.first_token + in, h, d, x);
+                if (d == 0) write_lse(w.first_token + in, h, m, l);
+            }
         }
     } else {
         if (own >= w.rows) return;
@@ -769,15 +854,22 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW>::kThreads), (Plan<T, C, DP, FE
     }
 }
 
-template <typename T, typename C, int DP> AttendKernel kernel_of(bool few)
+template <typename T, typename C, int DP, bool FEW, bool OWN> AttendKernel kernel_of()
 {
-    if (few) return {reinterpret_cast<const void*>(&attend_kernel<T, C, DP, true>), Plan<T, C, DP, true>::kThreads, Plan<T, C, DP, true>::kLds};
-    return {reinterpret_cast<const void*>(&attend_kernel<T, C, DP, false>), Plan<T, C, DP, false>::kThreads, Plan<T, C, DP, false>::kLds};
+    typedef Plan<T, C, DP, FEW, OWN> P;
+    static std::atomic<uint64_t> raised{0};
+    return {reinterpret_cast<const void*>(&attend_kernel<T, C, DP, FEW, OWN>), P::kThreads, P::kLds, &raised};
+}
+template <typename T, typename C, int DP> AttendKernel kernel_of(int dim, bool few)
+{
+    if constexpr (sizeof(T) == 2 && sizeof(C) == 1)
+        if (few && dim == DP) return kernel_of<T, C, DP, true, true>();
+    return few ? kernel_of<T, C, DP, true, false>() : kernel_of<T, C, DP, false, false>();
 }
 template <typename T, typename C> AttendKernel kernel_of(int dim, bool few)
 {
-    return dim <= 32 ? kernel_of<T, C, 32>(few) : dim <= 64 ? kernel_of<T, C, 64>(few) : dim <= 96 ? kernel_of<T, C, 96>(few) : dim <= 128 ? kernel_of<T, C, 128>(few)
-         : dim <= 192 ? kernel_of<T, C, 192>(few) : kernel_of<T, C, 256>(few);
+    return dim <= 32 ? kernel_of<T, C, 32>(dim, few) : dim <= 64 ? kernel_of<T, C, 64>(dim, few) : dim <= 96 ? kernel_of<T, C, 96>(dim, few) : dim <= 128 ? kernel_of<T, C, 128>(dim, few)
+         : dim <= 192 ? kernel_of<T, C, 192>(dim, few) : kernel_of<T, C, 256>(dim, few);
 }
 template <typename T> AttendKernel kernel_of(int cache_dtype, int dim, bool few)
 {

@@ -1,6 +1,4 @@
 // Attention over pages: the launches, and the kernel that joins the parts of a row's positions (see ttc_attend.h).
-#include <atomic>
-
 #include "ttc_attention_internal.h"
 #include "ttc_moves_device.h"
 
@@ -50,17 +48,13 @@ int launch_attend(const AttendArgs& a, const AttendShape& s, void* stream)
 {
     const AttendKernel k = a.dtype == TTC_F32 ? attend_kernel_f32(a.cache_dtype, (int)a.dim, s.few) : a.dtype == TTC_BF16 ? attend_kernel_bf16(a.cache_dtype, (int)a.dim, s.few)
                                                                                                     : attend_kernel_f16(a.cache_dtype, (int)a.dim, s.few);
-    // more than 64 KB of dynamic LDS has to be asked for, once per kernel and device: a bit for each of the kernels, types by caches by dims by forms
+    // more than 64 KB of dynamic LDS has to be asked for, once per kernel and device
     if (k.lds > 64 * 1024) {
-        static std::atomic<uint32_t> raised[64][3][3][6];
         int dev = 0;
         if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return TTC_ERR_HIP;
-        const int t = a.dtype == TTC_F32 ? 0 : a.dtype == TTC_BF16 ? 1 : 2, c = a.cache_dtype == TTC_F8 ? 1 : a.cache_dtype == TTC_Q4 ? 2 : 0;
-        const int d = a.dim <= 32 ? 0 : a.dim <= 64 ? 1 : a.dim <= 96 ? 2 : a.dim <= 128 ? 3 : a.dim <= 192 ? 4 : 5;
-        const uint32_t bit = s.few ? 1 : 2;
-        if (!(raised[dev][t][c][d].load(std::memory_order_acquire) & bit)) {
+        if (!((k.raised->load(std::memory_order_acquire) >> dev) & 1u)) {
             if (hipFuncSetAttribute(k.fn, hipFuncAttributeMaxDynamicSharedMemorySize, k.lds) != hipSuccess) return TTC_ERR_HIP;
-            raised[dev][t][c][d].fetch_or(bit, std::memory_order_release);
+            k.raised->fetch_or(uint64_t(1) << dev, std::memory_order_release);
         }
     }
     AttendArgs p = a;

@@ -2,6 +2,8 @@
 // kernels (ttc_heads.hip, ttc_attend*.hip).
 #pragma once
 
+#include <atomic>
+
 #include "ttc_attention.h"
 #include "ttc_moves_internal.h"
 
@@ -93,6 +95,7 @@ int launch_attend(const AttendArgs& a, const AttendShape& s, void* stream);
 struct AttendKernel {
     const void* fn;
     int         threads, lds;
+    std::atomic<uint64_t>* raised;         // bit d: its LDS has been asked for on device d
 };
 AttendKernel attend_kernel_f32(int cache_dtype, int dim, bool few);
 AttendKernel attend_kernel_bf16(int cache_dtype, int dim, bool few);
