@@ -2,17 +2,16 @@
 // type of the queries in ttc_attend_f32.hip, ttc_attend_bf16.hip and ttc_attend_f16.hip.
 //
 // The query heads that share a head of the cache are rows of one matrix product, token by token, so that a position's key and value are fetched once for
-// them all.  A wavefront has 32 rows.  It makes scores transposed, S^T = K Q^T, with the 32 x 32 matrix instructions: their result has a row in two lanes, half a wavefront
-// apart, and its positions in their registers.  The softmax's maximum and sum are then registers, too (one exchange between the two lanes for the
-// maximum of a tile, one for the sum at the end), and the exponentials are, without a move, what O^T = V^T P^T takes as its right operand: a product's
-// order of positions is free as long as both sides have the same one.  V^T is read from the tile by the transposing LDS loads, in that order.
+// them all.  A wavefront has M = 16 or 32 rows.  It makes scores transposed, S^T = K Q^T, with the M x M matrix instructions: their result has a row in 64 / M lanes
+// (its "parts", M lanes apart) and its positions in their registers.  The softmax's maximum and sum are then registers, too (an exchange between a row's
+// lanes for the maximum of a tile, one for the sum at the end), and the exponentials are, without a move, what O^T = V^T P^T takes as its right
+// operand: a product's order of positions is free as long as both sides have the same one.  V^T is read from the tile by the transposing LDS loads, in that order.
 //
-//   FEW   at most some 32 rows to a request (tokens that are generated one by one): the wavefronts of a workgroup have the same rows and every one its own tiles of 32
-//         positions, in LDS of its own; no barrier until they add up their results.  Bound by the cache's bytes.
-//   else  prompts: wavefronts have 32 rows each of the same 128 and share the tiles.  Bound by the matrix instructions, and the exponentials beside them.
-//
-//   OWN   FEW over narrow caches, where dim is what the kernel is compiled for: a lane has half the vector of a position of its own.  Keys are never in LDS: half a vector
-//         is what the left operand of S^T holds in a lane, in an order of the dims that the queries follow.
+//   ROWS 16, 32  few rows to a request (tokens that are generated one by one): the wavefronts of a workgroup have the same rows and every one its own tiles of 32
+//                positions, in LDS of its own; no barrier until they add up their results.  Bound by the cache's bytes.
+//   ROWS 128     prompts: wavefronts have 32 rows each of the same 128 and share the tiles.  Bound by the matrix instructions, and the exponentials beside them.
+//   OWN          few rows over narrow caches, where dim is what the kernel is compiled for: a lane has a part of the vectors of positions of its own.  Keys are
+//                never in LDS: these parts are what the left operand of S^T holds in a lane, in an order of the dims that the queries follow.
 //
 // A tile's loads are under way while the one before it is used, its entries of the block table one tile earlier.
 #pragma once
@@ -27,35 +26,45 @@
 namespace ttc {
 namespace attend {
 
-typedef float Acc __attribute__((ext_vector_type(16)));
 typedef short Short4 __attribute__((ext_vector_type(4)));
 typedef short Short8 __attribute__((ext_vector_type(8)));
 #define TTC_LDS __attribute__((address_space(3)))
 
-// What a lane holds of an operand: 16 bytes, kDims of the contracted index over the two lanes of a row.
-template <typename E> struct Fragment;
-template <> struct Fragment<__bf16> {
-    typedef __bf16 type __attribute__((ext_vector_type(8)));
-    static constexpr int kDims = 16;
-    static __device__ __forceinline__ void mul(type a, type b, Acc& c) { c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+template <int M> struct Result;            // of a product, M x M over the wavefront: register i of a lane is row kGap * (i / 4) + 4 * part + i % 4, its column lane % M
+template <> struct Result<32> {
+    typedef float type __attribute__((ext_vector_type(16)));
+    static constexpr int kRegisters = 16, kGap = 8;
 };
-template <> struct Fragment<_Float16> {
-    typedef _Float16 type __attribute__((ext_vector_type(8)));
-    static constexpr int kDims = 16;
-    static __device__ __forceinline__ void mul(type a, type b, Acc& c) { c = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
-};
-template <> struct Fragment<float> {
+template <> struct Result<16> {
     typedef float type __attribute__((ext_vector_type(4)));
-    static constexpr int kDims = 8;
-    static __device__ __forceinline__ void mul(type a, type b, Acc& c)
-    {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
-    }
+    static constexpr int kRegisters = 4, kGap = 16;
 };
 
+// What a lane holds of an operand: 16 bytes.
+template <typename E> struct Fragment;
+template <> struct Fragment<__bf16> { typedef __bf16 type __attribute__((ext_vector_type(8))); };
+template <> struct Fragment<_Float16> { typedef _Float16 type __attribute__((ext_vector_type(8))); };
+template <> struct Fragment<float> { typedef float type __attribute__((ext_vector_type(4))); };
+
+__device__ __forceinline__ void mul(Fragment<__bf16>::type a, Fragment<__bf16>::type b, Result<32>::type& c) { c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ void mul(Fragment<__bf16>::type a, Fragment<__bf16>::type b, Result<16>::type& c) { c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ void mul(Fragment<_Float16>::type a, Fragment<_Float16>::type b, Result<32>::type& c) { c = __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ void mul(Fragment<_Float16>::type a, Fragment<_Float16>::type b, Result<16>::type& c) { c = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ void mul(Fragment<float>::type a, Fragment<float>::type b, Result<32>::type& c)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
+}
+__device__ __forceinline__ void mul(Fragment<float>::type a, Fragment<float>::type b, Result<16>::type& c)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], c, 0, 0, 0);
+}
+
 // T: queries and results; C: the cache; DP: dim rounded up to what the kernel is compiled for.
-template <typename T, typename C, int DP, bool FEW, bool OWN> struct Plan {
+template <typename T, typename C, int DP, int ROWS, bool OWN> struct Plan {
+    static constexpr bool FEW = ROWS < 128;
+    static constexpr int  M = ROWS < 32 ? 16 : 32, kParts = kWave / M;
     typedef T K;                                                            // keys in LDS
     // Values in LDS, and the exponentials.  Codes of 4 bits are multiplied by exponentials times steps, of which fp16 would lose the small ones: bf16.
     typedef typename std::conditional<std::is_same<C, q4>::value && !std::is_same<T, float>::value, __bf16, T>::type V;
@@ -76,16 +85,17 @@ template <typename T, typename C, int DP, bool FEW, bool OWN> struct Plan {
     static constexpr int  kKeyRow = DP * (int)sizeof(K) + 16, kValueRow = DP * (int)sizeof(V) + (kWide ? 16 : 32);
     static constexpr int  kTile = kKeys * ((OWN ? 0 : kKeyRow) + kValueRow) + (kCodes ? 4 * kKeys * 4 : 0);
     // The queries' fragments in LDS, the same for all wavefronts, where keys and values on their way take the registers.
-    static constexpr bool kQueriesInLds = FEW && !OWN && sizeof(C) == 2;
-    static constexpr int  kQueries = kQueriesInLds ? DP / Fragment<K>::kDims * kWave * 16 : 0;
+    static constexpr bool kQueriesInLds = ROWS == 32 && !OWN && sizeof(C) == 2;
+    static constexpr int  kDims = kParts * 16 / (int)sizeof(K);              // of the contracted index, in a fragment over a row's lanes
+    static constexpr int  kQueries = kQueriesInLds ? DP / kDims * kWave * 16 : 0;
     static constexpr int  kMergeRows = 8;                                    // of the wavefronts' results that are added up at a time
     static constexpr int  kMergeRow = DP + 4;                                // floats
-    static constexpr int  kMerge = FEW ? kWaves * kMergeRows * kMergeRow * 4 + 3 * kWaves * 32 * 4 : 0;
+    static constexpr int  kMerge = FEW ? kWaves * kMergeRows * kMergeRow * 4 + 3 * kWaves * ROWS * 4 : 0;
     static constexpr int  kLds = kTile * kTeams + kQueries > kMerge ? kTile * kTeams + kQueries : kMerge;
     // workgroups that share a compute unit, and so its registers
     static constexpr int  kResident = !kWide && DP <= 128 && 2 * kLds <= kMaxLdsBytes ? 2 : 1;
-    // OWN: the words of half a vector, a lane's
-    static constexpr int  kWords = kRecords ? DP / 16 : DP / 2 * (int)sizeof(C) / 4;
+    // OWN: the words of a part of a vector, a lane's, and the positions that it has such a part of
+    static constexpr int  kWords = (kRecords ? DP / 2 : DP * (int)sizeof(C)) / kParts / 4, kPositions = kKeys / M;
     static_assert(kKeys * kChunks % kTeam == 0 && DP % 32 == 0 && kLds <= kMaxLdsBytes, "a tile is loaded in whole chunks");
 };
 
@@ -307,17 +317,19 @@ template <typename P, int TILE> __device__ __forceinline__ bool find_work(const 
     return split < w.parts;
 }
 
-// The larger, and the sum, of the two lanes of a row.
-__device__ __forceinline__ float max_of_row(float x)
+// The largest, and the sum, of a row's lanes.
+template <typename Join> __device__ __forceinline__ float over_row(float x, bool four, Join join)
 {
-    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
-    return __builtin_fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+    auto swap = [&](const auto& r) { return join(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1])); };
+    const uint32_t b = __builtin_bit_cast(uint32_t, x);
+    if (four) {
+        const uint32_t c = __builtin_bit_cast(uint32_t, swap(__builtin_amdgcn_permlane16_swap(b, b, false, false)));
+        return swap(__builtin_amdgcn_permlane32_swap(c, c, false, false));
+    }
+    return swap(__builtin_amdgcn_permlane32_swap(b, b, false, false));
 }
-__device__ __forceinline__ float sum_of_row(float x)
-{
-    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
-    return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
-}
+template <int M> __device__ __forceinline__ float max_of_row(float x) { return over_row(x, M == 16, [](float a, float b) { return __builtin_fmaxf(a, b); }); }
+template <int M> __device__ __forceinline__ float sum_of_row(float x) { return over_row(x, M == 16, [](float a, float b) { return a + b; }); }
 
 // The weights of a value's element in the count of what is neither finite: at most 64 of each in a tile.
 constexpr int kPlus = 1, kMinus = 128, kNan = 16384;
@@ -351,29 +363,32 @@ template <> struct Bad<float> {
     }
 };
 
-template <typename T, typename C, int DP, bool FEW, bool OWN>
-__global__ __launch_bounds__((Plan<T, C, DP, FEW, OWN>::kThreads), (Plan<T, C, DP, FEW, OWN>::kResident)) void attend_kernel(AttendArgs p)
+template <typename T, typename C, int DP, int ROWS, bool OWN>
+__global__ __launch_bounds__((Plan<T, C, DP, ROWS, OWN>::kThreads), (Plan<T, C, DP, ROWS, OWN>::kResident)) void attend_kernel(AttendArgs p)
 {
-    typedef Plan<T, C, DP, FEW, OWN> P;
+    typedef Plan<T, C, DP, ROWS, OWN> P;
+    constexpr bool FEW = P::FEW;
+    constexpr int M = P::M, kParts = P::kParts, kRegisters = Result<M>::kRegisters, kGap = Result<M>::kGap;
+    typedef typename Result<M>::type Acc;
     typedef typename P::K KE;
     typedef typename P::V VE;
     typedef typename Fragment<KE>::type KFrag;
     typedef typename Fragment<VE>::type VFrag;
-    constexpr int kTileRows = FEW ? kTileFew : kTileMany, kBlocks = P::kKeys / 32, kSteps = DP / Fragment<KE>::kDims, kOut = DP / 32;
+    constexpr int kBlocks = P::kKeys / M, kSteps = DP / P::kDims, kOut = DP / M;
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    const uint32_t lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), half = lane >> 5, column = lane & 31;
+    const uint32_t lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), part = lane / M, column = lane % M;
     const uint32_t head = blockIdx.y, slot = blockIdx.x, split = blockIdx.z;
     Work w;
-    if (!find_work<P, kTileRows>(p, p.slots_of_tiles - 1 - slot, split, w)) return;        // the last tiles see most: first
+    if (!find_work<P, ROWS>(p, p.slots_of_tiles - 1 - slot, split, w)) return;        // the last tiles see most: first
 
     // this lane's row; behind the request's last one, that one again
-    const uint32_t own = w.row0 + (FEW ? 0 : wave * 32) + column, row = own < w.rows ? own : w.rows - 1;
+    const uint32_t own = w.row0 + (FEW ? 0 : wave * M) + column, row = own < w.rows ? own : w.rows - 1;
     const uint32_t in_request = fdiv(row, p.group_div), q_head = head * p.group + (row - in_request * p.group);
     const uint32_t token = w.first_token + in_request, position = w.cached + in_request;
-    uint32_t first_row = w.row0 + (FEW ? 0 : wave * 32);
+    uint32_t first_row = w.row0 + (FEW ? 0 : wave * M);
     const bool idle = first_row >= w.rows;                                  // no row of this wavefront's is one
     first_row = first_row < w.rows ? first_row : w.rows - 1;
-    const uint32_t last_row = first_row + 31 < w.rows ? first_row + 31 : w.rows - 1;
+    const uint32_t last_row = first_row + M - 1 < w.rows ? first_row + M - 1 : w.rows - 1;
     const uint32_t lowest = w.cached + fdiv(first_row, p.group_div), highest = w.cached + fdiv(last_row, p.group_div);
 
     // scores times `scale` are exponents of 2; its sign goes into the queries, so that the largest product has the largest exponent
@@ -390,18 +405,18 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW, OWN>::kThreads), (Plan<T, C, D
         if (p.dim % E == 0) {
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                const uint32_t at = OWN ? half * (DP / 2) + i * E : i * Fragment<KE>::kDims + half * E;
+                const uint32_t at = OWN ? part * (DP / kParts) + i * E : i * P::kDims + part * E;
                 query[i] = __builtin_bit_cast(KFrag, load_vec<T, E, false>(from + (at < p.dim ? at : 0)));
             }
 #pragma unroll
             for (int i = 0; i < kSteps; ++i)
-                if (i * Fragment<KE>::kDims + half * E >= p.dim) query[i] = none;
+                if (!OWN && i * P::kDims + part * E >= p.dim) query[i] = none;
         } else {
 #pragma unroll
             for (int i = 0; i < kSteps; ++i)
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
-                    const uint32_t at = i * Fragment<KE>::kDims + half * E + j;
+                    const uint32_t at = i * P::kDims + part * E + j;
                     const T x = from[at < p.dim ? at : 0];
                     query[i][j] = at < p.dim ? x : (T)0.f;
                 }
@@ -418,7 +433,7 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW, OWN>::kThreads), (Plan<T, C, D
                 for (int j = 0; j < E; ++j) query_sum += (float)query[i][j];
             }
         }
-        if (P::kCodes) query_sum = sum_of_row(query_sum);
+        if (P::kCodes) query_sum = sum_of_row<M>(query_sum);
     }
 
     char* tile = lds + (FEW ? wave * P::kTile : 0);
@@ -501,48 +516,64 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW, OWN>::kThreads), (Plan<T, C, D
         }
         return bad;
     };
-    // OWN: half a vector of this lane's position
-    struct Half { uint32_t w[P::kWords], head; };
-    Half half_k, half_v;
-    auto load_half = [&](const char* cache, int64_t offset, Half& r) {
-        const char* from = cache + offset + (P::kRecords ? kRecordHead : 0) + half * (P::kWords * 4);
-        r.head = P::kRecords ? load_word(reinterpret_cast<const uint8_t*>(cache + offset)) : 0;
+    // OWN: a part of the vector of each of this lane's positions, column + M * b of the tile
+    struct Part { uint32_t w[P::kWords], head; };
+    Part part_k[P::kPositions], part_v[P::kPositions];
+    auto load_parts = [&](const char* cache, int64_t offset, Part* r) {
 #pragma unroll
-        for (int i = 0; i + 4 <= P::kWords; i += 4) {
-            const typename Bits<16>::type x = *reinterpret_cast<const typename Bits<16>::type*>(from + 4 * i);
-            __builtin_memcpy(r.w + i, &x, 16);
-        }
-        if constexpr (P::kWords % 4 != 0) {
-            const typename Bits<8>::type x = *reinterpret_cast<const typename Bits<8>::type*>(from + P::kWords / 4 * 16);
-            __builtin_memcpy(r.w + P::kWords / 4 * 4, &x, 8);
+        for (int b = 0; b < P::kPositions; ++b) {
+            int64_t place = offset;        // lane j has position j's
+            if constexpr (P::kPositions > 1) {
+                const uint32_t low = __shfl((uint32_t)offset, column + M * b), high = __shfl((uint32_t)(offset >> 32), column + M * b);
+                place = (int64_t)((uint64_t)high << 32 | low);
+            }
+            const char* from = cache + place + (P::kRecords ? kRecordHead : 0) + part * (P::kWords * 4);
+            r[b].head = P::kRecords ? load_word(reinterpret_cast<const uint8_t*>(cache + place)) : 0;
+#pragma unroll
+            for (int i = 0; i + 4 <= P::kWords; i += 4) {
+                const typename Bits<16>::type x = *reinterpret_cast<const typename Bits<16>::type*>(from + 4 * i);
+                __builtin_memcpy(r[b].w + i, &x, 16);
+            }
+            constexpr int kLeft = P::kWords % 4, kDone = P::kWords - kLeft;
+            if constexpr ((kLeft & 2) != 0) {
+                const typename Bits<8>::type x = *reinterpret_cast<const typename Bits<8>::type*>(from + 4 * kDone);
+                __builtin_memcpy(r[b].w + kDone, &x, 8);
+            }
+            if constexpr ((kLeft & 1) != 0) r[b].w[P::kWords - 1] = load_word(reinterpret_cast<const uint8_t*>(from + 4 * (P::kWords - 1)));
         }
     };
     // its eight elements number i, as LDS and the products have them
-    auto chunk_of_half = [&](const Half& r, int i) -> Chunk8<C> {
+    auto chunk_of_part = [&](const Part& r, int i) -> Chunk8<C> {
         Chunk8<C> c;
         if constexpr (P::kRecords) c = {r.w[i], r.head};
         else __builtin_memcpy(&c, r.w + i * (int)sizeof(C) * 2, sizeof(c));
         return c;
     };
-    auto put_half = [&](Half& r, uint64_t there, bool holes, bool look) -> bool {
+    auto put_parts = [&](Part* r, uint64_t there, bool holes, bool look) -> bool {
         bool bad = false;
-        if (holes && !(there >> column & 1)) r = {};
 #pragma unroll
-        for (int i = 0; i < DP / 16; ++i) {
-            const Chunk8<C> c = chunk_of_half(r, i);
-            store_chunk<VE, true>(values + column * P::kValueRow + (half * (DP / 2) + 8 * i) * sizeof(VE), c);
-            if (!P::kCodes && look) bad |= any_bad(c);
+        for (int b = 0; b < P::kPositions; ++b) {
+            if (holes && !(there >> (column + M * b) & 1)) r[b] = {};
+#pragma unroll
+            for (int i = 0; i < DP / kParts / 8; ++i) {
+                const Chunk8<C> c = chunk_of_part(r[b], i);
+                store_chunk<VE, true>(values + (column + M * b) * P::kValueRow + (part * (DP / kParts) + 8 * i) * sizeof(VE), c);
+                if (!P::kCodes && look) bad |= any_bad(c);
+            }
         }
         return bad;
     };
-    auto put_steps = [&](const Half& k, const Half& v) {
-        if (half == 0) {
-            const float ks = __builtin_bit_cast(float, k.head << 16), vs = __builtin_bit_cast(float, v.head << 16);
-            key_step[column] = ks;
-            key_low[column] = __builtin_fmaf(-16.f, ks, __builtin_bit_cast(float, k.head & 0xffff0000u));
-            value_step[column] = vs;
-            value_low[column] = __builtin_fmaf(8.f, vs, __builtin_bit_cast(float, v.head & 0xffff0000u));
-        }
+    auto put_steps = [&](const Part* k, const Part* v) {
+#pragma unroll
+        for (int b = 0; b < P::kPositions; ++b)
+            if (part == 0) {
+                const uint32_t key = column + M * b;
+                const float ks = __builtin_bit_cast(float, k[b].head << 16), vs = __builtin_bit_cast(float, v[b].head << 16);
+                key_step[key] = ks;
+                key_low[key] = __builtin_fmaf(-16.f, ks, __builtin_bit_cast(float, k[b].head & 0xffff0000u));
+                value_step[key] = vs;
+                value_low[key] = __builtin_fmaf(8.f, vs, __builtin_bit_cast(float, v[b].head & 0xffff0000u));
+            }
     };
     char* queries = lds + P::kTile * P::kTeams + lane * 16;
     if constexpr (P::kQueriesInLds) {
@@ -570,8 +601,8 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW, OWN>::kThreads), (Plan<T, C, D
     Spot spot = spot_of(at, entry);
     uint64_t here = __ballot(spot.here);
     if constexpr (OWN) {
-        load_half(k_cache, spot.offset, half_k);
-        load_half(v_cache, spot.offset, half_v);
+        load_parts(k_cache, spot.offset, part_k);
+        load_parts(v_cache, spot.offset, part_v);
         entry = look_up(at + P::kStep);
     } else if constexpr (P::kAhead) {
         load(k_cache, spot.offset, raw_k);
@@ -586,19 +617,20 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW, OWN>::kThreads), (Plan<T, C, D
         constexpr uint64_t kAll = P::kKeys == 64 ? ~0ull : (1ull << P::kKeys) - 1;
         const bool holes = (now & kAll) != kAll;
         const uint32_t tile_lowest = w.cached + fdiv(w.row0, p.group_div);
-        const bool look = holes || end > tile_lowest + 1 || (p.window && at + p.window <= w.cached + fdiv(w.row0 + kTileRows < w.rows ? w.row0 + kTileRows - 1 : w.rows - 1, p.group_div));
+        const bool look = holes || end > tile_lowest + 1 || (p.window && at + p.window <= w.cached + fdiv(w.row0 + ROWS < w.rows ? w.row0 + ROWS - 1 : w.rows - 1, p.group_div));
         bool bad;
         team_sync<FEW>();                                                   // the tile before has been used
-        Half now_k = {};
+        Part now_k[P::kPositions];
         if constexpr (OWN) {
-            now_k = half_k;
-            if constexpr (P::kCodes) put_steps(half_k, half_v);
-            bad = put_half(half_v, now, holes, look);
+#pragma unroll
+            for (int b = 0; b < P::kPositions; ++b) now_k[b] = part_k[b];
+            if constexpr (P::kCodes) put_steps(part_k, part_v);
+            bad = put_parts(part_v, now, holes, look);
             if (at + P::kStep < w.hi) {
                 spot = spot_of(at + P::kStep, entry);
                 here = __ballot(spot.here);
-                load_half(k_cache, spot.offset, half_k);
-                load_half(v_cache, spot.offset, half_v);
+                load_parts(k_cache, spot.offset, part_k);
+                load_parts(v_cache, spot.offset, part_v);
                 entry = look_up(at + 2 * P::kStep);
             }
         } else if constexpr (P::kAhead) {
@@ -634,29 +666,28 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW, OWN>::kThreads), (Plan<T, C, D
         Acc score[kBlocks] = {};
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) {
-            const char* from = keys + (b * 32 + column) * P::kKeyRow + half * 16;
-            if constexpr (OWN) {
+            const char* from = keys + (b * M + column) * P::kKeyRow + part * 16;
 #pragma unroll
-                for (int i = 0; i < kSteps; ++i) Fragment<KE>::mul(fragment_of<KE>(chunk_of_half(now_k, i)), query[i], score[b]);
-                continue;
+            for (int i = 0; i < kSteps; ++i) {
+                if constexpr (OWN) mul(fragment_of<KE>(chunk_of_part(now_k[b], i)), query[i], score[b]);
+                else mul(*reinterpret_cast<const KFrag*>(from + i * P::kDims * sizeof(KE)), query_of(i), score[b]);
             }
-#pragma unroll
-            for (int i = 0; i < kSteps; ++i) Fragment<KE>::mul(*reinterpret_cast<const KFrag*>(from + i * Fragment<KE>::kDims * sizeof(KE)), query_of(i), score[b]);
         }
-        // register i of block b is position 32 b + 8 (i / 4) + 4 half + i % 4
+        // register i of block b is position M b + kGap (i / 4) + 4 part + i % 4
         if constexpr (P::kCodes) {
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float4 step = *reinterpret_cast<const float4*>(key_step + b * 32 + j * 8 + half * 4), low = *reinterpret_cast<const float4*>(key_low + b * 32 + j * 8 + half * 4);
+                for (int j = 0; j < kRegisters / 4; ++j) {
+                    const uint32_t four = b * M + j * kGap + part * 4;
+                    const float4 step = *reinterpret_cast<const float4*>(key_step + four), low = *reinterpret_cast<const float4*>(key_low + four);
                     const float steps[4] = {step.x, step.y, step.z, step.w}, lows[4] = {low.x, low.y, low.z, low.w};
 #pragma unroll
                     for (int c = 0; c < 4; ++c) score[b][4 * j + c] = __builtin_fmaf(score[b][4 * j + c], steps[c], lows[c] * query_sum);
                 }
         }
         const bool masked = holes || end > lowest + 1 || (p.window && at + p.window <= highest);
-        uint32_t seen[kBlocks];                                             // bit 8 (i / 4) + i % 4 of block b: what register i is of
+        uint32_t seen[kBlocks];                                             // bit kGap (i / 4) + i % 4 of block b: what register i is of
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b) seen[b] = ~0u;
         if (masked) {
@@ -666,17 +697,17 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW, OWN>::kThreads), (Plan<T, C, D
             const uint64_t sees = upto & now & (out_of >= 64 ? 0 : ~0ull << out_of);
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b) {
-                seen[b] = (uint32_t)(sees >> (32 * b)) >> (4 * half);
+                seen[b] = (uint32_t)(sees >> (M * b)) >> (4 * part);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) score[b][i] = seen[b] >> (8 * (i / 4) + i % 4) & 1 ? score[b][i] : -__builtin_inff();
+                for (int i = 0; i < kRegisters; ++i) score[b][i] = seen[b] >> (kGap * (i / 4) + i % 4) & 1 ? score[b][i] : -__builtin_inff();
             }
         }
         float most = -__builtin_inff();
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) most = __builtin_fmaxf(most, score[b][i]);
-        most = max_of_row(most) * scale;
+            for (int i = 0; i < kRegisters; ++i) most = __builtin_fmaxf(most, score[b][i]);
+        most = max_of_row<M>(most) * scale;
         if (__ballot(most > top)) {
             const float higher = __builtin_fmaxf(top, most), factor = higher == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(top - higher);
             top = higher;
@@ -689,7 +720,7 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW, OWN>::kThreads), (Plan<T, C, D
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
+            for (int i = 0; i < kRegisters; ++i) {
                 score[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[b][i], scale, -base));
                 sum += score[b][i];
             }
@@ -697,42 +728,43 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW, OWN>::kThreads), (Plan<T, C, D
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float4 step = *reinterpret_cast<const float4*>(value_step + b * 32 + j * 8 + half * 4), low = *reinterpret_cast<const float4*>(value_low + b * 32 + j * 8 + half * 4);
+                for (int j = 0; j < kRegisters / 4; ++j) {
+                    const uint32_t four = b * M + j * kGap + part * 4;
+                    const float4 step = *reinterpret_cast<const float4*>(value_step + four), low = *reinterpret_cast<const float4*>(value_low + four);
                     const float steps[4] = {step.x, step.y, step.z, step.w}, lows[4] = {low.x, low.y, low.z, low.w};
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        low_sum = __builtin_fmaf(score[b][4 * j + c], masked && !(seen[b] >> (8 * j + c) & 1) ? 0.f : lows[c], low_sum);
-                        score[b][4 * j + c] *= masked && !(seen[b] >> (8 * j + c) & 1) ? 0.f : steps[c];        // not seen: 0, whatever the record says
+                        low_sum = __builtin_fmaf(score[b][4 * j + c], masked && !(seen[b] >> (kGap * j + c) & 1) ? 0.f : lows[c], low_sum);
+                        score[b][4 * j + c] *= masked && !(seen[b] >> (kGap * j + c) & 1) ? 0.f : steps[c];        // not seen: 0, whatever the record says
                     }
                 }
         }
-        // O^T += V^T P^T, 16 positions at a time (32 bits: eight)
-        constexpr int kParts = P::kKeys / Fragment<VE>::kDims, kEach = 16 / (int)sizeof(VE);
-        VFrag weight[kParts];
+        // O^T += V^T P^T, a fragment's positions at a time
+        constexpr int kEach = 16 / (int)sizeof(VE), kTakes = P::kKeys / (kParts * kEach);
+        VFrag weight[kTakes];
 #pragma unroll
-        for (int k = 0; k < kParts; ++k)
+        for (int k = 0; k < kTakes; ++k)
 #pragma unroll
-            for (int e = 0; e < kEach; ++e) weight[k][e] = (VE)score[k * kEach / 16][k * kEach % 16 + e];
+            for (int e = 0; e < kEach; ++e) weight[k][e] = (VE)score[(k * kEach + e) / kRegisters][(k * kEach + e) % kRegisters];
         if constexpr (P::kCodes) {
             typedef __bf16 Two __attribute__((ext_vector_type(2)));
             const Two back = {(__bf16)-24.f, (__bf16)-24.f};
 #pragma unroll
-            for (int k = 0; k < kParts; ++k)
+            for (int k = 0; k < kTakes; ++k)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) low_sum = __builtin_amdgcn_fdot2_f32_bf16(Two{weight[k][2 * e], weight[k][2 * e + 1]}, back, low_sum, false);
         }
         auto value = [&](int k, int d) -> VFrag {
             if constexpr (sizeof(VE) == 4) {
                 VFrag r;
-                const char* from = values + (k * 8 + half * 4) * P::kValueRow + (d * 32 + column) * 4;
+                const char* from = values + (k * 4 * kParts + part * 4) * P::kValueRow + (d * M + column) * 4;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) r[e] = *reinterpret_cast<const float*>(from + e * P::kValueRow);
                 return r;
             } else {
                 // four rows of 16 elements for each 16 lanes, which get a column of them each
-                const char* from = values + (k * 16 + half * 4 + (lane & 15) / 4) * P::kValueRow + (d * 32 + (lane >> 4 & 1) * 16 + (lane & 3) * 4) * 2;
-                const Short4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((TTC_LDS Short4*)from), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((TTC_LDS Short4*)(from + 8 * P::kValueRow));
+                const char* from = values + (k * 8 * kParts + part * 4 + (lane & 15) / 4) * P::kValueRow + (d * M + (M == 32 ? (lane >> 4 & 1) * 16 : 0) + (lane & 3) * 4) * 2;
+                const Short4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((TTC_LDS Short4*)from), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((TTC_LDS Short4*)(from + kGap * P::kValueRow));
                 return __builtin_bit_cast(VFrag, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
             }
         };
@@ -743,20 +775,20 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW, OWN>::kThreads), (Plan<T, C, D
             for (int d = 0; d < kOut; ++d) {
                 Acc count = {};
 #pragma unroll
-                for (int k = 0; k < kParts; ++k) {
+                for (int k = 0; k < kTakes; ++k) {
                     VFrag v = value(k, d);
                     const VFrag marks = Bad<VE>::marks(v);
-                    Fragment<VE>::mul(v, weight[k], out[d]);
+                    mul(v, weight[k], out[d]);
                     VFrag sees;
 #pragma unroll
                     for (int e = 0; e < kEach; ++e) {
-                        const int i = k * kEach % 16 + e;
-                        sees[e] = (VE)(seen[k * kEach / 16] >> (8 * (i / 4) + i % 4) & 1 ? 1.f : 0.f);
+                        const int b = (k * kEach + e) / kRegisters, i = (k * kEach + e) % kRegisters;
+                        sees[e] = (VE)(seen[b] >> (kGap * (i / 4) + i % 4) & 1 ? 1.f : 0.f);
                     }
-                    Fragment<VE>::mul(marks, sees, count);
+                    mul(marks, sees, count);
                 }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
+                for (int i = 0; i < kRegisters; ++i) {
                     const int n = (int)count[i];
                     const bool plus = n & (kMinus - 1), minus = n & (kNan - kMinus), nan = n >= kNan;
                     out[d][i] += nan || (plus && minus) ? __builtin_nanf("") : plus ? __builtin_inff() : minus ? -__builtin_inff() : 0.f;
@@ -766,12 +798,12 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW, OWN>::kThreads), (Plan<T, C, D
 #pragma unroll
             for (int d = 0; d < kOut; ++d)
 #pragma unroll
-                for (int k = 0; k < kParts; ++k) Fragment<VE>::mul(value(k, d), weight[k], out[d]);
+                for (int k = 0; k < kTakes; ++k) mul(value(k, d), weight[k], out[d]);
         }
     }
 
-    sum = sum_of_row(sum);
-    low_sum = sum_of_row(low_sum);
+    sum = sum_of_row<M>(sum);
+    low_sum = sum_of_row<M>(low_sum);
     const float v_scale = std::is_same<C, f8>::value && p.v_scale ? p.v_scale[head] : 1.f;
     // Writes four neighbouring elements of a row's result, normalized: to the result, or to this part's place.
     auto write = [&](uint32_t to_token, uint32_t to_head, uint32_t d, const float* x) {
@@ -799,17 +831,17 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW, OWN>::kThreads), (Plan<T, C, D
         // the wavefronts' results to the largest of their maxima, then added up
         __syncthreads();
         float* merged = reinterpret_cast<float*>(lds);
-        float *tops = merged + P::kWaves * P::kMergeRows * P::kMergeRow, *sums = tops + P::kWaves * 32, *lows = sums + P::kWaves * 32;
-        if (half == 0) { tops[wave * 32 + column] = top; sums[wave * 32 + column] = sum; lows[wave * 32 + column] = low_sum; }
-        const uint32_t rows = w.rows - w.row0 < 32 ? w.rows - w.row0 : 32;
+        float *tops = merged + P::kWaves * P::kMergeRows * P::kMergeRow, *sums = tops + P::kWaves * ROWS, *lows = sums + P::kWaves * ROWS;
+        if (part == 0) { tops[wave * ROWS + column] = top; sums[wave * ROWS + column] = sum; lows[wave * ROWS + column] = low_sum; }
+        const uint32_t rows = w.rows - w.row0 < ROWS ? w.rows - w.row0 : ROWS;
         for (uint32_t first = 0; first < rows; first += P::kMergeRows) {
             if (first > 0) __syncthreads();
             if (column - first < (uint32_t)P::kMergeRows) {
 #pragma unroll
                 for (int d = 0; d < kOut; ++d)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        *reinterpret_cast<float4*>(merged + (wave * P::kMergeRows + column - first) * P::kMergeRow + d * 32 + j * 8 + half * 4) =
+                    for (int j = 0; j < kRegisters / 4; ++j)
+                        *reinterpret_cast<float4*>(merged + (wave * P::kMergeRows + column - first) * P::kMergeRow + d * M + j * kGap + part * 4) =
                             make_float4(out[d][4 * j], out[d][4 * j + 1], out[d][4 * j + 2], out[d][4 * j + 3]);
             }
             __syncthreads();
@@ -818,15 +850,15 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW, OWN>::kThreads), (Plan<T, C, D
                 const uint32_t r = i / (DP / 4), row_of = first + r, d = i % (DP / 4) * 4;
                 float m = -__builtin_inff(), l = 0.f, low = 0.f, x[4] = {};
 #pragma unroll
-                for (int k = 0; k < P::kWaves; ++k) m = __builtin_fmaxf(m, tops[k * 32 + row_of]);
+                for (int k = 0; k < P::kWaves; ++k) m = __builtin_fmaxf(m, tops[k * ROWS + row_of]);
 #pragma unroll
                 for (int k = 0; k < P::kWaves; ++k) {
                     // a wavefront whose tiles none sees has no maximum, and 0 for everything else unless that is NaN
-                    const float s = sums[k * 32 + row_of], t = tops[k * 32 + row_of], factor = t == -__builtin_inff() ? (s != s ? 1.f : 0.f) : __builtin_amdgcn_exp2f(t - m);
+                    const float s = sums[k * ROWS + row_of], t = tops[k * ROWS + row_of], factor = t == -__builtin_inff() ? (s != s ? 1.f : 0.f) : __builtin_amdgcn_exp2f(t - m);
                     const float4 v = *reinterpret_cast<const float4*>(merged + (k * P::kMergeRows + r) * P::kMergeRow + d);
                     const bool any = factor != 0.f;
                     l = any ? __builtin_fmaf(s, factor, l) : l;
-                    low = any ? __builtin_fmaf(lows[k * 32 + row_of], factor, low) : low;
+                    low = any ? __builtin_fmaf(lows[k * ROWS + row_of], factor, low) : low;
                     x[0] = any ? __builtin_fmaf(v.x, factor, x[0]) : x[0]; x[1] = any ? __builtin_fmaf(v.y, factor, x[1]) : x[1];
                     x[2] = any ? __builtin_fmaf(v.z, factor, x[2]) : x[2]; x[3] = any ? __builtin_fmaf(v.w, factor, x[3]) : x[3];
                 }
@@ -844,36 +876,36 @@ __global__ __launch_bounds__((Plan<T, C, DP, FEW, OWN>::kThreads), (Plan<T, C, D
 #pragma unroll
         for (int d = 0; d < kOut; ++d)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < kRegisters / 4; ++j) {
                 float x[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) x[c] = (out[d][4 * j + c] + low_sum) * inverse;
-                write(token, q_head, d * 32 + j * 8 + half * 4, x);
+                write(token, q_head, d * M + j * kGap + part * 4, x);
             }
-        if (half == 0) write_lse(token, q_head, top, sum);
+        if (part == 0) write_lse(token, q_head, top, sum);
     }
 }
 
-template <typename T, typename C, int DP, bool FEW, bool OWN> AttendKernel kernel_of()
+template <typename T, typename C, int DP, int ROWS, bool OWN> AttendKernel kernel_of()
 {
-    typedef Plan<T, C, DP, FEW, OWN> P;
+    typedef Plan<T, C, DP, ROWS, OWN> P;
     static std::atomic<uint64_t> raised{0};
-    return {reinterpret_cast<const void*>(&attend_kernel<T, C, DP, FEW, OWN>), P::kThreads, P::kLds, &raised};
+    return {reinterpret_cast<const void*>(&attend_kernel<T, C, DP, ROWS, OWN>), P::kThreads, P::kLds, &raised};
 }
-template <typename T, typename C, int DP> AttendKernel kernel_of(int dim, bool few)
+template <typename T, typename C, int DP> AttendKernel kernel_of(int dim, int rows)
 {
     if constexpr (sizeof(T) == 2 && sizeof(C) == 1)
-        if (few && dim == DP) return kernel_of<T, C, DP, true, true>();
-    return few ? kernel_of<T, C, DP, true, false>() : kernel_of<T, C, DP, false, false>();
+        if (rows < 128 && dim == DP) return rows == 16 ? kernel_of<T, C, DP, 16, true>() : kernel_of<T, C, DP, 32, true>();
+    return rows == 16 ? kernel_of<T, C, DP, 16, false>() : rows == 32 ? kernel_of<T, C, DP, 32, false>() : kernel_of<T, C, DP, 128, false>();
 }
-template <typename T, typename C> AttendKernel kernel_of(int dim, bool few)
+template <typename T, typename C> AttendKernel kernel_of(int dim, int rows)
 {
-    return dim <= 32 ? kernel_of<T, C, 32>(dim, few) : dim <= 64 ? kernel_of<T, C, 64>(dim, few) : dim <= 96 ? kernel_of<T, C, 96>(dim, few) : dim <= 128 ? kernel_of<T, C, 128>(dim, few)
-         : dim <= 192 ? kernel_of<T, C, 192>(dim, few) : kernel_of<T, C, 256>(dim, few);
+    return dim <= 32 ? kernel_of<T, C, 32>(dim, rows) : dim <= 64 ? kernel_of<T, C, 64>(dim, rows) : dim <= 96 ? kernel_of<T, C, 96>(dim, rows)
+         : dim <= 128 ? kernel_of<T, C, 128>(dim, rows) : dim <= 192 ? kernel_of<T, C, 192>(dim, rows) : kernel_of<T, C, 256>(dim, rows);
 }
-template <typename T> AttendKernel kernel_of(int cache_dtype, int dim, bool few)
+template <typename T> AttendKernel kernel_of(int cache_dtype, int dim, int rows)
 {
-    return cache_dtype == TTC_F8 ? kernel_of<T, f8>(dim, few) : cache_dtype == TTC_Q4 ? kernel_of<T, q4>(dim, few) : kernel_of<T, T>(dim, few);
+    return cache_dtype == TTC_F8 ? kernel_of<T, f8>(dim, rows) : cache_dtype == TTC_Q4 ? kernel_of<T, q4>(dim, rows) : kernel_of<T, T>(dim, rows);
 }
 
 }  // namespace attend

@@ -46,8 +46,8 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs p)
 
 int launch_attend(const AttendArgs& a, const AttendShape& s, void* stream)
 {
-    const AttendKernel k = a.dtype == TTC_F32 ? attend_kernel_f32(a.cache_dtype, (int)a.dim, s.few) : a.dtype == TTC_BF16 ? attend_kernel_bf16(a.cache_dtype, (int)a.dim, s.few)
-                                                                                                    : attend_kernel_f16(a.cache_dtype, (int)a.dim, s.few);
+    const AttendKernel k = a.dtype == TTC_F32 ? attend_kernel_f32(a.cache_dtype, (int)a.dim, (int)s.tile) : a.dtype == TTC_BF16 ? attend_kernel_bf16(a.cache_dtype, (int)a.dim, (int)s.tile)
+                                                                                                    : attend_kernel_f16(a.cache_dtype, (int)a.dim, (int)s.tile);
     // more than 64 KB of dynamic LDS has to be asked for, once per kernel and device
     if (k.lds > 64 * 1024) {
         int dev = 0;

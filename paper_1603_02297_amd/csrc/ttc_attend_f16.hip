@@ -3,6 +3,6 @@
 
 namespace ttc {
 
-AttendKernel attend_kernel_f16(int cache_dtype, int dim, bool few) { return attend::kernel_of<_Float16>(cache_dtype, dim, few); }
+AttendKernel attend_kernel_f16(int cache_dtype, int dim, int rows) { return attend::kernel_of<_Float16>(cache_dtype, dim, rows); }
 
 }  // namespace ttc

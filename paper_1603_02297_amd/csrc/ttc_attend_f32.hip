@@ -3,6 +3,6 @@
 
 namespace ttc {
 
-AttendKernel attend_kernel_f32(int cache_dtype, int dim, bool few) { return attend::kernel_of<float>(cache_dtype, dim, few); }
+AttendKernel attend_kernel_f32(int cache_dtype, int dim, int rows) { return attend::kernel_of<float>(cache_dtype, dim, rows); }
 
 }  // namespace ttc

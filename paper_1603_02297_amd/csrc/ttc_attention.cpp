@@ -39,12 +39,11 @@ AttendShape attend_shape(int64_t requests, int64_t tokens, int64_t heads, int64_
 {
     AttendShape s = {};
     const int64_t rows = tokens * group;
-    s.few = rows <= (int64_t)kTileFew * 3 / 2 * requests;
-    s.tile = s.few ? kTileFew : kTileMany;
+    s.tile = rows <= 16 * requests ? 16 : rows <= 48 * requests ? 32 : kTileMany;
     // request r's tiles are numbered from starts[r] * group / tile + r on: always enough, and found without a sum over the requests
     s.slots = (uint32_t)(rows / s.tile + requests);
     // where tiles alone do not fill the device, several workgroups share a tile's positions, 128 of them at least
-    const int64_t groups = std::max<int64_t>((int64_t)s.slots * heads, 1), wanted = s.few ? 4096 : 1024;
+    const int64_t groups = std::max<int64_t>((int64_t)s.slots * heads, 1), wanted = s.tile < kTileMany ? 4096 : 1024;
     s.splits = (uint32_t)std::min<int64_t>({std::max<int64_t>(wanted / groups, 1), (longest + 127) / 128 + (longest < 1), kAttendMaxSplits});
     return s;
 }

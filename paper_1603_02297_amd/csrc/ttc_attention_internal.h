@@ -81,11 +81,10 @@ struct AttendArgs {
     int32_t        dtype, cache_dtype;
 };
 
-constexpr int kTileFew = 32, kTileMany = 128;          // rows of a workgroup: one wavefront's, its four each with other positions; or four wavefronts', with the same
+constexpr int kTileMany = 128;             // rows of a workgroup at most: four wavefronts'; where there are few, 16 or 32, every wavefront with other positions
 constexpr int kAttendMaxSplits = 32;
 
 struct AttendShape {
-    bool     few;
     uint32_t tile, slots, splits;          // rows of a tile, tiles at most, parts of the positions at most
 };
 AttendShape attend_shape(int64_t requests, int64_t tokens, int64_t heads, int64_t group, int64_t longest);
@@ -97,8 +96,8 @@ struct AttendKernel {
     int         threads, lds;
     std::atomic<uint64_t>* raised;         // bit d: its LDS has been asked for on device d
 };
-AttendKernel attend_kernel_f32(int cache_dtype, int dim, bool few);
-AttendKernel attend_kernel_bf16(int cache_dtype, int dim, bool few);
-AttendKernel attend_kernel_f16(int cache_dtype, int dim, bool few);
+AttendKernel attend_kernel_f32(int cache_dtype, int dim, int rows);
+AttendKernel attend_kernel_bf16(int cache_dtype, int dim, int rows);
+AttendKernel attend_kernel_f16(int cache_dtype, int dim, int rows);
 
 }  // namespace ttc

@@ -174,7 +174,10 @@ class Problem:
     ("f16", "f8", "heads", 3, 1, 17, 3, 0, [(50, 1), (0, 1), (400, 2)], 0), ("bf16", "bf16", "slots", 7, 7, 33, 9, 0, [(11, 150)], 5),
     ("bf16", "bf16", "slots", 40, 1, 64, 16, 0, [(20, 1), (77, 1)], 0), ("bf16", "bf16", "slots", 300, 2, 64, 16, 0, [(40, 2)], 0),
     ("bf16", "bf16", "heads", 16, 4, 128, 32, 128, [(0, 500), (700, 90), (1000, 1)], 0), ("f16", "f16", "slots", 2, 1, 1, 2, 0, [(5, 1), (0, 64)], 0),
-    ("bf16", "bf16", "slots", 2, 2, 128, 1, 1, [(300, 1), (2, 70)], 0), ("f16", "q4", "heads", 4, 1, 8, 16, 7, [(300, 100)], 0), ("f16", "q4", "heads", 4, 2, 192, 16, 0, [(300, 1), (128, 30)], 0)])
+    ("bf16", "bf16", "slots", 2, 2, 128, 1, 1, [(300, 1), (2, 70)], 0), ("f16", "q4", "heads", 4, 1, 8, 16, 7, [(300, 100)], 0), ("f16", "q4", "heads", 4, 2, 192, 16, 0, [(300, 1), (128, 30)], 0),
+    ("bf16", "q4", "heads", 24, 1, 128, 16, 0, [(300, 1), (65, 1)], 0), ("f16", "f8", "slots", 6, 2, 64, 16, 40, [(300, 9), (65, 8)], 0), ("f16", "q4", "slots", 8, 1, 96, 8, 0, [(200, 3), (65, 4)], 0),
+    ("bf16", "f8", "heads", 16, 1, 96, 16, 0, [(99, 1), (129, 1)], 0), ("f16", "f16", "heads", 20, 1, 256, 16, 0, [(99, 1), (129, 1)], 0), ("bf16", "q4", "slots", 3, 1, 32, 16, 0, [(99, 1), (700, 1)], 0),
+    ("bf16", "f8", "slots", 3, 1, 32, 16, 9, [(99, 1), (700, 1)], 0), ("bf16", "f8", "slots", 18, 1, 192, 16, 0, [(99, 1), (70, 1)], 0), ("f32", "f32", "slots", 24, 1, 64, 16, 0, [(99, 1), (70, 2)], 0)])
 def test_attend(kind, cache, order, hq, hk, dim, page, window, lengths, pad):
     Problem(kind, cache, order, hq, hk, dim, page, lengths, seed=dim + page, pad=pad).check(dim ** -0.5, window)
 
