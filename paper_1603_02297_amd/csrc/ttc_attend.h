@@ -251,23 +251,40 @@ template <bool WAVE> __device__ __forceinline__ void team_sync()
     }
 }
 
-// The tile of rows of a workgroup, the positions that it goes over, and which of the parts of these it is.
+// The same for all lanes, which the compiler cannot see.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t uniform(uint64_t x) { return (uint64_t)uniform((uint32_t)(x >> 32)) << 32 | uniform((uint32_t)x); }
+
+// Some rows of a request's for one head, and some of the positions that they see.
 struct Work {
     uint32_t request, row0, rows;          // rows: of the request
     uint32_t first_token;                  // of the request
     uint32_t cached;
-    uint32_t lo, hi;                       // of this part
-    uint32_t part, parts;
+    uint32_t lo, hi;
+    uint32_t head;
+    bool     partial;                      // others have other positions of these rows
+    uint32_t partial_row;                  // where row0's result goes then, the others' after it
+    uint32_t parts;                        // of these rows, where this is the first; else 0
 };
 
-// Tile number `slot` is request r's with starts[r] * group / tile + r <= slot: these numbers grow with r, so that the wavefront counts, 64 requests at a time.
-__device__ __forceinline__ uint32_t first_slot(const AttendArgs& p, uint32_t r, uint32_t tile)
+__device__ __forceinline__ uint32_t token_of(const AttendArgs& p, int32_t s) { return s < 0 ? 0u : (uint32_t)s < p.tokens ? (uint32_t)s : p.tokens; }
+
+// The positions that rows first .. last of a request see, within the table.
+__device__ __forceinline__ void positions_of(const AttendArgs& p, uint32_t cached, uint32_t first, uint32_t last, uint32_t* bottom, uint32_t* count)
 {
-    const int32_t s = p.starts[r];
-    return ((s < 0 ? 0u : (uint32_t)s < p.tokens ? (uint32_t)s : p.tokens) * p.group) / tile + r;
+    const uint64_t entries = (uint64_t)p.ld_table * p.page.div;
+    uint64_t hi = (uint64_t)cached + fdiv(last, p.group_div) + 1;
+    hi = hi < entries ? hi : entries;
+    const uint32_t top = hi < 0x7fffffffu ? (uint32_t)hi : 0x7fffffffu, from = cached + fdiv(first, p.group_div) + 1;
+    *bottom = p.window && from > p.window ? from - p.window : 0;
+    *count = top > *bottom ? top - *bottom : 0;
 }
 
-template <typename P, int TILE> __device__ __forceinline__ bool find_work(const AttendArgs& p, uint32_t slot, uint32_t split, Work& w)
+// Many rows: a workgroup a tile of rows, and one of `splits` parts of its positions at most.  Tile number `slot` is request r's with starts[r] * group / tile + r <= slot:
+// these numbers grow with r, so that the wavefront counts, 64 requests at a time.
+__device__ __forceinline__ uint32_t first_slot(const AttendArgs& p, uint32_t r, uint32_t tile) { return token_of(p, p.starts[r]) * p.group / tile + r; }
+
+template <typename P, int TILE> __device__ __forceinline__ bool find_tile(const AttendArgs& p, uint32_t slot, uint32_t split, Work& w)
 {
     const uint32_t lane = threadIdx.x & (kWave - 1);
     uint32_t lo = 0, n = p.requests;
@@ -280,10 +297,9 @@ template <typename P, int TILE> __device__ __forceinline__ bool find_work(const 
         n = n - (count - 1) * step < step ? n - (count - 1) * step : step;
         if (step == 1) n = 1;
     }
-    auto cut = [&](int32_t s) { return s < 0 ? 0u : (uint32_t)s < p.tokens ? (uint32_t)s : p.tokens; };
-    lo = __builtin_amdgcn_readfirstlane(lo);            // the same for all lanes, which the compiler cannot see
-    const uint32_t begin = cut(p.starts[lo]), end = cut(p.starts[lo + 1]);
-    const uint32_t base = first_slot(p, lo, TILE);
+    lo = uniform(lo);
+    const uint32_t begin = uniform(token_of(p, p.starts[lo])), end = uniform(token_of(p, p.starts[lo + 1]));
+    const uint32_t base = uniform(first_slot(p, lo, TILE));
     if (slot < base) return false;
     w.request = lo;
     w.first_token = begin;
@@ -291,30 +307,120 @@ template <typename P, int TILE> __device__ __forceinline__ bool find_work(const 
     w.rows = end > begin ? (end - begin) * p.group : 0;
     if (w.row0 >= w.rows) return false;
     const int32_t c = p.cached[lo];
-    w.cached = c < 0 ? 0 : (uint32_t)c;
-    // what the tile's rows see, within the table
-    const uint32_t last = w.row0 + TILE < w.rows ? w.row0 + TILE - 1 : w.rows - 1;
-    const uint64_t entries = (uint64_t)p.ld_table * p.page.div;
-    uint64_t hi = (uint64_t)w.cached + fdiv(last, p.group_div) + 1;
-    hi = hi < entries ? hi : entries;
-    const uint32_t top = hi < 0x7fffffffu ? (uint32_t)hi : 0x7fffffffu, first = w.cached + fdiv(w.row0, p.group_div) + 1;
-    const uint32_t bottom = p.window && first > p.window ? first - p.window : 0;
-    const uint32_t count = top > bottom ? top - bottom : 0;
-    constexpr uint32_t kUnit = P::kStep > 128 ? P::kStep : 128;
-    w.parts = (count + kUnit - 1) / kUnit;
-    w.parts = w.parts < p.splits ? w.parts : p.splits;
-    w.part = split;
-    if (w.parts <= 1) {
-        w.parts = 1;
-        w.lo = bottom;
-        w.hi = top > bottom ? top : bottom;
-        return split == 0;
+    w.cached = uniform(c < 0 ? 0 : (uint32_t)c);
+    uint32_t bottom, count;
+    positions_of(p, w.cached, w.row0, w.row0 + TILE < w.rows ? w.row0 + TILE - 1 : w.rows - 1, &bottom, &count);
+    uint32_t parts = (count + kAttendUnit - 1) / kAttendUnit, each = count;
+    parts = parts < p.splits ? parts : p.splits;
+    if (parts > 1) {
+        each = ((count + parts - 1) / parts + P::kStep - 1) / P::kStep * P::kStep;
+        parts = (count + each - 1) / each;
     }
-    const uint32_t each = ((count + w.parts - 1) / w.parts + P::kStep - 1) / P::kStep * P::kStep;
-    w.parts = (count + each - 1) / each;
+    w.parts = split == 0 ? (parts > 1 ? parts : 1) : 0;
+    w.partial = parts > 1;
+    if (split >= (parts > 1 ? parts : 1)) return false;
     w.lo = bottom + split * each;
-    w.hi = top - w.lo < each ? top : w.lo + each;
-    return split < w.parts;
+    w.hi = bottom + count - w.lo < each ? bottom + count : w.lo + each;
+    return true;
+}
+
+// Few rows: the work is cut into units, up to kAttendUnit positions of a tile of rows for one head, request by request, tile by tile, head by head; workgroup g has
+// the g-th share of them, equal but for one, whatever the requests' lengths are.  A share begins and ends within a tile's positions as a rule: at most
+// two of its results are partial ones, the first (of a tile that begins in another share: place 2 g) and the last (of one that ends in another: 2 g + 1).
+struct Units {
+    uint32_t tiles, each;                  // of the request's rows, units of one of them
+    uint32_t bottom, count;                // positions that some row sees
+    uint32_t begin, rows, cached;
+};
+template <int TILE> __device__ __forceinline__ Units units_of(const AttendArgs& p, uint32_t r)
+{
+    Units u = {};
+    u.begin = token_of(p, p.starts[r]);
+    const uint32_t end = token_of(p, p.starts[r + 1]);
+    if (end <= u.begin) return u;
+    const int32_t c = p.cached[r];
+    u.rows = (end - u.begin) * p.group;
+    u.cached = c < 0 ? 0 : (uint32_t)c;
+    positions_of(p, u.cached, 0, u.rows - 1, &u.bottom, &u.count);
+    u.tiles = (u.rows + TILE - 1) / TILE;
+    u.each = u.count > kAttendUnit ? (u.count + kAttendUnit - 1) / kAttendUnit : 1;        // none to see: still a result to write
+    return u;
+}
+
+struct Shares {
+    uint64_t all, each, more;              // units, units of a share, shares that have one more
+    __device__ __forceinline__ uint64_t first(uint32_t g) const { return each * g + (g < more ? g : more); }
+    __device__ __forceinline__ uint32_t of(uint64_t unit) const
+    {
+        const uint64_t large = more * (each + 1);
+        return (uint32_t)(unit < large ? unit / (each + 1) : more + (unit - large) / each);
+    }
+};
+
+// The request that this workgroup's share begins in, and the unit of it.
+struct Start {
+    uint32_t request;
+    uint64_t unit;
+};
+template <int TILE, int THREADS> __device__ __forceinline__ bool find_share(const AttendArgs& p, Shares& s, Start& start)
+{
+    constexpr int kWaves = THREADS / kWave;
+    __shared__ uint64_t totals[kWaves];
+    __shared__ uint32_t longest[kWaves];
+    __shared__ uint64_t found[2];
+    const uint32_t lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const uint32_t each = (p.requests + THREADS - 1) / THREADS, first = threadIdx.x * each, last = first + each < p.requests ? first + each : p.requests;
+    uint64_t mine = 0;
+    uint32_t most = 1;
+    for (uint32_t r = first; r < last; ++r) {
+        const Units u = units_of<TILE>(p, r);
+        mine += (uint64_t)u.tiles * u.each;
+        most = u.each > most ? u.each : most;
+    }
+    uint64_t sum = mine;                    // over this lane and those before it
+    for (int i = 1; i < kWave; i <<= 1) {
+        const uint64_t before = __shfl_up(sum, i);
+        const uint32_t other = __shfl_xor(most, i);
+        sum += lane >= (uint32_t)i ? before : 0;
+        most = other > most ? other : most;
+    }
+    if (lane == kWave - 1) { totals[wave] = sum; longest[wave] = most; }
+    __syncthreads();
+    uint64_t before = 0, all = 0;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+        before += (uint32_t)k < wave ? totals[k] : 0;
+        all += totals[k];
+        most = longest[k] > most ? longest[k] : most;
+    }
+    s.all = uniform(all * p.heads);
+    most = uniform(most);
+    if (s.all == 0) return false;
+    // a tile's positions lie in kAttendMaxParts shares at most
+    const uint64_t least = (most + kAttendMaxParts - 2) / (kAttendMaxParts - 1);
+    uint64_t shares = s.all / least;
+    shares = shares < 1 ? 1 : shares < gridDim.x ? shares : gridDim.x;
+    s.each = s.all / shares;
+    s.more = s.all - s.each * shares;
+    if (blockIdx.x >= shares) return false;
+    const uint64_t want = s.first(blockIdx.x);
+    uint64_t at = (before + sum - mine) * p.heads;
+    if (want >= at && want < at + mine * p.heads) {
+        for (uint32_t r = first; r < last; ++r) {
+            const Units u = units_of<TILE>(p, r);
+            const uint64_t n = (uint64_t)u.tiles * u.each * p.heads;
+            if (want < at + n) {
+                found[0] = r;
+                found[1] = want - at;
+                break;
+            }
+            at += n;
+        }
+    }
+    __syncthreads();
+    start.request = (uint32_t)uniform(found[0]);
+    start.unit = uniform(found[1]);
+    return true;
 }
 
 // The largest, and the sum, of a row's lanes.
@@ -364,7 +470,7 @@ template <> struct Bad<float> {
 };
 
 template <typename T, typename C, int DP, int ROWS, bool OWN>
-__global__ __launch_bounds__((Plan<T, C, DP, ROWS, OWN>::kThreads), (Plan<T, C, DP, ROWS, OWN>::kResident)) void attend_kernel(AttendArgs p)
+__device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, char* lds)
 {
     typedef Plan<T, C, DP, ROWS, OWN> P;
     constexpr bool FEW = P::FEW;
@@ -375,12 +481,10 @@ __global__ __launch_bounds__((Plan<T, C, DP, ROWS, OWN>::kThreads), (Plan<T, C, 
     typedef typename Fragment<KE>::type KFrag;
     typedef typename Fragment<VE>::type VFrag;
     constexpr int kBlocks = P::kKeys / M, kSteps = DP / P::kDims, kOut = DP / M;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
-    const uint32_t lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), part = lane / M, column = lane % M;
-    const uint32_t head = blockIdx.y, slot = blockIdx.x, split = blockIdx.z;
-    Work w;
-    if (!find_work<P, ROWS>(p, p.slots_of_tiles - 1 - slot, split, w)) return;        // the last tiles see most: first
-
+    uint32_t thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));        // what follows from it is found again for every piece of work: kept over them, it would take the registers of the loads
+    const uint32_t lane = thread & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(thread / kWave), part = lane / M, column = lane % M;
+    const uint32_t head = w.head;
     // this lane's row; behind the request's last one, that one again
     const uint32_t own = w.row0 + (FEW ? 0 : wave * M) + column, row = own < w.rows ? own : w.rows - 1;
     const uint32_t in_request = fdiv(row, p.group_div), q_head = head * p.group + (row - in_request * p.group);
@@ -440,7 +544,7 @@ __global__ __launch_bounds__((Plan<T, C, DP, ROWS, OWN>::kThreads), (Plan<T, C, 
     char *keys = tile, *values = tile + (OWN ? 0 : P::kKeys * P::kKeyRow);
     float* key_step = reinterpret_cast<float*>(values + P::kKeys * P::kValueRow);           // kCodes: four arrays of kKeys
     float *key_low = key_step + P::kKeys, *value_step = key_low + P::kKeys, *value_low = value_step + P::kKeys;
-    uint32_t member = FEW ? lane : threadIdx.x;
+    uint32_t member = FEW ? lane : thread;
     const char* k_cache = static_cast<const char*>(p.k_cache) + (int64_t)head * p.stride_head * (int64_t)sizeof(C);
     const char* v_cache = static_cast<const char*>(p.v_cache) + (int64_t)head * p.stride_head * (int64_t)sizeof(C);
     const int32_t* table = p.table + (int64_t)w.request * p.ld_table;
@@ -806,12 +910,11 @@ __global__ __launch_bounds__((Plan<T, C, DP, ROWS, OWN>::kThreads), (Plan<T, C, 
     low_sum = sum_of_row<M>(low_sum);
     const float v_scale = std::is_same<C, f8>::value && p.v_scale ? p.v_scale[head] : 1.f;
     // Writes four neighbouring elements of a row's result, normalized: to the result, or to this part's place.
-    auto write = [&](uint32_t to_token, uint32_t to_head, uint32_t d, const float* x) {
+    auto write = [&](uint32_t of, uint32_t to_token, uint32_t to_head, uint32_t d, const float* x) {
         if (d >= p.dim) return;
-        const int64_t r = (int64_t)to_token * p.q_heads + to_head;
         const uint32_t left = p.dim - d;
-        if (w.parts > 1) {
-            float* to = p.partial + (r * p.splits + w.part) * p.dim + d;
+        if (w.partial) {
+            float* to = p.partial + (int64_t)(w.partial_row + of - w.row0) * p.dim + d;
             if (left >= 4) { Vec<float, 4> v; narrow(x, v); store_vec<float, 4, false>(to, v); }
             else for (uint32_t i = 0; i < left; ++i) to[i] = x[i];
         } else {
@@ -820,12 +923,16 @@ __global__ __launch_bounds__((Plan<T, C, DP, ROWS, OWN>::kThreads), (Plan<T, C, 
             else for (uint32_t i = 0; i < left; ++i) to[i] = (T)x[i];
         }
     };
-    auto write_lse = [&](uint32_t to_token, uint32_t to_head, float m, float l) {
+    auto write_lse = [&](uint32_t of, uint32_t to_token, uint32_t to_head, float m, float l) {
         const int64_t r = (int64_t)to_token * p.q_heads + to_head;
+        const uint32_t place = w.partial_row + of - w.row0;
         const float value = l > 0.f || l != l ? m * 0.693147180559945f + __builtin_logf(l) : -__builtin_inff();
-        if (w.parts > 1) p.partial_lse[r * p.splits + w.part] = value;
+        if (w.partial) p.partial_lse[place] = value;
         else if (p.lse) p.lse[r] = value;
-        if (w.part == 0 && p.parts) p.parts[r] = (int32_t)w.parts;
+        if (w.parts && p.parts) {
+            p.parts[2 * r] = (int32_t)place;
+            p.parts[2 * r + 1] = (int32_t)w.parts;
+        }
     };
     if constexpr (FEW) {
         // the wavefronts' results to the largest of their maxima, then added up
@@ -846,7 +953,7 @@ __global__ __launch_bounds__((Plan<T, C, DP, ROWS, OWN>::kThreads), (Plan<T, C, 
             }
             __syncthreads();
             const uint32_t some = rows - first < (uint32_t)P::kMergeRows ? rows - first : P::kMergeRows;
-            for (uint32_t i = threadIdx.x; i < some * (DP / 4); i += P::kThreads) {
+            for (uint32_t i = thread; i < some * (DP / 4); i += P::kThreads) {
                 const uint32_t r = i / (DP / 4), row_of = first + r, d = i % (DP / 4) * 4;
                 float m = -__builtin_inff(), l = 0.f, low = 0.f, x[4] = {};
 #pragma unroll
@@ -866,8 +973,8 @@ __global__ __launch_bounds__((Plan<T, C, DP, ROWS, OWN>::kThreads), (Plan<T, C, 
                 const float inverse = l == 0.f ? 0.f : v_scale / l;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x[j] = (x[j] + low) * inverse;
-                write(w.first_token + in, h, d, x);
-                if (d == 0) write_lse(w.first_token + in, h, m, l);
+                write(w.row0 + row_of, w.first_token + in, h, d, x);
+                if (d == 0) write_lse(w.row0 + row_of, w.first_token + in, h, m, l);
             }
         }
     } else {
@@ -880,9 +987,67 @@ __global__ __launch_bounds__((Plan<T, C, DP, ROWS, OWN>::kThreads), (Plan<T, C, 
                 float x[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) x[c] = (out[d][4 * j + c] + low_sum) * inverse;
-                write(token, q_head, d * M + j * kGap + part * 4, x);
+                write(own, token, q_head, d * M + j * kGap + part * 4, x);
             }
-        if (part == 0) write_lse(token, q_head, top, sum);
+        if (part == 0) write_lse(own, token, q_head, top, sum);
+    }
+}
+
+template <typename T, typename C, int DP, int ROWS, bool OWN>
+__global__ __launch_bounds__((Plan<T, C, DP, ROWS, OWN>::kThreads), (Plan<T, C, DP, ROWS, OWN>::kResident)) void attend_kernel(AttendArgs p)
+{
+    typedef Plan<T, C, DP, ROWS, OWN> P;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    Work w;
+    if constexpr (!P::FEW) {
+        const uint32_t slot = p.slots_of_tiles - 1 - blockIdx.x;            // the last tiles see most: first
+        w.head = blockIdx.y;
+        if (!find_tile<P, ROWS>(p, slot, blockIdx.z, w)) return;
+        w.partial_row = ((slot * p.heads + w.head) * p.splits + blockIdx.z) * ROWS;
+        attend_work<T, C, DP, ROWS, OWN>(p, w, lds);
+    } else {
+        Shares s;
+        Start start;
+        if (!find_share<ROWS, P::kThreads>(p, s, start)) return;
+        uint64_t left = s.first(blockIdx.x + 1) - s.first(blockIdx.x), unit = s.first(blockIdx.x);
+        uint32_t r = start.request;
+        auto units = [&](uint32_t of) {
+            Units x = units_of<ROWS>(p, of);
+            x = {uniform(x.tiles), uniform(x.each), uniform(x.bottom), uniform(x.count), uniform(x.begin), uniform(x.rows), uniform(x.cached)};
+            return x;
+        };
+        Units u = units(r);
+        const uint64_t index = start.unit / u.each;
+        uint32_t done = (uint32_t)(start.unit - index * u.each), tile = (uint32_t)(index / p.heads), head = (uint32_t)(index - (uint64_t)tile * p.heads);
+        while (true) {
+            const uint32_t rest = u.each - done, take = left < rest ? (uint32_t)left : rest;
+            w.request = r;
+            w.row0 = tile * ROWS;
+            w.rows = u.rows;
+            w.first_token = u.begin;
+            w.cached = u.cached;
+            w.head = head;
+            const uint32_t from = done * kAttendUnit, to = (done + take) * kAttendUnit;
+            w.lo = u.bottom + (from < u.count ? from : u.count);
+            w.hi = u.bottom + (to < u.count ? to : u.count);
+            w.partial = take < u.each;
+            w.partial_row = (2 * blockIdx.x + (done == 0)) * ROWS;
+            w.parts = done ? 0 : w.partial ? s.of(unit + u.each - 1) - blockIdx.x + 1 : 1;
+            attend_work<T, C, DP, ROWS, OWN>(p, w, lds);
+            left -= take;
+            unit += take;
+            if (left == 0) break;
+            __syncthreads();                                                // LDS is used again
+            done = 0;
+            if (++head < p.heads) continue;
+            head = 0;
+            if (++tile < u.tiles) continue;
+            tile = 0;
+            do {
+                if (++r >= p.requests) return;
+                u = units(r);
+            } while (u.tiles == 0);
+        }
     }
 }
 

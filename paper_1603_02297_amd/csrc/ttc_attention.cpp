@@ -42,9 +42,16 @@ AttendShape attend_shape(int64_t requests, int64_t tokens, int64_t heads, int64_
     s.tile = rows <= 16 * requests ? 16 : rows <= 48 * requests ? 32 : kTileMany;
     // request r's tiles are numbered from starts[r] * group / tile + r on: always enough, and found without a sum over the requests
     s.slots = (uint32_t)(rows / s.tile + requests);
-    // where tiles alone do not fill the device, several workgroups share a tile's positions, 128 of them at least
-    const int64_t groups = std::max<int64_t>((int64_t)s.slots * heads, 1), wanted = s.tile < kTileMany ? 4096 : 1024;
-    s.splits = (uint32_t)std::min<int64_t>({std::max<int64_t>(wanted / groups, 1), (longest + 127) / 128 + (longest < 1), kAttendMaxSplits});
+    const int64_t groups = std::max<int64_t>((int64_t)s.slots * heads, 1), units = std::max<int64_t>((longest + kAttendUnit - 1) / kAttendUnit, 1);
+    if (s.tile < kTileMany) {
+        s.shares = (uint32_t)(groups >= kAttendShares / units ? std::min<int64_t>(kAttendShares, groups * units) : groups * units);
+        s.splits = 1;
+        s.partial_rows = units > 1 ? 2 * (int64_t)s.shares * s.tile : 0;
+    } else {
+        // where tiles alone do not fill the device, several workgroups share a tile's positions
+        s.splits = (uint32_t)std::min<int64_t>({std::max<int64_t>(1024 / groups, 1), units, kAttendMaxSplits});
+        s.partial_rows = s.splits > 1 ? groups * s.splits * s.tile : 0;
+    }
     return s;
 }
 
@@ -145,12 +152,13 @@ bool attend_sizes(const ttc_attend_s* a, int64_t requests, int64_t tokens, int64
            (__int128)(requests + tokens * a->q_heads) * a->heads <= INT32_MAX && ld_table <= (int64_t)1 << 40;
 }
 
-int64_t longest_context(const ttc_attend_s* a, int64_t ld_table)
+// Positions that the rows of a tile see together, at most.
+int64_t longest_context(const ttc_attend_s* a, int64_t tokens, int64_t ld_table)
 {
     int64_t n;
     if (__builtin_mul_overflow(ld_table, a->page, &n)) n = INT32_MAX;
     n = std::min<int64_t>(n, INT32_MAX);
-    return a->window ? std::min<int64_t>(n, a->window + kTileMany) : n;
+    return a->window ? std::min<int64_t>(n, a->window + std::max<int64_t>(tokens, kTileMany)) : n;
 }
 
 // An angle as a fraction of a turn in units of 2^-64, whole turns dropped.
@@ -334,9 +342,8 @@ int64_t ttc_attend_workspace(ttc_attend_t attend, int64_t requests, int64_t toke
     if (requests < 0 || tokens < 0 || ld_table < 0) return -TTC_ERR_INVALID_VALUE;
     if (!attend_sizes(attend, requests, tokens, ld_table)) return -TTC_ERR_OVERFLOW;
     if (requests == 0 || tokens == 0) return 0;
-    const AttendShape s = attend_shape(requests, tokens, attend->heads, attend->q_heads / attend->heads, longest_context(attend, ld_table));
-    const int64_t rows = tokens * attend->q_heads;
-    return s.splits > 1 ? rows * s.splits * (attend->dim + 1) * 4 + rows * 4 : 0;
+    const AttendShape s = attend_shape(requests, tokens, attend->heads, attend->q_heads / attend->heads, longest_context(attend, tokens, ld_table));
+    return s.partial_rows ? s.partial_rows * (attend->dim + 1) * 4 + tokens * attend->q_heads * 8 : 0;
 }
 
 int ttc_attend_pages(ttc_attend_t attend, int64_t requests, int64_t tokens, const void* q, int64_t ldq, const int32_t* starts, const int32_t* cached,
@@ -361,14 +368,13 @@ int ttc_attend_pages(ttc_attend_t attend, int64_t requests, int64_t tokens, cons
                                  {lse, 4 * (uint64_t)(tokens * attend->q_heads), 4, true}, {work ? workspace : nullptr, (uint64_t)work, 16, true}});
     if (st != TTC_OK) return st;
     const int64_t group = attend->q_heads / attend->heads;
-    const AttendShape s = attend_shape(requests, tokens, attend->heads, group, longest_context(attend, ld_table));
+    const AttendShape s = attend_shape(requests, tokens, attend->heads, group, longest_context(attend, tokens, ld_table));
     AttendArgs a = {};
     a.q = q; a.k_cache = k_cache; a.v_cache = v_cache; a.out = out; a.lse = lse;
     if (work) {
-        const int64_t n = tokens * attend->q_heads;
         a.partial = static_cast<float*>(workspace);
-        a.partial_lse = a.partial + n * s.splits * attend->dim;
-        a.parts = reinterpret_cast<int32_t*>(a.partial_lse + n * s.splits);
+        a.partial_lse = a.partial + s.partial_rows * attend->dim;
+        a.parts = reinterpret_cast<int32_t*>(a.partial_lse + s.partial_rows);
     }
     a.k_scale = k_scale; a.v_scale = v_scale;
     a.starts = starts; a.cached = cached; a.table = table;
@@ -378,6 +384,8 @@ int ttc_attend_pages(ttc_attend_t attend, int64_t requests, int64_t tokens, cons
     a.q_heads = (uint32_t)attend->q_heads; a.heads = (uint32_t)attend->heads; a.group = (uint32_t)group;
     a.dim = (uint32_t)attend->dim; a.pages = (uint32_t)attend->pages;
     a.splits = s.splits; a.slots_of_tiles = s.slots;
+    a.partial_rows = (uint32_t)s.partial_rows;
+    a.join_step = s.tile < kTileMany ? 2 * s.tile : s.tile; a.join_back = s.tile < kTileMany ? s.tile : 0;
     a.window = (uint32_t)attend->window;
     a.page = attend->page_div;
     a.group_div = make_fastdiv((uint32_t)group);

@@ -68,13 +68,15 @@ HeadsShape cut_heads(HeadsArgs& a);          // sets what the cut says of a, too
 struct AttendArgs {
     const void    *q, *k_cache, *v_cache;
     void          *out;
-    float         *lse, *partial, *partial_lse;        // partial results: [row][split][dim], [row][split], of row = token * q_heads + head
-    int32_t       *parts;                              // [row]: how many parts it has
+    float         *lse, *partial, *partial_lse;        // partial results: rows of dim elements, and the logarithms of their sums
+    int32_t       *parts;                              // [token][q_head][2]: the first of its partial results, and how many there are
     const float   *k_scale, *v_scale;
     const int32_t *starts, *cached, *table;
     int64_t        ld_q, ld_o, ld_table;
     int64_t        stride_head, stride_slot, stride_page;
     uint32_t       tokens, requests, q_heads, heads, group, dim, pages, splits, slots_of_tiles;
+    uint32_t       partial_rows;
+    uint32_t       join_step, join_back;               // part i > 0 of a row lies i * step - back behind its first
     uint32_t       window;                             // 0: none
     FastDiv        page, group_div;
     float          scale;                              // with log2(e)
@@ -83,9 +85,13 @@ struct AttendArgs {
 
 constexpr int kTileMany = 128;             // rows of a workgroup at most: four wavefronts'; where there are few, 16 or 32, every wavefront with other positions
 constexpr int kAttendMaxSplits = 32;
+constexpr int64_t kAttendShares = 768;
+constexpr uint32_t kAttendUnit = 128, kAttendMaxParts = 128;     // positions that are not shared among workgroups; results that a row may have to be joined from
 
 struct AttendShape {
     uint32_t tile, slots, splits;          // rows of a tile, tiles at most, parts of the positions at most
+    uint32_t shares;                       // workgroups, where rows are few
+    int64_t  partial_rows;                 // 0: every row's positions are one workgroup's
 };
 AttendShape attend_shape(int64_t requests, int64_t tokens, int64_t heads, int64_t group, int64_t longest);
 
