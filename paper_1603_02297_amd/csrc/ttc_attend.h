@@ -11,7 +11,8 @@
 //                positions, in LDS of its own; no barrier until they add up their results.  Bound by the cache's bytes.
 //   ROWS 128     prompts: wavefronts have 32 rows each of the same 128 and share the tiles.  Bound by the matrix instructions, and the exponentials beside them.
 //   OWN          few rows over narrow caches, where dim is what the kernel is compiled for: a lane has a part of the vectors of positions of its own.  Keys are
-//                never in LDS: these parts are what the left operand of S^T holds in a lane, in an order of the dims that the queries follow.
+//                never in LDS: these parts are what the left operand of S^T holds in a lane, in an order of the dims that the queries follow.  Values are there as the
+//                cache has them, and widened behind the transposing loads, which there are for 8 and 4 bits, too.
 //
 // A tile's loads are under way while the one before it is used, its entries of the block table one tile earlier.
 #pragma once
@@ -28,6 +29,7 @@ namespace attend {
 
 typedef short Short4 __attribute__((ext_vector_type(4)));
 typedef short Short8 __attribute__((ext_vector_type(8)));
+typedef int Int2 __attribute__((ext_vector_type(2)));
 #define TTC_LDS __attribute__((address_space(3)))
 
 template <int M> struct Result;            // of a product, M x M over the wavefront: register i of a lane is row kGap * (i / 4) + 4 * part + i % 4, its column lane % M
@@ -76,13 +78,14 @@ template <typename T, typename C, int DP, int ROWS, bool OWN> struct Plan {
     static constexpr int  kThreads = kWaves * kWave;
     static constexpr int  kTeams = FEW ? kWaves : 1;
     static constexpr int  kTeam = FEW ? kWave : kThreads;                    // threads that load a tile together
-    static constexpr int  kKeys = FEW || (kWide && DP > 128) ? 32 : 64;      // positions of a tile
+    static constexpr int  kKeys = (FEW && !(OWN && kRecords && M == 16)) || (kWide && DP > 128) ? 32 : 64;     // positions of a tile
     static constexpr int  kStep = kKeys * kTeams;
     static constexpr int  kChunks = DP / 8;                                  // of eight elements, of a vector
     static constexpr int  kMine = kKeys * kChunks / kTeam;                   // chunks of a tile that a thread loads
     static constexpr bool kAhead = !(FEW && kWide && DP > 128);              // loads of the next tile under way beside the products of this one
     // rows in LDS end 16 and 32 bytes later than their elements, so that eight rows (four, of values) meet all banks
-    static constexpr int  kKeyRow = DP * (int)sizeof(K) + 16, kValueRow = DP * (int)sizeof(V) + (kWide ? 16 : 32);
+    static constexpr int  kKeyRow = DP * (int)sizeof(K) + 16;
+    static constexpr int  kValueRow = OWN ? (kRecords ? DP / 2 : DP) + 8 : DP * (int)sizeof(V) + (kWide ? 16 : 32);
     static constexpr int  kTile = kKeys * ((OWN ? 0 : kKeyRow) + kValueRow) + (kCodes ? 4 * kKeys * 4 : 0);
     // The queries' fragments in LDS, the same for all wavefronts, where keys and values on their way take the registers.
     static constexpr bool kQueriesInLds = ROWS == 32 && !OWN && sizeof(C) == 2;
@@ -93,7 +96,8 @@ template <typename T, typename C, int DP, int ROWS, bool OWN> struct Plan {
     static constexpr int  kMerge = FEW ? kWaves * kMergeRows * kMergeRow * 4 + 3 * kWaves * ROWS * 4 : 0;
     static constexpr int  kLds = kTile * kTeams + kQueries > kMerge ? kTile * kTeams + kQueries : kMerge;
     // workgroups that share a compute unit, and so its registers
-    static constexpr int  kResident = !kWide && DP <= 128 && 2 * kLds <= kMaxLdsBytes ? 2 : 1;
+    static constexpr int  kResident = OWN ? attend_resident(sizeof(T), sizeof(C), DP, ROWS) : attend_resident(sizeof(T), sizeof(T), DP, ROWS);
+    static_assert(kResident * (kLds + 256) <= kMaxLdsBytes, "they share its LDS");
     // OWN: the words of a part of a vector, a lane's, and the positions that it has such a part of
     static constexpr int  kWords = (kRecords ? DP / 2 : DP * (int)sizeof(C)) / kParts / 4, kPositions = kKeys / M;
     static_assert(kKeys * kChunks % kTeam == 0 && DP % 32 == 0 && kLds <= kMaxLdsBytes, "a tile is loaded in whole chunks");
@@ -165,14 +169,15 @@ __device__ __forceinline__ bool any_bad(const Chunk8<q4>& c)
 
 // Eight codes as 16 + code, which 16 bits hold.  Scores take the 16 back with the minimum; values have 24 times the sum of their weights, as they were
 // rounded, taken back, so that a weight's rounding is off by that of code - 8 times the step.
-__device__ __forceinline__ void codes_of(uint32_t word, uint32_t one, int shift, uint32_t* w)
+// A byte's two codes go to the two halves of a word by a product: byte * (2^shift + 2^(shift + 12)).
+template <int SHIFT> __device__ __forceinline__ void codes_of(uint32_t word, uint32_t one, uint32_t* w)
 {
-    const uint32_t even = word & 0x0f0f0f0fu, odd = word >> 4 & 0x0f0f0f0fu;
+    asm("" : "+v"(one));                    // an instruction takes one constant from elsewhere than a vector register: the mask
 #pragma unroll
-    for (uint32_t k = 0; k < 4; ++k) w[k] = __builtin_amdgcn_perm(odd, even, 0x0c000c00u | (4 + k) << 16 | k) << shift | one;
+    for (int k = 0; k < 4; ++k) w[k] = (word >> (8 * k) & 0xffu) * (0x1001u << SHIFT) & (0x000f000fu << SHIFT) | one;
 }
-__device__ __forceinline__ void codes_of(uint32_t word, Vec<__bf16, 8>& r) { codes_of(word, 0x41804180u, 3, r.w); }
-__device__ __forceinline__ void codes_of(uint32_t word, Vec<_Float16, 8>& r) { codes_of(word, 0x4c004c00u, 6, r.w); }
+__device__ __forceinline__ void codes_of(uint32_t word, Vec<__bf16, 8>& r) { codes_of<3>(word, 0x41804180u, r.w); }
+__device__ __forceinline__ void codes_of(uint32_t word, Vec<_Float16, 8>& r) { codes_of<6>(word, 0x4c004c00u, r.w); }
 
 __device__ __forceinline__ void widen_eight(const Vec<f8, 8>& c, Vec<float, 8>& r)
 {
@@ -658,11 +663,13 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
 #pragma unroll
         for (int b = 0; b < P::kPositions; ++b) {
             if (holes && !(there >> (column + M * b) & 1)) r[b] = {};
+            char* to = values + (column + M * b) * P::kValueRow + part * (P::kWords * 4);
+            constexpr int kUnit = P::kWords % 2 ? 1 : 2;
 #pragma unroll
-            for (int i = 0; i < DP / kParts / 8; ++i) {
-                const Chunk8<C> c = chunk_of_part(r[b], i);
-                store_chunk<VE, true>(values + (column + M * b) * P::kValueRow + (part * (DP / kParts) + 8 * i) * sizeof(VE), c);
-                if (!P::kCodes && look) bad |= any_bad(c);
+            for (int i = 0; i < P::kWords; i += kUnit) __builtin_memcpy(__builtin_assume_aligned(to + 4 * i, 4 * kUnit), r[b].w + i, 4 * kUnit);
+            if (!P::kCodes && look) {
+#pragma unroll
+                for (int i = 0; i < DP / kParts / 8; ++i) bad |= any_bad(chunk_of_part(r[b], i));
             }
         }
         return bad;
@@ -724,19 +731,9 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
         const bool look = holes || end > tile_lowest + 1 || (p.window && at + p.window <= w.cached + fdiv(w.row0 + ROWS < w.rows ? w.row0 + ROWS - 1 : w.rows - 1, p.group_div));
         bool bad;
         team_sync<FEW>();                                                   // the tile before has been used
-        Part now_k[P::kPositions];
         if constexpr (OWN) {
-#pragma unroll
-            for (int b = 0; b < P::kPositions; ++b) now_k[b] = part_k[b];
             if constexpr (P::kCodes) put_steps(part_k, part_v);
             bad = put_parts(part_v, now, holes, look);
-            if (at + P::kStep < w.hi) {
-                spot = spot_of(at + P::kStep, entry);
-                here = __ballot(spot.here);
-                load_parts(k_cache, spot.offset, part_k);
-                load_parts(v_cache, spot.offset, part_v);
-                entry = look_up(at + 2 * P::kStep);
-            }
         } else if constexpr (P::kAhead) {
             put_keys(raw_k);
             bad = put_values(raw_v, now, holes, look);
@@ -765,7 +762,7 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
         } else {
             __syncthreads();
         }
-        if (idle || at > highest || (p.window && (uint64_t)end + p.window <= (uint64_t)lowest + 1)) continue;       // nothing that this wavefront's rows see
+        if (!FEW && (idle || at > highest || (p.window && (uint64_t)end + p.window <= (uint64_t)lowest + 1))) continue;       // nothing that this wavefront's rows see
 
         Acc score[kBlocks] = {};
 #pragma unroll
@@ -773,8 +770,17 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
             const char* from = keys + (b * M + column) * P::kKeyRow + part * 16;
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                if constexpr (OWN) mul(fragment_of<KE>(chunk_of_part(now_k[b], i)), query[i], score[b]);
+                if constexpr (OWN) mul(fragment_of<KE>(chunk_of_part(part_k[b], i)), query[i], score[b]);
                 else mul(*reinterpret_cast<const KFrag*>(from + i * P::kDims * sizeof(KE)), query_of(i), score[b]);
+            }
+        }
+        if constexpr (OWN) {
+            if (at + P::kStep < w.hi) {
+                spot = spot_of(at + P::kStep, entry);
+                here = __ballot(spot.here);
+                load_parts(k_cache, spot.offset, part_k);
+                load_parts(v_cache, spot.offset, part_v);
+                entry = look_up(at + 2 * P::kStep);
             }
         }
         // register i of block b is position M b + kGap (i / 4) + 4 part + i % 4
@@ -858,18 +864,38 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
 #pragma unroll
                 for (int e = 0; e < 4; ++e) low_sum = __builtin_amdgcn_fdot2_f32_bf16(Two{weight[k][2 * e], weight[k][2 * e + 1]}, back, low_sum, false);
         }
-        auto value = [&](int k, int d) -> VFrag {
-            if constexpr (sizeof(VE) == 4) {
-                VFrag r;
-                const char* from = values + (k * 4 * kParts + part * 4) * P::kValueRow + (d * M + column) * 4;
+        // the left operands of rows d * M ... of the result
+        auto values_of = [&](int d, VFrag* v) {
+            const uint32_t in = lane & 15, at_column = d * M + (M == 32 ? (lane >> 4 & 1) * 16 : 0);     // the first of these 16 lanes' columns
+            if constexpr (P::kCodes && OWN) {
+                // a lane's row of 16 codes, in the order of two fragments; a column of them back
+                static_assert(kTakes == 2, "two fragments of eight");
+                const char* from = values + ((in >> 3) * 8 * kParts + part * 4 + (in & 3) + (in >> 2 & 1) * kGap) * P::kValueRow + at_column / 2;
+                const auto r = __builtin_amdgcn_ds_read_tr4_b64_v2i32((TTC_LDS Int2*)from);
+                v[0] = fragment_of<VE>(Chunk8<q4>{(uint32_t)r[0], 0});
+                v[1] = fragment_of<VE>(Chunk8<q4>{(uint32_t)r[1], 0});
+            } else if constexpr (OWN) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) r[e] = *reinterpret_cast<const float*>(from + e * P::kValueRow);
-                return r;
+                for (int k = 0; k < kTakes; ++k) {
+                    const char* from = values + (k * 8 * kParts + part * 4 + (in >> 1 & 3) + (in >> 3) * kGap) * P::kValueRow + at_column + (in & 1) * 8;
+                    const auto r = __builtin_amdgcn_ds_read_tr8_b64_v2i32((TTC_LDS Int2*)from);
+                    v[k] = fragment_of<VE>(__builtin_bit_cast(Chunk8<C>, r));
+                }
+            } else if constexpr (sizeof(VE) == 4) {
+#pragma unroll
+                for (int k = 0; k < kTakes; ++k) {
+                    const char* from = values + (k * 4 * kParts + part * 4) * P::kValueRow + (d * M + column) * 4;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[k][e] = *reinterpret_cast<const float*>(from + e * P::kValueRow);
+                }
             } else {
-                // four rows of 16 elements for each 16 lanes, which get a column of them each
-                const char* from = values + (k * 8 * kParts + part * 4 + (lane & 15) / 4) * P::kValueRow + (d * M + (M == 32 ? (lane >> 4 & 1) * 16 : 0) + (lane & 3) * 4) * 2;
-                const Short4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((TTC_LDS Short4*)from), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((TTC_LDS Short4*)(from + kGap * P::kValueRow));
-                return __builtin_bit_cast(VFrag, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                for (int k = 0; k < kTakes; ++k) {
+                    // four rows of 16 elements for each 16 lanes, which get a column of them each
+                    const char* from = values + (k * 8 * kParts + part * 4 + in / 4) * P::kValueRow + (at_column + (in & 3) * 4) * 2;
+                    const Short4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((TTC_LDS Short4*)from), b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((TTC_LDS Short4*)(from + kGap * P::kValueRow));
+                    v[k] = __builtin_bit_cast(VFrag, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+                }
             }
         };
         if (!P::kCodes && masked && bad) {
@@ -878,11 +904,12 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
 #pragma unroll
             for (int d = 0; d < kOut; ++d) {
                 Acc count = {};
+                VFrag v[kTakes];
+                values_of(d, v);
 #pragma unroll
                 for (int k = 0; k < kTakes; ++k) {
-                    VFrag v = value(k, d);
-                    const VFrag marks = Bad<VE>::marks(v);
-                    mul(v, weight[k], out[d]);
+                    const VFrag marks = Bad<VE>::marks(v[k]);
+                    mul(v[k], weight[k], out[d]);
                     VFrag sees;
 #pragma unroll
                     for (int e = 0; e < kEach; ++e) {
@@ -900,9 +927,12 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
             }
         } else {
 #pragma unroll
-            for (int d = 0; d < kOut; ++d)
+            for (int d = 0; d < kOut; ++d) {
+                VFrag v[kTakes];
+                values_of(d, v);
 #pragma unroll
-                for (int k = 0; k < kTakes; ++k) mul(value(k, d), weight[k], out[d]);
+                for (int k = 0; k < kTakes; ++k) mul(v[k], weight[k], out[d]);
+            }
         }
     }
 
@@ -1060,13 +1090,19 @@ template <typename T, typename C, int DP, int ROWS, bool OWN> AttendKernel kerne
 template <typename T, typename C, int DP> AttendKernel kernel_of(int dim, int rows)
 {
     if constexpr (sizeof(T) == 2 && sizeof(C) == 1)
-        if (rows < 128 && dim == DP) return rows == 16 ? kernel_of<T, C, DP, 16, true>() : kernel_of<T, C, DP, 32, true>();
+        if (attend_own(sizeof(T), sizeof(C), dim, rows)) return rows == 16 ? kernel_of<T, C, DP, 16, true>() : kernel_of<T, C, DP, 32, true>();
     return rows == 16 ? kernel_of<T, C, DP, 16, false>() : rows == 32 ? kernel_of<T, C, DP, 32, false>() : kernel_of<T, C, DP, 128, false>();
 }
 template <typename T, typename C> AttendKernel kernel_of(int dim, int rows)
 {
-    return dim <= 32 ? kernel_of<T, C, 32>(dim, rows) : dim <= 64 ? kernel_of<T, C, 64>(dim, rows) : dim <= 96 ? kernel_of<T, C, 96>(dim, rows)
-         : dim <= 128 ? kernel_of<T, C, 128>(dim, rows) : dim <= 192 ? kernel_of<T, C, 192>(dim, rows) : kernel_of<T, C, 256>(dim, rows);
+    switch (attend_dim(dim)) {
+    case 32:  return kernel_of<T, C, 32>(dim, rows);
+    case 64:  return kernel_of<T, C, 64>(dim, rows);
+    case 96:  return kernel_of<T, C, 96>(dim, rows);
+    case 128: return kernel_of<T, C, 128>(dim, rows);
+    case 192: return kernel_of<T, C, 192>(dim, rows);
+    default:  return kernel_of<T, C, 256>(dim, rows);
+    }
 }
 template <typename T> AttendKernel kernel_of(int cache_dtype, int dim, int rows)
 {

@@ -35,16 +35,18 @@ HeadsShape cut_heads(HeadsArgs& a)
     return s;
 }
 
-AttendShape attend_shape(int64_t requests, int64_t tokens, int64_t heads, int64_t group, int64_t longest)
+AttendShape attend_shape(const ttc_attend_s* a, int64_t requests, int64_t tokens, int64_t longest)
 {
     AttendShape s = {};
-    const int64_t rows = tokens * group;
+    const int64_t heads = a->heads, rows = tokens * (a->q_heads / heads);
     s.tile = rows <= 16 * requests ? 16 : rows <= 48 * requests ? 32 : kTileMany;
     // request r's tiles are numbered from starts[r] * group / tile + r on: always enough, and found without a sum over the requests
     s.slots = (uint32_t)(rows / s.tile + requests);
     const int64_t groups = std::max<int64_t>((int64_t)s.slots * heads, 1), units = std::max<int64_t>((longest + kAttendUnit - 1) / kAttendUnit, 1);
     if (s.tile < kTileMany) {
-        s.shares = (uint32_t)(groups >= kAttendShares / units ? std::min<int64_t>(kAttendShares, groups * units) : groups * units);
+        // as many shares as workgroups fit the device at a time: 96 requests' step takes LATER
+        const int64_t most = 256 * attend_resident(elem_bytes(a->dtype), elem_bytes(a->cache_dtype), (int)a->dim, (int)s.tile);
+        s.shares = (uint32_t)(groups >= most / units ? std::min<int64_t>(most, groups * units) : groups * units);
         s.splits = 1;
         s.partial_rows = units > 1 ? 2 * (int64_t)s.shares * s.tile : 0;
     } else {
@@ -342,7 +344,7 @@ int64_t ttc_attend_workspace(ttc_attend_t attend, int64_t requests, int64_t toke
     if (requests < 0 || tokens < 0 || ld_table < 0) return -TTC_ERR_INVALID_VALUE;
     if (!attend_sizes(attend, requests, tokens, ld_table)) return -TTC_ERR_OVERFLOW;
     if (requests == 0 || tokens == 0) return 0;
-    const AttendShape s = attend_shape(requests, tokens, attend->heads, attend->q_heads / attend->heads, longest_context(attend, tokens, ld_table));
+    const AttendShape s = attend_shape(attend, requests, tokens, longest_context(attend, tokens, ld_table));
     return s.partial_rows ? s.partial_rows * (attend->dim + 1) * 4 + tokens * attend->q_heads * 8 : 0;
 }
 
@@ -368,7 +370,7 @@ int ttc_attend_pages(ttc_attend_t attend, int64_t requests, int64_t tokens, cons
                                  {lse, 4 * (uint64_t)(tokens * attend->q_heads), 4, true}, {work ? workspace : nullptr, (uint64_t)work, 16, true}});
     if (st != TTC_OK) return st;
     const int64_t group = attend->q_heads / attend->heads;
-    const AttendShape s = attend_shape(requests, tokens, attend->heads, group, longest_context(attend, tokens, ld_table));
+    const AttendShape s = attend_shape(attend, requests, tokens, longest_context(attend, tokens, ld_table));
     AttendArgs a = {};
     a.q = q; a.k_cache = k_cache; a.v_cache = v_cache; a.out = out; a.lse = lse;
     if (work) {

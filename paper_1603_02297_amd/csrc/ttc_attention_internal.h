@@ -85,7 +85,14 @@ struct AttendArgs {
 
 constexpr int kTileMany = 128;             // rows of a workgroup at most: four wavefronts'; where there are few, 16 or 32, every wavefront with other positions
 constexpr int kAttendMaxSplits = 32;
-constexpr int64_t kAttendShares = 768;
+// What the kernels are compiled for: dims up to these; and narrow caches of one of them, few rows, in the form that keeps keys out of LDS.
+constexpr int attend_dim(int dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 128 : dim <= 192 ? 192 : 256; }
+constexpr bool attend_own(int bytes, int cache_bytes, int dim, int tile) { return bytes == 2 && cache_bytes == 1 && dim == attend_dim(dim) && tile < 128; }
+// Workgroups that share a compute unit, by registers and LDS.
+constexpr int attend_resident(int bytes, int cache_bytes, int dim, int tile)
+{
+    return bytes == 4 || dim > 128 ? 1 : attend_own(bytes, cache_bytes, dim, tile) && tile == 16 ? 3 : 2;
+}
 constexpr uint32_t kAttendUnit = 128, kAttendMaxParts = 128;     // positions that are not shared among workgroups; results that a row may have to be joined from
 
 struct AttendShape {
@@ -93,7 +100,7 @@ struct AttendShape {
     uint32_t shares;                       // workgroups, where rows are few
     int64_t  partial_rows;                 // 0: every row's positions are one workgroup's
 };
-AttendShape attend_shape(int64_t requests, int64_t tokens, int64_t heads, int64_t group, int64_t longest);
+AttendShape attend_shape(const ttc_attend_s* a, int64_t requests, int64_t tokens, int64_t longest);
 
 int launch_attend(const AttendArgs& a, const AttendShape& s, void* stream);
 // The kernel of a type, and what it needs; one file each.
