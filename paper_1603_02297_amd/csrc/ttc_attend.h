@@ -96,10 +96,12 @@ template <typename T, typename C, int DP, int ROWS, bool OWN> struct Plan {
     static constexpr int  kMerge = FEW ? kWaves * kMergeRows * kMergeRow * 4 + 3 * kWaves * ROWS * 4 : 0;
     static constexpr int  kLds = kTile * kTeams + kQueries > kMerge ? kTile * kTeams + kQueries : kMerge;
     // workgroups that share a compute unit, and so its registers
-    static constexpr int  kResident = OWN ? attend_resident(sizeof(T), sizeof(C), DP, ROWS) : attend_resident(sizeof(T), sizeof(T), DP, ROWS);
+    static constexpr int  kResident = attend_resident(sizeof(T), OWN, kRecords, DP, ROWS);
     static_assert(kResident * (kLds + 256) <= kMaxLdsBytes, "they share its LDS");
     // OWN: the words of a part of a vector, a lane's, and the positions that it has such a part of
+    static constexpr bool kCarries = FEW && kAhead;                          // the next piece of work's first tile is loaded beside the end of this one
     static constexpr int  kWords = (kRecords ? DP / 2 : DP * (int)sizeof(C)) / kParts / 4, kPositions = kKeys / M;
+    struct Part { uint32_t w[kWords], head; };
     static_assert(kKeys * kChunks % kTeam == 0 && DP % 32 == 0 && kLds <= kMaxLdsBytes, "a tile is loaded in whole chunks");
 };
 
@@ -260,6 +262,11 @@ template <bool WAVE> __device__ __forceinline__ void team_sync()
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ uint64_t uniform(uint64_t x) { return (uint64_t)uniform((uint32_t)(x >> 32)) << 32 | uniform((uint32_t)x); }
 
+// What one lane reads for all of them, by a scalar load: it does not wait for the vector loads under way.
+template <typename X> __device__ __forceinline__ X scalar(const X* p, uint32_t i) { return ((const __attribute__((address_space(4))) X*)p)[i]; }
+// Numbers of 64 bits that mostly are of 32.
+__device__ __forceinline__ uint64_t quotient(uint64_t a, uint64_t b) { return (a | b) >> 32 ? a / b : (uint32_t)a / (uint32_t)b; }
+
 // Some rows of a request's for one head, and some of the positions that they see.
 struct Work {
     uint32_t request, row0, rows;          // rows: of the request
@@ -303,16 +310,16 @@ template <typename P, int TILE> __device__ __forceinline__ bool find_tile(const 
         if (step == 1) n = 1;
     }
     lo = uniform(lo);
-    const uint32_t begin = uniform(token_of(p, p.starts[lo])), end = uniform(token_of(p, p.starts[lo + 1]));
-    const uint32_t base = uniform(first_slot(p, lo, TILE));
+    const uint32_t begin = token_of(p, scalar(p.starts, lo)), end = token_of(p, scalar(p.starts, lo + 1));
+    const uint32_t base = begin * p.group / TILE + lo;
     if (slot < base) return false;
     w.request = lo;
     w.first_token = begin;
     w.row0 = (slot - base) * TILE;
     w.rows = end > begin ? (end - begin) * p.group : 0;
     if (w.row0 >= w.rows) return false;
-    const int32_t c = p.cached[lo];
-    w.cached = uniform(c < 0 ? 0 : (uint32_t)c);
+    const int32_t c = scalar(p.cached, lo);
+    w.cached = c < 0 ? 0 : (uint32_t)c;
     uint32_t bottom, count;
     positions_of(p, w.cached, w.row0, w.row0 + TILE < w.rows ? w.row0 + TILE - 1 : w.rows - 1, &bottom, &count);
     uint32_t parts = (count + kAttendUnit - 1) / kAttendUnit, each = count;
@@ -329,21 +336,21 @@ template <typename P, int TILE> __device__ __forceinline__ bool find_tile(const 
     return true;
 }
 
-// Few rows: the work is cut into units, up to kAttendUnit positions of a tile of rows for one head, request by request, tile by tile, head by head; workgroup g has
-// the g-th share of them, equal but for one, whatever the requests' lengths are.  A share begins and ends within a tile's positions as a rule: at most
-// two of its results are partial ones, the first (of a tile that begins in another share: place 2 g) and the last (of one that ends in another: 2 g + 1).
+// Few rows: a head's work is cut into units, up to kAttendUnit positions of a tile of rows, request by request, tile by tile; of the workgroups that have this head, number g
+// has the g-th share of them, equal but for one, whatever the requests' lengths are.  The heads' shares are alike and their workgroups next to each other, so
+// that a slot's heads, neighbours in the cache, are fetched at about the same time.  A share begins and ends within a tile's positions as a rule: at
+// most two of its results are partial ones, the first (of a tile that begins in another share: place 2 b, of workgroup b) and the last (of one that ends in another: 2 b + 1).
 struct Units {
     uint32_t tiles, each;                  // of the request's rows, units of one of them
     uint32_t bottom, count;                // positions that some row sees
     uint32_t begin, rows, cached;
 };
-template <int TILE> __device__ __forceinline__ Units units_of(const AttendArgs& p, uint32_t r)
+template <int TILE> __device__ __forceinline__ Units units_of(const AttendArgs& p, int32_t first, int32_t behind, int32_t c)
 {
     Units u = {};
-    u.begin = token_of(p, p.starts[r]);
-    const uint32_t end = token_of(p, p.starts[r + 1]);
+    u.begin = token_of(p, first);
+    const uint32_t end = token_of(p, behind);
     if (end <= u.begin) return u;
-    const int32_t c = p.cached[r];
     u.rows = (end - u.begin) * p.group;
     u.cached = c < 0 ? 0 : (uint32_t)c;
     positions_of(p, u.cached, 0, u.rows - 1, &u.bottom, &u.count);
@@ -358,7 +365,7 @@ struct Shares {
     __device__ __forceinline__ uint32_t of(uint64_t unit) const
     {
         const uint64_t large = more * (each + 1);
-        return (uint32_t)(unit < large ? unit / (each + 1) : more + (unit - large) / each);
+        return (uint32_t)(unit < large ? quotient(unit, each + 1) : more + quotient(unit - large, each));
     }
 };
 
@@ -367,7 +374,7 @@ struct Start {
     uint32_t request;
     uint64_t unit;
 };
-template <int TILE, int THREADS> __device__ __forceinline__ bool find_share(const AttendArgs& p, Shares& s, Start& start)
+template <int TILE, int THREADS> __device__ __forceinline__ bool find_share(const AttendArgs& p, uint32_t g, Shares& s, Start& start)
 {
     constexpr int kWaves = THREADS / kWave;
     __shared__ uint64_t totals[kWaves];
@@ -378,7 +385,7 @@ template <int TILE, int THREADS> __device__ __forceinline__ bool find_share(cons
     uint64_t mine = 0;
     uint32_t most = 1;
     for (uint32_t r = first; r < last; ++r) {
-        const Units u = units_of<TILE>(p, r);
+        const Units u = units_of<TILE>(p, p.starts[r], p.starts[r + 1], p.cached[r]);
         mine += (uint64_t)u.tiles * u.each;
         most = u.each > most ? u.each : most;
     }
@@ -398,22 +405,23 @@ template <int TILE, int THREADS> __device__ __forceinline__ bool find_share(cons
         all += totals[k];
         most = longest[k] > most ? longest[k] : most;
     }
-    s.all = uniform(all * p.heads);
+    s.all = uniform(all);
     most = uniform(most);
     if (s.all == 0) return false;
     // a tile's positions lie in kAttendMaxParts shares at most
     const uint64_t least = (most + kAttendMaxParts - 2) / (kAttendMaxParts - 1);
-    uint64_t shares = s.all / least;
-    shares = shares < 1 ? 1 : shares < gridDim.x ? shares : gridDim.x;
-    s.each = s.all / shares;
+    uint64_t shares = quotient(s.all, least);
+    const uint32_t most_shares = gridDim.x / p.heads;
+    shares = shares < 1 ? 1 : shares < most_shares ? shares : most_shares;
+    s.each = quotient(s.all, shares);
     s.more = s.all - s.each * shares;
-    if (blockIdx.x >= shares) return false;
-    const uint64_t want = s.first(blockIdx.x);
-    uint64_t at = (before + sum - mine) * p.heads;
-    if (want >= at && want < at + mine * p.heads) {
+    if (g >= shares) return false;
+    const uint64_t want = s.first(g);
+    uint64_t at = before + sum - mine;
+    if (want >= at && want < at + mine) {
         for (uint32_t r = first; r < last; ++r) {
-            const Units u = units_of<TILE>(p, r);
-            const uint64_t n = (uint64_t)u.tiles * u.each * p.heads;
+            const Units u = units_of<TILE>(p, p.starts[r], p.starts[r + 1], p.cached[r]);
+            const uint64_t n = (uint64_t)u.tiles * u.each;
             if (want < at + n) {
                 found[0] = r;
                 found[1] = want - at;
@@ -474,8 +482,121 @@ template <> struct Bad<float> {
     }
 };
 
+// A tile on its way: its keys and values as a thread loads them, which of its positions are there, and the table's entries of the tile after it.
+template <typename T, typename C, int DP, int ROWS, bool OWN> struct Flight {
+    typedef Plan<T, C, DP, ROWS, OWN> P;
+    Chunk8<C> raw_k[OWN ? 1 : P::kMine], raw_v[P::kAhead && !OWN ? P::kMine : 1];
+    typename P::Part part_k[P::kPositions], part_v[P::kPositions];
+    int64_t  offset;
+    uint64_t here;
+    int32_t  entry;
+};
+
+template <typename T, typename C, int DP, int ROWS, bool OWN> struct Reader {
+    typedef Plan<T, C, DP, ROWS, OWN> P;
+    typedef Flight<T, C, DP, ROWS, OWN> F;
+    const AttendArgs& p;
+    uint32_t lane, wave, member;
+    __device__ __forceinline__ Reader(const AttendArgs& args, uint32_t thread)
+        : p(args), lane(thread & (kWave - 1)), wave(uniform(thread / kWave)), member(P::FEW ? lane : thread) {}
+
+    __device__ __forceinline__ uint32_t first(const Work& w) const { return w.lo + (P::FEW ? wave : 0) * P::kKeys; }
+    __device__ __forceinline__ const char* keys_of(const Work& w) const { return static_cast<const char*>(p.k_cache) + (int64_t)w.head * p.stride_head * (int64_t)sizeof(C); }
+    __device__ __forceinline__ const char* values_of(const Work& w) const { return static_cast<const char*>(p.v_cache) + (int64_t)w.head * p.stride_head * (int64_t)sizeof(C); }
+
+    // lane j of every wavefront has position j of a tile: its entry of the table, then where its vectors are
+    __device__ __forceinline__ int32_t look_up(const Work& w, uint32_t at) const
+    {
+        const uint32_t key = at + (lane & (P::kKeys - 1));
+        return key < w.hi ? p.table[(int64_t)w.request * p.ld_table + fdiv(key, p.page)] : -1;
+    }
+    // A thread's chunks of a tile.  The last one of a vector is moved back to end with it, and those behind it are that one again.
+    __device__ __forceinline__ uint32_t chunk_of(int i) const
+    {
+        const uint32_t at = (member + i * P::kTeam) % P::kChunks * 8, last = p.dim < 8 ? 0 : p.dim - 8;
+        return at < last ? at : last;
+    }
+    __device__ __forceinline__ uint32_t key_of(int i) const { return (member + i * P::kTeam) / P::kChunks; }
+    __device__ __forceinline__ int64_t place(int64_t offset, uint32_t key) const
+    {
+        return (int64_t)((uint64_t)(uint32_t)__shfl((uint32_t)(offset >> 32), key) << 32 | (uint32_t)__shfl((uint32_t)offset, key));
+    }
+    __device__ __forceinline__ void load(const char* cache, int64_t offset, Chunk8<C>* raw) const
+    {
+#pragma unroll
+        for (int i = 0; i < P::kMine; ++i) raw[i] = load_chunk<C, DP == 32>(cache + place(offset, key_of(i)), chunk_of(i), p.dim);
+    }
+    // OWN: a part of the vector of each of this lane's positions, column + M * b of the tile
+    __device__ __forceinline__ void load_parts(const char* cache, int64_t offset, typename P::Part* r) const
+    {
+        const uint32_t part = lane / P::M, column = lane % P::M;
+#pragma unroll
+        for (int b = 0; b < P::kPositions; ++b) {
+            const char* vector = cache + (P::kPositions > 1 ? place(offset, column + P::M * b) : offset);
+            const char* from = vector + (P::kRecords ? kRecordHead : 0) + part * (P::kWords * 4);
+            r[b].head = P::kRecords ? load_word(reinterpret_cast<const uint8_t*>(vector)) : 0;
+#pragma unroll
+            for (int i = 0; i + 4 <= P::kWords; i += 4) {
+                const typename Bits<16>::type x = *reinterpret_cast<const typename Bits<16>::type*>(from + 4 * i);
+                __builtin_memcpy(r[b].w + i, &x, 16);
+            }
+            constexpr int kLeft = P::kWords % 4, kDone = P::kWords - kLeft;
+            if constexpr ((kLeft & 2) != 0) {
+                const typename Bits<8>::type x = *reinterpret_cast<const typename Bits<8>::type*>(from + 4 * kDone);
+                __builtin_memcpy(r[b].w + kDone, &x, 8);
+            }
+            if constexpr ((kLeft & 1) != 0) r[b].w[P::kWords - 1] = load_word(reinterpret_cast<const uint8_t*>(from + 4 * (P::kWords - 1)));
+        }
+    }
+    // The tile at `at`, whose entries are there; and the entries of the one after it.
+    __device__ __forceinline__ void follow(const Work& w, uint32_t at, F& f) const
+    {
+        const uint32_t key = at + (lane & (P::kKeys - 1)), inside = key - fdiv(key, p.page) * p.page.div;
+        const bool here = (uint32_t)f.entry < p.pages;
+        // not there: the first slot of the cache, whose values become 0 and whose scores are left out
+        f.offset = here ? ((int64_t)f.entry * p.stride_page + (int64_t)inside * p.stride_slot) * (int64_t)sizeof(C) : 0;
+        f.here = __ballot(here);
+        if constexpr (OWN) {
+            load_parts(keys_of(w), f.offset, f.part_k);
+            load_parts(values_of(w), f.offset, f.part_v);
+        } else if constexpr (P::kAhead) {
+            load(keys_of(w), f.offset, f.raw_k);
+            load(values_of(w), f.offset, f.raw_v);
+        }
+        f.entry = look_up(w, at + P::kStep);
+    }
+    // The queries of this lane's row; behind the request's last one, that one again.
+    __device__ __forceinline__ void queries(const Work& w, typename Fragment<typename P::K>::type* query) const
+    {
+        const uint32_t own = w.row0 + (P::FEW ? 0 : wave * P::M) + lane % P::M, row = own < w.rows ? own : w.rows - 1, in = fdiv(row, p.group_div), part = lane / P::M;
+        const T* from = static_cast<const T*>(p.q) + (int64_t)(w.first_token + in) * p.ld_q + (int64_t)(w.head * p.group + (row - in * p.group)) * p.dim;
+        constexpr int E = 16 / (int)sizeof(T);
+        if (p.dim % E == 0) {
+#pragma unroll
+            for (int i = 0; i < DP / P::kDims; ++i) {
+                const uint32_t at = OWN ? part * (DP / P::kParts) + i * E : i * P::kDims + part * E;
+                query[i] = __builtin_bit_cast(typename Fragment<typename P::K>::type, load_vec<T, E, false>(from + (at < p.dim ? at : 0)));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < DP / P::kDims; ++i)
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    const uint32_t at = i * P::kDims + part * E + j;
+                    query[i][j] = from[at < p.dim ? at : 0];
+                }
+        }
+    }
+    __device__ __forceinline__ void begin(const Work& w, F& f) const
+    {
+
+        f.entry = look_up(w, first(w));
+        follow(w, first(w), f);
+    }
+};
+
 template <typename T, typename C, int DP, int ROWS, bool OWN>
-__device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, char* lds)
+__device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, const Work& next, bool more, Flight<T, C, DP, ROWS, OWN>& f, char* lds)
 {
     typedef Plan<T, C, DP, ROWS, OWN> P;
     constexpr bool FEW = P::FEW;
@@ -490,6 +611,7 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
     asm volatile("" : "+v"(thread));        // what follows from it is found again for every piece of work: kept over them, it would take the registers of the loads
     const uint32_t lane = thread & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(thread / kWave), part = lane / M, column = lane % M;
     const uint32_t head = w.head;
+    Reader<T, C, DP, ROWS, OWN> read(p, thread);
     // this lane's row; behind the request's last one, that one again
     const uint32_t own = w.row0 + (FEW ? 0 : wave * M) + column, row = own < w.rows ? own : w.rows - 1;
     const uint32_t in_request = fdiv(row, p.group_div), q_head = head * p.group + (row - in_request * p.group);
@@ -502,33 +624,24 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
 
     // scores times `scale` are exponents of 2; its sign goes into the queries, so that the largest product has the largest exponent
     float scale = p.scale;
-    if (std::is_same<C, f8>::value && p.k_scale) scale *= p.k_scale[head];
+    if (std::is_same<C, f8>::value && p.k_scale) scale *= scalar(p.k_scale, head);
     const uint32_t keep = scale == 0.f ? 0u : ~0u, flip = scale < 0.f ? (sizeof(T) == 2 ? 0x80008000u : 0x80000000u) : 0u;
     scale = scale == 0.f ? 1.f : __builtin_fabsf(scale);
     KFrag query[kSteps];
+    read.queries(w, query);
     float query_sum = 0.f;
     {
-        const T* from = static_cast<const T*>(p.q) + (int64_t)token * p.ld_q + (int64_t)q_head * p.dim;
         constexpr int E = 16 / (int)sizeof(T);
         const KFrag none = {};
-        if (p.dim % E == 0) {
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                const uint32_t at = OWN ? part * (DP / kParts) + i * E : i * P::kDims + part * E;
-                query[i] = __builtin_bit_cast(KFrag, load_vec<T, E, false>(from + (at < p.dim ? at : 0)));
-            }
+        for (int i = 0; i < kSteps; ++i) {
+            if (OWN) continue;
+            const uint32_t at = i * P::kDims + part * E;                    // what lies behind the vector's end
+            if (at >= p.dim) query[i] = none;
+            else if (p.dim % E != 0)
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i)
-                if (!OWN && i * P::kDims + part * E >= p.dim) query[i] = none;
-        } else {
-#pragma unroll
-            for (int i = 0; i < kSteps; ++i)
-#pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    const uint32_t at = i * P::kDims + part * E + j;
-                    const T x = from[at < p.dim ? at : 0];
-                    query[i][j] = at < p.dim ? x : (T)0.f;
-                }
+                for (int j = 0; j < E; ++j)
+                    if (at + j >= p.dim) query[i][j] = (T)0.f;
         }
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
@@ -549,39 +662,10 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
     char *keys = tile, *values = tile + (OWN ? 0 : P::kKeys * P::kKeyRow);
     float* key_step = reinterpret_cast<float*>(values + P::kKeys * P::kValueRow);           // kCodes: four arrays of kKeys
     float *key_low = key_step + P::kKeys, *value_step = key_low + P::kKeys, *value_low = value_step + P::kKeys;
-    uint32_t member = FEW ? lane : thread;
-    const char* k_cache = static_cast<const char*>(p.k_cache) + (int64_t)head * p.stride_head * (int64_t)sizeof(C);
-    const char* v_cache = static_cast<const char*>(p.v_cache) + (int64_t)head * p.stride_head * (int64_t)sizeof(C);
-    const int32_t* table = p.table + (int64_t)w.request * p.ld_table;
-
-    // lane j of every wavefront has position j of a tile: its entry of the table, then where its vectors are
-    auto look_up = [&](uint32_t at) -> int32_t {
-        const uint32_t key = at + (lane & (P::kKeys - 1));
-        return key < w.hi ? table[fdiv(key, p.page)] : -1;
-    };
-    struct Spot { int64_t offset; bool here; };
-    auto spot_of = [&](uint32_t at, int32_t entry) -> Spot {
-        const uint32_t key = at + (lane & (P::kKeys - 1)), inside = key - fdiv(key, p.page) * p.page.div;
-        const bool here = (uint32_t)entry < p.pages;
-        // not there: the first slot of the cache, whose values become 0 and whose scores are left out
-        return {here ? ((int64_t)entry * p.stride_page + (int64_t)inside * p.stride_slot) * (int64_t)sizeof(C) : 0, here};
-    };
-    // A thread's chunks of a tile.  The last one of a vector is moved back to end with it, and those behind it are that one again.
+    // A thread's chunks of a tile.
     const bool whole = p.dim % 8 == 0;
-    const uint32_t last_chunk = p.dim < 8 ? 0 : p.dim - 8;
-    auto chunk_of = [&](int i) {
-        const uint32_t at = (member + i * P::kTeam) % P::kChunks * 8;
-        return at < last_chunk ? at : last_chunk;
-    };
-    auto key_of = [&](int i) { return (member + i * P::kTeam) / P::kChunks; };
-    Chunk8<C> raw_k[OWN ? 1 : P::kMine], raw_v[P::kAhead && !OWN ? P::kMine : 1];
-    auto load = [&](const char* cache, int64_t offset, Chunk8<C>* raw) {
-#pragma unroll
-        for (int i = 0; i < P::kMine; ++i) {
-            const uint32_t low = __shfl((uint32_t)offset, key_of(i)), high = __shfl((uint32_t)(offset >> 32), key_of(i));
-            raw[i] = load_chunk<C, DP == 32>(cache + (int64_t)((uint64_t)high << 32 | low), chunk_of(i), p.dim);
-        }
-    };
+    auto chunk_of = [&](int i) { return read.chunk_of(i); };
+    auto key_of = [&](int i) { return read.key_of(i); };
     auto put_keys = [&](const Chunk8<C>* raw) {
         auto all = [&](auto is_whole) {
 #pragma unroll
@@ -625,40 +709,14 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
         }
         return bad;
     };
-    // OWN: a part of the vector of each of this lane's positions, column + M * b of the tile
-    struct Part { uint32_t w[P::kWords], head; };
-    Part part_k[P::kPositions], part_v[P::kPositions];
-    auto load_parts = [&](const char* cache, int64_t offset, Part* r) {
-#pragma unroll
-        for (int b = 0; b < P::kPositions; ++b) {
-            int64_t place = offset;        // lane j has position j's
-            if constexpr (P::kPositions > 1) {
-                const uint32_t low = __shfl((uint32_t)offset, column + M * b), high = __shfl((uint32_t)(offset >> 32), column + M * b);
-                place = (int64_t)((uint64_t)high << 32 | low);
-            }
-            const char* from = cache + place + (P::kRecords ? kRecordHead : 0) + part * (P::kWords * 4);
-            r[b].head = P::kRecords ? load_word(reinterpret_cast<const uint8_t*>(cache + place)) : 0;
-#pragma unroll
-            for (int i = 0; i + 4 <= P::kWords; i += 4) {
-                const typename Bits<16>::type x = *reinterpret_cast<const typename Bits<16>::type*>(from + 4 * i);
-                __builtin_memcpy(r[b].w + i, &x, 16);
-            }
-            constexpr int kLeft = P::kWords % 4, kDone = P::kWords - kLeft;
-            if constexpr ((kLeft & 2) != 0) {
-                const typename Bits<8>::type x = *reinterpret_cast<const typename Bits<8>::type*>(from + 4 * kDone);
-                __builtin_memcpy(r[b].w + kDone, &x, 8);
-            }
-            if constexpr ((kLeft & 1) != 0) r[b].w[P::kWords - 1] = load_word(reinterpret_cast<const uint8_t*>(from + 4 * (P::kWords - 1)));
-        }
-    };
     // its eight elements number i, as LDS and the products have them
-    auto chunk_of_part = [&](const Part& r, int i) -> Chunk8<C> {
+    auto chunk_of_part = [&](const typename P::Part& r, int i) -> Chunk8<C> {
         Chunk8<C> c;
         if constexpr (P::kRecords) c = {r.w[i], r.head};
         else __builtin_memcpy(&c, r.w + i * (int)sizeof(C) * 2, sizeof(c));
         return c;
     };
-    auto put_parts = [&](Part* r, uint64_t there, bool holes, bool look) -> bool {
+    auto put_parts = [&](typename P::Part* r, uint64_t there, bool holes, bool look) -> bool {
         bool bad = false;
 #pragma unroll
         for (int b = 0; b < P::kPositions; ++b) {
@@ -674,7 +732,7 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
         }
         return bad;
     };
-    auto put_steps = [&](const Part* k, const Part* v) {
+    auto put_steps = [&](const typename P::Part* k, const typename P::Part* v) {
 #pragma unroll
         for (int b = 0; b < P::kPositions; ++b)
             if (part == 0) {
@@ -700,31 +758,21 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
     };
     // what lies behind the vectors' ends in the tile's rows: 0, once
     if (!OWN && p.dim < DP) {
-        for (uint32_t key = member / 32; key < P::kKeys; key += P::kTeam / 32)
-            for (uint32_t d = p.dim + member % 32; d < DP; d += 32) reinterpret_cast<KE*>(keys + key * P::kKeyRow)[d] = (KE)0.f;
+        for (uint32_t key = read.member / 32; key < P::kKeys; key += P::kTeam / 32)
+            for (uint32_t d = p.dim + read.member % 32; d < DP; d += 32) reinterpret_cast<KE*>(keys + key * P::kKeyRow)[d] = (KE)0.f;
     }
 
     Acc out[kOut] = {};
     float top = -__builtin_inff(), sum = 0.f, low_sum = 0.f;                // of this lane's row (sums: its half of the positions); top times scale
-    const uint32_t team = FEW ? wave : 0;
-    uint32_t at = w.lo + team * P::kKeys;
-    int32_t entry = look_up(at);
-    Spot spot = spot_of(at, entry);
-    uint64_t here = __ballot(spot.here);
-    if constexpr (OWN) {
-        load_parts(k_cache, spot.offset, part_k);
-        load_parts(v_cache, spot.offset, part_v);
-        entry = look_up(at + P::kStep);
-    } else if constexpr (P::kAhead) {
-        load(k_cache, spot.offset, raw_k);
-        load(v_cache, spot.offset, raw_v);
-        entry = look_up(at + P::kStep);
-    }
+    uint32_t at = read.first(w);
+    int32_t next_entry = -1;
+    if constexpr (P::kCarries) next_entry = read.look_up(next, read.first(next));
+    else read.begin(w, f);
     for (; at < w.hi; at += P::kStep) {
-        asm volatile("" : "+v"(member));    // places in the tile are found again each time: kept, they would take the registers of the loads
+        asm volatile("" : "+v"(read.member));    // places in the tile are found again each time: kept, they would take the registers of the loads
         // positions of the tile that some row of the workgroup's does not see
         const uint32_t end = at + P::kKeys;
-        const uint64_t now = here;
+        const uint64_t now = f.here;
         constexpr uint64_t kAll = P::kKeys == 64 ? ~0ull : (1ull << P::kKeys) - 1;
         const bool holes = (now & kAll) != kAll;
         const uint32_t tile_lowest = w.cached + fdiv(w.row0, p.group_div);
@@ -732,27 +780,19 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
         bool bad;
         team_sync<FEW>();                                                   // the tile before has been used
         if constexpr (OWN) {
-            if constexpr (P::kCodes) put_steps(part_k, part_v);
-            bad = put_parts(part_v, now, holes, look);
+            if constexpr (P::kCodes) put_steps(f.part_k, f.part_v);
+            bad = put_parts(f.part_v, now, holes, look);
         } else if constexpr (P::kAhead) {
-            put_keys(raw_k);
-            bad = put_values(raw_v, now, holes, look);
-            if (at + P::kStep < w.hi) {
-                spot = spot_of(at + P::kStep, entry);
-                here = __ballot(spot.here);
-                load(k_cache, spot.offset, raw_k);
-                load(v_cache, spot.offset, raw_v);
-                entry = look_up(at + 2 * P::kStep);
-            }
+            put_keys(f.raw_k);
+            bad = put_values(f.raw_v, now, holes, look);
+            if (at + P::kStep < w.hi) read.follow(w, at + P::kStep, f);
         } else {
-            load(k_cache, spot.offset, raw_k);
-            put_keys(raw_k);
-            load(v_cache, spot.offset, raw_k);
-            bad = put_values(raw_k, now, holes, look);
-            if (at + P::kStep < w.hi) {
-                spot = spot_of(at + P::kStep, look_up(at + P::kStep));
-                here = __ballot(spot.here);
-            }
+            const int64_t offset = f.offset;
+            read.load(read.keys_of(w), offset, f.raw_k);
+            put_keys(f.raw_k);
+            read.load(read.values_of(w), offset, f.raw_k);
+            bad = put_values(f.raw_k, now, holes, look);
+            if (at + P::kStep < w.hi) read.follow(w, at + P::kStep, f);
         }
         if constexpr (FEW) {
             bad = __ballot(bad) != 0;
@@ -770,19 +810,12 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
             const char* from = keys + (b * M + column) * P::kKeyRow + part * 16;
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                if constexpr (OWN) mul(fragment_of<KE>(chunk_of_part(part_k[b], i)), query[i], score[b]);
+                if constexpr (OWN) mul(fragment_of<KE>(chunk_of_part(f.part_k[b], i)), query[i], score[b]);
                 else mul(*reinterpret_cast<const KFrag*>(from + i * P::kDims * sizeof(KE)), query_of(i), score[b]);
             }
         }
-        if constexpr (OWN) {
-            if (at + P::kStep < w.hi) {
-                spot = spot_of(at + P::kStep, entry);
-                here = __ballot(spot.here);
-                load_parts(k_cache, spot.offset, part_k);
-                load_parts(v_cache, spot.offset, part_v);
-                entry = look_up(at + 2 * P::kStep);
-            }
-        }
+        if constexpr (OWN)
+            if (at + P::kStep < w.hi) read.follow(w, at + P::kStep, f);
         // register i of block b is position M b + kGap (i / 4) + 4 part + i % 4
         if constexpr (P::kCodes) {
 #pragma unroll
@@ -936,9 +969,16 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
         }
     }
 
+    // the next piece of work's first tile on its way beside the rest of this one
+    if constexpr (P::kCarries)
+        if (more) {
+            f.entry = next_entry;
+            read.follow(next, read.first(next), f);
+        }
+
     sum = sum_of_row<M>(sum);
     low_sum = sum_of_row<M>(low_sum);
-    const float v_scale = std::is_same<C, f8>::value && p.v_scale ? p.v_scale[head] : 1.f;
+    const float v_scale = std::is_same<C, f8>::value && p.v_scale ? scalar(p.v_scale, head) : 1.f;
     // Writes four neighbouring elements of a row's result, normalized: to the result, or to this part's place.
     auto write = [&](uint32_t of, uint32_t to_token, uint32_t to_head, uint32_t d, const float* x) {
         if (d >= p.dim) return;
@@ -1029,54 +1069,58 @@ __global__ __launch_bounds__((Plan<T, C, DP, ROWS, OWN>::kThreads), (Plan<T, C, 
     typedef Plan<T, C, DP, ROWS, OWN> P;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     Work w;
+    Flight<T, C, DP, ROWS, OWN> f;
     if constexpr (!P::FEW) {
         const uint32_t slot = p.slots_of_tiles - 1 - blockIdx.x;            // the last tiles see most: first
         w.head = blockIdx.y;
         if (!find_tile<P, ROWS>(p, slot, blockIdx.z, w)) return;
         w.partial_row = ((slot * p.heads + w.head) * p.splits + blockIdx.z) * ROWS;
-        attend_work<T, C, DP, ROWS, OWN>(p, w, lds);
+        attend_work<T, C, DP, ROWS, OWN>(p, w, w, false, f, lds);
     } else {
         Shares s;
         Start start;
-        if (!find_share<ROWS, P::kThreads>(p, s, start)) return;
-        uint64_t left = s.first(blockIdx.x + 1) - s.first(blockIdx.x), unit = s.first(blockIdx.x);
+        const uint32_t g = blockIdx.x / p.heads, head = blockIdx.x - g * p.heads;
+        if (!find_share<ROWS, P::kThreads>(p, g, s, start)) return;
+        auto units = [&](uint32_t of) { return units_of<ROWS>(p, scalar(p.starts, of), scalar(p.starts, of + 1), scalar(p.cached, of)); };
+        uint64_t unit = s.first(g), left = s.first(g + 1) - unit;
         uint32_t r = start.request;
-        auto units = [&](uint32_t of) {
-            Units x = units_of<ROWS>(p, of);
-            x = {uniform(x.tiles), uniform(x.each), uniform(x.bottom), uniform(x.count), uniform(x.begin), uniform(x.rows), uniform(x.cached)};
-            return x;
-        };
         Units u = units(r);
-        const uint64_t index = start.unit / u.each;
-        uint32_t done = (uint32_t)(start.unit - index * u.each), tile = (uint32_t)(index / p.heads), head = (uint32_t)(index - (uint64_t)tile * p.heads);
-        while (true) {
+        uint32_t tile = (uint32_t)quotient(start.unit, u.each), done = (uint32_t)(start.unit - (uint64_t)tile * u.each);
+        // the rows of a tile, and those of their positions that are this share's
+        auto piece = [&] {
+            Work x;
             const uint32_t rest = u.each - done, take = left < rest ? (uint32_t)left : rest;
-            w.request = r;
-            w.row0 = tile * ROWS;
-            w.rows = u.rows;
-            w.first_token = u.begin;
-            w.cached = u.cached;
-            w.head = head;
             const uint32_t from = done * kAttendUnit, to = (done + take) * kAttendUnit;
-            w.lo = u.bottom + (from < u.count ? from : u.count);
-            w.hi = u.bottom + (to < u.count ? to : u.count);
-            w.partial = take < u.each;
-            w.partial_row = (2 * blockIdx.x + (done == 0)) * ROWS;
-            w.parts = done ? 0 : w.partial ? s.of(unit + u.each - 1) - blockIdx.x + 1 : 1;
-            attend_work<T, C, DP, ROWS, OWN>(p, w, lds);
+            x.request = r;
+            x.row0 = tile * ROWS;
+            x.rows = u.rows;
+            x.first_token = u.begin;
+            x.cached = u.cached;
+            x.head = head;
+            x.lo = u.bottom + (from < u.count ? from : u.count);
+            x.hi = u.bottom + (to < u.count ? to : u.count);
+            x.partial = take < u.each;
+            x.partial_row = (2 * blockIdx.x + (done == 0)) * ROWS;
+            x.parts = done ? 0 : x.partial ? s.of(unit + u.each - 1) - g + 1 : 1;
             left -= take;
             unit += take;
-            if (left == 0) break;
-            __syncthreads();                                                // LDS is used again
             done = 0;
-            if (++head < p.heads) continue;
-            head = 0;
-            if (++tile < u.tiles) continue;
-            tile = 0;
-            do {
-                if (++r >= p.requests) return;
-                u = units(r);
-            } while (u.tiles == 0);
+            ++tile;
+            return x;
+        };
+        w = piece();
+        if constexpr (P::kCarries) Reader<T, C, DP, ROWS, OWN>(p, threadIdx.x).begin(w, f);
+        while (true) {
+            const bool more = left > 0;
+            if (more && tile == u.tiles) {
+                tile = 0;
+                do u = units(++r); while (u.tiles == 0 && r + 1 < p.requests);
+            }
+            const Work next = more ? piece() : w;
+            attend_work<T, C, DP, ROWS, OWN>(p, w, next, more, f, lds);
+            if (!more) break;
+            __syncthreads();                                                // LDS is used again
+            w = next;
         }
     }
 }

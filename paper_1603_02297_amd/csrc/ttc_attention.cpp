@@ -45,8 +45,10 @@ AttendShape attend_shape(const ttc_attend_s* a, int64_t requests, int64_t tokens
     const int64_t groups = std::max<int64_t>((int64_t)s.slots * heads, 1), units = std::max<int64_t>((longest + kAttendUnit - 1) / kAttendUnit, 1);
     if (s.tile < kTileMany) {
         // as many shares as workgroups fit the device at a time: 96 requests' step takes LATER
-        const int64_t most = 256 * attend_resident(elem_bytes(a->dtype), elem_bytes(a->cache_dtype), (int)a->dim, (int)s.tile);
-        s.shares = (uint32_t)(groups >= most / units ? std::min<int64_t>(most, groups * units) : groups * units);
+        const int64_t most = 256 * attend_resident(elem_bytes(a->dtype), attend_own(elem_bytes(a->dtype), elem_bytes(a->cache_dtype), (int)a->dim, (int)s.tile),
+                                                   a->cache_dtype == TTC_Q4, (int)a->dim, (int)s.tile);
+        const int64_t each = std::max<int64_t>(most / heads, 1);               // of a head
+        s.shares = (uint32_t)(heads * (s.slots >= each / units ? std::min<int64_t>(each, s.slots * units) : s.slots * units));
         s.splits = 1;
         s.partial_rows = units > 1 ? 2 * (int64_t)s.shares * s.tile : 0;
     } else {
@@ -387,7 +389,7 @@ int ttc_attend_pages(ttc_attend_t attend, int64_t requests, int64_t tokens, cons
     a.dim = (uint32_t)attend->dim; a.pages = (uint32_t)attend->pages;
     a.splits = s.splits; a.slots_of_tiles = s.slots;
     a.partial_rows = (uint32_t)s.partial_rows;
-    a.join_step = s.tile < kTileMany ? 2 * s.tile : s.tile; a.join_back = s.tile < kTileMany ? s.tile : 0;
+    a.join_step = s.tile < kTileMany ? 2 * s.tile * (uint32_t)attend->heads : s.tile; a.join_back = s.tile < kTileMany ? s.tile : 0;
     a.window = (uint32_t)attend->window;
     a.page = attend->page_div;
     a.group_div = make_fastdiv((uint32_t)group);

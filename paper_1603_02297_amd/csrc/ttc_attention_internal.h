@@ -89,9 +89,9 @@ constexpr int kAttendMaxSplits = 32;
 constexpr int attend_dim(int dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 128 : dim <= 192 ? 192 : 256; }
 constexpr bool attend_own(int bytes, int cache_bytes, int dim, int tile) { return bytes == 2 && cache_bytes == 1 && dim == attend_dim(dim) && tile < 128; }
 // Workgroups that share a compute unit, by registers and LDS.
-constexpr int attend_resident(int bytes, int cache_bytes, int dim, int tile)
+constexpr int attend_resident(int bytes, bool own, bool records, int dim, int tile)
 {
-    return bytes == 4 || dim > 128 ? 1 : attend_own(bytes, cache_bytes, dim, tile) && tile == 16 ? 3 : 2;
+    return bytes == 4 || dim > 128 ? 1 : own && records && tile == 16 ? 3 : 2;
 }
 constexpr uint32_t kAttendUnit = 128, kAttendMaxParts = 128;     // positions that are not shared among workgroups; results that a row may have to be joined from
 
