@@ -9,7 +9,7 @@
 
 namespace ttc {
 
-HeadsShape cut_heads(HeadsArgs& a)
+HeadsShape cut_heads(HeadsArgs& a, int groups)
 {
     HeadsShape s = {};
     const uint32_t wide = a.cache_dtype == TTC_Q4 ? 8 : 16 / elem_bytes(a.dtype), half = a.rotated / 2, rest = a.dim - a.rotated;
@@ -20,18 +20,19 @@ HeadsShape cut_heads(HeadsArgs& a)
     a.lanes_log = 0;
     while ((1u << a.lanes_log) < units && a.lanes_log < 6) ++a.lanes_log;
     const uint32_t each = 64u >> a.lanes_log;
+    a.full = units == 1u << a.lanes_log && a.dim % (2 * vec) == 0 && (a.paired || rest % (2 * vec) == 0) && (!a.q || a.q_heads % each == 0) && ((!a.k && !a.v) || a.kv_heads % each == 0);
     a.q_groups = a.q ? (a.q_heads + each - 1) / each : 0;
     a.k_groups = a.k ? (a.kv_heads + each - 1) / each : 0;
     a.v_groups = a.v ? (a.kv_heads + each - 1) / each : 0;
     // a wavefront for each token as long as that fills the launch, else its groups spread over several
     const uint32_t all = std::max<uint32_t>(a.q_groups + a.k_groups + a.v_groups, 1);
-    const int64_t waves = (int64_t)kHeadsGroups * (kHeadsThreads / kWave), per = kHeadsThreads / kWave;
+    const int64_t waves = (int64_t)groups * (kHeadsThreads / kWave), per = kHeadsThreads / kWave;
     const int64_t splits = std::min<int64_t>(std::max<int64_t>(waves / std::max<uint32_t>(a.tokens, 1), 1), all);
     a.per_wave = (uint32_t)((all + splits - 1) / splits);
     s.vec = (int)vec;
     s.splits = (all + a.per_wave - 1) / a.per_wave;
     a.split_div = make_fastdiv(s.splits);
-    s.groups = (int)std::min<int64_t>(((int64_t)a.tokens * s.splits + per - 1) / per, kHeadsGroups);
+    s.groups = (int)std::min<int64_t>(((int64_t)a.tokens * s.splits + per - 1) / per, groups);
     return s;
 }
 
@@ -61,7 +62,7 @@ AttendShape attend_shape(const ttc_attend_s* a, int64_t requests, int64_t tokens
 
 namespace {
 
-constexpr int64_t kGradPartials = kHeadsGroups;
+constexpr int64_t kGradPartials = kGradGroups;
 
 // Whether two tensors of `tokens` rows, rows wa and wb bytes long, share a byte.  Rows of one distance are told apart exactly; of two
 // distances in one span they are taken to meet.

@@ -28,7 +28,7 @@ namespace ttc {
 
 constexpr int kHeadsThreads = 256;
 // Workgroups of a launch at most: four on each compute unit, each over many tokens, so that angles and weights are fetched once.
-constexpr int kHeadsGroups = 1024;
+constexpr int kHeadsGroups = 1024, kGradGroups = 512;
 
 // Queries, keys and values of one call.  A head is cut into units of two vectors of V elements, the two sides of V rotations; `lanes` lanes
 // of a wavefront have one head, 64 / lanes heads at a time are a group, and `splits` wavefronts share a token's groups.
@@ -44,7 +44,7 @@ struct HeadsArgs {
     int32_t        dtype, cache_dtype;     // cache_dtype -1: packed results
     int32_t        paired, norm;
     float          eps;
-    int32_t        lanes_log;
+    int32_t        lanes_log, full;        // full: every lane has an element of its own in every group
     uint32_t       q_groups, k_groups, v_groups, per_wave;
     // the backward pass: q, k are the inputs, and beside them
     const void    *dq_out, *dk_out;
@@ -61,7 +61,7 @@ struct HeadsShape {
     int      groups;                       // workgroups
     uint32_t splits;
 };
-HeadsShape cut_heads(HeadsArgs& a);          // sets what the cut says of a, too
+HeadsShape cut_heads(HeadsArgs& a, int groups);          // sets what the cut says of a, too
 
 // Attention.  The rows of a request are its new tokens' query heads that share a head of the cache, token by token; a workgroup has `tile` rows of them
 // and a part of the positions that they see.

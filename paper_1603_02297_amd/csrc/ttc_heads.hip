@@ -42,7 +42,7 @@ __device__ __forceinline__ float over_head(float v, int log)
 }
 
 struct Unit {
-    uint32_t a, b;                         // its two vectors' first elements
+    uint32_t a, b;                         // its two vectors' first elements; where it has none, others of the head, which are loaded and not used
     bool     has_a, has_b, turned;
 };
 
@@ -65,34 +65,76 @@ template <int V> __device__ __forceinline__ Unit unit_of(const HeadsArgs& p, uin
     }
     r.has_a = r.a < p.dim;
     r.has_b = r.b < p.dim;
+    r.a = r.has_a ? r.a : 0;
+    r.b = r.has_b ? r.b : r.a;
     return r;
 }
 
-// A lane's units, with what it knows of them for a whole launch, and for a token.
-template <int V, int N> struct Lane {
-    Unit     unit[N];
-    uint64_t turn[N][V];
-    float    cosine[N][V], sine[N][V];
-    __device__ __forceinline__ void start(const HeadsArgs& p, uint32_t lane)
+// What a workgroup keeps of the call: angles and weights (1 where there are none).
+struct Kept {
+    uint64_t turns[TTC_HEADS_MAX_ROTATED / 2];
+    float    weights[2][TTC_HEADS_MAX_DIM];
+    __device__ __forceinline__ void fill(const HeadsArgs& p)
     {
         // by the segment that the launch filled: indexed by lane, the parameter itself would be copied to memory first
         const __attribute__((address_space(4))) char* args = (const __attribute__((address_space(4))) char*)__builtin_amdgcn_kernarg_segment_ptr();
-        const __attribute__((address_space(4))) uint64_t* turns = (const __attribute__((address_space(4))) uint64_t*)(args + offsetof(HeadsArgs, turns));
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            unit[n] = unit_of<V>(p, lane + ((uint32_t)n << p.lanes_log));
-            // paired: pairs a/2 ...; else the pair is its first element
-            const uint32_t first = p.paired ? unit[n].a / 2 : unit[n].a;
-#pragma unroll
-            for (int j = 0; j < V; ++j) turn[n][j] = unit[n].turned ? turns[first + j] : 0;
-        }
+        const __attribute__((address_space(4))) uint64_t* from = (const __attribute__((address_space(4))) uint64_t*)(args + offsetof(HeadsArgs, turns));
+        for (uint32_t i = threadIdx.x; i < p.rotated / 2; i += kHeadsThreads) turns[i] = from[i];
+        if (p.norm)
+            for (uint32_t i = threadIdx.x; i < p.dim; i += kHeadsThreads) {
+                weights[0][i] = p.q_weight ? p.q_weight[i] : 1.f;
+                weights[1][i] = p.k_weight ? p.k_weight[i] : 1.f;
+            }
+        __syncthreads();
     }
-    __device__ __forceinline__ void token(uint32_t position)
+};
+
+// A wavefront's accesses of LDS happen in order: only the compiler has to keep it.
+__device__ __forceinline__ void wave_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// 1 / sqrt(x), to a unit; the instruction takes numbers below the normal range for 0.
+__device__ __forceinline__ float inverse_root(float x)
+{
+    const bool tiny = x < 0x1p-64f;
+    return __builtin_amdgcn_rsqf(tiny ? x * 0x1p64f : x) * (tiny ? 0x1p32f : 1.f);
+}
+
+// A lane's units, the same of every head, and their rotation at a token's position.
+template <int V, int N> struct Lane {
+    Unit  unit[N];
+    float cosine[N][V], sine[N][V];
+    __device__ __forceinline__ Lane(const HeadsArgs& p, uint32_t lane)
     {
 #pragma unroll
-        for (int n = 0; n < N; ++n)
+        for (int n = 0; n < N; ++n) unit[n] = unit_of<V>(p, lane + ((uint32_t)n << p.lanes_log));
+    }
+    // A wavefront's lanes make the rotations, one or two each, and exchange them by LDS: every lane by itself would make those of its units for each of the
+    // heads that are under way at a time again, a fifth of all instructions.
+    __device__ __forceinline__ void token(const HeadsArgs& p, const Kept& kept, float2* circle, uint32_t position)
+    {
+        wave_order();                       // the last token's have been read
+        for (uint32_t i = threadIdx.x & (kWave - 1); i < p.rotated / 2; i += kWave) {
+            float2 c;
+            unit_circle(kept.turns[i] * position, &c.x, &c.y);
+            circle[i] = c;
+        }
+        wave_order();
 #pragma unroll
-            for (int j = 0; j < V; ++j) unit_circle(turn[n][j] * position, &cosine[n][j], &sine[n][j]);
+        for (int n = 0; n < N; ++n) {
+            // paired: pairs a/2 ...; else the pair is its first element
+            const uint32_t first = unit[n].turned ? p.paired ? unit[n].a / 2 : unit[n].a : 0;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float2 c = circle[first + j];
+                cosine[n][j] = unit[n].turned ? c.x : 1.f;
+                sine[n][j] = unit[n].turned ? c.y : 0.f;
+            }
+        }
     }
     // x[n] is unit n's 2 V elements; back: by the negative angle
     __device__ __forceinline__ void rotate(float (*x)[2 * V], int paired, bool back) const
@@ -113,39 +155,45 @@ template <int V, int N> struct Lane {
                 }
             }
     }
+    __device__ __forceinline__ void weights(const float* kept, float (*w)[2 * V]) const
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                w[n][j] = kept[unit[n].a + j];
+                w[n][V + j] = kept[unit[n].b + j];
+            }
+    }
 };
 
+// Loads go without conditions around them: under one, the compiler would wait for each before the next.  What lanes without an element of their own have
+// loaded is made 0, where there are such lanes (!full).
 template <typename T, int V> struct Raw { Vec<T, V> a, b; };
 
-template <typename T, int V> __device__ __forceinline__ Raw<T, V> load_unit(const T* p, const Unit& u, bool here)
+template <typename T, int V> __device__ __forceinline__ Raw<T, V> load_unit(const T* p, const Unit& u)
 {
-    Raw<T, V> r = {};
-    if (here && u.has_a) r.a = load_vec<T, V, false>(p + u.a);
-    if (here && u.has_b) r.b = load_vec<T, V, false>(p + u.b);
-    return r;
+    return {load_vec<T, V, false>(p + u.a), load_vec<T, V, false>(p + u.b)};
 }
-template <typename T, int V> __device__ __forceinline__ void widen_unit(const Raw<T, V>& r, float* x)
+template <typename T, int V> __device__ __forceinline__ void widen_unit(const Raw<T, V>& r, const Unit& u, bool full, bool here, float* x)
 {
     widen(r.a, x);
     widen(r.b, x + V);
-}
-template <typename T, int V> __device__ __forceinline__ void store_unit(T* p, const Unit& u, bool here, const float* x)
-{
-    Vec<T, V> r;
-    if (here && u.has_a) { narrow(x, r); store_vec<T, V, false>(p + u.a, r); }
-    if (here && u.has_b) { narrow(x + V, r); store_vec<T, V, false>(p + u.b, r); }
-}
-
-// A lane's share of the weights, 1 where there are none (and behind the end).
-template <int V, int N> __device__ __forceinline__ void load_weights(const float* w, const Lane<V, N>& lane, float (*x)[2 * V])
-{
-#pragma unroll
-    for (int n = 0; n < N; ++n)
+    if (!full) {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            x[n][j] = w && lane.unit[n].has_a ? w[lane.unit[n].a + j] : 1.f;
-            x[n][V + j] = w && lane.unit[n].has_b ? w[lane.unit[n].b + j] : 1.f;
+            x[j] = here && u.has_a ? x[j] : 0.f;
+            x[V + j] = here && u.has_b ? x[V + j] : 0.f;
         }
+    }
+}
+template <bool NT, typename T, int V> __device__ __forceinline__ void store_unit(T* p, const Unit& u, bool here, const float* x)
+{
+    Vec<T, V> a, b;
+    narrow(x, a);
+    narrow(x + V, b);
+    if (here && u.has_a) store_vec<T, V, NT>(p + u.a, a);
+    if (here && u.has_b) store_vec<T, V, NT>(p + u.b, b);
 }
 
 struct Place {                             // of a wavefront's item
@@ -163,14 +211,15 @@ __device__ __forceinline__ Place place_of(const HeadsArgs& p, uint32_t item)
     return r;
 }
 
-constexpr int kBatch = 4;                  // groups whose loads are under way together
+// Groups whose loads are under way together: a token's, as a rule.
+constexpr int kBatch = 4, kGradBatch = 2;
 
 // C: the cache's element type, or void for packed results.
 template <typename C> struct Cached { static constexpr bool value = true; };
 template <> struct Cached<void> { static constexpr bool value = false; };
 
 // One head's vector into the cache.
-template <typename T, typename C, int V, int N>
+template <typename T, typename C, int V, int N, bool NT>
 __device__ __forceinline__ void store_cached(void* cache, int64_t at, float scale, const Lane<V, N>& lane, bool here, float (*x)[2 * V], int lanes_log)
 {
     if constexpr (std::is_same<C, q4>::value) {
@@ -192,178 +241,188 @@ __device__ __forceinline__ void store_cached(void* cache, int64_t at, float scal
             const Unit& u = lane.unit[n];
             Vec<f8, V> r;
             f8* to = static_cast<f8*>(cache) + at;
-            if (here && u.has_a) { narrow_scaled(x[n], scale, r); store_vec<f8, V, false>(to + u.a, r); }
-            if (here && u.has_b) { narrow_scaled(x[n] + V, scale, r); store_vec<f8, V, false>(to + u.b, r); }
+            if (here && u.has_a) { narrow_scaled(x[n], scale, r); store_vec<f8, V, NT>(to + u.a, r); }
+            if (here && u.has_b) { narrow_scaled(x[n] + V, scale, r); store_vec<f8, V, NT>(to + u.b, r); }
         }
     } else {
 #pragma unroll
-        for (int n = 0; n < N; ++n) store_unit<T, V>(static_cast<T*>(cache) + at, lane.unit[n], here, x[n]);
+        for (int n = 0; n < N; ++n) store_unit<NT, T, V>(static_cast<T*>(cache) + at, lane.unit[n], here, x[n]);
     }
 }
 
-template <typename T, typename C, int V, int N>
-__global__ __launch_bounds__(kHeadsThreads) void heads_kernel(HeadsArgs p)
+template <typename T, typename C, int V, int N, bool NT>
+__global__ __launch_bounds__(kHeadsThreads, 4) void heads_kernel(HeadsArgs p)
 {
+    __shared__ Kept kept;
+    __shared__ float2 circle[kHeadsThreads / kWave][TTC_HEADS_MAX_ROTATED / 2];
+    constexpr int kLoads = N == 1 ? kBatch : 2;
     const uint32_t wave = blockIdx.x * (kHeadsThreads / kWave) + threadIdx.x / kWave, waves = gridDim.x * (kHeadsThreads / kWave);
     const uint32_t in_head = threadIdx.x & ((1u << p.lanes_log) - 1), sub = (threadIdx.x & (kWave - 1)) >> p.lanes_log, each = kWave >> p.lanes_log;
-    const uint32_t items = p.tokens * p.split_div.div;
-    Lane<V, N> lane;
-    lane.start(p, in_head);
-    float weight[2][N][2 * V];
-    if (p.norm) {
-        load_weights<V, N>(p.q_weight, lane, weight[0]);
-        load_weights<V, N>(p.k_weight, lane, weight[1]);
-    }
+    const uint32_t items = p.tokens * p.split_div.div, q_end = p.q_groups, k_end = q_end + p.k_groups;
+    Lane<V, N> lane(p, in_head);
     const float each_element = 1.f / (float)p.dim;
+    Raw<T, V> raw[kLoads][N];
+    // groups g0 ... of an item
+    auto load = [&](const Place& at, uint32_t g0) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const uint32_t g = g0 + i;
+            if (g >= at.end) break;
+            const bool q = g < q_end, k = g < k_end;
+            const T* row = static_cast<const T*>(q ? p.q : k ? p.k : p.v) + (int64_t)at.token * (q ? p.ld_q : k ? p.ld_k : p.ld_v);
+            const uint32_t head = (q ? g : k ? g - q_end : g - k_end) * each + sub, last = (q ? p.q_heads : p.kv_heads) - 1;
+#pragma unroll
+            for (int n = 0; n < N; ++n) raw[i][n] = load_unit<T, V>(row + (int64_t)(head < last ? head : last) * p.dim, lane.unit[n]);
+        }
+    };
+    kept.fill(p);
     for (uint32_t item = __builtin_amdgcn_readfirstlane(wave); item < items; item += waves) {
         const Place at = place_of(p, item);
         if (at.position < 0) continue;
-        lane.token((uint32_t)at.position);
-        uint32_t slot = 0;
+        load(at, at.group);
         int64_t in_cache = 0;
-        bool kept = true;
+        bool slotted = true;
         if constexpr (Cached<C>::value) {
-            slot = (uint32_t)p.slots[at.token];
-            kept = slot < p.slot_count;
-            const uint32_t page = kept ? fdiv(slot, p.page) : 0, inside = kept ? slot - page * p.page.div : 0;
+            const uint32_t slot = (uint32_t)p.slots[at.token];
+            slotted = slot < p.slot_count;
+            const uint32_t page = slotted ? fdiv(slot, p.page) : 0, inside = slotted ? slot - page * p.page.div : 0;
             in_cache = (int64_t)page * p.stride_page + (int64_t)inside * p.stride_slot;
         }
-        // queries, then keys, then values: the groups of a kind that are this wavefront's
-        auto run = [&](auto kind_of, uint32_t first, uint32_t groups, const void* from, int64_t ld, uint32_t heads) {
-            const uint32_t lo = at.group > first ? at.group - first : 0, hi = at.end > first ? (at.end - first < groups ? at.end - first : groups) : 0;
-            constexpr int kind = decltype(kind_of)::value;
-            const T* row = static_cast<const T*>(from) + (int64_t)at.token * ld;
-            for (uint32_t g0 = lo; g0 < hi; g0 += kBatch) {
-                Raw<T, V> raw[kBatch][N];
+        lane.token(p, kept, circle[threadIdx.x / kWave], (uint32_t)at.position);
+        // queries, then keys, then values
+        const uint32_t end = slotted ? at.end : at.end < q_end ? at.end : q_end;
+        for (uint32_t g0 = at.group; g0 < end; g0 += kLoads) {
+            if (g0 != at.group) load(at, g0);
 #pragma unroll
-                for (int i = 0; i < kBatch; ++i) {
-                    const uint32_t head = (g0 + i) * each + sub;
-                    const bool here = g0 + i < hi && head < heads;
-#pragma unroll
-                    for (int n = 0; n < N; ++n) raw[i][n] = load_unit<T, V>(row + (int64_t)head * p.dim, lane.unit[n], here);
-                }
-#pragma unroll
-                for (int i = 0; i < kBatch; ++i) {
-                    if (g0 + i >= hi) break;
-                    const uint32_t head = (g0 + i) * each + sub;
-                    const bool here = head < heads;
+            for (int i = 0; i < kLoads; ++i) {
+                const uint32_t g = g0 + i;
+                if (g >= end) break;
+                auto run = [&](auto kind_of) {
+                    constexpr int kind = decltype(kind_of)::value;
+                    const uint32_t head = (kind == 0 ? g : kind == 1 ? g - q_end : g - k_end) * each + sub;
+                    const bool here = head < (kind == 0 ? p.q_heads : p.kv_heads);
                     float x[N][2 * V];
 #pragma unroll
-                    for (int n = 0; n < N; ++n) widen_unit<T, V>(raw[i][n], x[n]);
+                    for (int n = 0; n < N; ++n) widen_unit<T, V>(raw[i][n], lane.unit[n], p.full, here, x[n]);
                     if constexpr (kind < 2) {
                         if (p.norm) {
-                            float sum = 0.f;
+                            float w[N][2 * V], sum = 0.f;
+                            lane.weights(kept.weights[kind], w);
 #pragma unroll
                             for (int n = 0; n < N; ++n)
 #pragma unroll
                                 for (int j = 0; j < 2 * V; ++j) sum = __builtin_fmaf(x[n][j], x[n][j], sum);
-                            const float r = 1.f / __builtin_sqrtf(__builtin_fmaf(over_head(sum, p.lanes_log), each_element, p.eps));
+                            const float r = inverse_root(__builtin_fmaf(over_head(sum, p.lanes_log), each_element, p.eps));
 #pragma unroll
                             for (int n = 0; n < N; ++n)
 #pragma unroll
-                                for (int j = 0; j < 2 * V; ++j) x[n][j] = x[n][j] * r * weight[kind][n][j];
+                                for (int j = 0; j < 2 * V; ++j) x[n][j] = x[n][j] * r * w[n][j];
                         }
                         lane.rotate(x, p.paired, false);
                     }
                     if constexpr (kind == 0 || !Cached<C>::value) {
                         T* to = static_cast<T*>(kind == 0 ? p.q_out : p.k_out) + (int64_t)at.token * (kind == 0 ? p.ld_qo : p.ld_ko) + (int64_t)head * p.dim;
 #pragma unroll
-                        for (int n = 0; n < N; ++n) store_unit<T, V>(to, lane.unit[n], here, x[n]);
+                        for (int n = 0; n < N; ++n) store_unit<NT, T, V>(to, lane.unit[n], here, x[n]);
                     } else {
                         const float* scales = kind == 1 ? p.k_scale : p.v_scale;
                         const float scale = std::is_same<C, f8>::value && scales && here ? scales[head] : 1.f;
-                        store_cached<T, C, V, N>(kind == 1 ? p.k_out : p.v_out, in_cache + (int64_t)head * p.stride_head, scale, lane, here, x, p.lanes_log);
+                        store_cached<T, C, V, N, NT>(kind == 1 ? p.k_out : p.v_out, in_cache + (int64_t)head * p.stride_head, scale, lane, here, x, p.lanes_log);
                     }
-                }
+                };
+                if (g < q_end) run(std::integral_constant<int, 0>{});
+                else if (!Cached<C>::value || g < k_end) run(std::integral_constant<int, 1>{});
+                else if constexpr (Cached<C>::value) run(std::integral_constant<int, 2>{});
             }
-        };
-        run(std::integral_constant<int, 0>{}, 0, p.q_groups, p.q, p.ld_q, p.q_heads);
-        if (!kept) continue;
-        run(std::integral_constant<int, 1>{}, p.q_groups, p.k_groups, p.k, p.ld_k, p.kv_heads);
-        if constexpr (Cached<C>::value) run(std::integral_constant<int, 2>{}, p.q_groups + p.k_groups, p.v_groups, p.v, p.ld_v, p.kv_heads);
+        }
     }
 }
 
 // The backward pass.  The weights' gradients are summed by every lane over its tokens and heads, by a workgroup over its lanes that have the same
 // elements, and over the workgroups by grad_sum_kernel, all in an order that the sizes alone give.
-template <typename T, int V, int N>
-__global__ __launch_bounds__(kHeadsThreads) void heads_grad_kernel(HeadsArgs p)
+template <typename T, int V, int N, bool NT>
+__global__ __launch_bounds__(kHeadsThreads, 2) void heads_grad_kernel(HeadsArgs p)
 {
-    constexpr int kWaves = kHeadsThreads / kWave;
+    constexpr int kWaves = kHeadsThreads / kWave, kLoads = N == 1 ? kGradBatch : 1;
+    __shared__ Kept kept;
+    __shared__ float2 circle[kHeadsThreads / kWave][TTC_HEADS_MAX_ROTATED / 2];
     __shared__ float sums[kWaves][2][TTC_HEADS_MAX_DIM];
     const uint32_t wave = blockIdx.x * kWaves + threadIdx.x / kWave, waves = gridDim.x * kWaves;
     const uint32_t in_head = threadIdx.x & ((1u << p.lanes_log) - 1), sub = (threadIdx.x & (kWave - 1)) >> p.lanes_log, each = kWave >> p.lanes_log;
-    const uint32_t items = p.tokens * p.split_div.div;
-    Lane<V, N> lane;
-    lane.start(p, in_head);
-    float weight[2][N][2 * V], total[2][N][2 * V] = {};
-    if (p.norm) {
-        load_weights<V, N>(p.q_weight, lane, weight[0]);
-        load_weights<V, N>(p.k_weight, lane, weight[1]);
-    }
+    const uint32_t items = p.tokens * p.split_div.div, q_end = p.q_groups;
+    Lane<V, N> lane(p, in_head);
+    float total[2][N][2 * V] = {};
     const float each_element = 1.f / (float)p.dim;
+    Raw<T, V> raw[kLoads][N], draw[kLoads][N];
+    auto load = [&](const Place& at, uint32_t g0) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const uint32_t g = g0 + i;
+            if (g >= at.end) break;
+            const bool q = g < q_end;
+            const T* row = static_cast<const T*>(q ? p.q : p.k) + (int64_t)at.token * (q ? p.ld_q : p.ld_k);
+            const T* drow = static_cast<const T*>(q ? p.dq_out : p.dk_out) + (int64_t)at.token * (q ? p.ld_dqo : p.ld_dko);
+            const uint32_t head = (q ? g : g - q_end) * each + sub, last = (q ? p.q_heads : p.kv_heads) - 1;
+            const int64_t from = (int64_t)(head < last ? head : last) * p.dim;
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                draw[i][n] = load_unit<T, V>(drow + from, lane.unit[n]);
+                raw[i][n] = load_unit<T, V>(row + from, lane.unit[n]);       // without a norm: the gradients again
+            }
+        }
+    };
+    kept.fill(p);
     for (uint32_t item = __builtin_amdgcn_readfirstlane(wave); item < items; item += waves) {
         const Place at = place_of(p, item);
         if (at.position < 0) continue;
-        lane.token((uint32_t)at.position);
-        auto run = [&](auto kind_of, uint32_t first, uint32_t groups, const void* from, int64_t ld, const void* dfrom, int64_t ldd, void* out, int64_t ldo, uint32_t heads) {
-            constexpr int kind = decltype(kind_of)::value;
-            const uint32_t lo = at.group > first ? at.group - first : 0, hi = at.end > first ? (at.end - first < groups ? at.end - first : groups) : 0;
-            const T* row = static_cast<const T*>(from) + (int64_t)at.token * ld;
-            const T* drow = static_cast<const T*>(dfrom) + (int64_t)at.token * ldd;
-            T* to = static_cast<T*>(out) + (int64_t)at.token * ldo;
-            constexpr int kPairs = 2;
-            for (uint32_t g0 = lo; g0 < hi; g0 += kPairs) {
-                Raw<T, V> raw[kPairs][N], draw[kPairs][N];
+        load(at, at.group);
+        lane.token(p, kept, circle[threadIdx.x / kWave], (uint32_t)at.position);
+        for (uint32_t g0 = at.group; g0 < at.end; g0 += kLoads) {
+            if (g0 != at.group) load(at, g0);
 #pragma unroll
-                for (int i = 0; i < kPairs; ++i) {
-                    const uint32_t head = (g0 + i) * each + sub;
-                    const bool here = g0 + i < hi && head < heads;
-#pragma unroll
-                    for (int n = 0; n < N; ++n) {
-                        draw[i][n] = load_unit<T, V>(drow + (int64_t)head * p.dim, lane.unit[n], here);
-                        raw[i][n] = load_unit<T, V>(row + (int64_t)head * p.dim, lane.unit[n], here && p.norm);
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < kPairs; ++i) {
-                    if (g0 + i >= hi) break;
-                    const uint32_t head = (g0 + i) * each + sub;
-                    const bool here = head < heads;
-                    float x[N][2 * V], g[N][2 * V];
+            for (int i = 0; i < kLoads; ++i) {
+                const uint32_t g = g0 + i;
+                if (g >= at.end) break;
+                auto run = [&](auto kind_of) {
+                    constexpr int kind = decltype(kind_of)::value;
+                    const uint32_t head = (kind == 0 ? g : g - q_end) * each + sub;
+                    const bool here = head < (kind == 0 ? p.q_heads : p.kv_heads);
+                    float x[N][2 * V], d[N][2 * V];
 #pragma unroll
                     for (int n = 0; n < N; ++n) {
-                        widen_unit<T, V>(draw[i][n], g[n]);
-                        widen_unit<T, V>(raw[i][n], x[n]);
+                        widen_unit<T, V>(draw[i][n], lane.unit[n], p.full, here, d[n]);
+                        widen_unit<T, V>(raw[i][n], lane.unit[n], p.full, here, x[n]);
                     }
-                    lane.rotate(g, p.paired, true);
+                    lane.rotate(d, p.paired, true);
                     if (p.norm) {
-                        float square = 0.f, both = 0.f;
+                        float w[N][2 * V], square = 0.f, both = 0.f;
+                        lane.weights(kept.weights[kind], w);
 #pragma unroll
                         for (int n = 0; n < N; ++n)
 #pragma unroll
                             for (int j = 0; j < 2 * V; ++j) {
                                 square = __builtin_fmaf(x[n][j], x[n][j], square);
-                                both = __builtin_fmaf(x[n][j] * weight[kind][n][j], g[n][j], both);
+                                both = __builtin_fmaf(x[n][j] * w[n][j], d[n][j], both);
                             }
-                        const float r = 1.f / __builtin_sqrtf(__builtin_fmaf(over_head(square, p.lanes_log), each_element, p.eps));
+                        const float r = inverse_root(__builtin_fmaf(over_head(square, p.lanes_log), each_element, p.eps));
                         const float mean = over_head(both, p.lanes_log) * each_element * r;       // of g * x / s
 #pragma unroll
                         for (int n = 0; n < N; ++n)
 #pragma unroll
                             for (int j = 0; j < 2 * V; ++j) {
                                 const float hat = x[n][j] * r;
-                                total[kind][n][j] = __builtin_fmaf(hat, g[n][j], total[kind][n][j]);
-                                g[n][j] = r * __builtin_fmaf(g[n][j], weight[kind][n][j], -(hat * mean));
+                                total[kind][n][j] = __builtin_fmaf(hat, d[n][j], total[kind][n][j]);
+                                d[n][j] = r * __builtin_fmaf(d[n][j], w[n][j], -(hat * mean));
                             }
                     }
+                    T* to = static_cast<T*>(kind == 0 ? p.q_out : p.k_out) + (int64_t)at.token * (kind == 0 ? p.ld_qo : p.ld_ko) + (int64_t)head * p.dim;
 #pragma unroll
-                    for (int n = 0; n < N; ++n) store_unit<T, V>(to + (int64_t)head * p.dim, lane.unit[n], here, g[n]);
-                }
+                    for (int n = 0; n < N; ++n) store_unit<NT, T, V>(to, lane.unit[n], here, d[n]);
+                };
+                if (g < q_end) run(std::integral_constant<int, 0>{});
+                else run(std::integral_constant<int, 1>{});
             }
-        };
-        run(std::integral_constant<int, 0>{}, 0, p.q_groups, p.q, p.ld_q, p.dq_out, p.ld_dqo, p.q_out, p.ld_qo, p.q_heads);
-        run(std::integral_constant<int, 1>{}, p.q_groups, p.k_groups, p.k, p.ld_k, p.dk_out, p.ld_dko, p.k_out, p.ld_ko, p.kv_heads);
+        }
     }
     if (!p.partial) return;
     const int mine = threadIdx.x / kWave;
@@ -414,21 +473,29 @@ __global__ __launch_bounds__(kSumColumns * kSumRows) void grad_sum_kernel(SumArg
     if (out) out[i < p.dim ? i : i - p.dim] = v;
 }
 
-template <typename T, typename C> const void* heads_fn(int vec)
+template <typename T, typename C> const void* heads_fn(int vec, bool nt)
 {
     constexpr int V = std::is_same<C, q4>::value ? 8 : 16 / (int)sizeof(T);
-    if (vec == V) return reinterpret_cast<const void*>(&heads_kernel<T, C, V, 1>);
+    if (vec == V) return nt ? reinterpret_cast<const void*>(&heads_kernel<T, C, V, 1, true>) : reinterpret_cast<const void*>(&heads_kernel<T, C, V, 1, false>);
     if constexpr (std::is_same<C, q4>::value) return nullptr;
-    else return reinterpret_cast<const void*>(&heads_kernel<T, C, 1, 4>);
+    else return reinterpret_cast<const void*>(&heads_kernel<T, C, 1, 4, false>);
 }
-template <typename T> const void* heads_fn(int vec, int cache)
+template <typename T> const void* heads_fn(int vec, int cache, bool nt)
 {
-    return cache < 0 ? heads_fn<T, void>(vec) : cache == TTC_F8 ? heads_fn<T, f8>(vec) : cache == TTC_Q4 ? heads_fn<T, q4>(vec) : heads_fn<T, T>(vec);
+    return cache < 0 ? heads_fn<T, void>(vec, nt) : cache == TTC_F8 ? heads_fn<T, f8>(vec, nt) : cache == TTC_Q4 ? heads_fn<T, q4>(vec, nt) : heads_fn<T, T>(vec, nt);
 }
-template <typename T> const void* grad_fn(int vec)
+template <typename T> const void* grad_fn(int vec, bool nt)
 {
     constexpr int V = 16 / (int)sizeof(T);
-    return vec == V ? reinterpret_cast<const void*>(&heads_grad_kernel<T, V, 1>) : reinterpret_cast<const void*>(&heads_grad_kernel<T, 1, 4>);
+    return vec != V ? reinterpret_cast<const void*>(&heads_grad_kernel<T, 1, 4, false>) : nt ? reinterpret_cast<const void*>(&heads_grad_kernel<T, V, 1, true>)
+                                                                                            : reinterpret_cast<const void*>(&heads_grad_kernel<T, V, 1, false>);
+}
+
+// Results of this many bytes are stored with the non-temporal hint.
+constexpr int64_t kStreamResults = int64_t(16) << 20;
+bool streams(const HeadsArgs& p)
+{
+    return (int64_t)p.tokens * ((p.q ? p.q_heads : 0) + (p.k ? p.kv_heads : 0)) * p.dim * elem_bytes(p.dtype) >= kStreamResults;
 }
 
 }  // namespace
@@ -436,18 +503,20 @@ template <typename T> const void* grad_fn(int vec)
 int launch_heads(const HeadsArgs& a, void* stream)
 {
     HeadsArgs p = a;
-    const HeadsShape s = cut_heads(p);
-    const void* fn = p.dtype == TTC_F32 ? heads_fn<float>(s.vec, p.cache_dtype) : p.dtype == TTC_BF16 ? heads_fn<__bf16>(s.vec, p.cache_dtype)
-                                        : heads_fn<_Float16>(s.vec, p.cache_dtype);
+    const HeadsShape s = cut_heads(p, kHeadsGroups);
+    const bool nt = streams(p);
+    const void* fn = p.dtype == TTC_F32 ? heads_fn<float>(s.vec, p.cache_dtype, nt) : p.dtype == TTC_BF16 ? heads_fn<__bf16>(s.vec, p.cache_dtype, nt)
+                                        : heads_fn<_Float16>(s.vec, p.cache_dtype, nt);
     return fn ? launch_blocks(fn, (uint64_t)s.groups, kHeadsThreads, 0, &p, stream) : TTC_ERR_INTERNAL;
 }
 
 int launch_heads_grad(const HeadsArgs& a, void* stream)
 {
     HeadsArgs p = a;
-    const HeadsShape s = cut_heads(p);
+    const HeadsShape s = cut_heads(p, kGradGroups);
+    const bool nt = streams(p);
     if (p.tokens) {
-        const void* fn = p.dtype == TTC_F32 ? grad_fn<float>(s.vec) : p.dtype == TTC_BF16 ? grad_fn<__bf16>(s.vec) : grad_fn<_Float16>(s.vec);
+        const void* fn = p.dtype == TTC_F32 ? grad_fn<float>(s.vec, nt) : p.dtype == TTC_BF16 ? grad_fn<__bf16>(s.vec, nt) : grad_fn<_Float16>(s.vec, nt);
         const int st = launch_blocks(fn, (uint64_t)s.groups, kHeadsThreads, 0, &p, stream);
         if (st != TTC_OK) return st;
     }
