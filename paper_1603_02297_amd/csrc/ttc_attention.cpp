@@ -64,17 +64,16 @@ namespace {
 
 constexpr int64_t kGradPartials = kGradGroups;
 
-// Whether two tensors of `tokens` rows, rows wa and wb bytes long, share a byte.  Rows of one distance are told apart exactly; of two
+// Whether two tensors of `tokens` rows, wa and wb bytes long and lda and ldb elements apart, share a byte.  Rows of one distance are told apart exactly; of two
 // distances in one span they are taken to meet.
-bool rows_meet(const void* a, int64_t lda, int64_t wa, uint64_t span_a, const void* b, int64_t ldb, int64_t wb, uint64_t span_b, int64_t tokens)
+bool rows_meet(const void* a, int64_t lda, int64_t wa, uint64_t span_a, const void* b, int64_t ldb, int64_t wb, uint64_t span_b, int64_t tokens, int eb)
 {
     const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
     if (!a || !b || !(x < y + span_b && y < x + span_a)) return false;
-    if (tokens == 1) return true;
-    if (lda != ldb) return true;
-    const int64_t apart = (int64_t)(y - x), step = apart / lda - (apart % lda < 0);
+    if (tokens == 1 || lda != ldb) return true;
+    const int64_t apart = (int64_t)(y - x), row = lda * eb, step = apart / row - (apart % row < 0);
     for (int64_t t = step; t <= step + 1; ++t) {
-        const int64_t d = apart - t * lda;  // from a's row to b's
+        const int64_t d = apart - t * row;  // from a's row to b's
         if (-tokens < t && t < tokens && -wb < d && d < wa) return true;
     }
     return false;
@@ -102,7 +101,7 @@ template <int N> int check_rows(Rows (&r)[N], int64_t tokens, int eb)
         for (int j = 0; j < N; ++j) {
             if (i == j || !r[i].p || !r[j].p || !r[i].written) continue;
             if (r[i].in_place_of == j && r[i].p == r[j].p && r[i].ld == r[j].ld) continue;
-            if (rows_meet(r[i].p, r[i].ld * eb, r[i].width * eb, r[i].span, r[j].p, r[j].ld * eb, r[j].width * eb, r[j].span, tokens)) return TTC_ERR_ALIAS;
+            if (rows_meet(r[i].p, r[i].ld, r[i].width * eb, r[i].span, r[j].p, r[j].ld, r[j].width * eb, r[j].span, tokens, eb)) return TTC_ERR_ALIAS;
         }
     return TTC_OK;
 }
