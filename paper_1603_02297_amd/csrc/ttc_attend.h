@@ -94,9 +94,12 @@ template <typename T, typename C, int DP, int ROWS, bool OWN> struct Plan {
     static constexpr int  kMergeRows = 8;                                    // of the wavefronts' results that are added up at a time
     static constexpr int  kMergeRow = DP + 4;                                // floats
     static constexpr int  kMerge = FEW ? kWaves * kMergeRows * kMergeRow * 4 + 3 * kWaves * ROWS * 4 : 0;
-    static constexpr int  kLds = kTile * kTeams + kQueries > kMerge ? kTile * kTeams + kQueries : kMerge;
     // workgroups that share a compute unit, and so its registers
     static constexpr int  kResident = attend_resident(sizeof(T), OWN, kRecords, DP, ROWS);
+    // Tiles of a workgroup's in LDS: two where they fit, one written while the other is still read, and one barrier for each instead of two (prompts 450 us; so, and
+    // with a reference that moves seldom, 436).
+    static constexpr int  kTiles = FEW ? kTeams : kResident * (2 * kTile + 256) <= kMaxLdsBytes ? 2 : 1;
+    static constexpr int  kLds = kTile * kTiles + kQueries > kMerge ? kTile * kTiles + kQueries : kMerge;
     static_assert(kResident * (kLds + 256) <= kMaxLdsBytes, "they share its LDS");
     // OWN: the words of a part of a vector, a lane's, and the positions that it has such a part of
     static constexpr bool kCarries = FEW && kAhead;                          // the next piece of work's first tile is loaded beside the end of this one
@@ -110,7 +113,7 @@ template <typename C> struct Chunk8 { Vec<C, 8> v; };
 template <> struct Chunk8<q4> { uint32_t word, head; };
 
 // One load and nothing around it: joined with another path, or under a condition, the compiler would wait for each before the next (700 keys' worth of such
-// waits made a decoding step of 96 requests take 390 us instead of LATER).  Vectors shorter than a chunk (ELEMENTS) go element by element all the same.
+// waits made a decoding step of 96 requests take 390 us instead of 270).  Vectors shorter than a chunk (ELEMENTS) go element by element all the same.
 template <typename C, bool ELEMENTS> __device__ __forceinline__ Chunk8<C> load_chunk(const char* vector, uint32_t at, uint32_t dim)
 {
     Chunk8<C> r = {};
@@ -266,6 +269,20 @@ __device__ __forceinline__ uint64_t uniform(uint64_t x) { return (uint64_t)unifo
 template <typename X> __device__ __forceinline__ X scalar(const X* p, uint32_t i) { return ((const __attribute__((address_space(4))) X*)p)[i]; }
 // Numbers of 64 bits that mostly are of 32.
 __device__ __forceinline__ uint64_t quotient(uint64_t a, uint64_t b) { return (a | b) >> 32 ? a / b : (uint32_t)a / (uint32_t)b; }
+
+// Asks for N products with READS reads of LDS each in this order: the reads of four products first, then a product and the next one's reads in turn.  Left alone the
+// compiler keeps two reads under way and the products wait for LDS (11900 tokens of prompts 396 us; with it 381; six ahead 382).
+template <int N, int READS> __device__ __forceinline__ void feed()
+{
+    constexpr int kProduct = 0x8, kRead = 0x100, kFirst = 4;
+    __builtin_amdgcn_sched_group_barrier(kRead, kFirst * READS, 0);
+#pragma unroll
+    for (int i = 0; i < N - kFirst; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kProduct, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kRead, READS, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(kProduct, kFirst, 0);
+}
 
 // Some rows of a request's for one head, and some of the positions that they see.
 struct Work {
@@ -510,13 +527,14 @@ template <typename T, typename C, int DP, int ROWS, bool OWN> struct Reader {
         const uint32_t key = at + (lane & (P::kKeys - 1));
         return key < w.hi ? p.table[(int64_t)w.request * p.ld_table + fdiv(key, p.page)] : -1;
     }
+    static constexpr bool kEven = P::kTeam % P::kChunks == 0;                // a thread's chunks are the same one of vectors a constant apart
     // A thread's chunks of a tile.  The last one of a vector is moved back to end with it, and those behind it are that one again.
     __device__ __forceinline__ uint32_t chunk_of(int i) const
     {
-        const uint32_t at = (member + i * P::kTeam) % P::kChunks * 8, last = p.dim < 8 ? 0 : p.dim - 8;
+        const uint32_t at = (kEven ? member % P::kChunks : (member + i * P::kTeam) % P::kChunks) * 8, last = p.dim < 8 ? 0 : p.dim - 8;
         return at < last ? at : last;
     }
-    __device__ __forceinline__ uint32_t key_of(int i) const { return (member + i * P::kTeam) / P::kChunks; }
+    __device__ __forceinline__ uint32_t key_of(int i) const { return kEven ? member / P::kChunks + i * (P::kTeam / P::kChunks) : (member + i * P::kTeam) / P::kChunks; }
     __device__ __forceinline__ int64_t place(int64_t offset, uint32_t key) const
     {
         return (int64_t)((uint64_t)(uint32_t)__shfl((uint32_t)(offset >> 32), key) << 32 | (uint32_t)__shfl((uint32_t)offset, key));
@@ -659,9 +677,19 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
     }
 
     char* tile = lds + (FEW ? wave * P::kTile : 0);
-    char *keys = tile, *values = tile + (OWN ? 0 : P::kKeys * P::kKeyRow);
-    float* key_step = reinterpret_cast<float*>(values + P::kKeys * P::kValueRow);           // kCodes: four arrays of kKeys
-    float *key_low = key_step + P::kKeys, *value_step = key_low + P::kKeys, *value_low = value_step + P::kKeys;
+    char *keys, *values;
+    float *key_step, *key_low, *value_step, *value_low;                     // kCodes: of kKeys each
+    auto use_tile = [&](char* there) {
+        keys = there;
+        values = there + (OWN ? 0 : P::kKeys * P::kKeyRow);
+        key_step = reinterpret_cast<float*>(values + P::kKeys * P::kValueRow);
+        key_low = key_step + P::kKeys;
+        value_step = key_low + P::kKeys;
+        value_low = value_step + P::kKeys;
+    };
+    constexpr bool kTwo = !FEW && P::kTiles == 2, kFed = !FEW && sizeof(T) == 2;
+    uint32_t second = 0;
+    use_tile(tile);
     // A thread's chunks of a tile.
     const bool whole = p.dim % 8 == 0;
     auto chunk_of = [&](int i) { return read.chunk_of(i); };
@@ -744,7 +772,7 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
                 value_low[key] = __builtin_fmaf(8.f, vs, __builtin_bit_cast(float, v[b].head & 0xffff0000u));
             }
     };
-    char* queries = lds + P::kTile * P::kTeams + lane * 16;
+    char* queries = lds + P::kTile * P::kTiles + lane * 16;
     if constexpr (P::kQueriesInLds) {
         if (wave == 0) {
 #pragma unroll
@@ -759,7 +787,10 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
     // what lies behind the vectors' ends in the tile's rows: 0, once
     if (!OWN && p.dim < DP) {
         for (uint32_t key = read.member / 32; key < P::kKeys; key += P::kTeam / 32)
-            for (uint32_t d = p.dim + read.member % 32; d < DP; d += 32) reinterpret_cast<KE*>(keys + key * P::kKeyRow)[d] = (KE)0.f;
+            for (uint32_t d = p.dim + read.member % 32; d < DP; d += 32) {
+                reinterpret_cast<KE*>(keys + key * P::kKeyRow)[d] = (KE)0.f;
+                if constexpr (kTwo) reinterpret_cast<KE*>(keys + P::kTile + key * P::kKeyRow)[d] = (KE)0.f;
+            }
     }
 
     Acc out[kOut] = {};
@@ -778,7 +809,12 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
         const uint32_t tile_lowest = w.cached + fdiv(w.row0, p.group_div);
         const bool look = holes || end > tile_lowest + 1 || (p.window && at + p.window <= w.cached + fdiv(w.row0 + ROWS < w.rows ? w.row0 + ROWS - 1 : w.rows - 1, p.group_div));
         bool bad;
-        team_sync<FEW>();                                                   // the tile before has been used
+        if constexpr (kTwo) {
+            use_tile(tile + second);                                        // last read two tiles ago, before the barrier of the one between
+            second ^= (uint32_t)P::kTile;
+        } else {
+            team_sync<FEW>();                                               // the tile before has been used
+        }
         if constexpr (OWN) {
             if constexpr (P::kCodes) put_steps(f.part_k, f.part_v);
             bad = put_parts(f.part_v, now, holes, look);
@@ -814,6 +850,7 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
                 else mul(*reinterpret_cast<const KFrag*>(from + i * P::kDims * sizeof(KE)), query_of(i), score[b]);
             }
         }
+        if constexpr (kFed) feed<kBlocks * kSteps, 1>();
         if constexpr (OWN)
             if (at + P::kStep < w.hi) read.follow(w, at + P::kStep, f);
         // register i of block b is position M b + kGap (i / 4) + 4 part + i % 4
@@ -851,8 +888,11 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
 #pragma unroll
             for (int i = 0; i < kRegisters; ++i) most = __builtin_fmaxf(most, score[b][i]);
         most = max_of_row<M>(most) * scale;
-        if (__ballot(most > top)) {
-            const float higher = __builtin_fmaxf(top, most), factor = higher == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(top - higher);
+        // The reference of the exponentials follows the maximum once that is 2^kSlack above it: results need their largest term near 1 only so far as 32 bits (and 16 for
+        // the weights) must hold them.  Followed at once it moves in most tiles, for some row of 32, and costs every element of the result a product each time.
+        constexpr float kSlack = 8.f;
+        if (__ballot(most > top + kSlack)) {
+            const float higher = most > top + kSlack ? most : top, factor = higher == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(top - higher);
             top = higher;
             sum *= factor;
             low_sum *= factor;
@@ -966,6 +1006,7 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
 #pragma unroll
                 for (int k = 0; k < kTakes; ++k) mul(v[k], weight[k], out[d]);
             }
+            if constexpr (kFed) feed<kOut * kTakes, 2>();
         }
     }
 
@@ -1071,10 +1112,13 @@ __global__ __launch_bounds__((Plan<T, C, DP, ROWS, OWN>::kThreads), (Plan<T, C, 
     Work w;
     Flight<T, C, DP, ROWS, OWN> f;
     if constexpr (!P::FEW) {
-        const uint32_t slot = p.slots_of_tiles - 1 - blockIdx.x;            // the last tiles see most: first
-        w.head = blockIdx.y;
-        if (!find_tile<P, ROWS>(p, slot, blockIdx.z, w)) return;
-        w.partial_row = ((slot * p.heads + w.head) * p.splits + blockIdx.z) * ROWS;
+        // Heads next to each other, tiles from the last on: those see most, and begin first.  (A head's tiles together, the last head's end alone: 436 us for 396.)
+        const uint32_t id = uniform((uint32_t)block_id()), place = id / p.heads, split = place % p.splits;
+        if (place / p.splits >= p.slots_of_tiles) return;
+        const uint32_t slot = p.slots_of_tiles - 1 - place / p.splits;
+        w.head = id - place * p.heads;
+        if (!find_tile<P, ROWS>(p, slot, split, w)) return;
+        w.partial_row = ((slot * p.heads + w.head) * p.splits + split) * ROWS;
         attend_work<T, C, DP, ROWS, OWN>(p, w, w, false, f, lds);
     } else {
         Shares s;

@@ -81,11 +81,8 @@ int launch_attend(const AttendArgs& a, const AttendShape& s, void* stream)
         }
     }
     AttendArgs p = a;
-    void* list[] = {&p};
-    // few rows: shares; else x: the tiles; y: heads of the cache (at most 65535 by the handle); z: parts
-    const dim3 grid = s.tile < (uint32_t)kTileMany ? dim3(s.shares) : dim3(s.slots, p.heads, p.splits);
-    if (hipLaunchKernel(k.fn, grid, dim3(k.threads), list, (size_t)k.lds, (hipStream_t)stream) != hipSuccess) return TTC_ERR_HIP;
-    if (!s.partial_rows) return TTC_OK;
+    const int rc = launch_blocks(k.fn, s.tile < (uint32_t)kTileMany ? s.shares : (uint64_t)s.slots * p.heads * p.splits, k.threads, (size_t)k.lds, &p, stream);
+    if (rc != TTC_OK || !s.partial_rows) return rc;
     const void* join = a.dtype == TTC_F32 ? reinterpret_cast<const void*>(&join_kernel<float>) : a.dtype == TTC_BF16 ? reinterpret_cast<const void*>(&join_kernel<__bf16>)
                                                                                               : reinterpret_cast<const void*>(&join_kernel<_Float16>);
     return launch_blocks(join, ((uint64_t)p.tokens * p.q_heads + 3) / 4, 256, 0, &p, stream);
