@@ -1177,9 +1177,16 @@ template <typename T, typename C, int DP, int ROWS, bool OWN> AttendKernel kerne
 }
 template <typename T, typename C, int DP> AttendKernel kernel_of(int dim, int rows)
 {
+    constexpr bool kHalf = attend_half(sizeof(T), std::is_same<C, q4>::value, DP);
     if constexpr (sizeof(T) == 2 && sizeof(C) == 1)
-        if (attend_own(sizeof(T), sizeof(C), dim, rows)) return rows == 16 ? kernel_of<T, C, DP, 16, true>() : kernel_of<T, C, DP, 32, true>();
-    return rows == 16 ? kernel_of<T, C, DP, 16, false>() : rows == 32 ? kernel_of<T, C, DP, 32, false>() : kernel_of<T, C, DP, 128, false>();
+        if (attend_own(sizeof(T), sizeof(C), dim, rows)) {
+            if constexpr (kHalf)
+                if (rows == 32) return kernel_of<T, C, DP, 32, true>();
+            return kernel_of<T, C, DP, 16, true>();
+        }
+    if constexpr (kHalf)
+        if (rows == 32) return kernel_of<T, C, DP, 32, false>();
+    return rows == 16 ? kernel_of<T, C, DP, 16, false>() : kernel_of<T, C, DP, 128, false>();
 }
 template <typename T, typename C> AttendKernel kernel_of(int dim, int rows)
 {

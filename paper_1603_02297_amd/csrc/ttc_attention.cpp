@@ -40,15 +40,22 @@ AttendShape attend_shape(const ttc_attend_s* a, int64_t requests, int64_t tokens
 {
     AttendShape s = {};
     const int64_t heads = a->heads, rows = tokens * (a->q_heads / heads);
-    s.tile = rows <= 16 * requests ? 16 : rows <= 48 * requests ? 32 : kTileMany;
+    // Rows of a tile, from how many rows a request has of a head on average.  Tiles of 16 and 32 rows: each wavefront has positions of its own; of many: each has rows
+    // of its own, and all share the positions in LDS.  32 requests behind 8000 positions, heads of 128, in us with tiles of 16, 32 and many: 32 rows 232, 233, 246; 48
+    // rows 570, 265, 222.  Codes of 4 bits, once widened in LDS, cost most with many (heads of 256, 48 rows: 449, 345, 643), and so do products in 32 bits (2000
+    // positions, heads of 128, 48 rows: 282, 240, 320).  Where 32 rows do not fit the registers, 32 rows take 697 in tiles of 16 and 417 in many, in 32 bits 288 and 452.
+    const int bytes = elem_bytes(a->dtype);
+    const bool records = a->cache_dtype == TTC_Q4;
+    if (rows <= 16 * requests) s.tile = 16;
+    else if (attend_half(bytes, records, attend_dim((int)a->dim))) s.tile = rows <= (bytes == 4 || records ? 48 : 32) * requests ? 32 : kTileMany;
+    else s.tile = bytes == 4 && rows <= 32 * requests ? 16 : kTileMany;
     // request r's tiles are numbered from starts[r] * group / tile + r on: always enough, and found without a sum over the requests
     s.slots = (uint32_t)(rows / s.tile + requests);
     const int64_t groups = std::max<int64_t>((int64_t)s.slots * heads, 1), units = std::max<int64_t>((longest + kAttendUnit - 1) / kAttendUnit, 1);
     if (s.tile < kTileMany) {
         // As many shares as workgroups fit the device at a time: 64 requests of 8000 positions in 16 bits take 5.84 TB/s, and less with one and a half, two or four
         // times as many.
-        const int64_t most = 256 * attend_resident(elem_bytes(a->dtype), attend_own(elem_bytes(a->dtype), elem_bytes(a->cache_dtype), (int)a->dim, (int)s.tile),
-                                                   a->cache_dtype == TTC_Q4, (int)a->dim, (int)s.tile);
+        const int64_t most = 256 * attend_resident(bytes, attend_own(bytes, elem_bytes(a->cache_dtype), (int)a->dim, (int)s.tile), records, (int)a->dim, (int)s.tile);
         const int64_t each = std::max<int64_t>(most / heads, 1);               // of a head
         s.shares = (uint32_t)(heads * (s.slots >= each / units ? std::min<int64_t>(each, s.slots * units) : s.slots * units));
         s.splits = 1;

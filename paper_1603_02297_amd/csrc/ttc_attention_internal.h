@@ -93,6 +93,8 @@ constexpr int attend_resident(int bytes, bool own, bool records, int dim, int ti
 {
     return bytes == 4 || dim > 128 ? 1 : own && records && tile == 16 ? 3 : 2;
 }
+// Whether there are tiles of 32 rows: their results, the queries and a tile of the cache on its way have to fit the registers.
+constexpr bool attend_half(int bytes, bool records, int dim) { return bytes == 4 ? dim <= 128 : dim <= 192 || records; }
 constexpr uint32_t kAttendUnit = 128, kAttendMaxParts = 128;     // positions that are not shared among workgroups; results that a row may have to be joined from
 
 struct AttendShape {
