@@ -68,12 +68,14 @@ template <typename T, typename C, int DP, int ROWS, bool OWN> struct Plan {
     static constexpr bool FEW = ROWS < 128;
     static constexpr int  M = ROWS < 32 ? 16 : 32, kParts = kWave / M;
     typedef T K;                                                            // keys in LDS
-    // Values in LDS, and the exponentials.  Codes of 4 bits are multiplied by exponentials times steps, of which fp16 would lose the small ones: bf16.
-    typedef typename std::conditional<std::is_same<C, q4>::value && !std::is_same<T, float>::value, __bf16, T>::type V;
+    typedef T V;                                                            // values in LDS, and the exponentials
     static constexpr bool kRecords = std::is_same<C, q4>::value;
     // records as codes (integers that 16 bits hold), step and minimum applied to scores and exponentials; in 32 bits as what they stand for
     static constexpr bool kCodes = kRecords && sizeof(T) == 2;
     static constexpr bool kWide = sizeof(T) == 4;
+    // Codes are multiplied by exponentials times steps.  fp16 would lose those of small steps and not hold those of large ones: there the exponentials' reference is the
+    // largest exponential times step, and the steps' logarithms lie beside them.
+    static constexpr bool kLogs = kCodes && std::is_same<T, _Float16>::value;
     static constexpr int  kWaves = FEW && kWide && DP > 128 ? 2 : 4;
     static constexpr int  kThreads = kWaves * kWave;
     static constexpr int  kTeams = FEW ? kWaves : 1;
@@ -86,7 +88,7 @@ template <typename T, typename C, int DP, int ROWS, bool OWN> struct Plan {
     // rows in LDS end 16 and 32 bytes later than their elements, so that eight rows (four, of values) meet all banks
     static constexpr int  kKeyRow = DP * (int)sizeof(K) + 16;
     static constexpr int  kValueRow = OWN ? (kRecords ? DP / 2 : DP) + 8 : DP * (int)sizeof(V) + (kWide ? 16 : 32);
-    static constexpr int  kTile = kKeys * ((OWN ? 0 : kKeyRow) + kValueRow) + (kCodes ? 4 * kKeys * 4 : 0);
+    static constexpr int  kTile = kKeys * ((OWN ? 0 : kKeyRow) + kValueRow) + (kCodes ? (kLogs ? 5 : 4) * kKeys * 4 : 0);
     // The queries' fragments in LDS, the same for all wavefronts, where keys and values on their way take the registers.
     static constexpr bool kQueriesInLds = ROWS == 32 && !OWN && sizeof(C) == 2;
     static constexpr int  kDims = kParts * 16 / (int)sizeof(K);              // of the contracted index, in a fragment over a row's lanes
@@ -678,7 +680,9 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
 
     char* tile = lds + (FEW ? wave * P::kTile : 0);
     char *keys, *values;
-    float *key_step, *key_low, *value_step, *value_low;                     // kCodes: of kKeys each
+    float *key_step, *key_low, *value_step, *value_low, *value_log;         // kCodes: of kKeys each
+    // of a step; results in fp16 see nothing of values below 2^-24
+    auto log_of = [](float step) { return __builtin_fminf(__builtin_fmaxf(__builtin_amdgcn_logf(step), -24.f), 100.f); };
     auto use_tile = [&](char* there) {
         keys = there;
         values = there + (OWN ? 0 : P::kKeys * P::kKeyRow);
@@ -686,6 +690,7 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
         key_low = key_step + P::kKeys;
         value_step = key_low + P::kKeys;
         value_low = value_step + P::kKeys;
+        value_log = value_low + P::kKeys;
     };
     constexpr bool kTwo = !FEW && P::kTiles == 2, kFed = !FEW && sizeof(T) == 2;
     uint32_t second = 0;
@@ -733,6 +738,7 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
                     const float step = __builtin_bit_cast(float, raw[i].head << 16);
                     value_step[key_of(i)] = step;
                     value_low[key_of(i)] = __builtin_fmaf(8.f, step, __builtin_bit_cast(float, raw[i].head & 0xffff0000u));
+                    if constexpr (P::kLogs) value_log[key_of(i)] = log_of(step);
                 }
         }
         return bad;
@@ -770,6 +776,7 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
                 key_low[key] = __builtin_fmaf(-16.f, ks, __builtin_bit_cast(float, k[b].head & 0xffff0000u));
                 value_step[key] = vs;
                 value_low[key] = __builtin_fmaf(8.f, vs, __builtin_bit_cast(float, v[b].head & 0xffff0000u));
+                if constexpr (P::kLogs) value_log[key] = log_of(vs);
             }
     };
     char* queries = lds + P::kTile * P::kTiles + lane * 16;
@@ -883,11 +890,24 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
             }
         }
         float most = -__builtin_inff();
+        if constexpr (P::kLogs) {
 #pragma unroll
-        for (int b = 0; b < kBlocks; ++b)
+            for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-            for (int i = 0; i < kRegisters; ++i) most = __builtin_fmaxf(most, score[b][i]);
-        most = max_of_row<M>(most) * scale;
+                for (int j = 0; j < kRegisters / 4; ++j) {
+                    const float4 log = *reinterpret_cast<const float4*>(value_log + b * M + j * kGap + part * 4);
+                    const float logs[4] = {log.x, log.y, log.z, log.w};
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) most = __builtin_fmaxf(most, __builtin_fmaf(score[b][4 * j + c], scale, logs[c]));
+                }
+            most = max_of_row<M>(most);
+        } else {
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int i = 0; i < kRegisters; ++i) most = __builtin_fmaxf(most, score[b][i]);
+            most = max_of_row<M>(most) * scale;
+        }
         // The reference of the exponentials follows the maximum once that is 2^kSlack above it: results need their largest term near 1 only so far as 32 bits (and 16 for
         // the weights) must hold them.  Followed at once it moves in most tiles, for some row of 32, and costs every element of the result a product each time.
         constexpr float kSlack = 8.f;
@@ -930,12 +950,16 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
 #pragma unroll
             for (int e = 0; e < kEach; ++e) weight[k][e] = (VE)score[(k * kEach + e) / kRegisters][(k * kEach + e) % kRegisters];
         if constexpr (P::kCodes) {
-            typedef __bf16 Two __attribute__((ext_vector_type(2)));
-            const Two back = {(__bf16)-24.f, (__bf16)-24.f};
+            typedef VE Two __attribute__((ext_vector_type(2)));
+            const Two back = {(VE)-24.f, (VE)-24.f};
 #pragma unroll
             for (int k = 0; k < kTakes; ++k)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) low_sum = __builtin_amdgcn_fdot2_f32_bf16(Two{weight[k][2 * e], weight[k][2 * e + 1]}, back, low_sum, false);
+                for (int e = 0; e < 4; ++e) {
+                    const Two two = {weight[k][2 * e], weight[k][2 * e + 1]};
+                    if constexpr (P::kLogs) low_sum = __builtin_amdgcn_fdot2(two, back, low_sum, false);
+                    else low_sum = __builtin_amdgcn_fdot2_f32_bf16(two, back, low_sum, false);
+                }
         }
         // the left operands of rows d * M ... of the result
         auto values_of = [&](int d, VFrag* v) {
