@@ -339,6 +339,87 @@ def test_same_bits_again_on_another_stream_and_in_graphs(lengths):
             p.call(attend, d[0], work[0])
 
 
+@gpu
+@pytest.mark.parametrize("kind,cache", [("bf16", "bf16"), ("f16", "f8"), ("f16", "q4"), ("bf16", "q4"), ("f32", "f32")])
+@pytest.mark.parametrize("fresh", [1, 100])
+def test_scores_that_rise_along_the_positions(kind, cache, fresh):
+    """The largest score so far moves by a little in every tile, and by much at some: each exponential is taken of a difference to some earlier maximum."""
+    p = Problem(kind, cache, "slots", 2, 1, 32, 16, [(900, fresh), (40, fresh)], seed=13)
+    p.q.fill_(0)
+    p.q[:, 0::32] = 1                                             # a score is 16 times the key's first element
+    for r in range(2):
+        c, f = int(p.cached[r]), int(p.starts[r + 1] - p.starts[r])
+        for at in range(c + f):
+            x, where = (at % 400) / 128 + 2 * (at // 400), (int(p.table[r, at // 16]), at % 16, 0)
+            if cache == "q4":
+                p.caches[0][where][:4] = torch.tensor([2.0 ** -7, x], dtype=torch.bfloat16).view(torch.uint8)
+                p.caches[0][where][4:] = 0
+            else:
+                p.caches[0][where][0] = x
+    if cache == "f8":
+        p.scales[0].fill_(1.0)
+    p.check(16.0)
+
+
+@gpu
+@pytest.mark.parametrize("lengths", [[(70, 1), (300, 1)], [(200, 20)], [(30, 100), (0, 64)]])
+def test_fp16_over_four_bits_keeps_its_precision(lengths):
+    """Steps from 2^-14 to 2^10, exponentials times steps rounded to fp16 and no further."""
+    p = Problem("f16", "q4", "slots", 4, 1, 128, 16, lengths, seed=14)
+    g = torch.Generator().manual_seed(15)
+    shape = p.caches[1].shape[:3]
+    step = (2.0 ** torch.randint(-14, 11, shape, generator=g) * (1 + torch.rand(shape, generator=g))).to(torch.bfloat16)
+    p.caches[1][..., :4] = torch.stack([step, -7 * step], -1).to(torch.bfloat16).view(torch.uint8)
+    out, limit, lse, lse_limit = p.expect(0.01)
+    # The limit without the roundings of weights has those to 2^-8 taken out: of w |16 step + min| all told.  In fp16 a weight is off by 2^-11 of itself, or by 2^-25 where
+    # that is more: of a scale on which the largest of the row is 1 at least.  A code's factor is 8 + 16 at most beside it.
+    step, low, code = ref.from_records(p.caches[1].contiguous().numpy())
+    k, _ = p.values(0)
+    q = moves.wide(p.q)[:, :4 * 128].reshape(p.tokens, 4, 128)
+    for r, (c, f) in enumerate(lengths):
+        for i in range(f):
+            at = np.arange(c + i + 1)
+            entry, slot = p.table[r, at // 16], at % 16
+            st, mag = np.abs(step[entry, slot, 0]).reshape(-1), (16 * np.abs(step) + np.abs(low))[entry, slot, 0].reshape(-1)
+            t = int(p.starts[r]) + i
+            for h in range(4):
+                s = 0.01 * (k[entry, slot, 0] @ q[t, h])
+                w = np.exp(s - s.max())
+                w /= w.sum()
+                limit[t, h] -= (2.0 ** -8 - 2.0 ** -11) * (w @ mag) * (1 + 2.0 ** -11)
+                limit[t, h] += (len(at) * 24 * 2.0 ** -25 * (w * st).max()) * (1 + 2.0 ** -11)
+    got, got_lse = p.run(0.01)
+    ref.assert_within(got, out, limit)
+    ref.assert_within(got_lse, lse, lse_limit, "lse")
+
+
+@gpu
+@pytest.mark.parametrize("kind,cache,dim", [("bf16", "bf16", 256), ("f16", "f8", 256), ("bf16", "q4", 256), ("f32", "f32", 192), ("f32", "q4", 256), ("bf16", "f8", 200)])
+@pytest.mark.parametrize("fresh", [3, 5, 7])
+def test_wide_heads_and_tiles_of_every_size(kind, cache, dim, fresh):
+    """24, 40 and 56 rows of a request's."""
+    Problem(kind, cache, "slots", 8, 1, dim, 16, [(150, fresh), (0, fresh), (31, fresh)], seed=16).check(0.05)
+
+
+@gpu
+def test_first_call_in_a_graph():
+    """A kernel that asks for more LDS than every launch may have asks for it on its first call, which may be a captured one."""
+    p = Problem("bf16", "bf16", "slots", 6, 1, 200, 16, [(40, 90)], seed=17)
+    pages, attend_of = p.handles(0.1, 0)
+    with pages as c, attend_of(c) as attend:
+        d, eager, work = p.to_gpu(), p.to_gpu(), p.workspace(attend)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            p.call(attend, d, work)
+        p.call(attend, eager, work)
+        for _ in range(3):
+            d["out"].fill_(9.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(d["out"], eager["out"]) and torch.equal(d["lse"], eager["lse"])
+
+
 # ---- refusals: before anything reaches a device -----------------------------------------------------------
 
 V, O, T, N, A, M = (getattr(ttc, "TTC_ERR_" + x) for x in ("INVALID_VALUE", "OVERFLOW", "UNSUPPORTED_DTYPE", "NULL_POINTER", "ALIAS", "MISALIGNED"))
