@@ -250,6 +250,8 @@ __device__ __forceinline__ void store_cached(void* cache, int64_t at, float scal
     }
 }
 
+// Bound by memory: 16384 tokens of 32 + 8 heads of 128 bf16 (336 MB) 55 us, 6.1 TB/s; 21300 tokens into 8 bits, queries packed beside them (480 MB), 88 us, 5.5.  Into
+// 4 bits a vector's extremes and codes take the time: 6900 tokens of 28 + 4 heads of 64 17 us, where the bytes take 9.  A decoding step (64 to 128 tokens) is 4.4 to 4.6 us of latency.
 template <typename T, typename C, int V, int N, bool NT>
 __global__ __launch_bounds__(kHeadsThreads, 4) void heads_kernel(HeadsArgs p)
 {
@@ -339,7 +341,8 @@ __global__ __launch_bounds__(kHeadsThreads, 4) void heads_kernel(HeadsArgs p)
 }
 
 // The backward pass.  The weights' gradients are summed by every lane over its tokens and heads, by a workgroup over its lanes that have the same
-// elements, and over the workgroups by grad_sum_kernel, all in an order that the sizes alone give.
+// elements, and over the workgroups by grad_sum_kernel, all in an order that the sizes alone give.  Bound by memory: 8192 tokens of 32 + 8 heads of 128 bf16 (252 MB)
+// 52 us, 4.9 TB/s, and 5 for the sums over the workgroups, which are a launch.
 template <typename T, int V, int N, bool NT>
 __global__ __launch_bounds__(kHeadsThreads, 2) void heads_grad_kernel(HeadsArgs p)
 {

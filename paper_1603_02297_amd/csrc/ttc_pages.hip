@@ -403,6 +403,7 @@ struct RecordArgs {
     FastDiv  heads;
 };
 
+// Records and vectors, a lane eight elements of one.  What 6900 tokens of 4 heads of 64 fp16 take in and out is a launch (4.8 us for 10 MB).
 template <typename T, bool WRITE>
 __global__ __launch_bounds__(kMoveThreads) void records_kernel(RecordArgs p)
 {
