@@ -6,12 +6,15 @@ namespace ttc {
 namespace {
 
 // A wavefront a row: its partial results, weighted by their share of all exponentials.  Rows of one part have been written, and so have, by
-// nobody, those before the first and behind the last request.  A chain of loads (requests, parts, sums, results) bounds it: 3 us for a token of 8 heads, 7 for 96 of 32.
-template <typename T>
+// nobody, those before the first and behind the last request.  A chain of loads (requests, parts, sums, results) bounds it: 3 us for a token of 8 heads.
+// So the first parts' results are loaded beside their sums, kBatch of them at a time (96 tokens of 32 heads 5.4 us; four at a time behind the sums 6.8, and 9.9 instead
+// of 5.8 where rows have up to 13).
+template <typename T, int EACH>
 __global__ __launch_bounds__(256) void join_kernel(AttendArgs p)
 {
     touch<AttendArgs>();
-    constexpr int kEach = TTC_ATTEND_MAX_DIM / kWave;
+    constexpr uint32_t kBatch = EACH > 2 ? 8 : 16;
+    static_assert(kAttendMaxParts == 2 * kWave, "two to a lane");
     const uint32_t lane = threadIdx.x & (kWave - 1);
     const uint32_t row = __builtin_amdgcn_readfirstlane(block_id() * (256 / kWave) + threadIdx.x / kWave);
     if (row >= p.tokens * p.q_heads) return;
@@ -28,7 +31,24 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs p)
 #pragma unroll
     for (uint32_t c = 0; c < kAttendMaxParts / kWave; ++c) {
         const uint32_t i = c * kWave + lane;
-        mine[c] = i < parts ? p.partial_lse[place(i)] : -__builtin_inff();
+        mine[c] = p.partial_lse[place(i < parts ? i : 0)];
+    }
+    float part[kBatch][EACH];
+    auto load = [&](uint32_t from) {
+#pragma unroll
+        for (uint32_t s = 0; s < kBatch; ++s) {
+            const float* there = p.partial + (int64_t)place(from + s < parts ? from + s : 0) * p.dim;
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) {
+                const uint32_t d = e * kWave + lane;
+                part[s][e] = there[d < p.dim ? d : 0];
+            }
+        }
+    };
+    load(0);
+#pragma unroll
+    for (uint32_t c = 0; c < kAttendMaxParts / kWave; ++c) {
+        mine[c] = c * kWave + lane < parts ? mine[c] : -__builtin_inff();
         top = __builtin_fmaxf(top, mine[c]);
     }
     for (int i = 1; i < kWave; i <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, i));
@@ -41,28 +61,28 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs p)
     }
     for (int i = 1; i < kWave; i <<= 1) sum += __shfl_xor(sum, i);
     const float inverse = sum == 0.f ? 0.f : 1.f / sum;
-    float x[kEach] = {};
+    float x[EACH] = {};
+    for (uint32_t from = 0; from < parts; from += kBatch) {
+        if (from) load(from);
 #pragma unroll
-    for (uint32_t c = 0; c < kAttendMaxParts / kWave; ++c) {
-        if (c * kWave >= parts) break;
-        const uint32_t some = parts - c * kWave < (uint32_t)kWave ? parts - c * kWave : kWave;
-#pragma unroll 4
-        for (uint32_t s = 0; s < some; ++s) {
-            const float f = __shfl(mine[c], s) * inverse;
-            const float* from = p.partial + (int64_t)place(c * kWave + s) * p.dim;
+        for (uint32_t s = 0; s < kBatch; ++s) {
+            const uint32_t i = from + s;
+            const float weight = __shfl(i < kWave ? mine[0] : mine[1], i % kWave) * inverse;          // 0 behind the last part
 #pragma unroll
-            for (int j = 0; j < kEach; ++j) {
-                const uint32_t d = j * kWave + lane;
-                const float v = from[d < p.dim ? d : 0];
-                x[j] = f == 0.f ? x[j] : __builtin_fmaf(f, v, x[j]);        // nothing seen, or nothing left of it
-            }
+            for (int e = 0; e < EACH; ++e) x[e] = weight == 0.f ? x[e] : __builtin_fmaf(weight, part[s][e], x[e]);        // nothing seen, or nothing left of it
         }
     }
     T* out = static_cast<T*>(p.out) + (int64_t)token * p.ld_o + (int64_t)head * p.dim;
 #pragma unroll
-    for (int j = 0; j < kEach; ++j)
-        if (j * kWave + lane < p.dim) out[j * kWave + lane] = (T)x[j];
+    for (int e = 0; e < EACH; ++e)
+        if (e * kWave + lane < p.dim) out[e * kWave + lane] = (T)x[e];
     if (p.lse && lane == 0) p.lse[row] = sum == 0.f ? -__builtin_inff() : base + __builtin_logf(sum);
+}
+
+template <typename T> const void* join_of(uint32_t dim)
+{
+    return dim <= 64 ? reinterpret_cast<const void*>(&join_kernel<T, 1>) : dim <= 128 ? reinterpret_cast<const void*>(&join_kernel<T, 2>)
+                                                                                       : reinterpret_cast<const void*>(&join_kernel<T, TTC_ATTEND_MAX_DIM / kWave>);
 }
 
 }  // namespace
@@ -83,8 +103,7 @@ int launch_attend(const AttendArgs& a, const AttendShape& s, void* stream)
     AttendArgs p = a;
     const int rc = launch_blocks(k.fn, s.tile < (uint32_t)kTileMany ? s.shares : (uint64_t)s.slots * p.heads * p.splits, k.threads, (size_t)k.lds, &p, stream);
     if (rc != TTC_OK || !s.partial_rows) return rc;
-    const void* join = a.dtype == TTC_F32 ? reinterpret_cast<const void*>(&join_kernel<float>) : a.dtype == TTC_BF16 ? reinterpret_cast<const void*>(&join_kernel<__bf16>)
-                                                                                              : reinterpret_cast<const void*>(&join_kernel<_Float16>);
+    const void* join = a.dtype == TTC_F32 ? join_of<float>(p.dim) : a.dtype == TTC_BF16 ? join_of<__bf16>(p.dim) : join_of<_Float16>(p.dim);
     return launch_blocks(join, ((uint64_t)p.tokens * p.q_heads + 3) / 4, 256, 0, &p, stream);
 }
 
