@@ -420,6 +420,42 @@ def test_first_call_in_a_graph():
             assert torch.equal(d["out"], eager["out"]) and torch.equal(d["lse"], eager["lse"])
 
 
+@gpu
+@pytest.mark.parametrize("kind,cache", [("bf16", "bf16"), ("f16", "q4"), ("f32", "f8")])
+@pytest.mark.parametrize("lengths", [[(100, 1), (0, 1)], [(0, 150), (33, 90)]])
+def test_rows_at_any_element_and_two_streams_at_once(kind, cache, lengths):
+    """Queries and results one element behind an aligned address, rows an odd distance apart; two streams beside each other, with a workspace each."""
+    p = Problem(kind, cache, "heads", 4, 2, 64, 16, lengths, seed=18)
+    out, limit, _, _ = p.expect(0.125)
+    pages, attend_of = p.handles(0.125, 0)
+    row = p.hq * p.dim
+    q = torch.zeros(p.tokens * (row + 3) + 1, dtype=p.dtype, device=DEV)
+    q[1:].view(p.tokens, row + 3)[:, :row] = p.q[:, :row].to(DEV)
+    with pages as c, attend_of(c) as attend:
+        d, got, works = p.to_gpu(), [torch.full((p.tokens * (row + 5) + 1,), 9.0, dtype=p.dtype, device=DEV) for _ in range(2)], [p.workspace(attend) for _ in range(2)]
+        torch.cuda.synchronize()
+        streams = [torch.cuda.Stream() for _ in range(2)]
+        for _ in range(20):
+            for s, x, work in zip(streams, got, works):
+                with torch.cuda.stream(s):
+                    ttc.ttc_attend_pages(attend, len(p.cached), p.tokens, q.data_ptr() + q.element_size(), row + 3, ptr(d["starts"]), ptr(d["cached"]), ptr(d["table"]), p.width,
+                                         ptr(d["k"]), ptr(d["v"]), ptr(d["ks"]), ptr(d["vs"]), x.data_ptr() + x.element_size(), row + 5, 0, ptr(work), stream())
+        torch.cuda.synchronize()
+    for x in got:
+        y = moves.wide(x)
+        assert y[0] == 9 and (y[1:].reshape(p.tokens, row + 5)[:, row:] == 9).all()
+        ref.assert_within(y[1:].reshape(p.tokens, row + 5)[:, :row].reshape(out.shape), out, limit)
+
+
+@gpu
+@pytest.mark.parametrize("lengths", [[(100, 1), (7, 2)], [(10, 150)]])
+def test_no_table_at_all(lengths):
+    """Tables of no entries: nothing is there, whatever the lengths say."""
+    p = Problem("bf16", "bf16", "slots", 2, 1, 64, 16, lengths, seed=19, width=0)
+    got, lse = p.run(0.125)
+    assert (got == 0).all() and np.isneginf(lse).all()
+
+
 # ---- refusals: before anything reaches a device -----------------------------------------------------------
 
 V, O, T, N, A, M = (getattr(ttc, "TTC_ERR_" + x) for x in ("INVALID_VALUE", "OVERFLOW", "UNSUPPORTED_DTYPE", "NULL_POINTER", "ALIAS", "MISALIGNED"))
