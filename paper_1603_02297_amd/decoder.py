@@ -158,7 +158,7 @@ class Heads:
     """Norms of a layer's queries and keys for each head (weights None: no norm), and the rotation of their first `rotated` elements by position."""
 
     def __init__(self, q_heads: int, kv_heads: int, dim: int, rotated: int, dtype: torch.dtype, norm: bool = True, base: float = 10000.0, eps: float = 1e-6):
-        self.q_heads, self.kv_heads, self.dim, self.dtype, self.norm = q_heads, kv_heads, dim, dtype, norm
+        self.q_heads, self.kv_heads, self.dim, self.rotated, self.dtype, self.norm = q_heads, kv_heads, dim, rotated, dtype, norm
         angles = [base ** (-2 * i / rotated) for i in range(rotated // 2)] if rotated else None
         self.handle = ttc.ttc_heads_create(CODES[dtype], q_heads, kv_heads, dim, rotated, 0, angles, int(norm), eps)
         weakref.finalize(self, ttc.ttc_heads_destroy, self.handle)
@@ -254,6 +254,9 @@ class PagedCache:
         if taken > self.free.numel():
             raise RuntimeError(f"{taken} pages wanted, {self.free.numel()} free")
         if rotation is not None:
+            if (rotation.kv_heads, rotation.dim, rotation.dtype) != (self.heads, self.dim, self.dtype) or (self.k.dtype == FOUR_BITS and rotation.rotated % 16):
+                raise ValueError(f"a rotation of {rotation.rotated} elements of {rotation.kv_heads} heads of {rotation.dim} {rotation.dtype}, the cache has {self.heads} of {self.dim} "
+                                 f"{self.dtype}" + (", and in 4 bits a multiple of 16" if self.k.dtype == FOUR_BITS else ""))
             q = _matrix(q, (tokens, rotation.q_heads * self.dim), self.dtype, device, "queries")
             _, q_weight, k_weight = rotation.check(torch.empty(tokens, dtype=torch.int32, device=device), q, weights)
             turned = torch.empty(tokens, rotation.q_heads * self.dim, dtype=self.dtype, device=device)

@@ -145,3 +145,17 @@ def test_what_is_not_fit_is_refused_before_anything_is_mapped(monkeypatch):
         with pytest.raises(ValueError):
             heads.rotate(*args)
     assert not called
+
+
+def test_a_rotation_of_other_heads_than_the_cache_is_refused_before_anything_is_mapped(monkeypatch):
+    called = []
+    for name in ("ttc_pages_map", "ttc_pages_append"):
+        monkeypatch.setattr(ttc, name, lambda *args: called.append(args))
+    one = torch.ones(3, dtype=torch.int32)
+    for cache_dtype, dim, others in ((torch.float32, 4, [(4, 1, 4, 4, torch.float32), (2, 2, 8, 4, torch.float32), (4, 2, 4, 4, torch.float16)]), (decoder.FOUR_BITS, 32, [(4, 2, 32, 8, torch.float32)])):
+        c = decoder.PagedCache(3, 2, dim, 8, 9, 24, torch.float32, cache_dtype, device="cpu")
+        k, q = torch.ones(3, 2 * dim), torch.ones(3, 4 * dim)
+        for args in others:
+            with pytest.raises(ValueError, match="rotation"):
+                c.append(one, k, k, q, decoder.Heads(*args))
+    assert not called
