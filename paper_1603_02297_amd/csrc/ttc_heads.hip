@@ -196,6 +196,9 @@ template <bool NT, typename T, int V> __device__ __forceinline__ void store_unit
     if (here && u.has_b) store_vec<T, V, NT>(p + u.b, b);
 }
 
+// What one lane reads for all of them, by a scalar load: it does not wait for the vector loads and stores under way.
+__device__ __forceinline__ int32_t scalar(const int32_t* p, uint32_t i) { return ((const __attribute__((address_space(4))) int32_t*)p)[i]; }
+
 struct Place {                             // of a wavefront's item
     uint32_t token, group, end;
     int32_t  position;
@@ -207,8 +210,37 @@ __device__ __forceinline__ Place place_of(const HeadsArgs& p, uint32_t item)
     r.group = (item - r.token * p.split_div.div) * p.per_wave;
     const uint32_t all = p.q_groups + p.k_groups + p.v_groups;
     r.end = r.group + p.per_wave < all ? r.group + p.per_wave : all;
-    r.position = p.positions ? p.positions[r.token] : 0;
+    r.position = p.positions ? scalar(p.positions, r.token) : 0;
     return r;
+}
+
+// The way of a wavefront over its items, group by group.
+struct Step {
+    uint32_t item, group;
+    Place    at;
+    bool     first;                        // of its item: the angles are another token's
+};
+__device__ __forceinline__ void settle(const HeadsArgs& p, uint32_t items, uint32_t waves, Step& s)        // on the first item from s.item on that is no padding
+{
+    for (; s.item < items; s.item += waves) {
+        const Place at = place_of(p, s.item);
+        if (at.position < 0) continue;
+        s.at = at;
+        s.group = at.group;
+        s.first = true;
+        break;
+    }
+}
+__device__ __forceinline__ Step after(const HeadsArgs& p, uint32_t items, uint32_t waves, Step s)          // behind the last one: that one again, and no item
+{
+    if (s.item >= items) return s;
+    s.first = false;
+    if (s.group + 1 < s.at.end) ++s.group;
+    else {
+        s.item += waves;
+        settle(p, items, waves, s);
+    }
+    return s;
 }
 
 // Groups whose loads are under way together: a token's, as a rule.
@@ -250,7 +282,8 @@ __device__ __forceinline__ void store_cached(void* cache, int64_t at, float scal
     }
 }
 
-// Bound by memory: 16384 tokens of 32 + 8 heads of 128 bf16 (336 MB) 55 us, 6.1 TB/s; 21300 tokens into 8 bits, queries packed beside them (480 MB), 88 us, 5.5.  Into
+// Bound by memory: 16384 tokens of 32 + 8 heads of 128 bf16 (336 MB) 66 us a call, 5.1 TB/s (55 where half of it is in the last-level
+// cache); 21300 tokens into 8 bits, queries packed beside them (480 MB), 95.  Into
 // 4 bits a vector's extremes and codes take the time: 6900 tokens of 28 + 4 heads of 64 17 us, where the bytes take 9.  A decoding step (64 to 128 tokens) is 4.4 to 4.6 us of latency.
 template <typename T, typename C, int V, int N, bool NT>
 __global__ __launch_bounds__(kHeadsThreads, 4) void heads_kernel(HeadsArgs p)
@@ -285,7 +318,7 @@ __global__ __launch_bounds__(kHeadsThreads, 4) void heads_kernel(HeadsArgs p)
         int64_t in_cache = 0;
         bool slotted = true;
         if constexpr (Cached<C>::value) {
-            const uint32_t slot = (uint32_t)p.slots[at.token];
+            const uint32_t slot = (uint32_t)scalar(p.slots, at.token);
             slotted = slot < p.slot_count;
             const uint32_t page = slotted ? fdiv(slot, p.page) : 0, inside = slotted ? slot - page * p.page.div : 0;
             in_cache = (int64_t)page * p.stride_page + (int64_t)inside * p.stride_slot;
@@ -342,7 +375,8 @@ __global__ __launch_bounds__(kHeadsThreads, 4) void heads_kernel(HeadsArgs p)
 
 // The backward pass.  The weights' gradients are summed by every lane over its tokens and heads, by a workgroup over its lanes that have the same
 // elements, and over the workgroups by grad_sum_kernel, all in an order that the sizes alone give.  Bound by memory: 8192 tokens of 32 + 8 heads of 128 bf16 (252 MB)
-// 52 us, 4.9 TB/s, and 5 for the sums over the workgroups, which are a launch.
+// 58.6 us a call, 4.3 TB/s, of which the sums over the workgroups are 5.  A group's place is loaded again as soon as it has been widened, before anything is stored: loads
+// of two groups once those before are stored take 62.8.  (Forward, where more is under way, the same takes 67 for 66 us, and 101 for 96 into 8 bits.)
 template <typename T, int V, int N, bool NT>
 __global__ __launch_bounds__(kHeadsThreads, 2) void heads_grad_kernel(HeadsArgs p)
 {
@@ -357,74 +391,76 @@ __global__ __launch_bounds__(kHeadsThreads, 2) void heads_grad_kernel(HeadsArgs 
     float total[2][N][2 * V] = {};
     const float each_element = 1.f / (float)p.dim;
     Raw<T, V> raw[kLoads][N], draw[kLoads][N];
-    auto load = [&](const Place& at, uint32_t g0) {
+    auto load = [&](int i, const Step& s) {
+        const bool q = s.group < q_end;
+        const T* row = static_cast<const T*>(q ? p.q : p.k) + (int64_t)s.at.token * (q ? p.ld_q : p.ld_k);
+        const T* drow = static_cast<const T*>(q ? p.dq_out : p.dk_out) + (int64_t)s.at.token * (q ? p.ld_dqo : p.ld_dko);
+        const uint32_t head = (q ? s.group : s.group - q_end) * each + sub, last = (q ? p.q_heads : p.kv_heads) - 1;
+        const int64_t from = (int64_t)(head < last ? head : last) * p.dim;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const uint32_t g = g0 + i;
-            if (g >= at.end) break;
-            const bool q = g < q_end;
-            const T* row = static_cast<const T*>(q ? p.q : p.k) + (int64_t)at.token * (q ? p.ld_q : p.ld_k);
-            const T* drow = static_cast<const T*>(q ? p.dq_out : p.dk_out) + (int64_t)at.token * (q ? p.ld_dqo : p.ld_dko);
-            const uint32_t head = (q ? g : g - q_end) * each + sub, last = (q ? p.q_heads : p.kv_heads) - 1;
-            const int64_t from = (int64_t)(head < last ? head : last) * p.dim;
-#pragma unroll
-            for (int n = 0; n < N; ++n) {
-                draw[i][n] = load_unit<T, V>(drow + from, lane.unit[n]);
-                raw[i][n] = load_unit<T, V>(row + from, lane.unit[n]);       // without a norm: the gradients again
-            }
+        for (int n = 0; n < N; ++n) {
+            draw[i][n] = load_unit<T, V>(drow + from, lane.unit[n]);
+            raw[i][n] = load_unit<T, V>(row + from, lane.unit[n]);       // without a norm: the gradients again
         }
     };
     kept.fill(p);
-    for (uint32_t item = __builtin_amdgcn_readfirstlane(wave); item < items; item += waves) {
-        const Place at = place_of(p, item);
-        if (at.position < 0) continue;
-        load(at, at.group);
-        lane.token(p, kept, circle[threadIdx.x / kWave], (uint32_t)at.position);
-        for (uint32_t g0 = at.group; g0 < at.end; g0 += kLoads) {
-            if (g0 != at.group) load(at, g0);
+    Step step[kLoads];
+    step[0].item = __builtin_amdgcn_readfirstlane(wave);
+    settle(p, items, waves, step[0]);
+    bool more = step[0].item < items;
+    if (more) {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const uint32_t g = g0 + i;
-                if (g >= at.end) break;
-                auto run = [&](auto kind_of) {
-                    constexpr int kind = decltype(kind_of)::value;
-                    const uint32_t head = (kind == 0 ? g : g - q_end) * each + sub;
-                    const bool here = head < (kind == 0 ? p.q_heads : p.kv_heads);
-                    float x[N][2 * V], d[N][2 * V];
+        for (int i = 0; i < kLoads; ++i) {
+            if (i) step[i] = after(p, items, waves, step[i - 1]);
+            load(i, step[i]);
+        }
+    }
+    while (more) {
 #pragma unroll
-                    for (int n = 0; n < N; ++n) {
-                        widen_unit<T, V>(draw[i][n], lane.unit[n], p.full, here, d[n]);
-                        widen_unit<T, V>(raw[i][n], lane.unit[n], p.full, here, x[n]);
-                    }
-                    lane.rotate(d, p.paired, true);
-                    if (p.norm) {
-                        float w[N][2 * V], square = 0.f, both = 0.f;
-                        lane.weights(kept.weights[kind], w);
+        for (int i = 0; i < kLoads; ++i) {
+            const Step now = step[i];
+            if (now.item >= items) { more = false; break; }
+            if (now.first) lane.token(p, kept, circle[threadIdx.x / kWave], (uint32_t)now.at.position);
+            const uint32_t g = now.group, head = (g < q_end ? g : g - q_end) * each + sub;
+            const bool here = head < (g < q_end ? p.q_heads : p.kv_heads);
+            float x[N][2 * V], d[N][2 * V];
 #pragma unroll
-                        for (int n = 0; n < N; ++n)
-#pragma unroll
-                            for (int j = 0; j < 2 * V; ++j) {
-                                square = __builtin_fmaf(x[n][j], x[n][j], square);
-                                both = __builtin_fmaf(x[n][j] * w[n][j], d[n][j], both);
-                            }
-                        const float r = inverse_root(__builtin_fmaf(over_head(square, p.lanes_log), each_element, p.eps));
-                        const float mean = over_head(both, p.lanes_log) * each_element * r;       // of g * x / s
-#pragma unroll
-                        for (int n = 0; n < N; ++n)
-#pragma unroll
-                            for (int j = 0; j < 2 * V; ++j) {
-                                const float hat = x[n][j] * r;
-                                total[kind][n][j] = __builtin_fmaf(hat, d[n][j], total[kind][n][j]);
-                                d[n][j] = r * __builtin_fmaf(d[n][j], w[n][j], -(hat * mean));
-                            }
-                    }
-                    T* to = static_cast<T*>(kind == 0 ? p.q_out : p.k_out) + (int64_t)at.token * (kind == 0 ? p.ld_qo : p.ld_ko) + (int64_t)head * p.dim;
-#pragma unroll
-                    for (int n = 0; n < N; ++n) store_unit<NT, T, V>(to, lane.unit[n], here, d[n]);
-                };
-                if (g < q_end) run(std::integral_constant<int, 0>{});
-                else run(std::integral_constant<int, 1>{});
+            for (int n = 0; n < N; ++n) {
+                widen_unit<T, V>(draw[i][n], lane.unit[n], p.full, here, d[n]);
+                widen_unit<T, V>(raw[i][n], lane.unit[n], p.full, here, x[n]);
             }
+            step[i] = after(p, items, waves, step[(i + kLoads - 1) % kLoads]);
+            load(i, step[i]);
+            auto run = [&](auto kind_of) {
+                constexpr int kind = decltype(kind_of)::value;
+                lane.rotate(d, p.paired, true);
+                if (p.norm) {
+                    float w[N][2 * V], square = 0.f, both = 0.f;
+                    lane.weights(kept.weights[kind], w);
+#pragma unroll
+                    for (int n = 0; n < N; ++n)
+#pragma unroll
+                        for (int j = 0; j < 2 * V; ++j) {
+                            square = __builtin_fmaf(x[n][j], x[n][j], square);
+                            both = __builtin_fmaf(x[n][j] * w[n][j], d[n][j], both);
+                        }
+                    const float r = inverse_root(__builtin_fmaf(over_head(square, p.lanes_log), each_element, p.eps));
+                    const float mean = over_head(both, p.lanes_log) * each_element * r;       // of g * x / s
+#pragma unroll
+                    for (int n = 0; n < N; ++n)
+#pragma unroll
+                        for (int j = 0; j < 2 * V; ++j) {
+                            const float hat = x[n][j] * r;
+                            total[kind][n][j] = __builtin_fmaf(hat, d[n][j], total[kind][n][j]);
+                            d[n][j] = r * __builtin_fmaf(d[n][j], w[n][j], -(hat * mean));
+                        }
+                }
+                T* to = static_cast<T*>(kind == 0 ? p.q_out : p.k_out) + (int64_t)now.at.token * (kind == 0 ? p.ld_qo : p.ld_ko) + (int64_t)head * p.dim;
+#pragma unroll
+                for (int n = 0; n < N; ++n) store_unit<NT, T, V>(to, lane.unit[n], here, d[n]);
+            };
+            if (g < q_end) run(std::integral_constant<int, 0>{});
+            else run(std::integral_constant<int, 1>{});
         }
     }
     if (!p.partial) return;
