@@ -245,6 +245,7 @@ __device__ __forceinline__ Step after(const HeadsArgs& p, uint32_t items, uint32
 
 // Groups whose loads are under way together: a token's, as a rule.
 constexpr int kBatch = 4, kGradBatch = 2;
+__device__ const float kOne = 1.f;
 
 // C: the cache's element type, or void for packed results.
 template <typename C> struct Cached { static constexpr bool value = true; };
@@ -297,6 +298,7 @@ __global__ __launch_bounds__(kHeadsThreads, 4) void heads_kernel(HeadsArgs p)
     Lane<V, N> lane(p, in_head);
     const float each_element = 1.f / (float)p.dim;
     Raw<T, V> raw[kLoads][N];
+    float scale_of[kLoads];                // beside them: a load between stores waits for those
     // groups g0 ... of an item
     auto load = [&](const Place& at, uint32_t g0) {
 #pragma unroll
@@ -308,6 +310,10 @@ __global__ __launch_bounds__(kHeadsThreads, 4) void heads_kernel(HeadsArgs p)
             const uint32_t head = (q ? g : k ? g - q_end : g - k_end) * each + sub, last = (q ? p.q_heads : p.kv_heads) - 1;
 #pragma unroll
             for (int n = 0; n < N; ++n) raw[i][n] = load_unit<T, V>(row + (int64_t)(head < last ? head : last) * p.dim, lane.unit[n]);
+            if constexpr (std::is_same<C, f8>::value) {
+                const float* scales = q ? nullptr : k ? p.k_scale : p.v_scale;
+                scale_of[i] = *(scales ? scales + (head < last ? head : last) : &kOne);
+            }
         }
     };
     kept.fill(p);
@@ -360,8 +366,7 @@ __global__ __launch_bounds__(kHeadsThreads, 4) void heads_kernel(HeadsArgs p)
 #pragma unroll
                         for (int n = 0; n < N; ++n) store_unit<NT, T, V>(to, lane.unit[n], here, x[n]);
                     } else {
-                        const float* scales = kind == 1 ? p.k_scale : p.v_scale;
-                        const float scale = std::is_same<C, f8>::value && scales && here ? scales[head] : 1.f;
+                        const float scale = std::is_same<C, f8>::value ? scale_of[i] : 1.f;
                         store_cached<T, C, V, N, NT>(kind == 1 ? p.k_out : p.v_out, in_cache + (int64_t)head * p.stride_head, scale, lane, here, x, p.lanes_log);
                     }
                 };
