@@ -15,20 +15,24 @@ namespace {
 
 // cos and sin of `turn` * 2^-64 turns: the nearest quarter turn by integers, exactly, then the two series on the rest, at most pi/4 away: their first
 // terms left out are below 2^-29.
+constexpr float kTurn = 1.46291807926715968e-9f, kTurnLow = -4.070940268e-17f;      // 2 pi / 2^32, as two
 __device__ __forceinline__ void unit_circle(uint64_t turn, float* c, float* s)
 {
     const uint32_t top = (uint32_t)(turn >> 32), quarter = (top + 0x20000000u) >> 30;
-    const float x = (float)(int32_t)(top - (quarter << 30)) * 1.46291807926715968e-9f;      // 2 pi / 2^32
+    const int32_t rest = (int32_t)(top - (quarter << 30));
+    const float f = (float)rest, x = f * kTurn;
+    // what the two roundings left out of it
+    const float less = __builtin_fmaf((float)(rest - (int32_t)f), kTurn, __builtin_fmaf(f, kTurnLow, __builtin_fmaf(f, kTurn, -x)));
     const float y = x * x;
     float sine = __builtin_fmaf(y, 2.75573192e-6f, -1.98412698e-4f);
     sine = __builtin_fmaf(y, sine, 8.33333333e-3f);
     sine = __builtin_fmaf(y, sine, -1.66666667e-1f);
-    sine = __builtin_fmaf(x * y, sine, x);
+    sine = __builtin_fmaf(x * y, sine, less) + x;
     float cosine = __builtin_fmaf(y, -2.75573192e-7f, 2.48015873e-5f);
     cosine = __builtin_fmaf(y, cosine, -1.38888889e-3f);
     cosine = __builtin_fmaf(y, cosine, 4.16666667e-2f);
     cosine = __builtin_fmaf(y, cosine, -0.5f);
-    cosine = __builtin_fmaf(y, cosine, 1.f);
+    cosine = __builtin_fmaf(y, cosine, -(x * less)) + 1.f;
     const float a = quarter & 1 ? sine : cosine, b = quarter & 1 ? cosine : sine;
     *c = (quarter + 1) & 2 ? -a : a;
     *s = quarter & 2 ? -b : b;
@@ -101,7 +105,9 @@ __device__ __forceinline__ void wave_order()
 __device__ __forceinline__ float inverse_root(float x)
 {
     const bool tiny = x < 0x1p-64f;
-    return __builtin_amdgcn_rsqf(tiny ? x * 0x1p64f : x) * (tiny ? 0x1p32f : 1.f);
+    const float z = tiny ? x * 0x1p64f : x, r = __builtin_amdgcn_rsqf(z);
+    const float better = __builtin_fmaf(r * 0.5f, __builtin_fmaf(-(z * r), r, 1.f), r);       // a step of Newton's
+    return (z > 0.f && z < __builtin_inff() ? better : r) * (tiny ? 0x1p32f : 1.f);
 }
 
 // A lane's units, the same of every head, and their rotation at a token's position.
@@ -500,9 +506,9 @@ constexpr int kSumColumns = 16, kSumRows = 16;
 
 __global__ __launch_bounds__(kSumColumns * kSumRows) void grad_sum_kernel(SumArgs p)
 {
-    __shared__ float sums[kSumRows][kSumColumns];
+    __shared__ double sums[kSumRows][kSumColumns];
     const uint32_t c = threadIdx.x % kSumColumns, r = threadIdx.x / kSumColumns, i = blockIdx.x * kSumColumns + c;
-    float v = 0.f;
+    double v = 0.0;                          // 512 sums of much the same size: their roundings would be most of the error
     if (i < 2 * p.dim) {
 #pragma unroll 8
         for (uint32_t j = r; j < p.rows; j += kSumRows) v += p.partial[(int64_t)j * 2 * p.dim + i];
@@ -510,11 +516,11 @@ __global__ __launch_bounds__(kSumColumns * kSumRows) void grad_sum_kernel(SumArg
     sums[r][c] = v;
     __syncthreads();
     if (r != 0 || i >= 2 * p.dim) return;
-    v = 0.f;
+    v = 0.0;
 #pragma unroll
     for (int j = 0; j < kSumRows; ++j) v += sums[j][c];
     float* out = i < p.dim ? p.q : p.k;
-    if (out) out[i < p.dim ? i : i - p.dim] = v;
+    if (out) out[i < p.dim ? i : i - p.dim] = (float)v;
 }
 
 template <typename T, typename C> const void* heads_fn(int vec, bool nt)
