@@ -386,7 +386,7 @@ __global__ __launch_bounds__(kHeadsThreads, 4) void heads_kernel(HeadsArgs p)
 
 // The backward pass.  The weights' gradients are summed by every lane over its tokens and heads, by a workgroup over its lanes that have the same
 // elements, and over the workgroups by grad_sum_kernel, all in an order that the sizes alone give.  Bound by memory: 8192 tokens of 32 + 8 heads of 128 bf16 (252 MB)
-// 58.6 us a call, 4.3 TB/s, of which the sums over the workgroups are 5.  A group's place is loaded again as soon as it has been widened, before anything is stored: loads
+// 59 us a call, of which the sums over the workgroups are 5.  A group's place is loaded again as soon as it has been widened, before anything is stored: loads
 // of two groups once those before are stored take 62.8.  (Forward, where more is under way, the same takes 67 for 66 us, and 101 for 96 into 8 bits.)
 template <typename T, int V, int N, bool NT>
 __global__ __launch_bounds__(kHeadsThreads, 2) void heads_grad_kernel(HeadsArgs p)
