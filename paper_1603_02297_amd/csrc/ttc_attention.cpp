@@ -20,7 +20,7 @@ HeadsShape cut_heads(HeadsArgs& a, int groups)
     a.lanes_log = 0;
     while ((1u << a.lanes_log) < units && a.lanes_log < 6) ++a.lanes_log;
     const uint32_t each = 64u >> a.lanes_log;
-    a.full = units == 1u << a.lanes_log && a.dim % (2 * vec) == 0 && (a.paired || rest % (2 * vec) == 0) && (!a.q || a.q_heads % each == 0) && ((!a.k && !a.v) || a.kv_heads % each == 0);
+    a.full = units == (vec > 1 ? 1u : (uint32_t)kHeadsRounds) << a.lanes_log && a.dim % (2 * vec) == 0 && (a.paired || rest % (2 * vec) == 0) && (!a.q || a.q_heads % each == 0) && ((!a.k && !a.v) || a.kv_heads % each == 0);
     a.q_groups = a.q ? (a.q_heads + each - 1) / each : 0;
     a.k_groups = a.k ? (a.kv_heads + each - 1) / each : 0;
     a.v_groups = a.v ? (a.kv_heads + each - 1) / each : 0;

@@ -29,6 +29,8 @@ namespace ttc {
 constexpr int kHeadsThreads = 256;
 // Workgroups of a launch at most: four on each compute unit, each over many tokens, so that angles and weights are fetched once (512 to 16384: none faster).
 constexpr int kHeadsGroups = 1024, kGradGroups = 512;
+// Units of a lane where heads go element by element: 64 lanes have the 256 pairs of the longest head.
+constexpr int kHeadsRounds = 4;
 
 // Queries, keys and values of one call.  A head is cut into units of two vectors of V elements, the two sides of V rotations; `lanes` lanes
 // of a wavefront have one head, 64 / lanes heads at a time are a group, and `splits` wavefronts share a token's groups.
@@ -44,7 +46,7 @@ struct HeadsArgs {
     int32_t        dtype, cache_dtype;     // cache_dtype -1: packed results
     int32_t        paired, norm;
     float          eps;
-    int32_t        lanes_log, full;        // full: every lane has an element of its own in every group
+    int32_t        lanes_log, full;        // full: every unit of every lane has elements of its own in every group
     uint32_t       q_groups, k_groups, v_groups, per_wave;
     // the backward pass: q, k are the inputs, and beside them
     const void    *dq_out, *dk_out;

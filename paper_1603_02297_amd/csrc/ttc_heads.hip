@@ -528,7 +528,7 @@ template <typename T, typename C> const void* heads_fn(int vec, bool nt)
     constexpr int V = std::is_same<C, q4>::value ? 8 : 16 / (int)sizeof(T);
     if (vec == V) return nt ? reinterpret_cast<const void*>(&heads_kernel<T, C, V, 1, true>) : reinterpret_cast<const void*>(&heads_kernel<T, C, V, 1, false>);
     if constexpr (std::is_same<C, q4>::value) return nullptr;
-    else return reinterpret_cast<const void*>(&heads_kernel<T, C, 1, 4, false>);
+    else return reinterpret_cast<const void*>(&heads_kernel<T, C, 1, kHeadsRounds, false>);
 }
 template <typename T> const void* heads_fn(int vec, int cache, bool nt)
 {
@@ -537,7 +537,7 @@ template <typename T> const void* heads_fn(int vec, int cache, bool nt)
 template <typename T> const void* grad_fn(int vec, bool nt)
 {
     constexpr int V = 16 / (int)sizeof(T);
-    return vec != V ? reinterpret_cast<const void*>(&heads_grad_kernel<T, 1, 4, false>) : nt ? reinterpret_cast<const void*>(&heads_grad_kernel<T, V, 1, true>)
+    return vec != V ? reinterpret_cast<const void*>(&heads_grad_kernel<T, 1, kHeadsRounds, false>) : nt ? reinterpret_cast<const void*>(&heads_grad_kernel<T, V, 1, true>)
                                                                                             : reinterpret_cast<const void*>(&heads_grad_kernel<T, V, 1, false>);
 }
 
