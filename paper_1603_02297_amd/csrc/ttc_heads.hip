@@ -455,7 +455,8 @@ __global__ __launch_bounds__(kHeadsThreads, 2) void heads_grad_kernel(HeadsArgs 
                             square = __builtin_fmaf(x[n][j], x[n][j], square);
                             both = __builtin_fmaf(x[n][j] * w[n][j], d[n][j], both);
                         }
-                    const float r = inverse_root(__builtin_fmaf(over_head(square, p.lanes_log), each_element, p.eps));
+                    // a lane without a head has zeros, whose root is that of eps alone: without one it is infinite, and would be in the sums
+                    const float root = inverse_root(__builtin_fmaf(over_head(square, p.lanes_log), each_element, p.eps)), r = here ? root : 0.f;
                     const float mean = over_head(both, p.lanes_log) * each_element * r;       // of g * x / s
 #pragma unroll
                     for (int n = 0; n < N; ++n)

@@ -2,6 +2,7 @@
 test_heads.py, with its limits."""
 import pytest
 
+import attention_reference as ref
 import test_heads
 
 gpu = pytest.mark.gpu
@@ -24,3 +25,13 @@ def test_full_lanes_element_by_element(case):
                          ids=lambda c: "-".join(map(str, c)))
 def test_full_lanes_into_the_cache(case):
     test_heads.test_append(*case)
+
+
+@gpu
+@pytest.mark.parametrize("hq,hk", [(1, 7), (3, 1), (4, 2), (5, 6)])
+@pytest.mark.parametrize("kind,dim,rotated,paired", [("bf16", 64, 64, 0), ("bf16", 128, 128, 0), ("f16", 80, 40, 0), ("f32", 128, 64, 1), ("f32", 64, 12, 0)])
+def test_without_an_epsilon(monkeypatch, kind, dim, rotated, paired, hq, hk):
+    """eps = 0: lanes of a group without a head hold zeros, whose norm is none."""
+    monkeypatch.setattr(ref, "EPS", 0.0)
+    test_heads.test_rotate(kind, 37, hq, hk, dim, rotated, paired, 1, 0, 0)
+    test_heads.test_grad(kind, 37, hq, hk, dim, rotated, paired, 1, 0, 0)
