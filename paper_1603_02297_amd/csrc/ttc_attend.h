@@ -1064,9 +1064,8 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
     auto write_lse = [&](uint32_t of, uint32_t to_token, uint32_t to_head, float m, float l) {
         const int64_t r = (int64_t)to_token * p.q_heads + to_head;
         const uint32_t place = w.partial_row + of - w.row0;
-        const float value = l > 0.f || l != l ? m * 0.693147180559945f + __builtin_logf(l) : -__builtin_inff();
-        if (w.partial) p.partial_lse[place] = value;
-        else if (p.lse) p.lse[r] = value;
+        if (w.partial) p.partial_sums[place] = {m, l};
+        else if (p.lse) p.lse[r] = l > 0.f || l != l ? m * 0.693147180559945f + __builtin_logf(l) : -__builtin_inff();
         if (w.parts && p.parts) {
             p.parts[2 * r] = (int32_t)place;
             p.parts[2 * r + 1] = (int32_t)w.parts;

@@ -27,11 +27,12 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs p)
         const uint32_t at = (uint32_t)first + (i ? i * p.join_step - p.join_back : 0);
         return at < p.partial_rows ? at : 0;
     };
-    float mine[kAttendMaxParts / kWave], top = -__builtin_inff();
+    PartSum mine[kAttendMaxParts / kWave];
+    float top = -__builtin_inff();
 #pragma unroll
     for (uint32_t c = 0; c < kAttendMaxParts / kWave; ++c) {
         const uint32_t i = c * kWave + lane;
-        mine[c] = p.partial_lse[place(i < parts ? i : 0)];
+        mine[c] = p.partial_sums[place(i < parts ? i : 0)];
     }
     float part[kBatch][EACH];
     auto load = [&](uint32_t from) {
@@ -48,16 +49,16 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs p)
     load(0);
 #pragma unroll
     for (uint32_t c = 0; c < kAttendMaxParts / kWave; ++c) {
-        mine[c] = c * kWave + lane < parts ? mine[c] : -__builtin_inff();
-        top = __builtin_fmaxf(top, mine[c]);
+        if (c * kWave + lane >= parts) mine[c] = {-__builtin_inff(), 0.f};
+        top = __builtin_fmaxf(top, mine[c].top);
     }
     for (int i = 1; i < kWave; i <<= 1) top = __builtin_fmaxf(top, __shfl_xor(top, i));
     const float base = top == -__builtin_inff() ? 0.f : top;
     float sum = 0.f;
 #pragma unroll
     for (uint32_t c = 0; c < kAttendMaxParts / kWave; ++c) {
-        mine[c] = __builtin_amdgcn_exp2f((mine[c] - base) * 1.44269504088896f);
-        sum += mine[c];
+        mine[c].sum *= __builtin_amdgcn_exp2f(mine[c].top - base);
+        sum += mine[c].sum;
     }
     for (int i = 1; i < kWave; i <<= 1) sum += __shfl_xor(sum, i);
     const float inverse = sum == 0.f ? 0.f : 1.f / sum;
@@ -67,7 +68,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs p)
 #pragma unroll
         for (uint32_t s = 0; s < kBatch; ++s) {
             const uint32_t i = from + s;
-            const float weight = __shfl(i < kWave ? mine[0] : mine[1], i % kWave) * inverse;          // 0 behind the last part
+            const float weight = __shfl(i < kWave ? mine[0].sum : mine[1].sum, i % kWave) * inverse;          // 0 behind the last part
 #pragma unroll
             for (int e = 0; e < EACH; ++e) x[e] = weight == 0.f ? x[e] : __builtin_fmaf(weight, part[s][e], x[e]);        // nothing seen, or nothing left of it
         }
@@ -76,7 +77,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs p)
 #pragma unroll
     for (int e = 0; e < EACH; ++e)
         if (e * kWave + lane < p.dim) out[e * kWave + lane] = (T)x[e];
-    if (p.lse && lane == 0) p.lse[row] = sum == 0.f ? -__builtin_inff() : base + __builtin_logf(sum);
+    if (p.lse && lane == 0) p.lse[row] = sum == 0.f ? -__builtin_inff() : base * 0.693147180559945f + __builtin_logf(sum);
 }
 
 template <typename T> const void* join_of(uint32_t dim)

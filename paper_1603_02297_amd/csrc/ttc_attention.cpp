@@ -355,7 +355,7 @@ int64_t ttc_attend_workspace(ttc_attend_t attend, int64_t requests, int64_t toke
     if (!attend_sizes(attend, requests, tokens, ld_table)) return -TTC_ERR_OVERFLOW;
     if (requests == 0 || tokens == 0) return 0;
     const AttendShape s = attend_shape(attend, requests, tokens, longest_context(attend, tokens, ld_table));
-    return s.partial_rows ? s.partial_rows * (attend->dim + 1) * 4 + tokens * attend->q_heads * 8 : 0;
+    return s.partial_rows ? s.partial_rows * (attend->dim + 2) * 4 + tokens * attend->q_heads * 8 : 0;
 }
 
 int ttc_attend_pages(ttc_attend_t attend, int64_t requests, int64_t tokens, const void* q, int64_t ldq, const int32_t* starts, const int32_t* cached,
@@ -385,8 +385,8 @@ int ttc_attend_pages(ttc_attend_t attend, int64_t requests, int64_t tokens, cons
     a.q = q; a.k_cache = k_cache; a.v_cache = v_cache; a.out = out; a.lse = lse;
     if (work) {
         a.partial = static_cast<float*>(workspace);
-        a.partial_lse = a.partial + s.partial_rows * attend->dim;
-        a.parts = reinterpret_cast<int32_t*>(a.partial_lse + s.partial_rows);
+        a.partial_sums = reinterpret_cast<PartSum*>(a.partial + s.partial_rows * attend->dim);
+        a.parts = reinterpret_cast<int32_t*>(a.partial_sums + s.partial_rows);
     }
     a.k_scale = k_scale; a.v_scale = v_scale;
     a.starts = starts; a.cached = cached; a.table = table;

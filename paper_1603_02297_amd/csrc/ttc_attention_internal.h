@@ -65,12 +65,19 @@ struct HeadsShape {
 };
 HeadsShape cut_heads(HeadsArgs& a, int groups);          // sets what the cut says of a, too
 
+// Of a partial result: the exponent of 2 that its exponentials are relative to, and their sum.  In one number, their logarithm, a part's weight would be off by
+// the rounding of that: 2^-24 of the whole score.
+struct PartSum {
+    float top, sum;
+};
+
 // Attention.  The rows of a request are its new tokens' query heads that share a head of the cache, token by token; a workgroup has `tile` rows of them
 // and a part of the positions that they see.
 struct AttendArgs {
     const void    *q, *k_cache, *v_cache;
     void          *out;
-    float         *lse, *partial, *partial_lse;        // partial results: rows of dim elements, and the logarithms of their sums
+    float         *lse, *partial;                      // partial results: rows of dim elements
+    PartSum       *partial_sums;
     int32_t       *parts;                              // [token][q_head][2]: the first of its partial results, and how many there are
     const float   *k_scale, *v_scale;
     const int32_t *starts, *cached, *table;
