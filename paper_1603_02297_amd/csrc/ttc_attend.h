@@ -804,7 +804,7 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
     }
 
     Acc out[kOut] = {};
-    float top = -__builtin_inff(), sum = 0.f, low_sum = 0.f;                // of this lane's row (sums: its half of the positions); top times scale
+    float top = -__builtin_inff(), sum = 0.f, low_sum = 0.f;                // of this lane's row (sums: its part of the positions); top times scale
     uint32_t at = read.first(w);
     int32_t next_entry = -1;
     if constexpr (P::kCarries) next_entry = read.look_up(next, read.first(next));
@@ -923,12 +923,14 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
             for (int d = 0; d < kOut; ++d) out[d] *= factor;
         }
         const float base = top == -__builtin_inff() ? 0.f : top;
+        // A tile's are added up by themselves first: one after the other onto a sum of 1 or more, exponentials below 2^-24 would all be rounded away.
+        float tile_sum = 0.f, tile_low = 0.f;
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
             for (int i = 0; i < kRegisters; ++i) {
                 score[b][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[b][i], scale, -base));
-                sum += score[b][i];
+                tile_sum += score[b][i];
             }
         if constexpr (P::kCodes) {
 #pragma unroll
@@ -940,7 +942,7 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
                     const float steps[4] = {step.x, step.y, step.z, step.w}, lows[4] = {low.x, low.y, low.z, low.w};
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        low_sum = __builtin_fmaf(score[b][4 * j + c], masked && !(seen[b] >> (kGap * j + c) & 1) ? 0.f : lows[c], low_sum);
+                        tile_low = __builtin_fmaf(score[b][4 * j + c], masked && !(seen[b] >> (kGap * j + c) & 1) ? 0.f : lows[c], tile_low);
                         score[b][4 * j + c] *= masked && !(seen[b] >> (kGap * j + c) & 1) ? 0.f : steps[c];        // not seen: 0, whatever the record says
                     }
                 }
@@ -960,10 +962,12 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const Two two = {weight[k][2 * e], weight[k][2 * e + 1]};
-                    if constexpr (P::kLogs) low_sum = __builtin_amdgcn_fdot2(two, back, low_sum, false);
-                    else low_sum = __builtin_amdgcn_fdot2_f32_bf16(two, back, low_sum, false);
+                    if constexpr (P::kLogs) tile_low = __builtin_amdgcn_fdot2(two, back, tile_low, false);
+                    else tile_low = __builtin_amdgcn_fdot2_f32_bf16(two, back, tile_low, false);
                 }
         }
+        sum += tile_sum;
+        low_sum += tile_low;
         // the left operands of rows d * M ... of the result
         auto values_of = [&](int d, VFrag* v) {
             const uint32_t in = lane & 15, at_column = d * M + (M == 32 ? (lane >> 4 & 1) * 16 : 0);     // the first of these 16 lanes' columns

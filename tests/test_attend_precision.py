@@ -59,3 +59,68 @@ def test_parts_of_large_scores_are_joined_as_exactly_as_small_ones(cache, length
                 assert np.abs(got[t, h] - values.mean(0)).max() <= (128 + 8) * 2.0 ** -24 * 5, (t, h)
                 want = 2.0 ** 20 * math.log(2) + math.log(n)
                 assert abs(lse[t, h] - want) <= 3 * 2.0 ** -24 * want
+
+
+def behind_a_large_one(kind, cache, fresh, spread=0.7):
+    """64 requests of the same pages, so that a workgroup has all positions of one: position 5 has a weight of 1, 32,768 others some 2^-25 of it each, and together a part of
+    the result.  Returns the problem, its scale, and the exponents of 2 and the values of the positions, the same for all heads."""
+    dim, heads, requests, positions = 64, 8, 64, 32768
+    p = Problem(kind, cache, "slots", heads, heads, dim, 64, [(positions, fresh)], seed=32)
+    g = torch.Generator().manual_seed(33)
+    total = positions + fresh
+    k, put_k = by_position(p, 0, 0, total)
+    v, put_v = by_position(p, 1, 0, total)
+    scores = -25.05 - spread * torch.rand(total, generator=g)
+    scores[5] = 0
+    values = (13 if cache == "q4" else 1) + torch.randint(0, 3, (total, dim), generator=g)
+    values[5] = 0
+    if cache == "q4":
+        # keys: a step of 0 and the score as the minimum, all of whose elements meet a query of one 1; values: steps of 1 and minima of 0
+        k[..., :4] = torch.stack([torch.zeros(total), scores], -1).to(torch.bfloat16).view(torch.uint8)[:, None]
+        v[..., :4] = torch.tensor([1.0, 0.0], dtype=torch.bfloat16).view(torch.uint8)
+        code = values.to(torch.uint8)[:, None]
+        v[..., 4:] = code[..., 0::2] | code[..., 1::2] << 4
+        put_k(k)
+        put_v(v)
+    else:
+        k, v = torch.zeros(k.shape), torch.zeros(v.shape)
+        k[:, :, 0:2] = (scores / 2)[:, None, None] if cache != "f8" else torch.tensor([-13.0, 0.0])        # 8 bits hold whole numbers there
+        k[5] = 0
+        v[:] = values[:, None].float()
+        put_k(k.to(p.caches[0].dtype))
+        put_v(v.to(p.caches[1].dtype))
+        if cache == "f8":
+            p.scales = [torch.ones(heads), torch.ones(heads)]
+    at = 1 if cache == "q4" else 2                                # elements of a query that are 1; those of 8 bits see scores of -26
+    p.tokens, p.cached, p.starts = requests * fresh, np.full(requests, positions, np.int32), np.arange(requests + 1, dtype=np.int32) * fresh
+    p.table = np.repeat(p.table, requests, 0)
+    p.q = torch.zeros(p.tokens, p.ldq, dtype=p.dtype)
+    for i in range(at):
+        p.q[:, i:heads * dim:dim] = 1
+    entry, slot = slot_of(p, 0, np.arange(total))
+    kk, vv = (p.values(i)[0][entry, slot, 0] for i in range(2))
+    s = kk[:, :at].sum(1) * (2 if cache == "f8" else 1)
+    assert s[5] == 0 and np.delete(s, 5).max() <= -25
+    return p, math.log(2) * (2 if cache == "f8" else 1), s, vv
+
+
+# Of the logarithm of n exponentials' sum, and so of the sum: 32 of them are added up in a lane, then the tiles of 64 positions, then lanes, wavefronts and 128 parts; each is
+# off by 2^-20 at most, and so is the logarithm of a number near 1.
+def off_of_sum(n):
+    return (32 + n / 64 + 140) * 2.0 ** -24 + 2 * 2.0 ** -20
+
+
+@gpu
+@pytest.mark.parametrize("kind,cache", [("f32", "f32"), ("f32", "f8"), ("f32", "q4"), ("bf16", "bf16"), ("bf16", "q4")])
+@pytest.mark.parametrize("fresh", [1, 40])
+def test_sums_of_many_small_weights_behind_a_large_one(kind, cache, fresh):
+    p, scale, s, v = behind_a_large_one(kind, cache, fresh)
+    got, lse = p.run(scale)
+    for i in range(fresh):
+        n = p.cached[0] + i + 1
+        w = 2.0 ** s[:n]
+        want = (w @ v[:n]) / w.sum()
+        for t in range(i, p.tokens, fresh):
+            assert np.abs(lse[t] - math.log(w.sum())).max() <= off_of_sum(n), (t, np.abs(lse[t] - math.log(w.sum())).max())
+            if kind == "f32":                                     # two products are added to a result at a time; position 5's value is 0
+                assert (np.abs(got[t] - want) - ((n / 2 + 60) * 2.0 ** -24 + off_of_sum(n)) * want).max() <= 0, t
