@@ -913,9 +913,10 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
         }
         // The reference of the exponentials follows the maximum once that is 2^kSlack above it: results need their largest term near 1 only so far as 32 bits (and 16 for
         // the weights) must hold them.  Followed at once it moves in most tiles, for some row of 32, and costs every element of the result a product each time.
+        // Their difference is exact where it counts; the sum of reference and slack is not, and fp16 has no weight of 2^16.
         constexpr float kSlack = 8.f;
-        if (__ballot(most > top + kSlack)) {
-            const float higher = most > top + kSlack ? most : top, factor = higher == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(top - higher);
+        if (__ballot(most - top > kSlack)) {
+            const float higher = most - top > kSlack ? most : top, factor = higher == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(top - higher);
             top = higher;
             sum *= factor;
             low_sum *= factor;

@@ -124,3 +124,31 @@ def test_sums_of_many_small_weights_behind_a_large_one(kind, cache, fresh):
             assert np.abs(lse[t] - math.log(w.sum())).max() <= off_of_sum(n), (t, np.abs(lse[t] - math.log(w.sum())).max())
             if kind == "f32":                                     # two products are added to a result at a time; position 5's value is 0
                 assert (np.abs(got[t] - want) - ((n / 2 + 60) * 2.0 ** -24 + off_of_sum(n)) * want).max() <= 0, t
+
+
+@gpu
+@pytest.mark.parametrize("kind,cache", [("f16", "f16"), ("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("requests,fresh,where", [(1, 90, 100), (2000, 1, 130)])
+def test_scores_whose_neighbours_are_sixteen_apart(kind, cache, requests, fresh, where):
+    """Exponents of 2 from 2^27 on: a score that is the next one in 32 bits has 2^16 times the weight of those before it, and comes in a later tile of the same wavefront."""
+    cached = 200
+    p = Problem(kind, cache, "slots", 1, 1, 64, 16, [(cached, fresh)], seed=34)
+    total = cached + fresh
+    k, put_k = by_position(p, 0, 0, total)
+    v, put_v = by_position(p, 1, 0, total)
+    k, v = torch.zeros(k.shape), torch.zeros(v.shape)
+    k[..., 0], k[..., 1], v[..., 0] = 2048, 1, 1
+    k[where, 0, 1], v[where, 0, 0], v[where, 0, 1] = 2, 0, 1
+    put_k(k.to(p.dtype))
+    put_v(v.to(p.dtype))
+    p.tokens, p.cached, p.starts = requests * fresh, np.full(requests, cached, np.int32), np.arange(requests + 1, dtype=np.int32) * fresh
+    p.table = np.repeat(p.table, requests, 0)
+    p.q = torch.zeros(p.tokens, p.ldq, dtype=p.dtype)
+    p.q[:, 0], p.q[:, 1] = 4096, 1                                # scores of 2^23 + 1, and of 2^23 + 2
+    got, _ = p.run(16 * math.log(2))
+    for i in range(fresh):
+        others = (cached + i) * 2.0 ** -16
+        want = np.zeros(64)
+        want[:2] = others / (1 + others), 1 / (1 + others)
+        # all weights are powers of 2, and their sums whole numbers of 2^-16
+        assert np.abs(got[i::fresh, 0] - want).max() <= ref.rounded(1.0, kind, 4 * 2.0 ** -24), (i, got[i, 0, :2], want[:2])
