@@ -79,6 +79,9 @@ template <typename T, typename C, int DP, int ROWS, bool OWN> struct Plan {
     // Codes are multiplied by exponentials times steps.  fp16 would lose those of small steps and not hold those of large ones: there the exponentials' reference is the
     // largest exponential times step, and the steps' logarithms lie beside them.
     static constexpr bool kLogs = kCodes && std::is_same<T, _Float16>::value;
+    // The reference of the exponentials follows the maximum once that is 2^kSlack above where it would be: results need their largest term near 1 only so far as 32 bits
+    // (and 16 for the weights) must hold them.  Followed at once it moves in most tiles, for some row of 32, and costs every element of the result a product each time.
+    static constexpr int kSlack = 8, kLift = attend_lift(std::is_same<T, _Float16>::value ? TTC_F16 : TTC_F32);
     static constexpr int  kWaves = FEW && kWide && DP > 128 ? 2 : 4;
     static constexpr int  kThreads = kWaves * kWave;
     static constexpr int  kTeams = FEW ? kWaves : 1;
@@ -804,7 +807,7 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
     }
 
     Acc out[kOut] = {};
-    float top = -__builtin_inff(), sum = 0.f, low_sum = 0.f;                // of this lane's row (sums: its part of the positions); top times scale
+    float top = -__builtin_inff(), sum = 0.f, low_sum = 0.f;                // of this lane's row (sums: its part of the positions); top, the exponentials' reference, times scale
     uint32_t at = read.first(w);
     int32_t next_entry = -1;
     if constexpr (P::kCarries) next_entry = read.look_up(next, read.first(next));
@@ -911,12 +914,10 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
                 for (int i = 0; i < kRegisters; ++i) most = __builtin_fmaxf(most, score[b][i]);
             most = max_of_row<M>(most) * scale;
         }
-        // The reference of the exponentials follows the maximum once that is 2^kSlack above it: results need their largest term near 1 only so far as 32 bits (and 16 for
-        // the weights) must hold them.  Followed at once it moves in most tiles, for some row of 32, and costs every element of the result a product each time.
-        // Their difference is exact where it counts; the sum of reference and slack is not, and fp16 has no weight of 2^16.
-        constexpr float kSlack = 8.f;
-        if (__ballot(most - top > kSlack)) {
-            const float higher = most - top > kSlack ? most : top, factor = higher == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(top - higher);
+        // Maximum and reference by their difference, which is exact where it counts; the sum of reference and slack is not, and fp16 has no weight of 2^16.
+        constexpr float kMost = P::kSlack + P::kLift;
+        if (__ballot(most - top > kMost)) {
+            const float higher = most - top > kMost ? most - P::kLift : top, factor = higher == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f(top - higher);
             top = higher;
             sum *= factor;
             low_sum *= factor;
@@ -1070,7 +1071,7 @@ __device__ __forceinline__ void attend_work(const AttendArgs& p, const Work& w, 
         const int64_t r = (int64_t)to_token * p.q_heads + to_head;
         const uint32_t place = w.partial_row + of - w.row0;
         if (w.partial) p.partial_sums[place] = {m, l};
-        else if (p.lse) p.lse[r] = l > 0.f || l != l ? m * 0.693147180559945f + __builtin_logf(l) : -__builtin_inff();
+        else if (p.lse) p.lse[r] = log_of_sum(m, l, P::kLift);
         if (w.parts && p.parts) {
             p.parts[2 * r] = (int32_t)place;
             p.parts[2 * r + 1] = (int32_t)w.parts;

@@ -1,4 +1,6 @@
 // Attention over pages: the launches, and the kernel that joins the parts of a row's positions (see ttc_attend.h).
+#include <type_traits>
+
 #include "ttc_attention_internal.h"
 #include "ttc_moves_device.h"
 
@@ -77,7 +79,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs p)
 #pragma unroll
     for (int e = 0; e < EACH; ++e)
         if (e * kWave + lane < p.dim) out[e * kWave + lane] = (T)x[e];
-    if (p.lse && lane == 0) p.lse[row] = sum == 0.f ? -__builtin_inff() : base * 0.693147180559945f + __builtin_logf(sum);
+    if (p.lse && lane == 0) p.lse[row] = log_of_sum(top, sum, attend_lift(std::is_same<T, _Float16>::value ? TTC_F16 : TTC_F32));
 }
 
 template <typename T> const void* join_of(uint32_t dim)

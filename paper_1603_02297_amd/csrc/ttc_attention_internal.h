@@ -65,6 +65,11 @@ struct HeadsShape {
 };
 HeadsShape cut_heads(HeadsArgs& a, int groups);          // sets what the cut says of a, too
 
+// The exponentials' reference is the maximum less this many powers of 2, and they are multiplied in fp16 by up to 2^(7 + 8): it holds less than 2^16.  Its smallest step is then
+// 2^-31 of the largest, and a million positions that it rounds away are less than the rounding of the result.  Relative to the maximum itself, positions below 2^-25 of it
+// were in the sum but not in the products: 32,768 of them 0.1 % of all weights.
+constexpr int attend_lift(int dtype) { return dtype == TTC_F16 ? 7 : 0; }
+
 // Of a partial result: the exponent of 2 that its exponentials are relative to, and their sum.  In one number, their logarithm, a part's weight would be off by
 // the rounding of that: 2^-24 of the whole score.
 struct PartSum {

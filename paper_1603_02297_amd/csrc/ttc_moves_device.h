@@ -247,6 +247,12 @@ template <int V> __device__ __forceinline__ void narrow_scaled(const float* x, f
     }
 }
 
+// The logarithm of a sum of exponentials relative to 2^top, which carry 2^lift: as that of small numbers where the scores are small.  -inf where there are none.
+__device__ __forceinline__ float log_of_sum(float top, float sum, int lift)
+{
+    return sum == 0.f ? -__builtin_inff() : (top + (float)lift) * 0.693147180559945f + __builtin_logf(sum * (1.f / (float)(1 << lift)));
+}
+
 // Inclusive combination over the lanes of a wavefront, in registers: data-parallel-primitive moves by 1, 2, 4 and 8 lanes inside the
 // rows of 16, then the last lane of a row to the next row, then of the first half to the second.  join(a, 0) has to be a.
 template <int CONTROL, int ROWS> __device__ __forceinline__ uint32_t moved(uint32_t v)

@@ -152,3 +152,26 @@ def test_scores_whose_neighbours_are_sixteen_apart(kind, cache, requests, fresh,
         want[:2] = others / (1 + others), 1 / (1 + others)
         # all weights are powers of 2, and their sums whole numbers of 2^-16
         assert np.abs(got[i::fresh, 0] - want).max() <= ref.rounded(1.0, kind, 4 * 2.0 ** -24), (i, got[i, 0, :2], want[:2])
+
+
+@gpu
+@pytest.mark.parametrize("cache", ["f16", "f8", "q4"])
+@pytest.mark.parametrize("fresh", [1, 40])
+def test_fp16_keeps_many_small_weights_behind_a_large_one(cache, fresh):
+    """Weights of less than half of fp16's smallest step beside one of 1."""
+    p, scale, s, v = behind_a_large_one("f16", cache, fresh)
+    got, lse = p.run(scale)
+    for i in range(fresh):
+        n = p.cached[0] + i + 1
+        w = 2.0 ** s[:n]
+        want = (w @ v[:n]) / w.sum()
+        # A weight in fp16 is off by 2^-11 of itself, or by half of fp16's smallest step where that is more: 2^-25 of a scale on which the largest is 2^7 at least.  It goes with the
+        # value, over 4 bits with code - 8, 8 at most.  Position 5's is a power of 2.  Products are added up 16 at a time and may be cut to 32 bits, over 4 bits those of
+        # 16 + code less 24 and more 8: 24 for position 5 alone and 31 of the others.
+        small = np.maximum(2.0 ** -11 * w, 2.0 ** -32)[np.arange(n) != 5].sum()
+        added = 24 + 31 * (w.sum() - 1) if cache == "q4" else 3 * (w.sum() - 1)
+        off = small * (8 if cache == "q4" else 3) + off_of_sum(n) * want + (n / 16 + 60) * 2.0 ** -23 * added
+        limit = ref.rounded(want, "f16", off)
+        for t in range(i, p.tokens, fresh):
+            assert (np.abs(got[t] - want) - limit).max() <= 0, (t, np.abs(got[t] - want).max(), want.max(), limit.max())
+            assert np.abs(lse[t] - math.log(w.sum())).max() <= off_of_sum(n)
