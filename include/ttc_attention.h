@@ -100,7 +100,8 @@ typedef struct ttc_attend_s* ttc_attend_t;
 ttc_attend_t ttc_attend_create(ttc_pages_t pages, int64_t q_heads, double scale, int64_t window);
 int ttc_attend_destroy(ttc_attend_t attend);
 
-/* Bytes of workspace for ttc_attend_pages with tables of ld_table entries (0 where it needs none), or a negative status. */
+/* Bytes of workspace for ttc_attend_pages with tables of ld_table entries (0 where it needs none), or a negative status: -TTC_ERR_OVERFLOW, as the call itself then, where
+ * requests or tokens*q_heads are 2^29 or more, tokens*q_heads and requests * the cache's heads together 2^31 or more, or a table of a request has more than 2^40 entries. */
 int64_t ttc_attend_workspace(ttc_attend_t attend, int64_t requests, int64_t tokens, int64_t ld_table);
 
 /*

@@ -157,11 +157,11 @@ HeadsArgs heads_args(const ttc_heads_s* h, int64_t tokens)
 // Tokens times groups of heads are counted in 32 bits.
 bool countable(const ttc_heads_s* h, int64_t tokens) { return tokens <= INT32_MAX && (__int128)tokens * (h->q_heads + 2 * h->kv_heads) <= INT32_MAX; }
 
-// Rows and tiles are counted in 32 bits, and so is a row of the table.
+// Rows of all heads are counted in 32 bits, and so are the tiles of them: as many as rows and requests of every head of the cache at most.
 bool attend_sizes(const ttc_attend_s* a, int64_t requests, int64_t tokens, int64_t ld_table)
 {
     return requests <= INT32_MAX / 4 && tokens <= INT32_MAX / 4 && (__int128)tokens * a->q_heads <= INT32_MAX / 4 &&
-           (__int128)(requests + tokens * a->q_heads) * a->heads <= INT32_MAX && ld_table <= (int64_t)1 << 40;
+           (__int128)requests * a->heads + tokens * a->q_heads <= INT32_MAX && ld_table <= (int64_t)1 << 40;
 }
 
 // Positions that the rows of a tile see together, at most.
