@@ -270,6 +270,13 @@ class PagedCache:
         self.free, self.before, self.cached = self.free[taken:].contiguous(), self.cached, self.cached + fresh
         return starts if rotation is None else (starts, turned)
 
+    def attends_of(self, q_heads: int) -> int:
+        """The handle of attention of that many query heads over this cache."""
+        if q_heads not in self.attends:
+            self.attends[q_heads] = ttc.ttc_attend_create(self.handle, q_heads, self.dim ** -0.5)
+            weakref.finalize(self, ttc.ttc_attend_destroy, self.attends[q_heads])
+        return self.attends[q_heads]
+
     def attend(self, q: torch.Tensor, starts: torch.Tensor, q_heads: int) -> torch.Tensor:
         """Attention of the tokens that the last append brought, q [tokens, q_heads*dim] at its packed offsets, over the pages of their requests."""
         tokens, width = q.shape[0], q_heads * self.dim
@@ -277,10 +284,7 @@ class PagedCache:
         if starts.dtype != torch.int32 or tuple(starts.shape) != (self.requests + 1,) or starts.device != q.device:
             raise ValueError(f"starts: {starts.dtype} {list(starts.shape)} on {starts.device}, wanted int32 [{self.requests + 1}] on {q.device}")
         starts = starts.contiguous()
-        if q_heads not in self.attends:
-            self.attends[q_heads] = ttc.ttc_attend_create(self.handle, q_heads, self.dim ** -0.5)
-            weakref.finalize(self, ttc.ttc_attend_destroy, self.attends[q_heads])
-        handle, blocks = self.attends[q_heads], self.table.shape[1]
+        handle, blocks = self.attends_of(q_heads), self.table.shape[1]
         work = torch.empty(ttc.ttc_attend_workspace(handle, self.requests, tokens, blocks), dtype=torch.uint8, device=q.device)
         out = torch.empty(tokens, width, dtype=self.dtype, device=q.device)
         ttc.ttc_attend_pages(handle, self.requests, tokens, _ptr(q), _rows_apart(q), _ptr(starts), _ptr(self.before), _ptr(self.table), blocks, _ptr(self.k), _ptr(self.v),
@@ -309,6 +313,9 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, heads: int, kv_
 def layer(x: torch.Tensor, fresh: torch.Tensor, cache: PagedCache, w: dict, heads: int, topk: int, rotation: Heads | None = None) -> torch.Tensor:
     """One layer over the packed new tokens of all requests."""
     kv = cache.heads * cache.dim
+    if heads % cache.heads:
+        raise ValueError(f"{heads} heads of queries for {cache.heads} heads of keys: wanted a multiple")
+    cache.attends_of(heads)                                       # what it refuses is refused before anything is in the cache
     q, k, v = (x @ w["qkv"]).split([heads * cache.dim, kv, kv], 1)
     if rotation is None:
         starts = cache.append(fresh, k, v)
