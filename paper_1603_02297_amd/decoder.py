@@ -311,18 +311,25 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, heads: int, kv_
 
 
 def layer(x: torch.Tensor, fresh: torch.Tensor, cache: PagedCache, w: dict, heads: int, topk: int, rotation: Heads | None = None) -> torch.Tensor:
-    """One layer over the packed new tokens of all requests."""
-    kv = cache.heads * cache.dim
+    """One layer over the packed new tokens of all requests.  Heads longer than the attention over pages has read every request's context and attend in plain torch."""
+    kv, over_pages = cache.heads * cache.dim, cache.dim <= ttc.TTC_ATTEND_MAX_DIM
     if heads % cache.heads:
         raise ValueError(f"{heads} heads of queries for {cache.heads} heads of keys: wanted a multiple")
-    cache.attends_of(heads)                                       # what it refuses is refused before anything is in the cache
+    if over_pages:
+        cache.attends_of(heads)                                   # what it refuses is refused before anything is in the cache
     q, k, v = (x @ w["qkv"]).split([heads * cache.dim, kv, kv], 1)
     if rotation is None:
         starts = cache.append(fresh, k, v)
     else:
         starts, q = cache.append(fresh, k, v, q, rotation, (w.get("q_norm"), w.get("k_norm")))
     if x.shape[0]:                                                # a step may bring nothing
-        x = x + cache.attend(q, starts, heads) @ w["out"]
+        if over_pages:
+            mixed = cache.attend(q, starts, heads)
+        else:
+            ends, k, v = cache.context()
+            starts, ends = starts.tolist(), ends.tolist()
+            mixed = torch.cat([attention(q[a:b], k[c:d], v[c:d], heads, cache.heads) for a, b, c, d in zip(starts, starts[1:], ends, ends[1:]) if b > a])
+        x = x + mixed @ w["out"]
     return x + experts_forward(x, w["router"], w["up"], w["down"], topk)
 
 
