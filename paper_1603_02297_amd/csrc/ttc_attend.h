@@ -1160,8 +1160,11 @@ __global__ __launch_bounds__((Plan<T, C, DP, ROWS, OWN>::kThreads), (Plan<T, C, 
         auto units = [&](uint32_t of) { return units_of<ROWS>(p, scalar(p.starts, of), scalar(p.starts, of + 1), scalar(p.cached, of)); };
         uint64_t unit = s.first(g), left = s.first(g + 1) - unit;
         uint32_t r = start.request;
+        // Lengths are read again here.  Should another stream have changed them since, which no call may: nothing is followed that they do not allow, and the loop ends.
+        if (r >= p.requests) return;
         Units u = units(r);
-        uint32_t tile = (uint32_t)quotient(start.unit, u.each), done = (uint32_t)(start.unit - (uint64_t)tile * u.each);
+        uint32_t tile = (uint32_t)quotient(start.unit, u.each > 0 ? u.each : 1), done = (uint32_t)(start.unit - (uint64_t)tile * u.each);
+        if (tile >= u.tiles) return;
         // the rows of a tile, and those of their positions that are this share's
         auto piece = [&] {
             Work x;
@@ -1187,10 +1190,12 @@ __global__ __launch_bounds__((Plan<T, C, DP, ROWS, OWN>::kThreads), (Plan<T, C, 
         w = piece();
         if constexpr (P::kCarries) Reader<T, C, DP, ROWS, OWN>(p, threadIdx.x).begin(w, f);
         while (true) {
-            const bool more = left > 0;
+            bool more = left > 0;
             if (more && tile == u.tiles) {
                 tile = 0;
-                do u = units(++r); while (u.tiles == 0 && r + 1 < p.requests);
+                u.tiles = 0;
+                while (u.tiles == 0 && r + 1 < p.requests) u = units(++r);
+                more = u.tiles > 0;
             }
             const Work next = more ? piece() : w;
             attend_work<T, C, DP, ROWS, OWN>(p, w, next, more, f, lds);
