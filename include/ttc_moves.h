@@ -33,8 +33,8 @@ extern "C" {
  * with four exponent and three mantissa bits, largest value 448, no infinities; it is a type of the cache only.
  * So is TTC_Q4: a vector of `dim` elements (a multiple of 8, at most 512) is a record of 4 + dim/2 bytes, a step and a minimum in bf16 (in this order) and the
  * codes, element 2i in the low and 2i+1 in the high half of byte i; element = minimum + code * step.  Written are the largest
- * minimum of bf16 that is no larger than the vector's, the smallest step of bf16 that reaches its maximum with code 15, and the nearest codes (to the even one in the middle): no
- * element is off by more than half a step.  A vector with a NaN, an infinity, an element beyond the range of bf16, or
+ * minimum of bf16 that is no larger than the vector's, the smallest step of bf16 that reaches its maximum with code 15, and the nearest codes (to the even one in the middle), all three
+ * from differences and quotients in 32 bits: no element is off by more than half a step and that rounding.  A vector with a NaN, an infinity, an element beyond the range of bf16, or
  * elements further apart than 32 bits can say becomes all NaN. */
 enum { TTC_BF16 = 8, TTC_F16 = 9, TTC_F8 = 10, TTC_Q4 = 11 };
 

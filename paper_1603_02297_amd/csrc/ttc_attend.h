@@ -8,14 +8,15 @@
 // operand: a product's order of positions is free as long as both sides have the same one.  V^T is read from the tile by the transposing LDS loads, in that order.
 //
 //   ROWS 16, 32  few rows to a request (tokens that are generated one by one): the wavefronts of a workgroup have the same rows and every one its own tiles of 32
-//                positions, in LDS of its own; no barrier until they add up their results.  Bound by the cache's bytes: 64 requests behind 8000 positions, 8 heads of 128 in 16
-//                bits, at 5.84 TB/s; shares are pieces of these tiles as long for every workgroup, so that lengths do not matter.
+//                positions (64 over 4 bits with 16 rows and keys out of LDS), in LDS of its own; no barrier until they add up their results.  Bound by the cache's bytes: 64 requests
+//                behind 8000 positions, 8 heads of 128 in 16 bits, 367 us, 5.7 TB/s; shares are pieces of these tiles as long for every workgroup, so that lengths do not matter.
 //   ROWS 128     prompts: wavefronts have 32 rows each of the same 128 and share the tiles.  Bound by the matrix instructions, and the exponentials beside them: 11900
-//                tokens behind up to 2048, 20 heads of 128 for 5, 976 TFLOP/s (a large product on this card: 1212).
+//                tokens behind up to 2048, 20 heads of 128 for 5, 365 to 410 us, 390 in the median, 930 TFLOP/s (a large product on this card: 1212).  Over 8 bits 355 us, over
+//                4 bits, whose codes are widened on the way into LDS, 570.
 //   OWN          few rows over narrow caches, where dim is what the kernel is compiled for: a lane has a part of the vectors of positions of its own.  Keys are
 //                never in LDS: these parts are what the left operand of S^T holds in a lane, in an order of the dims that the queries follow.  Values are there as the
 //                cache has them, and widened behind the transposing loads, which there are for 8 and 4 bits, too
-//                (8 bits 5.6 TB/s; 4 bits, where a code costs as many instructions as an element does elsewhere, 4.3).
+//                (64 requests behind 8000 positions in 8 bits 186 us, 5.6 TB/s; 48 to 32,768 in 4 bits, where a code costs as many instructions as an element does elsewhere, 133 us, 4.3).
 //
 // A tile's loads are under way while the one before it is used, its entries of the block table one tile earlier.
 #pragma once

@@ -53,7 +53,7 @@ AttendShape attend_shape(const ttc_attend_s* a, int64_t requests, int64_t tokens
     s.slots = (uint32_t)(rows / s.tile + requests);
     const int64_t groups = std::max<int64_t>((int64_t)s.slots * heads, 1), units = std::max<int64_t>((longest + kAttendUnit - 1) / kAttendUnit, 1);
     if (s.tile < kTileMany) {
-        // As many shares as workgroups fit the device at a time: 64 requests of 8000 positions in 16 bits take 5.84 TB/s, and less with one and a half, two or four
+        // As many shares as workgroups fit the device at a time: 64 requests of 8000 positions in 16 bits take 5.7 TB/s, and less with one and a half, two or four
         // times as many.
         const int64_t most = 256 * attend_resident(bytes, attend_own(bytes, elem_bytes(a->cache_dtype), (int)a->dim, (int)s.tile), records, (int)a->dim, (int)s.tile);
         const int64_t each = std::max<int64_t>(most / heads, 1);               // of a head
