@@ -118,7 +118,8 @@ int64_t ttc_attend_workspace(ttc_attend_t attend, int64_t requests, int64_t toke
  *   workspace  ttc_attend_workspace bytes, aligned to 16.
  * A token that sees nothing, or scores of -inf only, gets 0.  What a position that is not seen holds (NaN, infinities) has no effect.  Scores, exponentials and their sums are
  * 32 bits; with 16-bit queries the exponentials (over a cache in 4 bits: times the values' steps) are rounded to that type for their products with the values, once; in fp16
- * those below 2^-21 of a row's largest to multiples of 2^-31 of it at most.
+ * those below 2^-21 of a row's largest to multiples of 2^-31 of it at most.  Values are added up before they are divided by the sum of the exponentials: those above 2^116 / (positions seen)
+ * may become infinite on the way.
  */
 int ttc_attend_pages(ttc_attend_t attend, int64_t requests, int64_t tokens, const void* q, int64_t ldq, const int32_t* starts, const int32_t* cached,
                      const int32_t* table, int64_t ld_table, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
